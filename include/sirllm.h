@@ -77,6 +77,8 @@ extern "C" {
 #define SIRLLM_MAX_CAPACITY 49152
 /* Largest `head_dim` (K/V rows of at most 1 KB; the gather stages 32 rows per copy). */
 #define SIRLLM_MAX_HEAD_DIM 512
+/* Largest `head_dim` of sirllm_attend (one unit's queries and sums are held in registers). */
+#define SIRLLM_MAX_ATTEND_HEAD_DIM 256
 
 typedef struct sirllm_config {
     int32_t n_streams;   /* independent dialogue streams, >= 1 */
@@ -278,6 +280,84 @@ int sirllm_compact_kv(const sirllm_config *cfg, const void *k_src, const void *v
 int sirllm_rerotate_keys(const sirllm_config *cfg, void *k, const int32_t *keep_idx,
                          const int32_t *n_keep, double rope_base, int32_t layout,
                          void *cuda_stream);
+
+/*
+ * New tokens into one layer of the cache, at the positions of their slots (Section 3.3:
+ * positions are assigned by place in the cache).  For every stream s and t < n_new[s], with
+ * p = first_slot[s] + t the slot - and so the position - of the token in row s*max_new + t:
+ *     q_out[row][h]            = rope(norm(q[row][h], q_weight), p)       for the n_heads queries
+ *     K[s][layer][h][p][:]     = rope(norm(k_new[row][h], k_weight), p)   for the n_kv_heads keys
+ *     V[s][layer][h][p][:]     = v_new[row][h]
+ *     norm(x, w) = x * w / sqrt(mean(x^2) + eps), taken per head; without weight (NULL) norm(x) = x
+ *     rope(x, p) = pair i of x turned by the angle p * rope_base^(-2i/head_dim)
+ * Angles are formed in fp64, everything else in fp32, and each element is rounded once, to the
+ * K/V dtype; all tensors have that type.  Writing the rows is all the bookkeeping done here:
+ * live_len is left to the round (sirllm_step reads the rows behind it).
+ *   q, k_new, v_new   rows of n_heads / n_kv_heads / n_kv_heads heads of head_dim elements, rows
+ *                     *_row_stride elements apart (slices of one projection's output are fine);
+ *                     16-byte aligned, strides multiples of 8; head_dim % 16 == 0
+ *   q, q_out          both NULL with n_heads = 0: only keys and values.  q_out may be q itself
+ *                     with the same stride; otherwise no output may overlap an input
+ *   q_weight, k_weight [head_dim] or NULL, each on its own;  eps >= 0
+ *   first_slot        int32 [n_streams];  n_new int32 [n_streams] or NULL (max_new everywhere)
+ *   k, v              the caches, all layers;  layer in [0, n_layers)
+ *   ws                for the status word: a stream whose rows do not fit (first_slot < 0 or
+ *                     first_slot + n_new > capacity) is skipped, SIRLLM_STATUS_OVERFLOW
+ * Rows at or beyond n_new[s] are neither read nor written.
+ */
+int sirllm_append_kv(const sirllm_config *cfg, int32_t layer, const void *q, int32_t n_heads,
+                     int64_t q_row_stride, const void *k_new, int64_t k_row_stride, const void *v_new,
+                     int64_t v_row_stride, const void *q_weight, const void *k_weight, float eps,
+                     double rope_base, int32_t layout, const int32_t *first_slot, const int32_t *n_new,
+                     void *q_out, int64_t q_out_row_stride, void *k, void *v, void *ws, void *cuda_stream);
+
+/*
+ * Attention of ONE new token per stream over one layer of the cache (the retained slots are what
+ * the model attends to, Section 3.1; the token's own row is in the cache already, see
+ * sirllm_append_kv).  For every stream s and query head h, with g = h / (n_heads / n_kv_heads):
+ *     z_j = scale * <q[s][h], K[s][layer][g][j]>,   j < kv_len[s]
+ *     out[s][h][:] = sum_j softmax(z)_j V[s][layer][g][j][:],   lse[s][h] = log sum_j exp(z_j)
+ * Slots at or behind kv_len are not read, whatever they hold.  kv_len = 0: out = 0, lse = -inf.
+ * A length outside [0, capacity] raises SIRLLM_STATUS_OVERFLOW and leaves the stream's out and
+ * lse as they were.  Results do not depend on the timing of the GPU.
+ *   q, out    [n_streams] rows of n_heads * head_dim elements of the K/V dtype, *_row_stride
+ *             elements apart, 16-byte aligned, strides multiples of 8; out must not overlap an input
+ *   n_heads   a multiple of n_kv_heads
+ *   lse       fp32 [n_streams][n_heads] (natural logarithm) or NULL.  With it results over
+ *             disjoint parts of a context can be joined
+ *   ws        its own kind of workspace: sirllm_attend_workspace_bytes() bytes, 256-byte aligned,
+ *             set up once with sirllm_attend_workspace_init(); sirllm_status() reads its status
+ *   head_dim  at most SIRLLM_MAX_ATTEND_HEAD_DIM, else SIRLLM_ERR_TOO_LARGE
+ */
+size_t sirllm_attend_workspace_bytes(const sirllm_config *cfg);
+int sirllm_attend_workspace_init(const sirllm_config *cfg, void *ws, void *cuda_stream);
+int sirllm_attend(const sirllm_config *cfg, int32_t layer, const void *q, int32_t n_heads, int64_t q_row_stride,
+                  const void *k, const void *v, const int32_t *kv_len, float scale, void *out,
+                  int64_t out_row_stride, float *lse, void *ws, void *cuda_stream);
+
+/*
+ * The producer of sirllm_score_pairs' input: the LM head's product, reduced tile by tile as it is
+ * computed (Section 3.2's remark that the score is obtained while the token is generated), so
+ * that no logits are written.  With z[row][c] = <hidden[row], weight[c]> (fp32 sums of exact
+ * products) for the rows s*max_new + t, t < n_new[s], and the columns [col0, col0 + n_cols) of the
+ * vocabulary whose weight rows the caller holds:
+ *     pairs_out[row][i] = (max, sum exp(z - max)) over tile i of the columns, (0, 0) if all are -inf
+ *     target_out[row]   = z[row][token_ids[row]] if that column lies in the range, else 0
+ * sirllm_head_tiles() gives the number of tiles (0 for an invalid configuration or range); hand it
+ * to sirllm_score_pairs or sirllm_step_pairs as n_tiles.  Under a vocabulary-parallel head every
+ * rank calls this for its columns; the ranks gather the pairs and add up the targets.
+ * Logits must be finite or -inf as in sirllm_score.  Rows at or beyond n_new[s] are left untouched.
+ *   hidden    [n_streams*max_new] rows of d_model elements, hidden_row_stride apart
+ *   weight    [n_cols] rows of d_model elements, weight_row_stride apart
+ *   dtype     SIRLLM_BF16 or SIRLLM_F16, of both; 16-byte aligned, strides multiples of 8
+ *   pairs_out float[2] x [rows][pair_row_stride], 8-byte aligned, pair_row_stride >= tiles
+ *   ws        for the status word (SIRLLM_STATUS_TIMEOUT: a device-side wait gave up)
+ */
+int32_t sirllm_head_tiles(const sirllm_config *cfg, int64_t n_cols);
+int sirllm_head_pairs(const sirllm_config *cfg, const void *hidden, int64_t hidden_row_stride, const void *weight,
+                      int64_t weight_row_stride, int32_t d_model, int32_t dtype, int64_t col0, int64_t n_cols,
+                      const int32_t *token_ids, const int32_t *n_new, void *pairs_out, int64_t pair_row_stride,
+                      float *target_out, void *ws, void *cuda_stream);
 
 /*
  * One whole round (Algorithm 1's loop body): score the n_new[s] new tokens, append

@@ -21,12 +21,15 @@ F32, BF16, F16 = 0, 1, 2
 OK, ERR_NULL, ERR_BAD_CONFIG, ERR_ALIGN, ERR_CUDA, ERR_TOO_LARGE = 0, -1, -2, -3, -4, -5
 STATUS_TOKEN_RANGE, STATUS_OVERFLOW, STATUS_TIMEOUT, STATUS_BAD_KEEP = 1, 2, 4, 8
 MAX_CAPACITY = 49152
+MAX_ATTEND_HEAD_DIM = 256
 POLICY_STREAM, POLICY_RANDOM, POLICY_INTERVAL = 1, 2, 3
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 
 EXPORTS = ["sirllm_workspace_bytes", "sirllm_workspace_init", "sirllm_score", "sirllm_score_static",
            "sirllm_score_partial",
            "sirllm_score_pairs", "sirllm_step_pairs", "sirllm_decay_select", "sirllm_keep_policy", "sirllm_rerotate_keys",
+           "sirllm_append_kv", "sirllm_attend_workspace_bytes", "sirllm_attend_workspace_init", "sirllm_attend",
+           "sirllm_head_tiles", "sirllm_head_pairs",
            "sirllm_compact_kv", "sirllm_step", "sirllm_step_phases", "sirllm_step_host",
            "sirllm_selftest_bounded_wait", "sirllm_status", "sirllm_strerror",
            "sirllm_last_cuda_error"]
@@ -112,6 +115,20 @@ def lib():
         L.sirllm_keep_policy.argtypes = [cfgp, i32, vp, ctypes.c_uint64, i32, i32, vp, vp, vp, vp]
         L.sirllm_rerotate_keys.restype = ctypes.c_int
         L.sirllm_rerotate_keys.argtypes = [cfgp, vp, vp, vp, ctypes.c_double, i32, vp]
+        i64, f32 = ctypes.c_int64, ctypes.c_float
+        L.sirllm_append_kv.restype = ctypes.c_int
+        L.sirllm_append_kv.argtypes = [cfgp, i32, vp, i32, i64, vp, i64, vp, i64, vp, vp, f32, ctypes.c_double,
+                                       i32, vp, vp, vp, i64, vp, vp, vp, vp]
+        L.sirllm_attend_workspace_bytes.restype = ctypes.c_size_t
+        L.sirllm_attend_workspace_bytes.argtypes = [cfgp]
+        L.sirllm_attend_workspace_init.restype = ctypes.c_int
+        L.sirllm_attend_workspace_init.argtypes = [cfgp, vp, vp]
+        L.sirllm_attend.restype = ctypes.c_int
+        L.sirllm_attend.argtypes = [cfgp, i32, vp, i32, i64, vp, vp, vp, f32, vp, i64, vp, vp, vp]
+        L.sirllm_head_tiles.restype = i32
+        L.sirllm_head_tiles.argtypes = [cfgp, i64]
+        L.sirllm_head_pairs.restype = ctypes.c_int
+        L.sirllm_head_pairs.argtypes = [cfgp, vp, i64, vp, i64, i32, i32, i64, i64, vp, vp, vp, i64, vp, vp, vp]
         L.sirllm_compact_kv.restype = ctypes.c_int
         L.sirllm_compact_kv.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.sirllm_step.restype = ctypes.c_int
@@ -481,6 +498,156 @@ def sirllm_rerotate_keys(cfg: Config, k, keep_idx, n_keep, rope_base: float, lay
     """Turns the moved rows of a compacted post-rotary K cache to their new positions."""
     _call(lib().sirllm_rerotate_keys, cfg, _kv(cfg, k, "k"), *_keep_args(cfg, keep_idx, n_keep),
           float(rope_base), int(layout), _stream())
+
+
+class _HeadsArg(_Arg):
+    """Rows of attention heads [>= rows, heads, head_dim] of the K/V dtype: heads and elements dense,
+    rows any multiple of 8 elements apart (a slice of a wider projection is fine)."""
+
+    def __init__(self, cfg, t, name, rows, heads=None):
+        super().__init__(t, None, name)
+        self.cfg, self.rows, self.want_heads = cfg, rows, heads
+
+    def check_shape(self):
+        cfg, t = self.cfg, self.t
+        if t is None:
+            return
+        if _DTYPE_CODE.get(t.dtype) != cfg.kv_dtype:
+            raise SirllmError(ERR_BAD_CONFIG, f"{self.name} dtype {t.dtype} does not match the config")
+        if t.dim() != 3 or t.shape[0] < self.rows or t.shape[2] != cfg.head_dim or \
+                (self.want_heads is not None and t.shape[1] != self.want_heads):
+            raise SirllmError(ERR_BAD_CONFIG, f"{self.name} has shape {tuple(t.shape)}, the configuration needs "
+                                              f"[>= {self.rows}, {self.want_heads or 'heads'}, {cfg.head_dim}]")
+        if (t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != cfg.head_dim):
+            raise SirllmError(ERR_ALIGN, f"{self.name} heads must be dense")
+        if t.shape[0] > 1 and t.stride(0) < t.shape[1] * cfg.head_dim:
+            raise SirllmError(ERR_ALIGN, f"{self.name} rows overlap")
+
+    @property
+    def heads(self) -> int:
+        return 0 if self.t is None else int(self.t.shape[1])
+
+    @property
+    def row_stride(self) -> int:
+        t = self.t
+        return 0 if t is None else int(t.stride(0)) if t.shape[0] > 1 else self.heads * self.cfg.head_dim
+
+
+def sirllm_append_kv(cfg: Config, layer: int, q, k_new, v_new, q_weight, k_weight, eps: float, rope_base: float,
+                     layout: int, first_slot, n_new, q_out, k, v, ws) -> None:
+    """New tokens into one layer of the cache: norms per head (where a weight is given), rotation to
+    the position of the slot, K/V rows written at ``first_slot[s] + t``.  ``q``, ``q_out``
+    ``[rows, n_heads, head_dim]`` (or both None), ``k_new``, ``v_new`` ``[rows, n_kv_heads, head_dim]``."""
+    rows, D = _rows(cfg), cfg.head_dim
+    qa, ka = _HeadsArg(cfg, q, "q", rows), _HeadsArg(cfg, k_new, "k_new", rows, cfg.n_kv_heads)
+    va = _HeadsArg(cfg, v_new, "v_new", rows, cfg.n_kv_heads)
+    for a in (qa, ka, va):
+        a.check_shape()
+    oa = _HeadsArg(cfg, q_out, "q_out", rows, qa.heads if q is not None else None)
+    oa.check_shape()
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None and _DTYPE_CODE.get(w.dtype) != cfg.kv_dtype:
+            raise SirllmError(ERR_BAD_CONFIG, f"{name} dtype {w.dtype} does not match the config")
+    _call(lib().sirllm_append_kv, cfg, int(layer), qa, qa.heads, qa.row_stride, ka, ka.row_stride, va, va.row_stride,
+          _dev(q_weight, _KV, "q_weight", D), _dev(k_weight, _KV, "k_weight", D), float(eps), float(rope_base),
+          int(layout), _dev(first_slot, torch.int32, "first_slot", cfg.n_streams),
+          _dev(n_new, torch.int32, "n_new", cfg.n_streams), oa, oa.row_stride, _kv(cfg, k, "k"), _kv(cfg, v, "v"),
+          _ws(cfg, ws), _stream())
+
+
+def sirllm_attend_workspace_bytes(cfg: Config) -> int:
+    return lib().sirllm_attend_workspace_bytes(ctypes.byref(cfg))
+
+
+def _attend_ws(cfg: Config, ws) -> _Arg:
+    return _dev(ws, torch.uint8, "ws", sirllm_attend_workspace_bytes(cfg))
+
+
+def new_attend_workspace(cfg: Config, device="cuda") -> torch.Tensor:
+    """Allocates (with torch) and initialises a workspace for :func:`sirllm_attend`."""
+    n = sirllm_attend_workspace_bytes(cfg)
+    if n == 0:
+        raise SirllmError(ERR_BAD_CONFIG, "invalid configuration")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    sirllm_attend_workspace_init(cfg, ws)
+    return ws
+
+
+def sirllm_attend_workspace_init(cfg: Config, ws: torch.Tensor) -> None:
+    _call(lib().sirllm_attend_workspace_init, cfg, _attend_ws(cfg, ws), _stream())
+
+
+def sirllm_attend(cfg: Config, layer: int, q, k, v, kv_len, scale: Optional[float], out, lse, ws) -> None:
+    """Attention of one new token per stream over ``kv_len[s]`` slots of a layer's planes.  ``q``, ``out``
+    ``[n_streams, n_heads, head_dim]``; ``scale`` None = 1/sqrt(head_dim); ``lse`` fp32
+    ``[n_streams, n_heads]`` or None; ``ws`` from :func:`new_attend_workspace`."""
+    S = cfg.n_streams
+    qa = _HeadsArg(cfg, q, "q", S)
+    qa.check_shape()
+    oa = _HeadsArg(cfg, out, "out", S, qa.heads if q is not None else None)
+    oa.check_shape()
+    _call(lib().sirllm_attend, cfg, int(layer), qa, qa.heads, qa.row_stride, _kv(cfg, k, "k"), _kv(cfg, v, "v"),
+          _dev(kv_len, torch.int32, "kv_len", S), cfg.head_dim ** -0.5 if scale is None else float(scale), oa,
+          oa.row_stride, _dev(lse, torch.float32, "lse", S * qa.heads), _attend_ws(cfg, ws), _stream())
+
+
+class _MatrixArg(_Arg):
+    """A matrix [>= rows, width] of 16-bit elements with dense rows any multiple of 8 elements apart."""
+
+    def __init__(self, t, name, rows):
+        super().__init__(t, None, name)
+        self.rows = rows
+
+    def check_shape(self):
+        t = self.t
+        if t is None:
+            raise SirllmError(ERR_NULL, f"{self.name} is required")
+        if t.dtype not in _KV:
+            raise SirllmError(ERR_BAD_CONFIG, f"{self.name} has dtype {t.dtype}")
+        if t.dim() != 2 or t.shape[0] < self.rows or t.shape[1] < 1:
+            raise SirllmError(ERR_BAD_CONFIG, f"{self.name} has shape {tuple(t.shape)}, the call needs "
+                                              f"[>= {self.rows}, d_model]")
+        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise SirllmError(ERR_ALIGN, f"{self.name} rows must be dense")
+
+    @property
+    def row_stride(self) -> int:
+        t = self.t
+        return int(t.stride(0)) if t.shape[0] > 1 else (int(t.shape[1]) + 7) // 8 * 8
+
+
+def sirllm_head_tiles(cfg: Config, n_cols: int) -> int:
+    """Pairs per row that :func:`sirllm_head_pairs` writes for ``n_cols`` vocabulary columns."""
+    return lib().sirllm_head_tiles(ctypes.byref(cfg), int(n_cols))
+
+
+def sirllm_head_pairs(cfg: Config, hidden, weight, col0: int, token_ids, n_new, pairs_out, target_out, ws) -> None:
+    """Per-tile ``(max, sum exp)`` pairs and target logits of ``hidden @ weight.T`` for
+    :func:`sirllm_score_pairs` / :func:`sirllm_step_pairs`, without the logits.  ``hidden``
+    ``[rows, d_model]``, ``weight`` ``[n_cols, d_model]`` (rows ``[col0, col0 + n_cols)`` of the LM
+    head), ``pairs_out`` fp32 ``[rows, sirllm_head_tiles(cfg, n_cols), 2]``, ``target_out`` fp32 ``[rows]``."""
+    rows = _rows(cfg)
+    ha, wa = _MatrixArg(hidden, "hidden", rows), _MatrixArg(weight, "weight", 1)
+    ha.check_shape()
+    wa.check_shape()
+    if hidden.dtype != weight.dtype or hidden.shape[1] != weight.shape[1]:
+        raise SirllmError(ERR_BAD_CONFIG, f"hidden {tuple(hidden.shape)} {hidden.dtype} and weight "
+                                          f"{tuple(weight.shape)} {weight.dtype} do not match")
+    n_cols = int(weight.shape[0])
+    pa = _PairsArg(cfg, pairs_out)
+    pa.check_shape()
+    tiles = sirllm_head_tiles(cfg, n_cols)
+    if tiles == 0 or pa.n_tiles != tiles:
+        raise SirllmError(ERR_BAD_CONFIG, f"pairs_out holds {pa.n_tiles} tiles per row, {n_cols} columns need {tiles}")
+    _call(lib().sirllm_head_pairs, cfg, ha, ha.row_stride, wa, wa.row_stride, int(hidden.shape[1]),
+          _DTYPE_CODE[hidden.dtype], int(col0), n_cols, *_head_out(cfg, token_ids, n_new, pa, target_out),
+          _ws(cfg, ws), _stream())
+
+
+def _head_out(cfg: Config, token_ids, n_new, pa: _PairsArg, target_out):
+    ids, nn, tgt = _score_args(cfg, token_ids, n_new, target_out)
+    tgt.name = "target_out"
+    return ids, nn, pa, pa.row_stride, tgt
 
 
 def sirllm_compact_kv(cfg: Config, k_src, v_src, k_dst, v_dst, keep_idx, n_keep, ws) -> None:

@@ -109,6 +109,17 @@ WorkspaceLayout workspace_layout(const sirllm_config& c) {
     return L;
 }
 
+AttendLayout attend_layout(const sirllm_config& c) {
+    AttendLayout L;
+    const size_t parts = (size_t)2 * kAttendMaxCtas * kAttendPartHeads;
+    L.tickets_off = 256;
+    L.part_ml_off = align_up(L.tickets_off + (size_t)kAttendMaxCtas * 4, 256);
+    L.zeroed = L.part_ml_off;
+    L.part_o_off = align_up(L.part_ml_off + parts * sizeof(float2), 256);
+    L.total = align_up(L.part_o_off + parts * c.head_dim * sizeof(float), 256);
+    return L;
+}
+
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
 static ScoreParams score_params(const sirllm_config& c, const WorkspaceLayout& L, const void* logits,
@@ -612,6 +623,171 @@ int sirllm_rerotate_keys(const sirllm_config* cfg, void* k, const int32_t* keep_
     cudaError_t e = launch_rerotate(p, cfg->n_streams, cfg->kv_dtype == SIRLLM_BF16,
                                     (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "rerotate");
+}
+
+int sirllm_append_kv(const sirllm_config* cfg, int32_t layer, const void* q, int32_t n_heads,
+                     int64_t q_row_stride, const void* k_new, int64_t k_row_stride, const void* v_new,
+                     int64_t v_row_stride, const void* q_weight, const void* k_weight, float eps,
+                     double rope_base, int32_t layout, const int32_t* first_slot, const int32_t* n_new,
+                     void* q_out, int64_t q_out_row_stride, void* k, void* v, void* ws, void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (!k_new || !v_new || !first_slot || !k || !v || !ws || (q == nullptr) != (q_out == nullptr))
+        return SIRLLM_ERR_NULL;
+    const int64_t kv_width = (int64_t)cfg->n_kv_heads * cfg->head_dim;
+    const int64_t q_width = (int64_t)n_heads * cfg->head_dim;
+    if (layer < 0 || layer >= cfg->n_layers || cfg->head_dim % 16 != 0 || n_heads < 0 ||
+        (q != nullptr) != (n_heads > 0) || (int64_t)n_heads + 2 * (int64_t)cfg->n_kv_heads > 0x3FFFFFFF)
+        return SIRLLM_ERR_BAD_CONFIG;
+    if (!(rope_base > 0.0) || !std::isfinite(rope_base) ||
+        (layout != SIRLLM_ROPE_HALF && layout != SIRLLM_ROPE_INTERLEAVED) || !(eps >= 0.0f) || !std::isfinite(eps))
+        return SIRLLM_ERR_BAD_CONFIG;
+    if (k_row_stride < kv_width || v_row_stride < kv_width ||
+        (q && (q_row_stride < q_width || q_out_row_stride < q_width)))
+        return SIRLLM_ERR_BAD_CONFIG;
+    const void* vectors[8] = {q, k_new, v_new, q_weight, k_weight, q_out, k, v};
+    for (const void* x : vectors)
+        if (x && misaligned(x, 16)) return SIRLLM_ERR_ALIGN;
+    if (k_row_stride % 8 != 0 || v_row_stride % 8 != 0 || (q && (q_row_stride % 8 != 0 || q_out_row_stride % 8 != 0)))
+        return SIRLLM_ERR_ALIGN;
+    if (misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
+    AppendParams p;
+    memset(&p, 0, sizeof p);
+    p.q = (const char*)q;
+    p.k_new = (const char*)k_new;
+    p.v_new = (const char*)v_new;
+    p.q_weight = q_weight;
+    p.k_weight = k_weight;
+    p.normed = q_weight != nullptr || k_weight != nullptr;
+    p.first_slot = first_slot;
+    p.n_new = n_new;
+    p.q_out = (char*)q_out;
+    p.k = (char*)k;
+    p.v = (char*)v;
+    p.status = (int32_t*)ws;
+    p.q_stride = q_row_stride;
+    p.k_stride = k_row_stride;
+    p.v_stride = v_row_stride;
+    p.q_out_stride = q_out_row_stride;
+    for (int i = 0; i < cfg->head_dim / 2; ++i)
+        p.turns[i] = std::pow(rope_base, -2.0 * (double)i / (double)cfg->head_dim) / 6.283185307179586476925;
+    p.eps = eps;
+    p.n_heads = n_heads;
+    p.n_kv_heads = cfg->n_kv_heads;
+    p.head_dim = cfg->head_dim;
+    p.capacity = cfg->capacity;
+    p.max_new = cfg->max_new;
+    p.n_streams = cfg->n_streams;
+    p.layout = layout;
+    p.planes_per_stream = cfg->n_layers * cfg->n_kv_heads;
+    p.layer_plane = layer * cfg->n_kv_heads;
+    p.heads_all = n_heads + 2 * cfg->n_kv_heads;
+    cudaError_t e = launch_append(p, cfg->kv_dtype == SIRLLM_BF16, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "append_kv");
+}
+
+size_t sirllm_attend_workspace_bytes(const sirllm_config* cfg) {
+    if (validate_config(cfg) != SIRLLM_OK || cfg->head_dim > SIRLLM_MAX_ATTEND_HEAD_DIM) return 0;
+    return attend_layout(*cfg).total;
+}
+
+int sirllm_attend_workspace_init(const sirllm_config* cfg, void* ws, void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (ws == nullptr) return SIRLLM_ERR_NULL;
+    if (cfg->head_dim > SIRLLM_MAX_ATTEND_HEAD_DIM) return SIRLLM_ERR_TOO_LARGE;
+    if (misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
+    // the parts are written before they are read; status word and tickets must start at zero
+    cudaError_t e = cudaMemsetAsync(ws, 0, attend_layout(*cfg).zeroed, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "cudaMemsetAsync");
+}
+
+int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_t n_heads, int64_t q_row_stride,
+                  const void* k, const void* v, const int32_t* kv_len, float scale, void* out,
+                  int64_t out_row_stride, float* lse, void* ws, void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (!q || !k || !v || !kv_len || !out || !ws) return SIRLLM_ERR_NULL;
+    const int64_t width = (int64_t)n_heads * cfg->head_dim;
+    if (layer < 0 || layer >= cfg->n_layers || n_heads < 1 || n_heads % cfg->n_kv_heads != 0 || width > 0x7FFFFFFF ||
+        !std::isfinite(scale) || q_row_stride < width || out_row_stride < width)
+        return SIRLLM_ERR_BAD_CONFIG;
+    if (cfg->head_dim > SIRLLM_MAX_ATTEND_HEAD_DIM) return SIRLLM_ERR_TOO_LARGE;
+    const void* vectors[4] = {q, k, v, out};
+    for (const void* x : vectors)
+        if (misaligned(x, 16)) return SIRLLM_ERR_ALIGN;
+    if (q_row_stride % 8 != 0 || out_row_stride % 8 != 0 || misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
+    const AttendLayout L = attend_layout(*cfg);
+    AttendParams p;
+    memset(&p, 0, sizeof p);
+    p.q = (const char*)q;
+    p.k = (const char*)k;
+    p.v = (const char*)v;
+    p.kv_len = kv_len;
+    p.out = (uint16_t*)out;
+    p.lse = lse;
+    p.status = (int32_t*)ws;
+    p.tickets = (int32_t*)((char*)ws + L.tickets_off);
+    p.part_ml = (float2*)((char*)ws + L.part_ml_off);
+    p.part_o = (float*)((char*)ws + L.part_o_off);
+    p.q_stride = q_row_stride;
+    p.out_stride = out_row_stride;
+    p.scale_log2 = scale * kLog2e;
+    p.n_streams = cfg->n_streams;
+    p.n_heads = n_heads;
+    p.head_dim = cfg->head_dim;
+    p.capacity = cfg->capacity;
+    p.group = n_heads / cfg->n_kv_heads;
+    const int unit = attend_unit_heads(p.group);
+    p.blocks = (p.group + unit - 1) / unit;
+    p.units = cfg->n_kv_heads * p.blocks;
+    p.planes_per_stream = cfg->n_layers * cfg->n_kv_heads;
+    p.layer_plane = layer * cfg->n_kv_heads;
+    p.part_heads = kAttendPartHeads;
+    cudaError_t e = launch_attend(p, cfg->kv_dtype == SIRLLM_BF16, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "attend");
+}
+
+int32_t sirllm_head_tiles(const sirllm_config* cfg, int64_t n_cols) {
+    if (validate_config(cfg) != SIRLLM_OK || n_cols < 1 || n_cols > cfg->vocab) return 0;
+    const int64_t rows = (int64_t)cfg->n_streams * cfg->max_new;
+    const int cols = head_tile_cols(rows, n_cols);
+    return (int32_t)((n_cols + cols - 1) / cols);
+}
+
+int sirllm_head_pairs(const sirllm_config* cfg, const void* hidden, int64_t hidden_row_stride, const void* weight,
+                      int64_t weight_row_stride, int32_t d_model, int32_t dtype, int64_t col0, int64_t n_cols,
+                      const int32_t* token_ids, const int32_t* n_new, void* pairs_out, int64_t pair_row_stride,
+                      float* target_out, void* ws, void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (!hidden || !weight || !token_ids || !pairs_out || !target_out || !ws) return SIRLLM_ERR_NULL;
+    if (d_model < 1 || (dtype != SIRLLM_BF16 && dtype != SIRLLM_F16) || n_cols < 1 || col0 < 0 ||
+        col0 > cfg->vocab - n_cols || hidden_row_stride < d_model || weight_row_stride < d_model ||
+        hidden_row_stride > ((int64_t)1 << 38) || weight_row_stride > ((int64_t)1 << 38) ||
+        pair_row_stride < sirllm_head_tiles(cfg, n_cols))
+        return SIRLLM_ERR_BAD_CONFIG;
+    if (misaligned(hidden, 16) || misaligned(weight, 16) || hidden_row_stride % 8 != 0 || weight_row_stride % 8 != 0 ||
+        misaligned(pairs_out, 8) || misaligned(target_out, 4) || misaligned(ws, 256))
+        return SIRLLM_ERR_ALIGN;
+    HeadParams p;
+    memset(&p, 0, sizeof p);
+    p.token_ids = token_ids;
+    p.n_new = n_new;
+    p.pairs_out = (float2*)pairs_out;
+    p.target_out = target_out;
+    p.status = (int32_t*)ws;
+    p.rows = (int64_t)cfg->n_streams * cfg->max_new;
+    p.n_cols = n_cols;
+    p.col0 = col0;
+    p.pair_stride = pair_row_stride;
+    p.max_new = cfg->max_new;
+    p.d_model = d_model;
+    p.tile_cols = head_tile_cols(p.rows, n_cols);
+    p.n_tiles = sirllm_head_tiles(cfg, n_cols);
+    p.bf16 = dtype == SIRLLM_BF16;
+    cudaError_t e = launch_head(p, hidden, hidden_row_stride, weight, weight_row_stride, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "head_pairs");
 }
 
 int sirllm_selftest_bounded_wait(const sirllm_config* cfg, void* ws, uint32_t polls,

@@ -1,0 +1,492 @@
+// Attention of one new token per stream over a layer's planes:
+//     z_j = scale * <q, K_j>,   out = sum_j softmax(z)_j V_j,   lse = log sum_j exp z_j,   j < kv_len
+// for every query head; heads g*G .. g*G+G-1 share the planes of K/V head g.
+//
+// A token does 2 multiply-adds per cache element it reads and per head that shares the element,
+// so HBM bounds it: every live K and V row has to come in once.  The cache is cut into tiles of
+// 16 slots.  All tiles of all (stream, K/V head) units stand in one line, and every CTA takes an
+// equal stretch of it - whatever the lengths are, the CTAs read the same amount (a unit that
+// spans CTAs leaves partial results (max, sum, weighted rows) in the workspace; the CTA that
+// finishes last, by ticket, joins them in a fixed order, so results do not depend on timing).
+// Inside a CTA every warp streams its own tiles through its own ring of cp.async stages and
+// keeps a running softmax; nothing but the end of a unit makes warps wait for one another, and
+// the ring runs ahead across units.
+//
+// The products run on mma.sync (m16n8k16) with K and V as the LEFT operand: z^T = K q^T puts 16
+// slots on the rows and 8 query heads on the columns, out^T = V^T p^T 16 elements on the rows.
+// The group of heads that shares a plane is the narrow side (1 to 8 columns, kTiles * 8 with
+// larger groups), so a tile costs one pass over K and one over V whatever the group is; tcgen05
+// wants 128 rows of queries or 64+ of K per instruction and a round trip through TMEM for the
+// probabilities, and has nothing to give where HBM is the bound.
+// fp32: scores, running maximum and sum, output sums, the join.  Rounded to 16 bits: the
+// probabilities on their way into the second product (relative to a reference that the true
+// maximum exceeds by less than 2^8, so fp16 cannot overflow), and the result.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace sirllm {
+
+namespace {
+
+constexpr int kKeys = 16;  // slots per tile
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+template <bool kBf16>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if (kBf16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+                     "{%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+                     "{%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    uint32_t out;
+    if (kBf16)
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(out) : "f"(hi), "f"(lo));
+    return out;
+}
+template <bool kBf16>
+__device__ __forceinline__ uint16_t round16(float v) {
+    if (kBf16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    return __half_as_ushort(__float2half_rn(v));
+}
+
+// slots of a stream that count, 0 for a length outside the planes
+__device__ __forceinline__ int live_slots(const AttendParams& p, int s) {
+    const int n = p.kv_len[s];
+    return n < 0 || n > p.capacity ? 0 : n;
+}
+
+// A walk along the line of tiles: segments of units, as far as this CTA's stretch goes.
+struct Walk {
+    int64_t left;   // tiles of the stretch from this segment's first on
+    int64_t unit0;  // line position of the unit's first tile
+    int s, unit;    // stream; unit within the stream (K/V head, block of query heads)
+    int len;        // live slots of the stream
+    int t0, t1;     // this segment's tiles of the unit
+
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ int tiles() const { return (len + kKeys - 1) / kKeys; }
+    __device__ __forceinline__ void set_end() {
+        const int T = tiles();
+        t1 = (int64_t)(T - t0) > left ? t0 + (int)left : T;
+    }
+    __device__ __forceinline__ void next(const AttendParams& p) {
+        left -= t1 - t0;
+        if (left <= 0) return;
+        unit0 += tiles();
+        t0 = 0;
+        if (++unit == p.units) {
+            unit = 0;
+            for (len = 0; len == 0;) {  // tiles are left, so a stream with slots follows
+                if (++s >= p.n_streams) {  // (unless the lengths changed under the call)
+                    left = 0;
+                    return;
+                }
+                len = live_slots(p, s);
+            }
+        }
+        set_end();
+    }
+};
+
+// kDim: head_dim rounded up to 64, 128 or 256 (the columns behind head_dim are zeros in shared
+// memory); kTiles: blocks of 8 query heads that a unit carries.
+template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages>
+__global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendParams p) {
+    constexpr int kThreads = kWarps * 32;
+    constexpr int kChunks = kDim / 8;               // 16-byte vectors of a row
+    constexpr int kTileBytes = kKeys * kDim * 2;    // K or V of one tile
+    constexpr int kHeads = kTiles * 8;
+    constexpr int kPass = 4;                        // heads whose output sums are merged at a time
+    extern __shared__ __align__(128) unsigned char smem[];
+    unsigned char* ring = smem;                                                   // [warp][stage][K, V]
+    float* merge = reinterpret_cast<float*>(smem + kWarps * kStages * 2 * kTileBytes);  // [warp][kPass][kDim]
+    __shared__ int64_t scan[kWarps];
+    __shared__ Walk first;
+    __shared__ float stat_m[kWarps][kHeads], stat_l[kWarps][kHeads];
+    __shared__ float part_w[kHeads];
+    __shared__ int last_one;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // ---- the line of tiles, this CTA's stretch of it -------------------------------------
+    const int slice = (p.n_streams + kThreads - 1) / kThreads;
+    const int s_lo = min(p.n_streams, tid * slice), s_hi = min(p.n_streams, s_lo + slice);
+    int64_t mine = 0;
+    for (int s = s_lo; s < s_hi; ++s) mine += (int64_t)((live_slots(p, s) + kKeys - 1) / kKeys) * p.units;
+    int64_t before = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xFFFFFFFFu, before, o);
+        if (lane >= o) before += v;
+    }
+    if (lane == 31) scan[warp] = before;
+    __syncthreads();
+    int64_t total = 0, warps_before = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) warps_before += scan[w];
+        total += scan[w];
+    }
+    before += warps_before - mine;  // tiles in front of this thread's streams
+    // at least one tile per warp, so that short caches are not joined from needlessly many parts
+    int64_t per = (total + gridDim.x - 1) / gridDim.x;
+    if (per < kWarps) per = kWarps;
+    const int64_t r0 = (int64_t)blockIdx.x * per;
+    const int64_t r1 = r0 + per < total ? r0 + per : total;
+    if (r0 >= before && r0 < before + mine) {  // exactly one thread, if the stretch is not empty
+        int64_t at = before;
+        int s = s_lo, len = 0;
+        int64_t T = 0;
+        for (; s < s_hi; ++s) {
+            len = live_slots(p, s);
+            T = (len + kKeys - 1) / kKeys;
+            if (r0 < at + T * p.units) break;
+            at += T * p.units;
+        }
+        first.left = s < s_hi ? r1 - r0 : 0;
+        if (s < s_hi) {
+            first.s = s;
+            first.len = len;
+            first.unit = (int)((r0 - at) / T);
+            first.unit0 = at + (int64_t)first.unit * T;
+            first.t0 = (int)(r0 - first.unit0);
+            first.set_end();
+        }
+    }
+    // streams without slots: nothing to weigh, the result is zero and its log-sum -inf; a length
+    // outside the planes is reported and its rows are left alone
+    for (int s = blockIdx.x; s < p.n_streams; s += gridDim.x) {
+        const int n = p.kv_len[s];
+        if (n < 0 || n > p.capacity) {
+            if (tid == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
+        } else if (n == 0) {
+            for (int i = tid; i < p.n_heads * p.head_dim; i += kThreads)
+                p.out[(int64_t)s * p.out_stride + i] = 0;
+            if (p.lse != nullptr)
+                for (int i = tid; i < p.n_heads; i += kThreads)
+                    p.lse[(int64_t)s * p.n_heads + i] = __uint_as_float(0xFF800000u);
+        }
+    }
+    __syncthreads();
+    if (r0 >= total) return;
+
+    // ---- the warp's ring ------------------------------------------------------------------
+    const uint32_t ring0 = smem_u32(ring) + warp * kStages * 2 * kTileBytes;
+    Walk ahead = first;                 // what the loads have reached
+    int ahead_tile = ahead.t0 + warp;
+    constexpr int kRowsAtOnce = 32 / kChunks;  // rows that one load instruction of the warp covers
+    const int chunk = lane % kChunks, row_in = lane / kChunks;
+    const bool chunk_on = chunk * 8 < p.head_dim;
+    auto load_next = [&](int stage) {  // the warp's next tile, if there is one, into a stage; one group
+        while (ahead.more() && ahead_tile >= ahead.t1) {
+            ahead.next(p);
+            ahead_tile = ahead.t0 + warp;
+        }
+        if (ahead.more()) {
+            const int g = ahead.unit / p.blocks;
+            const int64_t plane = (int64_t)ahead.s * p.planes_per_stream + p.layer_plane + g;
+            const int key0 = ahead_tile * kKeys;
+            const int64_t off = ((plane * p.capacity + key0) * p.head_dim + (chunk_on ? chunk * 8 : 0)) * 2;
+            const uint32_t dst0 = ring0 + stage * 2 * kTileBytes;
+#pragma unroll
+            for (int i = 0; i < kKeys / kRowsAtOnce; ++i) {
+                const int r = i * kRowsAtOnce + row_in;
+                const bool valid = chunk_on && key0 + r < ahead.len;
+                const int64_t o = valid ? off + (int64_t)r * p.head_dim * 2 : off;
+                const uint32_t d = dst0 + r * (kDim * 2) + ((chunk ^ (r & 7)) << 4);
+                cp_async16(d, p.k + o, valid);
+                cp_async16(d + kTileBytes, p.v + o, valid);
+            }
+            ahead_tile += kWarps;
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) load_next(i);
+    int stage = 0;
+
+    // ---- the units ------------------------------------------------------------------------
+    const int hc = 2 * (lane & 3);  // this lane's two heads within a block of 8
+    for (Walk w = first; w.more(); w.next(p)) {
+        const int g = w.unit / p.blocks, block = w.unit - g * p.blocks;
+        const int head0 = g * p.group + block * kHeads;            // first query head of the unit
+        const int heads = min(kHeads, p.group - block * kHeads);   // query heads it really has
+        // queries as the right operand: lane holds elements 2(lane%4), +1 (and +8, +9) of head lane/4
+        uint32_t qf[kTiles][kDim / 16][2];
+        const char* qrow = p.q + ((int64_t)w.s * p.q_stride + (int64_t)head0 * p.head_dim) * 2;
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+            const int h = n * 8 + (lane >> 2);
+#pragma unroll
+            for (int ks = 0; ks < kDim / 16; ++ks) {
+                const int e = ks * 16 + hc;
+                const char* src = qrow + ((int64_t)h * p.head_dim + e) * 2;
+                qf[n][ks][0] = h < heads && e < p.head_dim ? *reinterpret_cast<const uint32_t*>(src) : 0u;
+                qf[n][ks][1] = h < heads && e + 8 < p.head_dim ? *reinterpret_cast<const uint32_t*>(src + 16) : 0u;
+            }
+        }
+        float o[kTiles][kDim / 16][4];
+        float m[kTiles][2], l[kTiles][2];  // reference in units of log2, sum of this lane's slots
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+            for (int d = 0; d < kDim / 16; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[n][d][i] = 0.f;
+            m[n][0] = m[n][1] = kNegHuge;
+            l[n][0] = l[n][1] = 0.f;
+        }
+        for (int tile = w.t0 + warp; tile < w.t1; tile += kWarps) {
+            cp_wait<kStages - 2>();
+            __syncwarp();
+            load_next(stage == 0 ? kStages - 1 : stage - 1);  // the stage that was consumed last
+            const uint32_t kt = ring0 + stage * 2 * kTileBytes, vt = kt + kTileBytes;
+            float z[kTiles][4];
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[n][i] = 0.f;
+            {
+                const int r = lane & 15;
+                const uint32_t base = kt + r * (kDim * 2);
+#pragma unroll
+                for (int ks = 0; ks < kDim / 16; ++ks) {
+                    uint32_t a[4];
+                    ldsm4(a, base + (((2 * ks + (lane >> 4)) ^ (r & 7)) << 4));
+#pragma unroll
+                    for (int n = 0; n < kTiles; ++n) mma16816<kBf16>(z[n], a, qf[n][ks][0], qf[n][ks][1]);
+                }
+            }
+            // z[n][0..1]: slot lane/4, this lane's two heads; z[n][2..3]: slot lane/4 + 8
+            const int key = tile * kKeys + (lane >> 2);
+            const bool in0 = key < w.len, in1 = key + 8 < w.len;
+            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z[n][i] = (i < 2 ? in0 : in1) ? z[n][i] * p.scale_log2 : __uint_as_float(0xFF800000u);
+                    raise |= z[n][i] > m[n][i & 1] + 8.f;
+                }
+            }
+            // The reference moves only when a score passes it by more than 2^8; the sums stay exact.
+            if (__any_sync(0xFFFFFFFFu, raise)) {
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float top = fmaxf(z[n][i], z[n][i + 2]);
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+                        const float up = fmaxf(m[n][i], top);
+                        const float f = ex2_approx(m[n][i] - up);
+                        m[n][i] = up;
+                        l[n][i] *= f;
+#pragma unroll
+                        for (int d = 0; d < kDim / 16; ++d) {
+                            o[n][d][i] *= f;
+                            o[n][d][i + 2] *= f;
+                        }
+                    }
+            }
+            uint32_t pb[kTiles][2];
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[n][i] = ex2_approx(z[n][i] - m[n][i & 1]);
+                l[n][0] += z[n][0] + z[n][2];
+                l[n][1] += z[n][1] + z[n][3];
+                pb[n][0] = transpose8x8(pack16<kBf16>(z[n][0], z[n][1]));
+                pb[n][1] = transpose8x8(pack16<kBf16>(z[n][2], z[n][3]));
+            }
+            {
+                const int r = (lane & 7) + ((lane >> 4) << 3);
+                const uint32_t base = vt + r * (kDim * 2);
+#pragma unroll
+                for (int d = 0; d < kDim / 16; ++d) {
+                    uint32_t a[4];
+                    ldsm4_trans(a, base + (((2 * d + ((lane >> 3) & 1)) ^ (r & 7)) << 4));
+#pragma unroll
+                    for (int n = 0; n < kTiles; ++n) mma16816<kBf16>(o[n][d], a, pb[n][0], pb[n][1]);
+                }
+            }
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+        }
+        // ---- the warps' sums into one ------------------------------------------------------
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], x);
+                if (lane < 4) {
+                    stat_m[warp][n * 8 + hc + i] = m[n][i];
+                    stat_l[warp][n * 8 + hc + i] = l[n][i];
+                }
+            }
+        __syncthreads();
+        const bool whole = w.t0 == 0 && w.t1 == w.tiles();
+        const int c_first = (int)(w.unit0 / per);
+        const int64_t slot = 2 * (int64_t)blockIdx.x + ((int)blockIdx.x == c_first ? 1 : 0);
+        float* part_o = p.part_o + slot * p.part_heads * p.head_dim;
+        float2* part_ml = p.part_ml + slot * p.part_heads;
+        float top[kTiles][2];
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float t = kNegHuge;
+#pragma unroll
+                for (int x = 0; x < kWarps; ++x) t = fmaxf(t, stat_m[x][n * 8 + hc + i]);
+                top[n][i] = t;
+            }
+        if (tid < heads) {
+            float t = kNegHuge, sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < kWarps; ++x) t = fmaxf(t, stat_m[x][tid]);
+#pragma unroll
+            for (int x = 0; x < kWarps; ++x) sum += stat_l[x][tid] * ex2_approx(stat_m[x][tid] - t);
+            if (whole) {
+                part_w[tid] = 1.0f / sum;
+                if (p.lse != nullptr)
+                    p.lse[(int64_t)w.s * p.n_heads + head0 + tid] = (t + log2f(sum)) * (float)kLn2;
+            } else {
+                part_ml[tid] = make_float2(t, sum);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kHeads / kPass; ++q) {
+            if (q * kPass >= heads) break;  // heads is the same for the whole CTA
+            const int n = q >> 1;           // block of 8; its lower or upper four heads
+            if (((lane & 3) >> 1) == (q & 1)) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float f = ex2_approx(m[n][i] - top[n][i]);
+                    float* row = merge + (warp * kPass + (hc & 3) + i) * kDim + (lane >> 2);
+#pragma unroll
+                    for (int d = 0; d < kDim / 16; ++d) {
+                        row[d * 16] = o[n][d][i] * f;
+                        row[d * 16 + 8] = o[n][d][i + 2] * f;
+                    }
+                }
+            }
+            __syncthreads();
+            for (int x = tid; x < kPass * kDim; x += kThreads) {
+                const int h = q * kPass + x / kDim, e = x % kDim;
+                if (h >= heads || e >= p.head_dim) continue;
+                float sum = 0.f;
+#pragma unroll
+                for (int y = 0; y < kWarps; ++y) sum += merge[y * kPass * kDim + x];
+                if (whole)
+                    p.out[(int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e] =
+                        round16<kBf16>(sum * part_w[h]);
+                else
+                    part_o[h * p.head_dim + e] = sum;
+            }
+            __syncthreads();
+        }
+        if (whole) continue;
+        // ---- a unit that several CTAs share: the last one to finish joins the parts --------------
+        const int c_last = (int)((w.unit0 + w.tiles() - 1) / per);
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) last_one = atomicAdd(&p.tickets[c_first], 1) == c_last - c_first;
+        __syncthreads();
+        if (!last_one) continue;
+        __threadfence();
+        if (tid == 0) p.tickets[c_first] = 0;  // for the next call
+        auto ml_of = [&](int c, int h) {
+            return __ldcg(&p.part_ml[(2 * (int64_t)c + (c == c_first ? 1 : 0)) * p.part_heads + h]);
+        };
+        for (int x = tid; x < heads * p.head_dim; x += kThreads) {
+            const int h = x / p.head_dim, e = x - h * p.head_dim;
+            float t = kNegHuge;
+            for (int c = c_first; c <= c_last; ++c) t = fmaxf(t, ml_of(c, h).x);
+            float sum = 0.f, acc = 0.f;
+#pragma unroll 4
+            for (int c = c_first; c <= c_last; ++c) {
+                const float2 ml = ml_of(c, h);
+                const float f = ex2_approx(ml.x - t);
+                sum += ml.y * f;
+                acc += __ldcg(&p.part_o[((2 * (int64_t)c + (c == c_first ? 1 : 0)) * p.part_heads + h) * p.head_dim +
+                                        e]) *
+                       f;
+            }
+            p.out[(int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e] = round16<kBf16>(acc / sum);
+            if (e == 0 && p.lse != nullptr)
+                p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (t + log2f(sum)) * (float)kLn2;
+        }
+        __syncthreads();  // last_one is written again by the next shared unit
+    }
+    cp_wait<0>();
+}
+
+template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages>
+cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
+    static unsigned char allowed[kMaxDevices];
+    auto kernel = attend_kernel<kBf16, kDim, kTiles, kWarps, kStages>;
+    cudaError_t e = allow_max_dynamic_smem((const void*)kernel, dp, allowed);
+    if (e != cudaSuccess) return e;
+    const size_t smem = (size_t)kWarps * kStages * 2 * kKeys * kDim * 2 + (size_t)kWarps * 4 * kDim * 4;
+    const int grid = dp.n_sm < kAttendMaxCtas ? dp.n_sm : kAttendMaxCtas;
+    kernel<<<grid, kWarps * 32, smem, st>>>(p);
+    return cudaGetLastError();
+}
+
+template <bool kBf16>
+cudaError_t launch_dim(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
+    const bool wide = p.group > 8;
+    if (p.head_dim <= 64)
+        return wide ? launch<kBf16, 64, 2, 8, 6>(p, dp, st) : launch<kBf16, 64, 1, 8, 6>(p, dp, st);
+    if (p.head_dim <= 128)
+        return wide ? launch<kBf16, 128, 2, 8, 3>(p, dp, st) : launch<kBf16, 128, 1, 8, 3>(p, dp, st);
+    return wide ? launch<kBf16, 256, 2, 4, 3>(p, dp, st) : launch<kBf16, 256, 1, 4, 3>(p, dp, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st) {
+    TraceRange trace("sirllm:attend");
+    DeviceProps dp;
+    cudaError_t e = device_props(&dp);
+    if (e != cudaSuccess) return e;
+    return bf16 ? launch_dim<true>(p, dp, st) : launch_dim<false>(p, dp, st);
+}
+
+}  // namespace sirllm

@@ -140,6 +140,60 @@ struct RopeParams {
     int32_t capacity, keep_stride, planes_per_stream, head_dim, layout, planes_per_group;
 };
 
+struct AppendParams {
+    const char *q, *k_new, *v_new;           // rows [n_streams*max_new], strides in elements
+    const void *q_weight, *k_weight;         // nullable: [head_dim] of the cache's type
+    const int32_t *first_slot, *n_new;       // n_new nullable: max_new for every stream
+    char *q_out, *k, *v;
+    int32_t* status;
+    int64_t q_stride, k_stride, v_stride, q_out_stride;
+    // theta_i / 2pi for the d/2 pairs of a head, computed once per call on the host
+    double turns[SIRLLM_MAX_HEAD_DIM / 2];
+    float eps;
+    int32_t n_heads, n_kv_heads, head_dim, capacity, max_new, n_streams, layout, normed;
+    int32_t planes_per_stream, layer_plane;  // planes of a stream, the layer's first
+    int32_t heads_all;                       // n_heads + 2 * n_kv_heads
+    int32_t team, heads_per_group, groups;   // set by the launcher
+};
+
+constexpr int kAttendMaxCtas = 256;   // CTAs of an attention call, at most
+constexpr int kAttendPartHeads = 16;  // query heads of a unit, at most
+
+// ---- workspace of the attention call ------------------------------------------------------
+//   [0, 256)                     header: int32 status word
+//   tickets[kAttendMaxCtas]      arrivals at the unit whose first part a CTA holds
+//   part_ml[2*kAttendMaxCtas][kAttendPartHeads]            (reference, sum) per part and head
+//   part_o[2*kAttendMaxCtas][kAttendPartHeads][head_dim]   weighted rows per part and head
+struct AttendLayout {
+    size_t tickets_off, part_ml_off, part_o_off, zeroed, total;
+};
+
+struct AttendParams {
+    const char *q, *k, *v;
+    const int32_t* kv_len;
+    uint16_t* out;
+    float* lse;                              // nullable
+    int32_t* status;
+    int32_t* tickets;
+    float2* part_ml;
+    float* part_o;
+    int64_t q_stride, out_stride;            // elements between streams
+    float scale_log2;                        // scale * log2 e
+    int32_t n_streams, n_heads, head_dim, capacity;
+    int32_t group, blocks, units;            // query heads per K/V head; blocks of them; units per stream
+    int32_t planes_per_stream, layer_plane;
+    int32_t part_heads;
+};
+
+struct HeadParams {
+    const int32_t *token_ids, *n_new;        // n_new nullable: max_new for every stream
+    float2* pairs_out;                       // [rows][pair_stride]
+    float* target_out;                       // [rows]
+    int32_t* status;
+    int64_t rows, row0, n_cols, col0, pair_stride;
+    int32_t max_new, d_model, n_tiles, tile_cols, row_blocks, bf16;
+};
+
 struct CompactParams {
     const char* src[2];  // K, V (nullable)
     char* dst[2];
@@ -170,6 +224,14 @@ bool compact_is_small_job(int64_t planes, int keep_stride, int row_bytes);
 cudaError_t launch_select(const SelectParams& p, int n_streams, cudaStream_t st, bool overlap);
 cudaError_t launch_policy_ranks(const PolicyParams& p, int n_streams, cudaStream_t st);
 cudaError_t launch_rerotate(const RopeParams& p, int n_streams, bool bf16, cudaStream_t st);
+cudaError_t launch_append(const AppendParams& p, bool bf16, cudaStream_t st);
+// `group` > 8 query heads per K/V head: units of 16 query heads, else of 8
+inline int attend_unit_heads(int group) { return group > 8 ? 16 : 8; }
+cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st);
+// vocabulary columns of one tile of the LM head's product, for a call of so many rows and columns
+int head_tile_cols(int64_t rows, int64_t n_cols);
+cudaError_t launch_head(const HeadParams& p, const void* hidden, int64_t hidden_stride, const void* weight,
+                        int64_t weight_stride, cudaStream_t st);
 cudaError_t launch_compact_plan(const CompactParams& p, int n_streams, int32_t* first_moved,
                                 cudaStream_t st);
 cudaError_t launch_compact(const CompactParams& p, cudaStream_t st, bool overlap);

@@ -1,0 +1,185 @@
+"""What the calls of a decode step refuse, on the host and before anything is enqueued (no GPU
+needed): ``sirllm_append_kv``, ``sirllm_attend``, ``sirllm_head_pairs``."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2405_12528_b200 import binding as B
+
+
+@pytest.fixture(scope="module")
+def lib(cuda_library):
+    return B.lib()
+
+
+def cfg(**kw):
+    base = dict(n_streams=2, n_layers=3, n_kv_heads=2, head_dim=64, capacity=128, budget=64, n_sink=4, n_recent=8,
+                max_new=8, vocab=1000, logits_dtype="f32", kv_dtype="bf16")
+    base.update(kw)
+    return B.make_config(**base)
+
+
+P, WS = 0x2000, 0x1000      # never dereferenced
+
+
+def append(lib, c=None, **kw):
+    a = dict(layer=0, q=P, n_heads=4, qs=256, k_new=P, ks=128, v_new=P, vs=128, wq=None, wk=None, eps=1e-6, base=1e4,
+             layout=0, first=P, n_new=None, q_out=P, os=256, k=P, v=P, ws=WS)
+    a.update(kw)
+    return lib.sirllm_append_kv(ctypes.byref(c or cfg()), *a.values(), None)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (B.ERR_NULL, dict(k_new=None)), (B.ERR_NULL, dict(v_new=None)), (B.ERR_NULL, dict(first=None)),
+    (B.ERR_NULL, dict(k=None)), (B.ERR_NULL, dict(v=None)), (B.ERR_NULL, dict(ws=None)),
+    (B.ERR_NULL, dict(q=None)), (B.ERR_NULL, dict(q_out=None)),
+    (B.ERR_BAD_CONFIG, dict(layer=-1)), (B.ERR_BAD_CONFIG, dict(layer=3)), (B.ERR_BAD_CONFIG, dict(n_heads=0)),
+    (B.ERR_BAD_CONFIG, dict(n_heads=-4)), (B.ERR_BAD_CONFIG, dict(q=None, q_out=None)),
+    (B.ERR_BAD_CONFIG, dict(n_heads=0x3FFFFFFF)),
+    (B.ERR_BAD_CONFIG, dict(base=0.0)), (B.ERR_BAD_CONFIG, dict(base=-1.0)), (B.ERR_BAD_CONFIG, dict(base=math.inf)),
+    (B.ERR_BAD_CONFIG, dict(base=math.nan)), (B.ERR_BAD_CONFIG, dict(layout=2)), (B.ERR_BAD_CONFIG, dict(eps=-1e-6)),
+    (B.ERR_BAD_CONFIG, dict(eps=math.nan)), (B.ERR_BAD_CONFIG, dict(qs=248)), (B.ERR_BAD_CONFIG, dict(os=248)),
+    (B.ERR_BAD_CONFIG, dict(ks=120)), (B.ERR_BAD_CONFIG, dict(vs=120)),
+    (B.ERR_ALIGN, dict(q=P + 8)), (B.ERR_ALIGN, dict(k=P + 2)), (B.ERR_ALIGN, dict(wk=P + 2)), (B.ERR_ALIGN, dict(qs=260)),
+    (B.ERR_ALIGN, dict(vs=132)), (B.ERR_ALIGN, dict(ws=WS + 16)),
+])
+def test_append_refusals(lib, want, kw):
+    assert append(lib, **kw) == want
+
+
+def test_append_refuses_heads_of_half_vectors(lib):
+    assert append(lib, cfg(head_dim=40), qs=160, os=160, ks=80, vs=80) == B.ERR_BAD_CONFIG
+    assert append(lib, cfg(budget=5)) == B.ERR_BAD_CONFIG
+
+
+def attend(lib, c=None, **kw):
+    a = dict(layer=0, q=P, n_heads=4, qs=256, k=P, v=P, kv_len=P, scale=0.1, out=P, os=256, lse=None, ws=WS)
+    a.update(kw)
+    return lib.sirllm_attend(ctypes.byref(c or cfg()), *a.values(), None)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (B.ERR_NULL, dict(q=None)), (B.ERR_NULL, dict(k=None)), (B.ERR_NULL, dict(v=None)), (B.ERR_NULL, dict(kv_len=None)),
+    (B.ERR_NULL, dict(out=None)), (B.ERR_NULL, dict(ws=None)), (B.ERR_BAD_CONFIG, dict(layer=3)),
+    (B.ERR_BAD_CONFIG, dict(layer=-1)), (B.ERR_BAD_CONFIG, dict(n_heads=0)), (B.ERR_BAD_CONFIG, dict(n_heads=3)),
+    (B.ERR_BAD_CONFIG, dict(n_heads=-2)), (B.ERR_BAD_CONFIG, dict(scale=math.nan)),
+    (B.ERR_BAD_CONFIG, dict(scale=math.inf)), (B.ERR_BAD_CONFIG, dict(qs=128)), (B.ERR_BAD_CONFIG, dict(os=128)),
+    (B.ERR_ALIGN, dict(q=P + 2)), (B.ERR_ALIGN, dict(out=P + 8)), (B.ERR_ALIGN, dict(qs=258)), (B.ERR_ALIGN, dict(os=260)),
+    (B.ERR_ALIGN, dict(ws=WS + 8)),
+])
+def test_attend_refusals(lib, want, kw):
+    assert attend(lib, **kw) == want
+
+
+def test_attend_refuses_heads_wider_than_its_registers(lib):
+    wide = cfg(head_dim=264)
+    assert attend(lib, wide, qs=2048, os=2048) == B.ERR_TOO_LARGE
+    assert B.sirllm_attend_workspace_bytes(wide) == 0
+    assert lib.sirllm_attend_workspace_init(ctypes.byref(wide), WS, None) == B.ERR_TOO_LARGE
+    n = B.sirllm_attend_workspace_bytes(cfg())
+    assert n > 0 and n % 256 == 0 and n < B.sirllm_attend_workspace_bytes(cfg(head_dim=B.MAX_ATTEND_HEAD_DIM))
+    assert B.sirllm_attend_workspace_bytes(cfg(budget=5)) == 0
+    assert lib.sirllm_attend_workspace_init(ctypes.byref(cfg()), None, None) == B.ERR_NULL
+    assert lib.sirllm_attend_workspace_init(ctypes.byref(cfg()), WS + 8, None) == B.ERR_ALIGN
+
+
+def head(lib, c=None, **kw):
+    a = dict(hidden=P, hs=64, weight=P, wst=64, d=64, dtype=B.BF16, col0=0, n_cols=1000, ids=P, n_new=None, pairs=P,
+             ps=1000, target=P, ws=WS)
+    a.update(kw)
+    return lib.sirllm_head_pairs(ctypes.byref(c or cfg()), *a.values(), None)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (B.ERR_NULL, dict(hidden=None)), (B.ERR_NULL, dict(weight=None)), (B.ERR_NULL, dict(ids=None)),
+    (B.ERR_NULL, dict(pairs=None)), (B.ERR_NULL, dict(target=None)), (B.ERR_NULL, dict(ws=None)),
+    (B.ERR_BAD_CONFIG, dict(d=0)), (B.ERR_BAD_CONFIG, dict(dtype=B.F32)), (B.ERR_BAD_CONFIG, dict(n_cols=0)),
+    (B.ERR_BAD_CONFIG, dict(n_cols=1001)), (B.ERR_BAD_CONFIG, dict(col0=1)), (B.ERR_BAD_CONFIG, dict(col0=-1)),
+    (B.ERR_BAD_CONFIG, dict(hs=56)), (B.ERR_BAD_CONFIG, dict(wst=56)), (B.ERR_BAD_CONFIG, dict(ps=1)),
+    (B.ERR_BAD_CONFIG, dict(wst=1 << 39)),
+    (B.ERR_ALIGN, dict(hidden=P + 2)), (B.ERR_ALIGN, dict(weight=P + 8)), (B.ERR_ALIGN, dict(hs=68)),
+    (B.ERR_ALIGN, dict(wst=66)), (B.ERR_ALIGN, dict(pairs=P + 4)), (B.ERR_ALIGN, dict(target=P + 2)),
+    (B.ERR_ALIGN, dict(ws=WS + 4)),
+])
+def test_head_refusals(lib, want, kw):
+    assert head(lib, **kw) == want
+
+
+def test_head_tiles_cover_the_columns(lib):
+    for rows in (1, 128, 129, 4096):
+        for n in (1, 31, 32, 33, 255, 257, 32000, 50257, 128256):
+            c = cfg(n_streams=1, capacity=max(rows, 64), max_new=rows, vocab=128256)
+            t = B.sirllm_head_tiles(c, n)
+            assert 1 <= t <= (n + 15) // 16 + 1 and t == B.sirllm_head_tiles(c, n)
+    assert B.sirllm_head_tiles(cfg(), 0) == 0 and B.sirllm_head_tiles(cfg(), 1001) == 0
+    assert B.sirllm_head_tiles(cfg(budget=5), 10) == 0
+
+
+def test_binding_refuses_wrong_tensors_before_the_library(lib):
+    c = cfg(head_dim=64)
+    bf = torch.bfloat16
+    z = lambda *s, dt=bf: torch.zeros(*s, dtype=dt)
+    i = lambda n: torch.zeros(n, dtype=torch.int32)
+    kv = z(2, 3, 2, 128, 64)
+    ws = torch.zeros(B.sirllm_workspace_bytes(c), dtype=torch.uint8)
+    wa = torch.zeros(B.sirllm_attend_workspace_bytes(c), dtype=torch.uint8)
+
+    def refused(fn, *a, needle):
+        with pytest.raises(B.SirllmError) as err:
+            fn(c, *a)
+        assert needle in str(err.value), str(err.value)
+
+    def app(needle, **kw):
+        a = dict(layer=0, q=z(16, 4, 64), k_new=z(16, 2, 64), v_new=z(16, 2, 64), q_weight=z(64), k_weight=None,
+                 eps=1e-6, rope_base=1e4, layout=0, first_slot=i(2), n_new=i(2), q_out=z(16, 4, 64), k=kv, v=kv, ws=ws)
+        a.update(kw)
+        refused(B.sirllm_append_kv, *a.values(), needle=needle)
+
+    app("CUDA tensor")                                   # all sizes right: as far as residence
+    app("q has shape", q=z(15, 4, 64), q_out=z(16, 4, 64))
+    app("q_out has shape", q_out=z(16, 3, 64))
+    app("k_new has shape", k_new=z(16, 3, 64))
+    app("v_new has shape", v_new=z(16, 2, 32))
+    app("dtype", q=z(16, 4, 64, dt=torch.float16))
+    app("dtype", q_weight=z(64, dt=torch.float32))
+    app("needs", k_weight=z(63))
+    app("heads must be dense", k_new=z(16, 64, 2).transpose(1, 2))
+    app("rows overlap", v_new=z(2, 64).as_strided((16, 2, 64), (0, 64, 1)))
+    app("needs", first_slot=i(1))
+    app("needs", k=kv[:, :2])
+    app("needs", ws=ws[:-1])
+
+    def att(needle, **kw):
+        a = dict(layer=0, q=z(2, 4, 64), k=kv, v=kv, kv_len=i(2), scale=None, out=z(2, 4, 64), lse=None, ws=wa)
+        a.update(kw)
+        refused(B.sirllm_attend, *a.values(), needle=needle)
+
+    att("CUDA tensor")
+    att("q has shape", q=z(1, 4, 64))
+    att("out has shape", out=z(2, 5, 64))
+    att("dtype", out=z(2, 4, 64, dt=torch.float32))
+    att("needs", kv_len=i(1))
+    att("needs", lse=torch.zeros(7))
+    att("needs", ws=wa[:-1])
+
+    tiles = B.sirllm_head_tiles(c, 1000)
+    pairs = torch.zeros(16, tiles, 2)
+
+    def hd(needle, **kw):
+        a = dict(hidden=z(16, 96), weight=z(1000, 96), col0=0, token_ids=i(16), n_new=None, pairs_out=pairs,
+                 target_out=torch.zeros(16), ws=ws)
+        a.update(kw)
+        refused(B.sirllm_head_pairs, *a.values(), needle=needle)
+
+    hd("CUDA tensor")
+    hd("hidden has shape", hidden=z(15, 96))
+    hd("do not match", weight=z(1000, 88))
+    hd("do not match", weight=z(1000, 96, dt=torch.float16))
+    hd("hidden has dtype", hidden=z(16, 96, dt=torch.float32), weight=z(1000, 96, dt=torch.float32))
+    hd("tiles per row", pairs_out=torch.zeros(16, tiles + 1, 2))
+    hd("tiles per row", weight=z(1001, 96))
+    hd("rows must be dense", weight=z(96, 1000).t())
+    hd("needs", token_ids=i(15))
+    hd("needs", target_out=torch.zeros(15))
