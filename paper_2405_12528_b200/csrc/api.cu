@@ -485,7 +485,8 @@ int sirllm_score_pairs(const sirllm_config* cfg, const void* pairs, int32_t n_ti
     if ((rc = check_pairs(src)) != SIRLLM_OK) return rc;
     PairScoreParams pp = pair_params(*cfg, src, token_ids, n_new, ws);
     pp.out_entropy = out_entropy;
-    cudaError_t e = launch_score_pairs(pp, (cudaStream_t)cuda_stream, false);
+    // launched programmatically: it waits for all earlier work on the stream before it reads anything
+    cudaError_t e = launch_score_pairs(pp, (cudaStream_t)cuda_stream, true);
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "score_pairs");
 }
 
@@ -750,9 +751,7 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
 
 int32_t sirllm_head_tiles(const sirllm_config* cfg, int64_t n_cols) {
     if (validate_config(cfg) != SIRLLM_OK || n_cols < 1 || n_cols > cfg->vocab) return 0;
-    const int64_t rows = (int64_t)cfg->n_streams * cfg->max_new;
-    const int cols = head_tile_cols(rows, n_cols);
-    return (int32_t)((n_cols + cols - 1) / cols);
+    return head_tiling((int64_t)cfg->n_streams * cfg->max_new, n_cols).n_parts;
 }
 
 int sirllm_head_pairs(const sirllm_config* cfg, const void* hidden, int64_t hidden_row_stride, const void* weight,
@@ -764,9 +763,12 @@ int sirllm_head_pairs(const sirllm_config* cfg, const void* hidden, int64_t hidd
     if (!hidden || !weight || !token_ids || !pairs_out || !target_out || !ws) return SIRLLM_ERR_NULL;
     if (d_model < 1 || (dtype != SIRLLM_BF16 && dtype != SIRLLM_F16) || n_cols < 1 || col0 < 0 ||
         col0 > cfg->vocab - n_cols || hidden_row_stride < d_model || weight_row_stride < d_model ||
-        hidden_row_stride > ((int64_t)1 << 38) || weight_row_stride > ((int64_t)1 << 38) ||
-        pair_row_stride < sirllm_head_tiles(cfg, n_cols))
+        hidden_row_stride > ((int64_t)1 << 38) || weight_row_stride > ((int64_t)1 << 38))
         return SIRLLM_ERR_BAD_CONFIG;
+    // rows and columns are counted in 32 bits
+    if ((int64_t)cfg->n_streams * cfg->max_new > 0x7FFF0000 || n_cols > 0x7FFF0000) return SIRLLM_ERR_TOO_LARGE;
+    const HeadTiling tiling = head_tiling((int64_t)cfg->n_streams * cfg->max_new, n_cols);
+    if (pair_row_stride < tiling.n_parts) return SIRLLM_ERR_BAD_CONFIG;
     if (misaligned(hidden, 16) || misaligned(weight, 16) || hidden_row_stride % 8 != 0 || weight_row_stride % 8 != 0 ||
         misaligned(pairs_out, 8) || misaligned(target_out, 4) || misaligned(ws, 256))
         return SIRLLM_ERR_ALIGN;
@@ -783,10 +785,8 @@ int sirllm_head_pairs(const sirllm_config* cfg, const void* hidden, int64_t hidd
     p.pair_stride = pair_row_stride;
     p.max_new = cfg->max_new;
     p.d_model = d_model;
-    p.tile_cols = head_tile_cols(p.rows, n_cols);
-    p.n_tiles = sirllm_head_tiles(cfg, n_cols);
     p.bf16 = dtype == SIRLLM_BF16;
-    cudaError_t e = launch_head(p, hidden, hidden_row_stride, weight, weight_row_stride, (cudaStream_t)cuda_stream);
+    cudaError_t e = launch_head(p, tiling, hidden, hidden_row_stride, weight, weight_row_stride, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "head_pairs");
 }
 

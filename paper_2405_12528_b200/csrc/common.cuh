@@ -190,8 +190,20 @@ struct HeadParams {
     float2* pairs_out;                       // [rows][pair_stride]
     float* target_out;                       // [rows]
     int32_t* status;
-    int64_t rows, row0, n_cols, col0, pair_stride;
-    int32_t max_new, d_model, n_tiles, tile_cols, row_blocks, bf16;
+    int64_t rows, n_cols, col0, pair_stride;
+    int32_t max_new, d_model, bf16;
+    // set by the launcher
+    int32_t row0;                            // first row of this launch
+    int32_t row_blocks;                      // blocks of rows of this launch
+    int32_t n_parts, n_tiles, part_tiles, tile_cols, half_cols;
+    int32_t a_bytes, b_bytes, load_bytes, stage_bytes, stages;  // a box of each, a stage of boxes
+};
+
+// How the LM head's product is cut: column ranges ("parts", one pair per row each) of part_tiles
+// tiles of tile_cols columns, computed by one CTA or a pair of CTAs.
+struct HeadTiling {
+    int32_t ctas, n_parts, part_tiles, tile_cols;
+    int32_t half_cols;  // columns of a tile that the first of a row's two threads reduces
 };
 
 struct CompactParams {
@@ -228,10 +240,9 @@ cudaError_t launch_append(const AppendParams& p, bool bf16, cudaStream_t st);
 // `group` > 8 query heads per K/V head: units of 16 query heads, else of 8
 inline int attend_unit_heads(int group) { return group > 8 ? 16 : 8; }
 cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st);
-// vocabulary columns of one tile of the LM head's product, for a call of so many rows and columns
-int head_tile_cols(int64_t rows, int64_t n_cols);
-cudaError_t launch_head(const HeadParams& p, const void* hidden, int64_t hidden_stride, const void* weight,
-                        int64_t weight_stride, cudaStream_t st);
+HeadTiling head_tiling(int64_t rows, int64_t n_cols);
+cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hidden, int64_t hidden_stride,
+                        const void* weight, int64_t weight_stride, cudaStream_t st);
 cudaError_t launch_compact_plan(const CompactParams& p, int n_streams, int32_t* first_moved,
                                 cudaStream_t st);
 cudaError_t launch_compact(const CompactParams& p, cudaStream_t st, bool overlap);

@@ -6,16 +6,24 @@
 // pairs feed sirllm_score_pairs and sirllm_step_pairs.
 //
 // 2 * rows * columns * d operations on the tensor cores against columns * d * 2 bytes of weight:
-// many rows are bound by tcgen05, up to about a hundred rows by reading the weight once.  A
-// persistent CTA per SM walks output tiles of 128 rows x up to 256 vocabulary columns, rows
-// fastest so that the CTAs at work share weight tiles in L2 and the weight leaves HBM once.
-// Warp roles: one lane feeds a ring of TMA loads (64 elements of d per stage, 128-byte swizzle),
-// one lane issues tcgen05.mma, four warps reduce the finished accumulator - one thread per row,
-// no exchange between threads - while the next tile is multiplied into the other half of TMEM.
-// Rows behind the end of a batch or of the vocabulary come in as zeros from TMA and are left out
-// of the reduction.  With one block of rows the tile width is chosen so that the tiles fill whole
-// waves of SMs.  Products and sums are fp32 (the tensor core's accumulator); nothing is rounded to
-// 16 bits on the way.
+// many rows are bound by tcgen05 (and by what feeds it), up to about a hundred rows by reading
+// the weight once.  Two forms of one kernel, both persistent:
+//   kCtas = 2  more than 128 rows.  A pair of CTAs (cta_group::2) multiplies 256 rows by up to 256
+//              columns; each CTA loads its own 128 rows and half of the columns, so an SM takes in
+//              64 bytes per clock of tensor work where a single CTA's 128 x 256 tile needs 96 -
+//              more than L2 delivers.  Tiles go rows fastest: the CTAs at work share weight tiles
+//              in L2 and the weight leaves HBM once.
+//   kCtas = 1  up to 128 rows.  Every CTA streams an equal range of weight rows past the one block
+//              of hidden rows (only as many of them as there are, so that the ring's space goes
+//              to the weight) and keeps one running pair per row for its whole range.
+// Warp roles: one lane feeds a ring of TMA loads (128 elements of d per stage, 128-byte swizzle),
+// one lane issues tcgen05.mma, eight warps take the accumulators out of TMEM, which holds two
+// of them - one is read while the other is multiplied into.
+//
+// Precision: the tensor core's fp32 accumulator truncates; measured, its sums run short by 1e-9 of
+// the logit per element of d (4e-6 at d = 4096, a bias that does not average out).  So d is cut
+// into chunks of kChunkSteps stages: a chunk is summed in TMEM, the chunks in registers with
+// rounded additions (128 columns of one row per thread).  Nothing is rounded to 16 bits.
 #include <atomic>
 
 #include <cuda.h>
@@ -26,105 +34,181 @@ namespace sirllm {
 
 namespace {
 
-constexpr int kHeadRows = 128;       // rows of a tile (TMEM lanes)
-constexpr int kHeadMaxCols = 256;    // vocabulary columns of a tile, a multiple of 32
-constexpr int kHeadDepth = 64;       // elements of d per stage: one 128-byte swizzle row
-constexpr int kHeadStages = 4;
-constexpr int kHeadThreads = 256;
+constexpr int kHeadRows = 128;       // rows of a CTA (TMEM lanes)
+constexpr int kHeadMaxCols = 256;    // vocabulary columns of a tile, at most
+constexpr int kHeadDepth = 64;       // elements of d per TMA box: one 128-byte swizzle row
+constexpr int kBoxes = 2;            // boxes of A and of B per stage
+constexpr int kHeadMaxStages = 8;
+constexpr int kChunkSteps = 8;       // stages summed in TMEM before they are added up in registers
+constexpr int kHeadReducers = 256;   // threads that reduce: two per row, half of the columns each
+constexpr int kHeadThreads = 128 + kHeadReducers;
+// Registers: 168 a thread at launch (64512 for 384 threads).  The reducers hold 128 sums each; the
+// four warps in front of them hand over what they do not need: 128 * 72 + 256 * 216 = 64512.
+constexpr int kFeedRegs = 72, kReduceRegs = 216;
+static_assert(128 * kFeedRegs + kHeadReducers * kReduceRegs <= kHeadThreads * 168, "more registers than the launch has");
 constexpr int kHeadRowBlocks = 4096; // row blocks per launch (the list of blocks with work)
+constexpr int kARoom = kHeadRows * kHeadDepth * 2;  // what an instruction reads of A, loaded or not
+constexpr int kHeadRing = 212 * 1024;
+constexpr size_t kHeadSmem = 1024 + kHeadRing;
+constexpr uint32_t kNapNs = 20000, kNapLimit = 1u << 17;  // a wait gives up after seconds
 constexpr float kNoLogit = -2.0e38f;  // below any running maximum; times log2 e it is still finite
-constexpr int kABytes = kHeadRows * kHeadDepth * 2;
-constexpr int kBBytes = kHeadMaxCols * kHeadDepth * 2;
-constexpr int kStageBytes = kABytes + kBBytes;
-constexpr size_t kHeadSmem = 1024 + (size_t)kHeadStages * kStageBytes;
 
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+template <int kCtas>
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if (kCtas == 2)  // the barrier may be the pair's other CTA's
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, "
+            "%4}], [%2];" ::"r"(dst),
+            "l"(map), "r"(bar), "r"(x), "r"(y)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::
+                "r"(dst),
+            "l"(map), "r"(bar), "r"(x), "r"(y)
+            : "memory");
+}
+// Polls of a barrier go through shared memory, which the tensor core needs for its operands: a
+// waiting thread sleeps in the poll (up to kNapNs) instead of spinning.
+__device__ __forceinline__ bool mbar_nap(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
-            dst),
-        "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y)
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(kNapNs)
         : "memory");
+    return ok != 0;
 }
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+// the address of a shared variable in the pair's first CTA
+__device__ __forceinline__ uint32_t in_first_cta(const void* p) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
+    return a;
 }
-// Shared-memory operand of tcgen05.mma, K-major rows of 128 bytes with the 128-byte swizzle:
-// groups of 8 rows are 1024 bytes apart.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) |
-           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
-        : "memory");
+// Shared-memory operand of tcgen05.mma, K-major rows of 128 bytes with the 128-byte swizzle: the
+// low word holds the address / 16, the high word says that groups of 8 rows are 1024 bytes apart.
+__device__ __forceinline__ uint32_t operand_lo(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
+constexpr uint32_t kOperandHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+template <int kCtas>
+__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, bool accumulate) {
+    if (kCtas == 2)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+            "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)accumulate), "r"(kOperandHi)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+            "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)accumulate), "r"(kOperandHi)
+            : "memory");
 }
+// signals the barrier (in both CTAs of a pair) once the products issued so far are done
+template <int kCtas>
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-                 : "memory");
+    if (kCtas == 2)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                smem_u32(bar)),
+            "h"((uint16_t)3)
+            : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+                     : "memory");
 }
-__device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t addr) {
-    uint32_t r[32];
+template <int kCtas>
+__device__ __forceinline__ void tmem_alloc(uint32_t* where) {
+    if (kCtas == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(512u)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(512u)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <int kCtas>
+__device__ __forceinline__ void tmem_free(uint32_t tmem) {
+    if (kCtas == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+__device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t addr) {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,"
-        "%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+template <int kCtas>
+__device__ __forceinline__ void cta_or_pair_sync() {
+    if (kCtas == 2)
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else
+        __syncthreads();
 }
 
-// new tokens of a stream that are scored
-__device__ __forceinline__ int stream_rows(const HeadParams& p, int64_t s) {
-    return p.n_new ? min(p.n_new[s], p.max_new) : p.max_new;
+// whether a row holds a token to score: t < n_new[s]
+__device__ __forceinline__ bool row_scored(const HeadParams& p, int row) {
+    if (row >= p.rows) return false;
+    if (p.n_new == nullptr) return true;
+    const int s = row / p.max_new;
+    return row - s * p.max_new < p.n_new[s];
 }
 
+template <int kCtas>
 __global__ void __launch_bounds__(kHeadThreads, 1)
 head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t full[kHeadStages], empty[kHeadStages], acc_full[2], acc_empty[2], drained;
+    __shared__ __align__(8) uint64_t full[kHeadMaxStages], empty[kHeadMaxStages], acc_full[2], acc_empty[2], drained;
+    __shared__ float4 other_half[2][kHeadRows];
     __shared__ uint32_t tmem_base;
     __shared__ int n_active;
     __shared__ volatile int gave_up;
     __shared__ unsigned short active[kHeadRowBlocks];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = kCtas == 2 ? (int)(blockIdx.x & 1) : 0;  // a cluster is two consecutive CTAs
     const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    constexpr int kBlockRows = kHeadRows * kCtas;
 
     if (tid == 0) {
-        for (int i = 0; i < kHeadStages; ++i) {
+        for (int i = 0; i < kHeadMaxStages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
-            mbar_init(&acc_empty[i], 4);
+            mbar_init(&acc_empty[i], kCtas * kHeadReducers / 32);
         }
         mbar_init(&drained, 1);
         mbar_init_fence();
         gave_up = 0;
     }
-    if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)),
-                     "r"(512u)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    // row blocks with a row to score, in order
+    if (warp == 1) tmem_alloc<kCtas>(&tmem_base);
+    // Everything above overlaps the end of the kernel before; from here on its results are read.
+    // (Dependents are not released early: CTAs of the next kernel that take an SM's last room while
+    // this one drains set the CTAs of the call after it out of step, which cost 8-25 %.)
+    grid_dependency_wait();
+    // row blocks with a row to score, in order (a single block is not looked at: without a row to
+    // score nothing is written)
     for (int b = warp; b < p.row_blocks; b += kHeadThreads / 32) {
-        bool any = false;
-        for (int i = lane; i < kHeadRows; i += 32) {
-            const int64_t row = p.row0 + (int64_t)b * kHeadRows + i;
-            if (row < p.rows) {
-                const int64_t s = row / p.max_new;
-                any |= (int)(row - s * p.max_new) < stream_rows(p, s);
-            }
-        }
+        bool any = p.row_blocks == 1;
+        for (int i = lane; i < kBlockRows && p.row_blocks > 1; i += 32) any |= row_scored(p, p.row0 + b * kBlockRows + i);
         any = __any_sync(0xFFFFFFFFu, any);
         if (lane == 0) active[b] = any;
     }
@@ -142,165 +226,228 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    cta_or_pair_sync<kCtas>();  // the pair's barriers are set up before either CTA signals them
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_base;
     const int blocks = n_active;
-    const int64_t n_work = (int64_t)blocks * p.n_tiles;
-    const int depth_steps = (p.d_model + kHeadDepth - 1) / kHeadDepth;
+    const int n_work = blocks * p.n_parts;  // the launcher keeps it below 2^30
+    const int w0 = blockIdx.x / kCtas, w_step = gridDim.x / kCtas;
+    const int steps = (p.d_model + kBoxes * kHeadDepth - 1) / (kBoxes * kHeadDepth);
+    const int chunks = (steps + kChunkSteps - 1) / kChunkSteps;
+    // tiles of a part that hold a column
+    auto tiles_of = [&](int part) {
+        return min(p.part_tiles, p.n_tiles - part * p.part_tiles);
+    };
 
     // A wait that runs out raises the flag and every role leaves; the others see it or run out too.
     auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-        for (uint32_t i = 0; i < kMbarSpinLimit; ++i) {
-            if (mbar_try_wait(bar, parity)) return true;
+        for (uint32_t i = 0; i < kNapLimit; ++i) {
+            if (mbar_nap(bar, parity)) return true;
             if (gave_up) return false;
         }
         gave_up = 1;
         return false;
     };
 
-    if (warp == 0) {
-        if (lane == 0) {  // loads
-            int stage = 0;
-            uint32_t phase = 0;
-            int64_t issued = 0;
-            const uint32_t bytes = (uint32_t)(kABytes + p.tile_cols * kHeadDepth * 2);
-            bool ok = true;
-            for (int64_t w = blockIdx.x; w < n_work && ok; w += gridDim.x) {
-                const int row = (int)(p.row0 + (int64_t)active[w % blocks] * kHeadRows);
-                const int col = (int)(w / blocks) * p.tile_cols;
-                for (int k = 0; k < depth_steps; ++k) {
-                    if (!wait(&empty[stage], phase ^ 1u)) {
-                        ok = false;
-                        break;
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFeedRegs));
+        // The loops of these two roles are run by whole warps, so that counters and descriptors stay
+        // in uniform registers; one lane issues.  A single thread's instructions are what the tensor
+        // core waits for: 64 elements of d (4 instructions) per barrier left it idle 40 % of the
+        // time, hence stages of two boxes.
+        const bool issuer = lane == 0;
+        if (warp == 0) {  // loads
+            int issued = 0;
+            auto feed = [&]() -> bool {
+                int stage = 0;
+                uint32_t phase = 0;
+                for (int w = w0; w < n_work; w += w_step) {
+                    const int row = p.row0 + active[w % blocks] * kBlockRows + rank * kHeadRows;
+                    const int part = w / blocks;
+                    const int n_tiles = tiles_of(part);
+                    for (int t = 0; t < n_tiles; ++t) {
+                        const int col = (part * p.part_tiles + t) * p.tile_cols + rank * (p.tile_cols / kCtas);
+                        for (int k = 0; k < steps; ++k) {
+                            if (!wait(&empty[stage], phase ^ 1u)) return false;
+                            if (issuer) {
+                                const uint32_t a = tiles + stage * p.stage_bytes, b = a + kBoxes * p.a_bytes;
+                                const uint32_t bar = kCtas == 2 ? in_first_cta(&full[stage]) : smem_u32(&full[stage]);
+                                if (rank == 0) mbar_expect_tx(&full[stage], p.load_bytes * kCtas);
+#pragma unroll
+                                for (int i = 0; i < kBoxes; ++i) {
+                                    tma_load_2d<kCtas>(a + i * p.a_bytes, &map_a, (k * kBoxes + i) * kHeadDepth, row, bar);
+                                    tma_load_2d<kCtas>(b + i * p.b_bytes, &map_b, (k * kBoxes + i) * kHeadDepth, col, bar);
+                                }
+                            }
+                            if (issued < p.stages) ++issued;
+                            if (++stage == p.stages) {
+                                stage = 0;
+                                phase ^= 1u;
+                            }
+                        }
                     }
-                    const uint32_t a = tiles + stage * kStageBytes;
-                    mbar_expect_tx(&full[stage], bytes);
-                    tma_load_2d(a, &map_a, k * kHeadDepth, row, &full[stage]);
-                    tma_load_2d(a + kABytes, &map_b, k * kHeadDepth, col, &full[stage]);
-                    ++issued;
-                    if (++stage == kHeadStages) {
+                }
+                // leave only when every stage was consumed (and, in a pair, this CTA was told so)
+                for (int i = 0; i < p.stages; ++i) {
+                    if (!wait(&empty[stage], phase ^ 1u)) return false;
+                    if (++stage == p.stages) {
                         stage = 0;
                         phase ^= 1u;
                     }
                 }
+                return true;
+            };
+            if (!feed() && issuer && rank == 0) {  // gave up: let the loads in flight land
+                for (int i = 0; i < issued; ++i)
+                    for (uint32_t parity = 0; parity < 2; ++parity) mbar_wait_bounded(&full[i], parity, 1u << 14);
             }
-            if (!ok) {  // let what is in flight land before the CTA's shared memory goes
-                const int n = issued < kHeadStages ? (int)issued : kHeadStages;
-                for (int i = 0; i < n; ++i) {
-                    const int64_t at = issued - 1 - i;
-                    mbar_wait_bounded(&full[at % kHeadStages], (uint32_t)((at / kHeadStages) & 1), kMbarSpinLimit);
+        } else if (warp == 1) {
+            auto multiply = [&]() {  // products, for both CTAs of a pair
+                // D fp32, A and B of the weight's type, both K-major
+                const uint32_t idesc = (1u << 4) | ((uint32_t)p.bf16 << 7) | ((uint32_t)p.bf16 << 10) |
+                                       ((uint32_t)(p.tile_cols >> 3) << 17) | ((uint32_t)(kBlockRows >> 4) << 24);
+                const uint32_t a_first = operand_lo(tiles), b_first = operand_lo(tiles + kBoxes * p.a_bytes);
+                const uint32_t a_box = p.a_bytes >> 4, b_box = p.b_bytes >> 4, next = p.stage_bytes >> 4;
+                int stage = 0, buf = 0;
+                uint32_t phase = 0, buf_phase = 0, at = 0;
+                for (int w = w0; w < n_work; w += w_step) {
+                    const int n_chunks = tiles_of(w / blocks) * chunks;
+                    int left = steps;
+                    for (int c = 0; c < n_chunks; ++c) {
+                        if (!wait(&acc_empty[buf], buf_phase ^ 1u)) return;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t acc = tmem + buf * kHeadMaxCols;
+                        const int n = min(left, kChunkSteps);
+                        left = left == n ? steps : left - n;
+                        for (int k = 0; k < n; ++k) {
+                            if (!wait(&full[stage], phase)) return;
+                            if (issuer) {
+#pragma unroll
+                                for (int i = 0; i < kBoxes; ++i)
+#pragma unroll
+                                    for (int j = 0; j < kHeadDepth / 16; ++j)  // 32 bytes of the swizzled rows each
+                                        mma_f16<kCtas>(acc, a_first + at + i * a_box + 2 * j,
+                                                       b_first + at + i * b_box + 2 * j, idesc, (k | i | j) != 0);
+                                mma_commit<kCtas>(&empty[stage]);
+                            }
+                            at += next;
+                            if (++stage == p.stages) {
+                                stage = 0;
+                                at = 0;
+                                phase ^= 1u;
+                            }
+                        }
+                        if (issuer) mma_commit<kCtas>(&acc_full[buf]);
+                        buf ^= 1;
+                        if (buf == 0) buf_phase ^= 1u;
+                    }
                 }
+            };
+            if (rank == 0) {
+                multiply();
+                if (issuer) mma_commit<kCtas>(&drained);
             }
+            // products still under way use both CTAs' shared memory and TMEM
+            if (issuer && !mbar_wait_bounded(&drained, 0, kMbarSpinLimit)) gave_up = 1;
         }
-    } else if (warp == 1) {
-        if (lane == 0) {  // products
-            // D fp32, A and B of the weight's type, both K-major, 128 rows, tile_cols columns
-            const uint32_t idesc = (1u << 4) | ((uint32_t)p.bf16 << 7) | ((uint32_t)p.bf16 << 10) |
-                                   ((uint32_t)(p.tile_cols >> 3) << 17) | ((uint32_t)(kHeadRows >> 4) << 24);
-            int stage = 0, buf = 0;
-            uint32_t phase = 0, buf_phase = 0;
-            bool ok = true;
-            for (int64_t w = blockIdx.x; w < n_work && ok; w += gridDim.x) {
-                ok = wait(&acc_empty[buf], buf_phase ^ 1u);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int k = 0; k < depth_steps; ++k) {
-                    ok = wait(&full[stage], phase);
+    } else {  // sums of the chunks, then the reduction: a thread has half of a tile's columns of one row
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kReduceRegs));
+        const int quarter = warp & 3;               // the TMEM lanes a warp may read
+        const int half = (warp - 4) >> 2;
+        const int r = quarter * 32 + lane;
+        const int col_first = half == 0 ? 0 : p.half_cols;
+        const int width = half == 0 ? p.half_cols : p.tile_cols - p.half_cols;
+        const uint32_t lanes = tmem + ((uint32_t)quarter << 21) + col_first;
+        int buf = 0, turn = 0;
+        uint32_t buf_phase = 0;
+        bool ok = true;
+        // the row of a piece of work, whether it is scored, and its target's column within the range
+        auto row_of = [&](int w) { return p.row0 + active[w % blocks] * kBlockRows + rank * kHeadRows + r; };
+        auto scored = [&](int w) { return w < n_work && row_scored(p, row_of(w)); };
+        auto target_of = [&](int w, bool on) { return on ? (int64_t)p.token_ids[row_of(w)] - p.col0 : (int64_t)-1; };
+        bool next_on = scored(w0);
+        int64_t next_at = target_of(w0, next_on);
+        for (int w = w0; w < n_work; w += w_step) {
+            const int row = row_of(w), part = w / blocks;
+            const int n_tiles = tiles_of(part);
+            const bool on = next_on;
+            const int64_t at = next_at;
+            next_on = scored(w + w_step);  // asked for now, needed after this piece's arithmetic
+            next_at = target_of(w + w_step, next_on);
+            // sum of exp(z) so far = sum * 2^ref, ref = m * log2 e rounded once
+            float m = kNoLogit, ref = kNoLogit * kLog2e, sum = 0.f;
+            for (int t = 0; t < n_tiles && ok; ++t) {
+                // Always 128 columns: what stands behind a narrower tile's is read and left out below.
+                float z[kHeadMaxCols / 2];
+#pragma unroll
+                for (int i = 0; i < kHeadMaxCols / 2; ++i) z[i] = 0.f;
+                for (int c = 0; c < chunks; ++c) {
+                    // one lane waits (32 would poll 32 times), then every lane looks for itself
+                    if (lane == 0) ok = wait(&acc_full[buf], buf_phase);
+                    ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+                    ok = __all_sync(0xFFFFFFFFu, ok && wait(&acc_full[buf], buf_phase));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t a = operand_desc(tiles + stage * kStageBytes);
-                    const uint64_t b = operand_desc(tiles + stage * kStageBytes + kABytes);
 #pragma unroll
-                    for (int i = 0; i < kHeadDepth / 16; ++i)  // 32 bytes of the swizzled rows per step
-                        mma_f16(tmem + buf * kHeadMaxCols, a + 2 * i, b + 2 * i, idesc, (k | i) != 0);
-                    mma_commit(&empty[stage]);
-                    if (++stage == kHeadStages) {
-                        stage = 0;
-                        phase ^= 1u;
+                    for (int j = 0; j < kHeadMaxCols / 32; ++j) {
+                        float v[16];
+                        tmem_load16(v, lanes + buf * kHeadMaxCols + j * 16);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) z[j * 16 + i] += v[i];
                     }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive_cluster(kCtas == 2 ? in_first_cta(&acc_empty[buf]) : smem_u32(&acc_empty[buf]));
+                    buf ^= 1;
+                    if (buf == 0) buf_phase ^= 1u;
                 }
                 if (!ok) break;
-                mma_commit(&acc_full[buf]);
-                buf ^= 1;
-                if (buf == 0) buf_phase ^= 1u;
-            }
-            if (!ok) {  // products still under way read shared memory and write TMEM
-                mma_commit(&drained);
-                mbar_wait_bounded(&drained, 0, kMbarSpinLimit);
-            }
-        }
-    } else if (warp >= 4) {  // reduction: one thread per row
-        int buf = 0;
-        uint32_t buf_phase = 0;
-        for (int64_t w = blockIdx.x; w < n_work; w += gridDim.x) {
-            const int64_t row = p.row0 + (int64_t)active[w % blocks] * kHeadRows + (tid & 127);
-            const int tile = (int)(w / blocks);
-            const int64_t col = (int64_t)tile * p.tile_cols;
-            const int cols = (int)(p.n_cols - col < p.tile_cols ? p.n_cols - col : p.tile_cols);
-            bool on = false;
-            int64_t want = -1;  // the target's column within this tile, if it has it
-            bool elsewhere = true;
-            if (row < p.rows) {
-                const int64_t s = row / p.max_new;
-                on = (int)(row - s * p.max_new) < stream_rows(p, s);
-                if (on) {
-                    const int64_t at = (int64_t)p.token_ids[row] - p.col0;
-                    elsewhere = at < 0 || at >= p.n_cols;
-                    want = at - col;
-                }
-            }
-            if (!wait(&acc_full[buf], buf_phase)) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t acc = tmem + ((uint32_t)(warp & 3) << 21) + buf * kHeadMaxCols;
-            // sum of exp(z) so far = sum * 2^ref, ref = m * log2 e rounded once
-            float m = kNoLogit, ref = kNoLogit * kLog2e, sum = 0.f, target = 0.f;
-            for (int c = 0; c < cols; c += 32) {
-                float z[32];
-                tmem_load32(z, acc + c);
-                if (c + 32 > cols) {
+                const int64_t col = ((int64_t)part * p.part_tiles + t) * p.tile_cols + col_first;
+                const int cols = (int)max((int64_t)0, min((int64_t)width, p.n_cols - col));
+                if (cols < kHeadMaxCols / 2) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c + i >= cols) z[i] = __uint_as_float(0xFF800000u);
+                    for (int i = 0; i < kHeadMaxCols / 2; ++i)
+                        if (i >= cols) z[i] = __uint_as_float(0xFF800000u);
                 }
-                if (want >= c && want < c + 32) {
+                if (on && at >= col && at < col + cols) {
+                    const int want = (int)(at - col);
+                    float target = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (want == c + i) target = z[i];
+                    for (int i = 0; i < kHeadMaxCols / 2; ++i)
+                        if (i == want) target = z[i];
+                    p.target_out[row] = target;
                 }
-                float top = z[0];
+                float top[4] = {m, m, m, m};  // four chains each: a thread is alone with its row
 #pragma unroll
-                for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
-                m = fmaxf(top, m);
+                for (int i = 0; i < kHeadMaxCols / 2; ++i) top[i & 3] = fmaxf(top[i & 3], z[i]);
+                m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 const float old = ref;
                 ref = m * kLog2e;
-                float s0 = sum * ex2_approx(old - ref), s1 = 0.f;
+                float s[4] = {sum * ex2_approx(old - ref), 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    s0 += ex2_approx(fmaf(z[i], kLog2e, -ref));
-                    s1 += ex2_approx(fmaf(z[i + 1], kLog2e, -ref));
-                }
-                sum = s0 + s1;
+                for (int i = 0; i < kHeadMaxCols / 2; ++i) s[i & 3] += ex2_approx(fmaf(z[i], kLog2e, -ref));
+                sum = (s[0] + s[1]) + (s[2] + s[3]);
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&acc_empty[buf]);
-            if (on) {
-                // a tile whose logits are all -inf counts for nothing: (0, 0)
-                p.pairs_out[row * p.pair_stride + tile] = sum == 0.f ? make_float2(0.f, 0.f) : make_float2(m, sum);
-                if (want >= 0 && want < cols)
-                    p.target_out[row] = target;
-                else if (tile == 0 && elsewhere)
-                    p.target_out[row] = 0.f;
+            // the row's two halves into one pair (warps that gave up still meet the others here)
+            if (half == 1) other_half[turn][r] = make_float4(m, ref, sum, 0.f);
+            asm volatile("bar.sync 1, %0;" ::"n"(kHeadReducers) : "memory");
+            if (half == 0 && on && ok) {
+                const float4 o = other_half[turn][r];
+                const float top = fmaxf(m, o.x), base = top * kLog2e;
+                const float s = sum * ex2_approx(ref - base) + o.z * ex2_approx(o.y - base);
+                // a part whose logits are all -inf counts for nothing: (0, 0)
+                p.pairs_out[(int64_t)row * p.pair_stride + part] = s == 0.f ? make_float2(0.f, 0.f) : make_float2(top, s);
+                if (part == 0 && (at < 0 || at >= p.n_cols)) p.target_out[row] = 0.f;  // the token is elsewhere
             }
-            buf ^= 1;
-            if (buf == 0) buf_phase ^= 1u;
+            turn ^= 1;
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    cta_or_pair_sync<kCtas>();  // neither CTA's memory goes while the other may still use it
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == 2)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+    if (warp == 1) tmem_free<kCtas>(tmem);
     if (tid == 0 && gave_up) atomicOr(p.status, SIRLLM_STATUS_TIMEOUT);
 }
 
@@ -337,21 +484,69 @@ cudaError_t row_map(EncodeTiled encode, CUtensorMap* map, const void* base, int6
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-}  // namespace
-
-int head_tile_cols(int64_t rows, int64_t n_cols) {
-    // Several row blocks: the widest tile, which feeds the tensor core with the fewest bytes.
-    if (rows > kHeadRows) return kHeadMaxCols;
-    // One row block: reading the weight bounds the call, so its columns are dealt out evenly over
-    // whole waves of SMs (a B200 has 148; on another count the result stays right).
-    constexpr int64_t kSms = 148;
-    const int64_t waves = (n_cols + kSms * kHeadMaxCols - 1) / (kSms * kHeadMaxCols);
-    const int64_t share = (n_cols + kSms * waves - 1) / (kSms * waves);
-    return (int)((share + 31) / 32 * 32);
+template <int kCtas>
+cudaError_t launch(const HeadParams& p, unsigned grid, const DeviceProps& dp, const CUtensorMap& a, const CUtensorMap& b,
+                   cudaStream_t st) {
+    static unsigned char allowed[kMaxDevices];
+    cudaError_t e = allow_max_dynamic_smem((const void*)head_kernel<kCtas>, dp, allowed);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kHeadThreads);
+    cfg.dynamicSmemBytes = kHeadSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCtas;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kCtas == 2 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, head_kernel<kCtas>, p, a, b);
 }
 
-cudaError_t launch_head(const HeadParams& p, const void* hidden, int64_t hidden_stride, const void* weight,
-                        int64_t weight_stride, cudaStream_t st) {
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
+
+// The cut depends on the sizes alone (callers size their pairs by it), for the 148 SMs of a B200;
+// on another count of SMs the results are the same and only the balance differs.
+HeadTiling head_tiling(int64_t rows, int64_t n_cols) {
+    constexpr int64_t kSms = 148;
+    HeadTiling t;
+    if (rows <= kHeadRows) {
+        // One block of rows: reading the weight bounds the call, so its columns are dealt out evenly,
+        // one range per SM, each cut into equal tiles.
+        t.ctas = 1;
+        const int64_t share = ceil_div(ceil_div(n_cols, kSms), 16) * 16;
+        t.part_tiles = (int32_t)ceil_div(share, kHeadMaxCols);
+        t.tile_cols = (int32_t)(ceil_div(ceil_div(share, t.part_tiles), 16) * 16);
+        t.half_cols = (int32_t)ceil_div(t.tile_cols / 2, 16) * 16;
+    } else {
+        // The widest tile feeds the tensor core with the fewest bytes; a narrower one is taken where
+        // it shortens the last wave of tiles by more than that costs.
+        t.ctas = 2;
+        t.part_tiles = 1;
+        const int64_t blocks = ceil_div(rows, 2 * kHeadRows);
+        int64_t best = 0;
+        t.tile_cols = kHeadMaxCols;
+        for (int64_t c = kHeadMaxCols; c >= 64; c -= 32) {
+            const int64_t cost = ceil_div(blocks * ceil_div(n_cols, c), kSms / 2) * (c + 16);
+            if (best == 0 || cost * 33 < best * 32) {
+                best = cost;
+                t.tile_cols = (int32_t)c;
+            }
+        }
+        t.half_cols = t.tile_cols / 2;
+    }
+    t.n_parts = (int32_t)ceil_div(n_cols, (int64_t)t.part_tiles * t.tile_cols);
+    return t;
+}
+
+cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hidden, int64_t hidden_stride,
+                        const void* weight, int64_t weight_stride, cudaStream_t st) {
     TraceRange trace("sirllm:head_pairs");
     if (p.rows == 0) return cudaSuccess;
     DeviceProps dp;
@@ -359,22 +554,38 @@ cudaError_t launch_head(const HeadParams& p, const void* hidden, int64_t hidden_
     if (e != cudaSuccess) return e;
     EncodeTiled encode;
     if ((e = encoder(&encode)) != cudaSuccess) return e;
-    static unsigned char allowed[kMaxDevices];
-    if ((e = allow_max_dynamic_smem((const void*)head_kernel, dp, allowed)) != cudaSuccess) return e;
+    const int a_rows = t.ctas == 2 ? kHeadRows : (int)ceil_div(p.rows, 8) * 8;
+    const int b_rows = t.tile_cols / t.ctas;
     CUtensorMap map_a, map_b;
-    if ((e = row_map(encode, &map_a, hidden, p.rows, p.d_model, hidden_stride, kHeadRows, p.bf16)) != cudaSuccess)
+    if ((e = row_map(encode, &map_a, hidden, p.rows, p.d_model, hidden_stride, a_rows, p.bf16)) != cudaSuccess) return e;
+    if ((e = row_map(encode, &map_b, weight, p.n_cols, p.d_model, weight_stride, b_rows, p.bf16)) != cudaSuccess)
         return e;
-    if ((e = row_map(encode, &map_b, weight, p.n_cols, p.d_model, weight_stride, p.tile_cols, p.bf16)) != cudaSuccess)
-        return e;
-    const int64_t all_blocks = (p.rows + kHeadRows - 1) / kHeadRows;
-    for (int64_t b = 0; b < all_blocks; b += kHeadRowBlocks) {
-        HeadParams q = p;
-        q.row0 = b * kHeadRows;
-        q.row_blocks = (int32_t)(all_blocks - b < kHeadRowBlocks ? all_blocks - b : kHeadRowBlocks);
-        const int64_t work = (int64_t)q.row_blocks * q.n_tiles;
-        const unsigned grid = (unsigned)(work < dp.n_sm ? work : dp.n_sm);
-        head_kernel<<<grid, kHeadThreads, kHeadSmem, st>>>(q, map_a, map_b);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    HeadParams q = p;
+    q.n_parts = t.n_parts;
+    q.n_tiles = (int32_t)ceil_div(p.n_cols, t.tile_cols);
+    q.part_tiles = t.part_tiles;
+    q.tile_cols = t.tile_cols;
+    q.half_cols = t.half_cols;
+    // a stage: the rows that are loaded, swizzle groups of 8 rows (1 KB) at a time
+    q.a_bytes = a_rows * kHeadDepth * 2;
+    q.b_bytes = b_rows * kHeadDepth * 2;
+    q.load_bytes = kBoxes * (q.a_bytes + q.b_bytes);
+    q.stage_bytes = q.load_bytes;
+    // an instruction reads 128 rows of A from a stage's start; the ring leaves room for that at its end
+    q.stages = (kHeadRing - (kARoom - q.a_bytes)) / q.stage_bytes;
+    if (q.stages > kHeadMaxStages) q.stages = kHeadMaxStages;
+    const int64_t block_rows = (int64_t)kHeadRows * t.ctas;
+    const int64_t all_blocks = ceil_div(p.rows, block_rows);
+    int64_t at_once = ((int64_t)1 << 30) / t.n_parts;  // row blocks of a launch: its work is counted in 32 bits
+    if (at_once < 1) at_once = 1;
+    if (at_once > kHeadRowBlocks) at_once = kHeadRowBlocks;
+    for (int64_t b = 0; b < all_blocks; b += at_once) {
+        q.row0 = (int32_t)(b * block_rows);
+        q.row_blocks = (int32_t)(all_blocks - b < at_once ? all_blocks - b : at_once);
+        const int64_t work = (int64_t)q.row_blocks * q.n_parts, fit = dp.n_sm / t.ctas;
+        const unsigned grid = (unsigned)((work < fit ? work : fit) * t.ctas);
+        e = t.ctas == 2 ? launch<2>(q, grid, dp, map_a, map_b, st) : launch<1>(q, grid, dp, map_a, map_b, st);
+        if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
