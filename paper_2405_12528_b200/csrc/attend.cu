@@ -21,6 +21,8 @@
 // fp32: scores, running maximum and sum, output sums, the join.  Rounded to 16 bits: the
 // probabilities on their way into the second product (relative to a reference that the true
 // maximum exceeds by less than 2^8, so fp16 cannot overflow), and the result.
+#include <atomic>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -31,6 +33,12 @@ namespace sirllm {
 namespace {
 
 constexpr int kKeys = 16;  // slots per tile
+// What an SM reads in the time that joining a unit's parts takes, through memory (6 us at the 110 GB/s
+// that one SM takes in, and for each part's rows four times their bytes) and within a cluster (2 us), and
+// how many SMs at that rate make up HBM's.
+constexpr float kJoinBytes = 640 * 1024, kClusterBytes = 220 * 1024;
+constexpr float kBusySms = 58.f;
+constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0)
@@ -86,27 +94,78 @@ __device__ __forceinline__ uint16_t round16(float v) {
     return __half_as_ushort(__float2half_rn(v));
 }
 
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a shared variable of another CTA of the cluster
+__device__ __forceinline__ uint32_t of_rank(const void* p, int rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float2 ld_cluster2(uint32_t a) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(a)
+                 : "memory");
+    return v;
+}
+
 // slots of a stream that count, 0 for a length outside the planes
 __device__ __forceinline__ int live_slots(const AttendParams& p, int s) {
     const int n = p.kv_len[s];
     return n < 0 || n > p.capacity ? 0 : n;
 }
 
-// A walk along the line of tiles: segments of units, as far as this CTA's stretch goes.
+// A CTA's way through the work, segment by segment.  Two ways: along its stretch of the line of
+// tiles, or (whole_units) from unit to unit, `step` units apart.
 struct Walk {
-    int64_t left;   // tiles of the stretch from this segment's first on
-    int64_t unit0;  // line position of the unit's first tile
+    int left;       // tiles of the stretch from this segment's first on; whole units: 1 until the end
+    int unit0;      // line position of the unit's first tile; whole units: the unit's number
     int s, unit;    // stream; unit within the stream (K/V head, block of query heads)
     int len;        // live slots of the stream
     int t0, t1;     // this segment's tiles of the unit
+    int step;       // 0: along the line
 
     __device__ __forceinline__ bool more() const { return left > 0; }
     __device__ __forceinline__ int tiles() const { return (len + kKeys - 1) / kKeys; }
     __device__ __forceinline__ void set_end() {
         const int T = tiles();
-        t1 = (int64_t)(T - t0) > left ? t0 + (int)left : T;
+        t1 = step == 0 && T - t0 > left ? t0 + left : T;
+    }
+    // from the unit numbered unit0, the first one with slots, in steps
+    __device__ __forceinline__ void find_unit(const AttendParams& p) {
+        const int n_units = p.n_streams * p.units;
+        left = 0;
+        for (; unit0 < n_units; unit0 += step) {
+            s = unit0 / p.units;
+            unit = unit0 - s * p.units;
+            len = live_slots(p, s);
+            if (len > 0) {
+                left = 1;
+                break;
+            }
+        }
+        t0 = 0;
+        set_end();
     }
     __device__ __forceinline__ void next(const AttendParams& p) {
+        if (step > 0) {
+            unit0 += step;
+            find_unit(p);
+            return;
+        }
         left -= t1 - t0;
         if (left <= 0) return;
         unit0 += tiles();
@@ -136,56 +195,110 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     constexpr int kPass = 4;                        // heads whose output sums are merged at a time
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* ring = smem;                                                   // [warp][stage][K, V]
-    float* merge = reinterpret_cast<float*>(smem + kWarps * kStages * 2 * kTileBytes);  // [warp][kPass][kDim]
-    __shared__ int64_t scan[kWarps];
+    float* cta_o = reinterpret_cast<float*>(smem + kWarps * kStages * 2 * kTileBytes);  // [head][head_dim]
+    float* merge = cta_o + kHeads * kDim;  // [warp][kPass][kDim]
+    __shared__ int scan[kWarps];
+    __shared__ int longest[kWarps];
     __shared__ Walk first;
     __shared__ float stat_m[kWarps][kHeads], stat_l[kWarps][kHeads];
     __shared__ float part_w[kHeads];
+    __shared__ __align__(8) float2 cta_ml[kHeads];
     __shared__ int last_one;
+    __shared__ float4 team_sum[kThreads];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    grid_dependency_wait();
+    grid_launch_dependents();
 
     // ---- the line of tiles, this CTA's stretch of it -------------------------------------
     const int slice = (p.n_streams + kThreads - 1) / kThreads;
     const int s_lo = min(p.n_streams, tid * slice), s_hi = min(p.n_streams, s_lo + slice);
-    int64_t mine = 0;
-    for (int s = s_lo; s < s_hi; ++s) mine += (int64_t)((live_slots(p, s) + kKeys - 1) / kKeys) * p.units;
-    int64_t before = mine;
+    int mine = 0;
+    int long_unit = 0;
+    for (int s = s_lo; s < s_hi; ++s) {
+        const int T = (live_slots(p, s) + kKeys - 1) / kKeys;
+        mine += T * p.units;
+        long_unit = max(long_unit, T);
+    }
+    long_unit = __reduce_max_sync(0xFFFFFFFFu, long_unit);
+    int before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xFFFFFFFFu, before, o);
+        const int v = __shfl_up_sync(0xFFFFFFFFu, before, o);
         if (lane >= o) before += v;
     }
-    if (lane == 31) scan[warp] = before;
+    if (lane == 31) {
+        scan[warp] = before;
+        longest[warp] = long_unit;
+    }
     __syncthreads();
-    int64_t total = 0, warps_before = 0;
+    int total = 0, warps_before = 0;  // below 2^31: the caches of so many tiles fit no device
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) warps_before += scan[w];
         total += scan[w];
+        long_unit = max(long_unit, longest[w]);
     }
     before += warps_before - mine;  // tiles in front of this thread's streams
-    // at least one tile per warp, so that short caches are not joined from needlessly many parts
-    int64_t per = (total + gridDim.x - 1) / gridDim.x;
-    if (per < kWarps) per = kWarps;
-    const int64_t r0 = (int64_t)blockIdx.x * per;
-    const int64_t r1 = r0 + per < total ? r0 + per : total;
-    if (r0 >= before && r0 < before + mine) {  // exactly one thread, if the stretch is not empty
-        int64_t at = before;
-        int s = s_lo, len = 0;
-        int64_t T = 0;
+    // Three ways to deal out the work.  (1) An equal share of the line per CTA; units that CTAs share
+    // are joined through memory.  (2) Whole units in turn to the CTAs: nothing to join, but no
+    // balance between units of different length.  (3) As (2) to the clusters, a unit's tiles in turn
+    // to the cluster's CTAs, joined through shared memory.  The estimate is in tiles that the
+    // busiest SM takes in (at 110 GB/s alone, 80 GB/s among many): what HBM takes for all of them
+    // (1/kBusySms of the tiles), what the busiest has left when the others are done, and what ends
+    // a unit.
+    const float tile_bytes = (float)(kKeys * 4 * p.head_dim);
+    const float part_tiles = 4.f * (float)(min(kHeads, p.group) * p.head_dim * 4) / tile_bytes;
+    // (1): a few very long units are cut into fewer parts than there are SMs: with `per` tiles in a
+    // part and long_unit / per parts to join, the sum of both is least at the root
+    const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, max((int)sqrtf((float)long_unit * part_tiles), 1));
+    const int n_units = p.n_streams * p.units;
+    const float hbm = (float)total / kBusySms;
+    auto estimate = [&](int size) {
+        const int groups = gridDim.x / size;
+        const float dealt = (float)((n_units + groups - 1) / groups) * (float)((long_unit + size - 1) / size);
+        return fmaxf(dealt * (4.f / 3.f), hbm + dealt - (float)total / (float)(min(n_units, groups) * size));
+    };
+    float least = fmaxf((float)per * (4.f / 3.f), hbm) + kJoinBytes / tile_bytes +
+                  ((float)long_unit / (float)per + 1.f) * part_tiles;
+    bool whole_units = false;
+    int team = 1;  // CTAs that share a unit
+    const float alone = estimate(1);
+    if (alone <= least) {
+        whole_units = true;
+        least = alone;
+    }
+    if (p.cluster > 1 && estimate(p.cluster) + kClusterBytes / tile_bytes < least) {
+        whole_units = true;
+        team = p.cluster;
+    }
+    const int rank = team > 1 ? (int)cluster_rank() : 0;
+    // the warp's first tile of a segment and its way to the next
+    const int lead = rank * kWarps + warp, stride = team * kWarps;
+    const int r0 = total / per >= (int)blockIdx.x ? (int)blockIdx.x * per : total;  // (no overflow)
+    const int r1 = min(total, r0 + min(per, total - r0));
+    if (whole_units) {
+        if (tid == 0) {
+            first.step = gridDim.x / team;
+            first.unit0 = blockIdx.x / team;
+            first.find_unit(p);
+        }
+    } else if (r0 >= before && r0 < before + mine) {  // exactly one thread, if the stretch is not empty
+        int at = before;
+        int s = s_lo, len = 0, T = 0;
         for (; s < s_hi; ++s) {
             len = live_slots(p, s);
             T = (len + kKeys - 1) / kKeys;
             if (r0 < at + T * p.units) break;
             at += T * p.units;
         }
+        first.step = 0;
         first.left = s < s_hi ? r1 - r0 : 0;
         if (s < s_hi) {
             first.s = s;
             first.len = len;
-            first.unit = (int)((r0 - at) / T);
-            first.unit0 = at + (int64_t)first.unit * T;
-            first.t0 = (int)(r0 - first.unit0);
+            first.unit = (r0 - at) / T;
+            first.unit0 = at + first.unit * T;
+            first.t0 = r0 - first.unit0;
             first.set_end();
         }
     }
@@ -204,19 +317,19 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         }
     }
     __syncthreads();
-    if (r0 >= total) return;
+    if (!whole_units && r0 >= total) return;
 
     // ---- the warp's ring ------------------------------------------------------------------
     const uint32_t ring0 = smem_u32(ring) + warp * kStages * 2 * kTileBytes;
     Walk ahead = first;                 // what the loads have reached
-    int ahead_tile = ahead.t0 + warp;
+    int ahead_tile = ahead.t0 + lead;
     constexpr int kRowsAtOnce = 32 / kChunks;  // rows that one load instruction of the warp covers
     const int chunk = lane % kChunks, row_in = lane / kChunks;
     const bool chunk_on = chunk * 8 < p.head_dim;
     auto load_next = [&](int stage) {  // the warp's next tile, if there is one, into a stage; one group
         while (ahead.more() && ahead_tile >= ahead.t1) {
             ahead.next(p);
-            ahead_tile = ahead.t0 + warp;
+            ahead_tile = ahead.t0 + lead;
         }
         if (ahead.more()) {
             const int g = ahead.unit / p.blocks;
@@ -233,7 +346,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 cp_async16(d, p.k + o, valid);
                 cp_async16(d + kTileBytes, p.v + o, valid);
             }
-            ahead_tile += kWarps;
+            ahead_tile += stride;
         }
         cp_commit();
     };
@@ -272,7 +385,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             m[n][0] = m[n][1] = kNegHuge;
             l[n][0] = l[n][1] = 0.f;
         }
-        for (int tile = w.t0 + warp; tile < w.t1; tile += kWarps) {
+        for (int tile = w.t0 + lead; tile < w.t1; tile += stride) {
             cp_wait<kStages - 2>();
             __syncwarp();
             load_next(stage == 0 ? kStages - 1 : stage - 1);  // the stage that was consumed last
@@ -361,8 +474,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 }
             }
         __syncthreads();
-        const bool whole = w.t0 == 0 && w.t1 == w.tiles();
-        const int c_first = (int)(w.unit0 / per);
+        const bool shared_unit = team > 1;  // with the cluster's other CTAs
+        const bool whole = w.t0 == 0 && w.t1 == w.tiles() && !shared_unit;
+        const int c_first = whole_units ? 0 : w.unit0 / per;
         const int64_t slot = 2 * (int64_t)blockIdx.x + ((int)blockIdx.x == c_first ? 1 : 0);
         float* part_o = p.part_o + slot * p.part_heads * p.head_dim;
         float2* part_ml = p.part_ml + slot * p.part_heads;
@@ -386,6 +500,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 part_w[tid] = 1.0f / sum;
                 if (p.lse != nullptr)
                     p.lse[(int64_t)w.s * p.n_heads + head0 + tid] = (t + log2f(sum)) * (float)kLn2;
+            } else if (shared_unit) {
+                cta_ml[tid] = make_float2(t, sum);
             } else {
                 part_ml[tid] = make_float2(t, sum);
             }
@@ -416,43 +532,159 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 if (whole)
                     p.out[(int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e] =
                         round16<kBf16>(sum * part_w[h]);
+                else if (shared_unit)
+                    cta_o[h * p.head_dim + e] = sum;
                 else
                     part_o[h * p.head_dim + e] = sum;
             }
             __syncthreads();
         }
         if (whole) continue;
+        if (shared_unit) {
+            // ---- the cluster's CTAs into one: each writes its share of the unit's outputs --------
+            cluster_sync();
+            const int quads = p.head_dim >> 2, items = heads * quads;
+            const int share = (items + team - 1) / team;
+            const int end = min(items, (rank + 1) * share);
+            for (int item = rank * share + tid; item < end; item += kThreads) {
+                const int h = item / quads, e = (item - h * quads) * 4;
+                float2 ml[kMaxCluster];
+                float4 v[kMaxCluster];
+                float t = kNegHuge;
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c) {
+                    if (c >= team) break;
+                    ml[c] = ld_cluster2(of_rank(&cta_ml[h], c));
+                    v[c] = ld_cluster4(of_rank(&cta_o[h * p.head_dim + e], c));
+                    t = fmaxf(t, ml[c].x);
+                }
+                float sum = 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c) {
+                    if (c >= team) break;
+                    const float f = ex2_approx(ml[c].x - t);
+                    sum = fmaf(ml[c].y, f, sum);
+                    acc.x = fmaf(v[c].x, f, acc.x);
+                    acc.y = fmaf(v[c].y, f, acc.y);
+                    acc.z = fmaf(v[c].z, f, acc.z);
+                    acc.w = fmaf(v[c].w, f, acc.w);
+                }
+                const float f = 1.0f / sum;
+                *reinterpret_cast<uint2*>(p.out + (int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e) =
+                    make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
+                if (e == 0 && p.lse != nullptr)
+                    p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (t + log2f(sum)) * (float)kLn2;
+            }
+            cluster_sync();  // the others have read this CTA's sums
+            continue;
+        }
         // ---- a unit that several CTAs share: the last one to finish joins the parts --------------
-        const int c_last = (int)((w.unit0 + w.tiles() - 1) / per);
-        __threadfence();
+        const int c_last = (w.unit0 + w.tiles() - 1) / per, parts = c_last - c_first + 1;
         __syncthreads();
-        if (tid == 0) last_one = atomicAdd(&p.tickets[c_first], 1) == c_last - c_first;
+        if (tid == 0) {
+            // release: this CTA's part (all threads' stores, ordered by the barrier) before the ticket;
+            // acquire: the ticket before the others' parts are read
+            int before_me;
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before_me) : "l"(&p.tickets[c_first]) : "memory");
+            last_one = before_me == parts - 1;
+            if (last_one) p.tickets[c_first] = 0;  // for the next call
+        }
         __syncthreads();
         if (!last_one) continue;
-        __threadfence();
-        if (tid == 0) p.tickets[c_first] = 0;  // for the next call
-        auto ml_of = [&](int c, int h) {
-            return __ldcg(&p.part_ml[(2 * (int64_t)c + (c == c_first ? 1 : 0)) * p.part_heads + h]);
+        auto slot_of = [&](int i) { return 2 * (int64_t)(c_first + i) + (i == 0 ? 1 : 0); };
+        // four elements per thread; threads that are left over share the parts.  The first rows are
+        // asked for before the weights are worked out.
+        const int quads = p.head_dim >> 2, items = heads * quads;
+        const int teams = items < kThreads ? kThreads / items : 1;
+        const int mine = teams > 1 ? tid / items : 0;
+        auto row_of = [&](int i, int item) {
+            const int h = item / quads;
+            return __ldcg(reinterpret_cast<const float4*>(
+                &p.part_o[(slot_of(i) * p.part_heads + h) * p.head_dim + (item - h * quads) * 4]));
         };
-        for (int x = tid; x < heads * p.head_dim; x += kThreads) {
-            const int h = x / p.head_dim, e = x - h * p.head_dim;
+        constexpr int kEarly = 8;
+        float4 early[kEarly];
+        const int first_item = tid - mine * items;
+        const bool early_on = mine < teams && first_item < items;
+#pragma unroll
+        for (int j = 0; j < kEarly; ++j)
+            early[j] = early_on && mine + j * teams < parts ? row_of(mine + j * teams, first_item)
+                                                            : make_float4(0.f, 0.f, 0.f, 0.f);
+        // a warp per head: the parts' weights relative to the largest reference, and their sum
+        float* weight = merge;  // [part][head]
+        for (int h = warp; h < heads; h += kWarps) {
+            float2 ml[kAttendMaxCtas / 32];
             float t = kNegHuge;
-            for (int c = c_first; c <= c_last; ++c) t = fmaxf(t, ml_of(c, h).x);
-            float sum = 0.f, acc = 0.f;
-#pragma unroll 4
-            for (int c = c_first; c <= c_last; ++c) {
-                const float2 ml = ml_of(c, h);
-                const float f = ex2_approx(ml.x - t);
-                sum += ml.y * f;
-                acc += __ldcg(&p.part_o[((2 * (int64_t)c + (c == c_first ? 1 : 0)) * p.part_heads + h) * p.head_dim +
-                                        e]) *
-                       f;
+#pragma unroll
+            for (int j = 0; j < kAttendMaxCtas / 32; ++j) {
+                const int i = j * 32 + lane;
+                ml[j] = i < parts ? __ldcg(&p.part_ml[slot_of(i) * p.part_heads + h]) : make_float2(kNegHuge, 0.f);
+                t = fmaxf(t, ml[j].x);
             }
-            p.out[(int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e] = round16<kBf16>(acc / sum);
-            if (e == 0 && p.lse != nullptr)
-                p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (t + log2f(sum)) * (float)kLn2;
+#pragma unroll
+            for (int x = 16; x > 0; x >>= 1) t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, x));
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < kAttendMaxCtas / 32; ++j) {
+                const float f = ex2_approx(ml[j].x - t);
+                if (j * 32 + lane < parts) {
+                    sum += ml[j].y * f;
+                    weight[(j * 32 + lane) * kHeads + h] = f;
+                }
+            }
+#pragma unroll
+            for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+            if (lane == 0) {
+                part_w[h] = 1.0f / sum;
+                if (p.lse != nullptr)
+                    p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (t + log2f(sum)) * (float)kLn2;
+            }
         }
-        __syncthreads();  // last_one is written again by the next shared unit
+        __syncthreads();
+        for (int base = 0; base < items; base += kThreads) {
+            const int item = base + first_item;
+            const bool busy = mine < teams && item < items;
+            const int h = busy ? item / quads : 0, e = busy ? (item - h * quads) * 4 : 0;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            auto add = [&](int i, const float4& v) {
+                const float f = weight[i * kHeads + h];
+                acc.x = fmaf(v.x, f, acc.x);
+                acc.y = fmaf(v.y, f, acc.y);
+                acc.z = fmaf(v.z, f, acc.z);
+                acc.w = fmaf(v.w, f, acc.w);
+            };
+            if (busy) {
+                int i = mine;
+                if (base == 0) {
+#pragma unroll
+                    for (int j = 0; j < kEarly; ++j, i += teams)
+                        if (i < parts) add(i, early[j]);
+                }
+#pragma unroll 8
+                for (; i < parts; i += teams) add(i, row_of(i, item));
+            }
+            if (teams > 1) {
+                team_sum[tid] = acc;
+                __syncthreads();
+                if (busy && mine == 0) {
+                    for (int x = 1; x < teams; ++x) {
+                        const float4 v = team_sum[x * items + item];
+                        acc.x += v.x;
+                        acc.y += v.y;
+                        acc.z += v.z;
+                        acc.w += v.w;
+                    }
+                }
+            }
+            if (busy && mine == 0) {
+                const float f = part_w[h];
+                const uint2 packed = make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
+                *reinterpret_cast<uint2*>(p.out + (int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e) =
+                    packed;
+            }
+        }
+        __syncthreads();  // the merge buffer and last_one are used again by the next unit
     }
     cp_wait<0>();
 }
@@ -463,20 +695,66 @@ cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st
     auto kernel = attend_kernel<kBf16, kDim, kTiles, kWarps, kStages>;
     cudaError_t e = allow_max_dynamic_smem((const void*)kernel, dp, allowed);
     if (e != cudaSuccess) return e;
-    const size_t smem = (size_t)kWarps * kStages * 2 * kKeys * kDim * 2 + (size_t)kWarps * 4 * kDim * 4;
-    const int grid = dp.n_sm < kAttendMaxCtas ? dp.n_sm : kAttendMaxCtas;
-    kernel<<<grid, kWarps * 32, smem, st>>>(p);
-    return cudaGetLastError();
+    // the ring, a CTA's sums, and a buffer that takes [warp][4 heads][kDim] sums or [part][head] weights
+    const size_t sums = (size_t)kWarps * 4 * kDim * 4, weights = (size_t)kAttendMaxCtas * kTiles * 8 * 4;
+    const size_t smem = (size_t)kWarps * kStages * 2 * kKeys * kDim * 2 + (size_t)kTiles * 8 * kDim * 4 +
+                        (sums > weights ? sums : weights);
+    // the largest clusters of which the device holds one per unit
+    const int64_t n_units = (int64_t)p.n_streams * p.units;
+    AttendParams q = p;
+    q.cluster = 1;
+    int grid = dp.n_sm < kAttendMaxCtas ? dp.n_sm : kAttendMaxCtas;
+    static std::atomic<int> held_cache[kMaxDevices][4];
+    for (int i = 3; i > 0; --i) {
+        const int size = 1 << i;
+        if (n_units * size > grid) continue;
+        const bool cached = dp.device >= 0 && dp.device < kMaxDevices;
+        int held = cached ? held_cache[dp.device][i].load(std::memory_order_acquire) : 0;
+        if (held == 0) {
+            cudaLaunchConfig_t ask = {};
+            ask.gridDim = dim3(grid / size * size);
+            ask.blockDim = dim3(kWarps * 32);
+            ask.dynamicSmemBytes = smem;
+            cudaLaunchAttribute dim[1];
+            dim[0].id = cudaLaunchAttributeClusterDimension;
+            dim[0].val.clusterDim.x = size;
+            dim[0].val.clusterDim.y = dim[0].val.clusterDim.z = 1;
+            ask.attrs = dim;
+            ask.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&held, kernel, &ask);
+            if (e != cudaSuccess) return e;
+            if (cached && held > 0) held_cache[dp.device][i].store(held, std::memory_order_release);
+        }
+        if (n_units <= held) {
+            q.cluster = size;
+            grid = (held < grid / size ? held : grid / size) * size;
+            break;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = q.cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = q.cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, q);
 }
 
 template <bool kBf16>
 cudaError_t launch_dim(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
-    const bool wide = p.group > 8;
+    const bool wide = attend_unit_heads(p.group, p.head_dim) == 16;
     if (p.head_dim <= 64)
         return wide ? launch<kBf16, 64, 2, 8, 6>(p, dp, st) : launch<kBf16, 64, 1, 8, 6>(p, dp, st);
     if (p.head_dim <= 128)
         return wide ? launch<kBf16, 128, 2, 8, 3>(p, dp, st) : launch<kBf16, 128, 1, 8, 3>(p, dp, st);
-    return wide ? launch<kBf16, 256, 2, 4, 3>(p, dp, st) : launch<kBf16, 256, 1, 4, 3>(p, dp, st);
+    return launch<kBf16, 256, 1, 4, 3>(p, dp, st);
 }
 
 }  // namespace

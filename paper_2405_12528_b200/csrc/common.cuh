@@ -183,6 +183,7 @@ struct AttendParams {
     int32_t group, blocks, units;            // query heads per K/V head; blocks of them; units per stream
     int32_t planes_per_stream, layer_plane;
     int32_t part_heads;
+    int32_t cluster;                         // CTAs of a cluster, set by the launcher
 };
 
 struct HeadParams {
@@ -237,8 +238,9 @@ cudaError_t launch_select(const SelectParams& p, int n_streams, cudaStream_t st,
 cudaError_t launch_policy_ranks(const PolicyParams& p, int n_streams, cudaStream_t st);
 cudaError_t launch_rerotate(const RopeParams& p, int n_streams, bool bf16, cudaStream_t st);
 cudaError_t launch_append(const AppendParams& p, bool bf16, cudaStream_t st);
-// `group` > 8 query heads per K/V head: units of 16 query heads, else of 8
-inline int attend_unit_heads(int group) { return group > 8 ? 16 : 8; }
+// query heads of a unit: 16 where more than 8 share a K/V head, so that K and V are read once for
+// them - unless the head is so wide that two blocks' queries and sums do not fit the registers
+inline int attend_unit_heads(int group, int head_dim) { return group > 8 && head_dim <= 128 ? 16 : 8; }
 cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st);
 HeadTiling head_tiling(int64_t rows, int64_t n_cols);
 cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hidden, int64_t hidden_stride,
