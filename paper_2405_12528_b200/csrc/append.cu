@@ -22,12 +22,19 @@ namespace sirllm {
 namespace {
 
 constexpr int kAppendThreads = 128;
+constexpr int kAppendTrips = 8;  // trips of a warp, at most: 1 KB of shared memory each
+constexpr int kAppendWarps = kAppendThreads / 32;
 
 template <bool kBf16>
 __device__ __forceinline__ float2 unpack16(uint32_t w) {
     if (kBf16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
     const __half2 h = *reinterpret_cast<const __half2*>(&w);
     return __half22float2(h);
+}
+template <bool kBf16>
+__device__ __forceinline__ float element(const void* p, int i) {
+    const uint16_t w = static_cast<const uint16_t*>(p)[i];
+    return kBf16 ? __uint_as_float((uint32_t)w << 16) : __half2float(__ushort_as_half(w));
 }
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
@@ -54,107 +61,155 @@ __device__ __forceinline__ uint4 pack_vec(const float (&f)[8]) {
                       pack16<kBf16>(f[6], f[7]));
 }
 
-template <bool kBf16>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendParams p) {
-    const int lane = threadIdx.x & 31;
-    const int64_t item = (int64_t)blockIdx.x * (kAppendThreads >> 5) + (threadIdx.x >> 5);
-    const int64_t row = item / p.groups;
-    const int group = (int)(item - row * p.groups);
-    if (row >= (int64_t)p.n_streams * p.max_new) return;
-    const int s = (int)(row / p.max_new);
-    const int t = (int)(row - (int64_t)s * p.max_new);
+__device__ __forceinline__ void copy_async(uint4* dst, const uint4* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
+// kHalf: pairs (row[i], row[i + d/2]), else (row[2i], row[2i+1]); kNorm: queries, keys or both have weights.
+template <bool kBf16, bool kHalf, bool kNorm>
+__global__ void __launch_bounds__(kAppendThreads, 8) append_kernel(const __grid_constant__ AppendParams p) {
+    // Per pair what turns it: (cosine, sine) - or, with norms, the rotation with the weights folded
+    // in, for queries and for keys: a' = r * (a * x + b * y), b' = r * (a * z + b * w), r the
+    // reciprocal norm.  Pair 8c + j stands at 32j + c, so that the lanes of a team read side by side.
+    __shared__ float2 turned[kNorm ? 1 : SIRLLM_MAX_HEAD_DIM / 2];
+    __shared__ float4 folded[kNorm ? 2 : 1][kNorm ? SIRLLM_MAX_HEAD_DIM / 2 : 1];
+    extern __shared__ uint4 staged[];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int row = blockIdx.x / p.groups, group = blockIdx.x - row * p.groups;
+    const int s = row / p.max_new, t = row - s * p.max_new;
+    const int first = p.first_slot[s];
     const int T = p.n_new ? min(p.n_new[s], p.max_new) : p.max_new;
     if (t >= T) return;
-    const int first = p.first_slot[s];
     if (first < 0 || first > p.capacity - T) {
-        if (t == 0 && group == 0 && lane == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
+        if (t == 0 && group == 0 && tid == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
         return;
     }
     const int slot = first + t;
 
     // a lane's vectors: pairs 8c .. 8c+7 of a head
     const int units = p.head_dim >> 4;  // lanes of a team with work
-    const int c = lane & (p.team - 1);
+    const int c = lane & (p.team - 1), teams = 32 / p.team, member = lane / p.team;
     const bool on = c < units;
-    const int va = p.layout == SIRLLM_ROPE_HALF ? c : 2 * c;
-    const int vb = p.layout == SIRLLM_ROPE_HALF ? c + units : 2 * c + 1;
-    float cs[8], sn[8];
-    if (on) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const double turns = (double)slot * p.turns[8 * c + j];
-            const float frac = (float)(turns - rint(turns));  // [-0.5, 0.5] of a turn
-            sincospif(2.0f * frac, &sn[j], &cs[j]);
+    const int va = kHalf ? c : 2 * c, vb = kHalf ? c + units : 2 * c + 1;
+    // A trip is one head per team; first the queries' trips, then the keys', then the values'.
+    const int q_trips = (p.n_heads + teams - 1) / teams, kv_trips = (p.n_kv_heads + teams - 1) / teams;
+    const int trip0 = group * p.trips_per_block + warp;
+    const int trip_end = min(p.trips, (group + 1) * p.trips_per_block);
+    // All of the warp's vectors are asked for at once, into shared memory: a lane reads back what it
+    // asked for itself.
+    uint4* const box = staged + warp * p.trips_per_warp * 64 + lane;
+    uint4* to = box;
+    for (int trip = trip0; trip < trip_end; trip += kAppendWarps, to += 64) {
+        const bool is_q = trip < q_trips, is_v = trip >= q_trips + kv_trips;
+        const int h = (is_q ? trip : is_v ? trip - q_trips - kv_trips : trip - q_trips) * teams + member;
+        const char* base = is_q ? p.q : is_v ? p.v_new : p.k_new;
+        const int64_t stride = is_q ? p.q_stride : is_v ? p.v_stride : p.k_stride;
+        if (on && h < (is_q ? p.n_heads : p.n_kv_heads)) {
+            const uint4* src = reinterpret_cast<const uint4*>(base + (row * stride + h * p.head_dim) * 2);
+            copy_async(to, &src[va]);
+            copy_async(to + 32, &src[vb]);
+        } else {
+            to[0] = to[32] = make_uint4(0, 0, 0, 0);
         }
     }
-    const int teams = 32 / p.team;
-    const int h_end = min(p.heads_all, (group + 1) * p.heads_per_group);
-    for (int h0 = group * p.heads_per_group; h0 < h_end; h0 += teams) {
-        // heads 0 .. n_heads-1 are queries, then come the keys, then the values
-        const int h = h0 + lane / p.team;
-        const bool has = on && h < h_end;
-        const bool is_q = h < p.n_heads, is_v = h >= p.n_heads + p.n_kv_heads;
-        const int hk = is_v ? h - p.n_heads - p.n_kv_heads : h - p.n_heads;
-        const char* src = is_q   ? p.q + (row * p.q_stride + (int64_t)h * p.head_dim) * 2
-                          : is_v ? p.v_new + (row * p.v_stride + (int64_t)hk * p.head_dim) * 2
-                                 : p.k_new + (row * p.k_stride + (int64_t)hk * p.head_dim) * 2;
-        uint4 xa = make_uint4(0, 0, 0, 0), xb = xa;
-        if (has) {
-            xa = reinterpret_cast<const uint4*>(src)[va];
-            xb = reinterpret_cast<const uint4*>(src)[vb];
-        }
-        const char* w = static_cast<const char*>(is_q ? p.q_weight : p.k_weight);
-        float a[8], b[8];
-        unpack_vec<kBf16>(xa, a);
-        unpack_vec<kBf16>(xb, b);
-        if (p.normed) {
-            float sum = 0.f;
+    // meanwhile the row's angles, one thread per pair
+    for (int i = tid; i < p.head_dim / 2; i += kAppendThreads) {
+        const double turns = (double)slot * p.turns[i];
+        const float x = 6.283185307f * (float)(turns - rint(turns));  // [-pi, pi]
+        const float cosine = __cosf(x), sine = __sinf(x);
+        const int at = (i & 7) * 32 + (i >> 3);
+        if (!kNorm) {
+            turned[at] = make_float2(cosine, sine);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(a[j], a[j], fmaf(b[j], b[j], sum));
-            for (int o = p.team >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            if (has && !is_v && w != nullptr) {
-                const float r = rsqrtf(sum / (float)p.head_dim + p.eps);
-                float wa[8], wb[8];
-                unpack_vec<kBf16>(reinterpret_cast<const uint4*>(w)[va], wa);
-                unpack_vec<kBf16>(reinterpret_cast<const uint4*>(w)[vb], wb);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    a[j] = a[j] * r * wa[j];
-                    b[j] = b[j] * r * wb[j];
-                }
+            for (int kind = 0; kind < 2; ++kind) {
+                const void* w = kind == 0 ? p.q_weight : p.k_weight;
+                const float w1 = w ? element<kBf16>(w, kHalf ? i : 2 * i) : 1.f;
+                const float w2 = w ? element<kBf16>(w, kHalf ? i + p.head_dim / 2 : 2 * i + 1) : 1.f;
+                folded[kind][at] = make_float4(w1 * cosine, -(w2 * sine), w1 * sine, w2 * cosine);
             }
         }
-        if (!has) continue;
+    }
+    __syncthreads();
+    float cs[8], sn[8];
+#pragma unroll
+    for (int j = 0; j < 8 && !kNorm; ++j) {
+        const float2 v = turned[32 * j + (on ? c : 0)];
+        cs[j] = v.x;
+        sn[j] = v.y;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    const uint4* from = box;
+    for (int trip = trip0; trip < trip_end; trip += kAppendWarps, from += 64) {
+        const bool is_q = trip < q_trips, is_v = trip >= q_trips + kv_trips;
+        const int h = (is_q ? trip : is_v ? trip - q_trips - kv_trips : trip - q_trips) * teams + member;
+        uint4 xa = from[0], xb = from[32];
         if (!is_v) {
-            float u[8], v[8];
-            if (p.layout == SIRLLM_ROPE_HALF) {  // a holds the pairs' first elements, b their second
+            float a[8], b[8];
+            unpack_vec<kBf16>(xa, a);
+            unpack_vec<kBf16>(xb, b);
+            float r = 1.f;
+            if (kNorm && (is_q ? p.q_weight : p.k_weight) != nullptr) {
+                float sum = 0.f, sum2 = 0.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    u[j] = fmaf(a[j], cs[j], -(b[j] * sn[j]));
-                    v[j] = fmaf(a[j], sn[j], b[j] * cs[j]);
+                    sum = fmaf(a[j], a[j], sum);
+                    sum2 = fmaf(b[j], b[j], sum2);
                 }
-            } else {  // pairs side by side: four in a, four in b
+                sum += sum2;
+                for (int o = p.team >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                r = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
+            }
+            float u[8], v[8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    u[2 * j] = fmaf(a[2 * j], cs[j], -(a[2 * j + 1] * sn[j]));
-                    u[2 * j + 1] = fmaf(a[2 * j], sn[j], a[2 * j + 1] * cs[j]);
-                    v[2 * j] = fmaf(b[2 * j], cs[4 + j], -(b[2 * j + 1] * sn[4 + j]));
-                    v[2 * j + 1] = fmaf(b[2 * j], sn[4 + j], b[2 * j + 1] * cs[4 + j]);
+            for (int j = 0; j < 8; ++j) {
+                // pair j: (a[j], b[j]), or two neighbours in a (j < 4) or b
+                const float x = kHalf ? a[j] : j < 4 ? a[2 * (j & 3)] : b[2 * (j & 3)];
+                const float y = kHalf ? b[j] : j < 4 ? a[2 * (j & 3) + 1] : b[2 * (j & 3) + 1];
+                float x2, y2;
+                if (kNorm) {
+                    const float4 f = folded[is_q ? 0 : 1][32 * j + (on ? c : 0)];
+                    x2 = fmaf(x, f.x, y * f.y) * r;
+                    y2 = fmaf(x, f.z, y * f.w) * r;
+                } else {
+                    x2 = fmaf(x, cs[j], -(y * sn[j]));
+                    y2 = fmaf(x, sn[j], y * cs[j]);
+                }
+                if (kHalf) {
+                    u[j] = x2;
+                    v[j] = y2;
+                } else if (j < 4) {
+                    u[2 * (j & 3)] = x2;
+                    u[2 * (j & 3) + 1] = y2;
+                } else {
+                    v[2 * (j & 3)] = x2;
+                    v[2 * (j & 3) + 1] = y2;
                 }
             }
             xa = pack_vec<kBf16>(u);
             xb = pack_vec<kBf16>(v);
         }
-        char* dst;
-        if (is_q) {
-            dst = p.q_out + (row * p.q_out_stride + (int64_t)h * p.head_dim) * 2;
-        } else {
-            const int64_t plane = (int64_t)s * p.planes_per_stream + p.layer_plane + hk;
-            dst = (is_v ? p.v : p.k) + (plane * p.capacity + slot) * p.head_dim * 2;
+        if (on && h < (is_q ? p.n_heads : p.n_kv_heads)) {
+            const int64_t plane = (int64_t)s * p.planes_per_stream + p.layer_plane + h;
+            char* dst = is_q ? p.q_out + (row * p.q_out_stride + h * p.head_dim) * 2
+                             : (is_v ? p.v : p.k) + (plane * p.capacity + slot) * p.head_dim * 2;
+            reinterpret_cast<uint4*>(dst)[va] = xa;
+            reinterpret_cast<uint4*>(dst)[vb] = xb;
         }
-        reinterpret_cast<uint4*>(dst)[va] = xa;
-        reinterpret_cast<uint4*>(dst)[vb] = xb;
     }
+}
+
+template <bool kBf16, bool kHalf>
+cudaError_t launch_norm(const cudaLaunchConfig_t& cfg, const AppendParams& p) {
+    return p.q_weight != nullptr || p.k_weight != nullptr
+               ? cudaLaunchKernelEx(&cfg, append_kernel<kBf16, kHalf, true>, p)
+               : cudaLaunchKernelEx(&cfg, append_kernel<kBf16, kHalf, false>, p);
+}
+template <bool kBf16>
+cudaError_t launch_pairing(const cudaLaunchConfig_t& cfg, const AppendParams& p) {
+    return p.layout == SIRLLM_ROPE_HALF ? launch_norm<kBf16, true>(cfg, p) : launch_norm<kBf16, false>(cfg, p);
 }
 
 }  // namespace
@@ -171,21 +226,26 @@ cudaError_t launch_append(const AppendParams& p, bool bf16, cudaStream_t st) {
     q.team = 1;
     while (q.team < units) q.team *= 2;
     const int teams = 32 / q.team;
-    // Few rows: a warp takes one head per team, so that a single token's heads spread over the
-    // device.  Many rows: a warp walks more of a row's heads with the same angles.
-    const int trips = (p.heads_all + teams - 1) / teams;
-    int64_t per_warp = rows * trips / ((int64_t)dp.n_sm * 32);
-    if (per_warp < 1) per_warp = 1;
-    if (per_warp > trips) per_warp = trips;
-    q.heads_per_group = (int32_t)per_warp * teams;
-    q.groups = (p.heads_all + q.heads_per_group - 1) / q.heads_per_group;
-    const int64_t blocks = (rows * q.groups + (kAppendThreads / 32) - 1) / (kAppendThreads / 32);
-    if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
-    if (bf16)
-        append_kernel<true><<<(unsigned)blocks, kAppendThreads, 0, st>>>(q);
-    else
-        append_kernel<false><<<(unsigned)blocks, kAppendThreads, 0, st>>>(q);
-    return cudaGetLastError();
+    q.inv_dim = 1.0f / (float)p.head_dim;
+    q.trips = (p.n_heads + teams - 1) / teams + 2 * ((p.n_kv_heads + teams - 1) / teams);
+    // Few rows: one trip per warp, so that a single token's heads spread over the device.  Many rows:
+    // a block takes a whole row, whose angles it computes once.
+    const int most = rows >= (int64_t)dp.n_sm * 2 ? kAppendTrips : 1;
+    q.groups = (q.trips + most * kAppendWarps - 1) / (most * kAppendWarps);
+    q.trips_per_block = (q.trips + q.groups - 1) / q.groups;
+    q.trips_per_warp = (q.trips_per_block + kAppendWarps - 1) / kAppendWarps;
+    if (rows * q.groups > 0x7FFFFFFF) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * q.groups));
+    cfg.blockDim = dim3(kAppendThreads);
+    cfg.dynamicSmemBytes = (size_t)q.trips_per_warp * 1024 * kAppendWarps;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return bf16 ? launch_pairing<true>(cfg, q) : launch_pairing<false>(cfg, q);
 }
 
 }  // namespace sirllm

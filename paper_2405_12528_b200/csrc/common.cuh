@@ -150,10 +150,11 @@ struct AppendParams {
     // theta_i / 2pi for the d/2 pairs of a head, computed once per call on the host
     double turns[SIRLLM_MAX_HEAD_DIM / 2];
     float eps;
-    int32_t n_heads, n_kv_heads, head_dim, capacity, max_new, n_streams, layout, normed;
+    int32_t n_heads, n_kv_heads, head_dim, capacity, max_new, n_streams, layout;
     int32_t planes_per_stream, layer_plane;  // planes of a stream, the layer's first
-    int32_t heads_all;                       // n_heads + 2 * n_kv_heads
-    int32_t team, heads_per_group, groups;   // set by the launcher
+    // set by the launcher
+    float inv_dim;
+    int32_t team, trips, trips_per_block, trips_per_warp, groups;
 };
 
 constexpr int kAttendMaxCtas = 256;   // CTAs of an attention call, at most
