@@ -209,17 +209,28 @@ class Prepared:
     def __init__(self, fn, cfg, args):
         self._fn, self._cfg = fn, Config.from_buffer_copy(cfg)
         self._keep = [a.t for a in args if isinstance(a, _Arg)]
-        self._raw = [a.ptr() if isinstance(a, _Arg) else a for a in args]
-        self._stream_at = [i for i, a in enumerate(args) if isinstance(a, _CurrentStream)]
-        self._cfg_ref = ctypes.byref(self._cfg)
+        # arguments as instances of the C types, converted once
+        self._stream = ctypes.c_void_p()
+        raw = [self._stream if isinstance(a, _CurrentStream) else a.ptr() if isinstance(a, _Arg) else a for a in args]
+        self._args = [ctypes.byref(self._cfg)] + [
+            t(a) if t in _PLAIN and not isinstance(a, t) else a for t, a in zip(fn.argtypes[1:], raw)]
+        self._device = torch.cuda.current_device()
 
     def __call__(self) -> None:
-        raw = self._raw
-        for i in self._stream_at:
-            raw[i] = torch.cuda.current_stream().cuda_stream
-        rc = self._fn(self._cfg_ref, *raw)
+        self._stream.value = _raw_stream(self._device)
+        rc = self._fn(*self._args)
         if rc != OK:
             _check(rc)
+
+
+_PLAIN = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float,
+          ctypes.c_double)
+
+
+def _raw_stream(device: int) -> int:
+    """Handle of the device's current stream (torch's short way where this torch has it)."""
+    short = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return short(device) if short is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 _preparing = threading.local()
