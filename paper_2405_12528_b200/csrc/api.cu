@@ -638,8 +638,12 @@ int sirllm_append_kv(const sirllm_config* cfg, int32_t layer, const void* q, int
     const int64_t kv_width = (int64_t)cfg->n_kv_heads * cfg->head_dim;
     const int64_t q_width = (int64_t)n_heads * cfg->head_dim;
     if (layer < 0 || layer >= cfg->n_layers || cfg->head_dim % 16 != 0 || n_heads < 0 ||
-        (q != nullptr) != (n_heads > 0) || q_width > 0x3FFFFFFF || kv_width > 0x3FFFFFFF)
+        (q != nullptr) != (n_heads > 0))
         return SIRLLM_ERR_BAD_CONFIG;
+    // heads of all rows, and elements of a row, are counted in 32 bits
+    if (q_width > 0x3FFFFFFF || kv_width > 0x1FFFFFFF ||
+        ((int64_t)n_heads + 2 * (int64_t)cfg->n_kv_heads) * cfg->n_streams > 0x7FFFFFFF / (cfg->max_new > 0 ? cfg->max_new : 1))
+        return SIRLLM_ERR_TOO_LARGE;
     if (!(rope_base > 0.0) || !std::isfinite(rope_base) ||
         (layout != SIRLLM_ROPE_HALF && layout != SIRLLM_ROPE_INTERLEAVED) || !(eps >= 0.0f) || !std::isfinite(eps))
         return SIRLLM_ERR_BAD_CONFIG;

@@ -37,7 +37,7 @@ def append(lib, c=None, **kw):
     (B.ERR_NULL, dict(q=None)), (B.ERR_NULL, dict(q_out=None)),
     (B.ERR_BAD_CONFIG, dict(layer=-1)), (B.ERR_BAD_CONFIG, dict(layer=3)), (B.ERR_BAD_CONFIG, dict(n_heads=0)),
     (B.ERR_BAD_CONFIG, dict(n_heads=-4)), (B.ERR_BAD_CONFIG, dict(q=None, q_out=None)),
-    (B.ERR_BAD_CONFIG, dict(n_heads=0x3FFFFFFF)),
+    (B.ERR_TOO_LARGE, dict(n_heads=0x3FFFFFFF)),
     (B.ERR_BAD_CONFIG, dict(base=0.0)), (B.ERR_BAD_CONFIG, dict(base=-1.0)), (B.ERR_BAD_CONFIG, dict(base=math.inf)),
     (B.ERR_BAD_CONFIG, dict(base=math.nan)), (B.ERR_BAD_CONFIG, dict(layout=2)), (B.ERR_BAD_CONFIG, dict(eps=-1e-6)),
     (B.ERR_BAD_CONFIG, dict(eps=math.nan)), (B.ERR_BAD_CONFIG, dict(qs=248)), (B.ERR_BAD_CONFIG, dict(os=248)),
@@ -52,6 +52,11 @@ def test_append_refusals(lib, want, kw):
 def test_append_refuses_heads_of_half_vectors(lib):
     assert append(lib, cfg(head_dim=40), qs=160, os=160, ks=80, vs=80) == B.ERR_BAD_CONFIG
     assert append(lib, cfg(budget=5)) == B.ERR_BAD_CONFIG
+
+
+def test_append_refuses_more_heads_than_it_counts(lib):
+    big = cfg(n_streams=2**20, max_new=128, n_layers=1)
+    assert append(lib, big, n_heads=16, qs=1024, os=1024) == B.ERR_TOO_LARGE
 
 
 def attend(lib, c=None, **kw):

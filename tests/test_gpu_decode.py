@@ -83,6 +83,8 @@ APPEND = [  # S, M, H, KH, D, first, capacity
     (2, 300, 8, 1, 64, [40000, 5], 40300),
     (2, 3, 2, 2, 512, [11, 0], 14),
     (4, 5, 3, 3, 112, [0, 1, 2, 3], 9),
+    (2, 200, 40, 3, 512, [0, 7], 210),       # more heads than one block takes
+    (300, 1, 5, 5, 32, [17] * 300, 20),
 ]
 
 
@@ -272,6 +274,15 @@ def test_attend_many_streams_of_all_lengths():
 def test_attend_only_the_last_stream_has_slots():
     attend_case(600, 2, 1, 64, 40, [0] * 599 + [33], seed=9)
     attend_case(5, 2, 1, 128, 40, [0] * 5, seed=9)
+
+
+@pytest.mark.parametrize("S,KH", [(1, 1), (1, 8), (3, 5), (1, 16), (2, 15), (3, 11), (1, 34), (2, 30), (2, 37), (5, 15),
+                                  (4, 37), (1, 149)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_however_the_units_are_dealt_out(S, KH, D):
+    # whole units per CTA, per cluster of 2, 4 or 8, or shares of the line: even and uneven lengths
+    attend_case(S, 2 * KH, KH, D, 3100, [3100 - 3 * s for s in range(S)], seed=S * KH)
+    attend_case(S, KH, KH, D, 3100, [[3000, 31, 0, 1500, 700][s % 5] for s in range(S)], seed=S + KH)
 
 
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 30.0])
@@ -464,6 +475,36 @@ def test_head_ragged_rows_leave_the_rest_alone(S, M, lens):
     assert B.sirllm_status(ws) == 0
 
 
+def test_head_many_row_blocks_some_without_work():
+    g = gen(25)
+    S, M, W, V = 50, 300, 64, 300
+    lens = [0 if s % 3 == 0 else (M if s % 3 == 1 else 17) for s in range(S)]
+    cfg = config(S=S, C=M, M=M, V=V)
+    hidden = randn(g, S * M, W, dtype=torch.bfloat16)
+    weight = randn(g, V, W, dtype=torch.bfloat16, scale=0.2)
+    ids = torch.randint(0, V, (S * M,), generator=g, device="cuda", dtype=torch.int32)
+    used = torch.zeros(S * M, dtype=torch.bool, device="cuda")
+    for s, n in enumerate(lens):
+        used[s * M:s * M + n] = True
+    pairs, target, ent, ws = head_scores(cfg, hidden, weight, ids, i32(*lens))
+    assert (ent[~used] == 7).all() and (pairs[~used] == 7).all()
+    _, want, walk = ref_scores(hidden[used], weight, ids[used])
+    assert_scores(ent[used], want, walk)
+
+
+def test_head_more_rows_than_one_launch_takes():
+    g = gen(26)
+    S, M, W, V = 22, 49152, 8, 40                                      # 1,081,344 rows
+    cfg = config(S=S, C=M, M=M, V=V)
+    hidden = randn(g, S * M, W, dtype=torch.bfloat16)
+    weight = randn(g, V, W, dtype=torch.bfloat16)
+    ids = torch.randint(0, V, (S * M,), generator=g, device="cuda", dtype=torch.int32)
+    _, _, ent, ws = head_scores(cfg, hidden, weight, ids, None)
+    _, want, walk = ref_scores(hidden, weight, ids)
+    assert_scores(ent, want, walk)
+    assert B.sirllm_status(ws) == 0
+
+
 def test_head_column_ranges_add_up_to_the_whole():
     g = gen(21)
     rows, W, V = 150, 320, 5000
@@ -612,3 +653,94 @@ def test_dialogue_rounds_of_decode_steps():
             mk[s, :, :, :n], mv[s, :, :, :n] = mk[s, :, :, rows].clone(), mv[s, :, :, rows].clone()
             assert same_bits(k[s, :, :, :n], mk[s, :, :, :n]) and same_bits(v[s, :, :, :n], mv[s, :, :, :n])
     assert evicted
+
+
+def test_decode_steps_back_to_back_and_replayed_equal_steps_one_by_one():
+    """append -> attend -> head -> score for every token of a turn: launched without a wait between
+    them, replayed from one graph, and with a synchronisation after every call."""
+    g = gen(32)
+    S, L, KH, H, D, C, M, V, W = 3, 2, 4, 8, 128, 700, 6, 3000, 256
+    dt = torch.bfloat16
+    cfg = B.make_config(n_streams=S, n_layers=L, n_kv_heads=KH, head_dim=D, capacity=C, budget=600, n_sink=2,
+                        n_recent=8, max_new=1, vocab=V, logits_dtype="f32", kv_dtype="bf16")
+    k0, v0 = (randn(g, S, L, KH, C, D, dtype=dt) for _ in range(2))
+    qkv = randn(g, M, L, S, H + 2 * KH, D, dtype=dt)
+    hidden, weight = randn(g, M, S, W, dtype=dt), randn(g, V, W, dtype=dt, scale=0.2)
+    ids = torch.randint(0, V, (M, S), generator=g, device="cuda", dtype=torch.int32)
+    start = torch.tensor([600, 0, 333], dtype=torch.int32, device="cuda")
+    wq, wk = randn(g, D, dtype=dt), randn(g, D, dtype=dt)
+
+    def buffers():
+        return dict(k=k0.clone(), v=v0.clone(), q=torch.zeros(M, L, S, H, D, dtype=dt, device="cuda"),
+                    out=torch.zeros(M, L, S, H, D, dtype=dt, device="cuda"), ent=torch.zeros(M, S, device="cuda"),
+                    first=start.clone(), lens=start + 1, ws=B.new_workspace(cfg), wa=B.new_attend_workspace(cfg),
+                    pairs=torch.zeros(S, B.sirllm_head_tiles(cfg, V), 2, device="cuda"),
+                    target=torch.zeros(S, device="cuda"))
+
+    def run(b, wait):
+        for t in range(M):
+            for layer in range(L):
+                x = qkv[t, layer]
+                B.sirllm_append_kv(cfg, layer, x[:, :H], x[:, H:H + KH], x[:, H + KH:], wq, wk, 1e-6, 1e4, B.ROPE_HALF,
+                                   b["first"], None, b["q"][t, layer], b["k"], b["v"], b["ws"])
+                wait()
+                B.sirllm_attend(cfg, layer, b["q"][t, layer], b["k"], b["v"], b["lens"], None, b["out"][t, layer], None,
+                                b["wa"])
+                wait()
+            B.sirllm_head_pairs(cfg, hidden[t], weight, 0, ids[t], None, b["pairs"], b["target"], b["ws"])
+            wait()
+            B.sirllm_score_pairs(cfg, b["pairs"], b["target"], ids[t], None, b["ent"][t], b["ws"])
+            wait()
+            b["first"] += 1
+            b["lens"] += 1
+
+    def same(x, y):
+        return all(torch.equal(x[n].view(torch.uint8), y[n].view(torch.uint8)) for n in ("k", "v", "q", "out", "ent"))
+
+    one, loose, graphed = buffers(), buffers(), buffers()
+    run(one, torch.cuda.synchronize)
+    run(loose, lambda: None)
+    torch.cuda.synchronize()
+    assert same(one, loose)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr, stream=side):
+        run(graphed, lambda: None)
+    for _ in range(3):                               # the same turn again from the same start
+        graphed["first"].copy_(start)
+        graphed["lens"].copy_(start + 1)
+        gr.replay()
+        torch.cuda.synchronize()
+        assert same(one, graphed)
+    assert B.sirllm_status(graphed["ws"]) == 0 and B.sirllm_status(graphed["wa"]) == 0
+
+
+def test_calls_at_once_on_two_streams():
+    g = gen(33)
+    dt = torch.bfloat16
+    cfg = config(S=2, KH=8, D=128, C=4096, M=1, V=9000)
+    k, v = (randn(g, 2, 1, 8, 4096, 128, dtype=dt) for _ in range(2))
+    q, hidden = randn(g, 2, 32, 128, dtype=dt), randn(g, 2, 512, dtype=dt)
+    weight = randn(g, 9000, 512, dtype=dt, scale=0.1)
+    ids, lens = i32(5, 8999), i32(4096, 1777)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    torch.cuda.synchronize()
+    for st in streams:                               # each stream has workspaces of its own
+        with torch.cuda.stream(st):
+            wa, ws = B.new_attend_workspace(cfg), B.new_workspace(cfg)
+            out, pairs = torch.zeros_like(q), torch.zeros(2, B.sirllm_head_tiles(cfg, 9000), 2, device="cuda")
+            target, ent = torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+            got.append((out, ent, wa, ws, pairs, target))
+    for _ in range(20):
+        for st, (out, ent, wa, ws, pairs, target) in zip(streams, got):
+            with torch.cuda.stream(st):
+                B.sirllm_attend(cfg, 0, q, k, v, lens, None, out, None, wa)
+                B.sirllm_head_pairs(cfg, hidden, weight, 0, ids, None, pairs, target, ws)
+                B.sirllm_score_pairs(cfg, pairs, target, ids, None, ent, ws)
+    torch.cuda.synchronize()
+    assert same_bits(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    check_attend(q, k, v, [4096, 1777], 128 ** -0.5, got[0][0], None)
+    _, want, walk = ref_scores(hidden, weight, ids)
+    assert_scores(got[0][1], want, walk)
