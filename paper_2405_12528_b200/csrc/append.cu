@@ -67,7 +67,7 @@ __device__ __forceinline__ void copy_async(uint4* dst, const uint4* src) {
 
 // kHalf: pairs (row[i], row[i + d/2]), else (row[2i], row[2i+1]); kNorm: queries, keys or both have weights.
 template <bool kBf16, bool kHalf, bool kNorm>
-__global__ void __launch_bounds__(kAppendThreads, 8) append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, 9) append_kernel(const __grid_constant__ AppendParams p) {
     // Per pair what turns it: (cosine, sine) - or, with norms, the rotation with the weights folded
     // in, for queries and for keys: a' = r * (a * x + b * y), b' = r * (a * z + b * w), r the
     // reciprocal norm.  Pair 8c + j stands at 32j + c, so that the lanes of a team read side by side.
