@@ -4,14 +4,19 @@
 //   norm    y_j = x_j * rsqrt(mean_j x_j^2 + eps) * w_j          (only with weights)
 //   rotary  pair i of the head times exp(i * p * theta_i),  theta_i = base^(-2i/d)
 //
-// Bytes are all there is: every element is read once and written once.  A head is handled by a
-// team of lanes (d/16 of them, each holding the two 16-byte vectors that carry eight pairs), so
-// the norm's sum is a few shuffles inside the team, and a row's angles (the same for all of its
-// heads) are computed once per warp and kept in registers while the warp walks the heads.
+// Bytes are all there is: every element is read once and written once.  A block takes one token's
+// row (few tokens: a share of its heads), asks for all of it at once and computes the row's
+// angles, the same for every head, one thread per pair, while the vectors are on their way.  A
+// head is handled by a team of lanes (d/16 of them, each with the two 16-byte vectors that carry
+// eight pairs), so the norm's sum is a few shuffles inside the team.
 // Angles are positions of up to tens of thousands times frequencies down from 1: the number of
 // TURNS p * theta / 2pi is formed and reduced in fp64 and only the fraction of a turn goes to
-// fp32 (its sine and cosine carry 2^-24 of absolute error wherever the token sits).  Sums,
-// norm and rotation are fp32; each element is rounded once, to the cache's type.
+// fp32, so sine and cosine (fast forms, on [-pi, pi]) carry 5e-7 of absolute error wherever the
+// token sits: a hundredth of the rounding to fp16.  Sums, norm and rotation are fp32; each element is
+// rounded once, to the cache's type.
+// Measured, 4096 tokens x 48 heads x 128 bf16 (50 MB in, 50 MB out): 20.9 us with norms (0.75 of the
+// copy rate), 18.1 us without; 16384 tokens with norms 68.5 us (0.91); one token 2.4 us.  What is
+// left at 4096 tokens is the start and the last, partly filled wave of blocks.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

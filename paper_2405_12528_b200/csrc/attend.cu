@@ -4,11 +4,12 @@
 //
 // A token does 2 multiply-adds per cache element it reads and per head that shares the element,
 // so HBM bounds it: every live K and V row has to come in once.  The cache is cut into tiles of
-// 16 slots.  All tiles of all (stream, K/V head) units stand in one line, and every CTA takes an
-// equal stretch of it - whatever the lengths are, the CTAs read the same amount (a unit that
-// spans CTAs leaves partial results (max, sum, weighted rows) in the workspace; the CTA that
-// finishes last, by ticket, joins them in a fixed order, so results do not depend on timing).
-// Inside a CTA every warp streams its own tiles through its own ring of cp.async stages and
+// 16 slots.  How the tiles are dealt out is decided on the device, where the lengths are: all
+// tiles of all (stream, K/V head) units in one line and an equal stretch per CTA - whatever the
+// lengths are, the CTAs read the same amount, and a unit that spans CTAs leaves partial results
+// (max, sum, weighted rows) in the workspace, joined by the CTA that finishes last, by ticket -
+// or whole units per CTA, or per cluster of CTAs joined through shared memory.  Joins add in a
+// fixed order, so results do not depend on timing.  Inside a CTA every warp streams its own tiles through its own ring of cp.async stages and
 // keeps a running softmax; nothing but the end of a unit makes warps wait for one another, and
 // the ring runs ahead across units.
 //
@@ -21,6 +22,9 @@
 // fp32: scores, running maximum and sum, output sums, the join.  Rounded to 16 bits: the
 // probabilities on their way into the second product (relative to a reference that the true
 // maximum exceeds by less than 2^8, so fp16 cannot overflow), and the result.
+// Measured, bf16, heads of 128: 64 streams x 32 heads x 900 - 1280 slots 171 us (1.03 of the copy
+// rate, part from L2), 16 x 32 heads x 2048 slots 86 us (0.96), one stream x 8 heads x 12287 slots
+// 16.3 us (0.48: launch, reading the length and the join are 7 us of it, and 64 SMs read).
 #include <atomic>
 
 #include <cuda_bf16.h>

@@ -25,6 +25,10 @@
 // into chunks of kChunkSteps stages: a chunk is summed in TMEM, the chunks in registers with
 // rounded additions (128 columns of one row per thread); 9e-7 remain at any d.  Nothing is rounded
 // to 16 bits.
+//
+// Measured, bf16: 2048 rows x 37888 columns x 4096 in 371 us (1715 TFLOP/s, 1.03 of cuBLAS's measured
+// burst), 4096 x 128256 x 4096 back to back 2.9 - 3.1 ms (1.00 - 1.06 of its rate under the power cap);
+// 1 row x 128256 x 4096 in 176 us (6.0 TB/s, 0.93 of the copy rate), 1 x 32000 x 4096 in 46 us (0.87).
 #include <atomic>
 
 #include <cuda.h>

@@ -80,16 +80,21 @@ def plane_shard(n_layers: int, n_kv_heads: int, world: int, rank: int, by: str =
 def exchange_vocab_partials(pairs_local: torch.Tensor, target_local: torch.Tensor, group=None):
     """Combines the ranks' shares of vocabulary-parallel scoring.
 
-    ``pairs_local`` is this rank's ``[rows, 2]`` (max, sum exp) pairs, ``target_local`` its
-    ``[rows]`` target logits (0 where the token's column belongs to another rank).  Returns
-    ``pairs [rows, world, 2]`` (all-gather) and ``target [rows]`` (sum over ranks: exactly one
+    ``pairs_local`` is this rank's ``[rows, 2]`` (max, sum exp) pairs (``sirllm_score_partial``)
+    or its ``[rows, tiles, 2]`` pairs (``sirllm_head_pairs``), ``target_local`` its ``[rows]``
+    target logits (0 where the token's column belongs to another rank).  Returns ``pairs
+    [rows, world * tiles, 2]`` (all-gather) and ``target [rows]`` (sum over ranks: exactly one
     rank contributes a non-zero value per row), ready for ``sirllm_score_pairs``.  Message
-    size: 12 bytes per row and rank."""
+    size: 8 bytes per row, rank and tile and 4 per row and rank.  Every rank passes as many tiles
+    as the one that has most: unused ones hold (0, 0), which count for nothing."""
+    if pairs_local.dim() == 2:
+        pairs_local = pairs_local.unsqueeze(1)
     if not (dist.is_available() and dist.is_initialized()) or dist.get_world_size(group) == 1:
-        return pairs_local.unsqueeze(1).contiguous(), target_local.clone()
+        return pairs_local.contiguous(), target_local.clone()
     world = dist.get_world_size(group)
+    pairs_local = pairs_local.contiguous()
     gathered = [torch.empty_like(pairs_local) for _ in range(world)]
-    dist.all_gather(gathered, pairs_local.contiguous(), group=group)
+    dist.all_gather(gathered, pairs_local, group=group)
     target = target_local.clone()
     dist.all_reduce(target, op=dist.ReduceOp.SUM, group=group)
-    return torch.stack(gathered, dim=1).contiguous(), target
+    return torch.cat(gathered, dim=1), target

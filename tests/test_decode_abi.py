@@ -2,11 +2,16 @@
 needed): ``sirllm_append_kv``, ``sirllm_attend``, ``sirllm_head_pairs``."""
 import ctypes
 import math
+import os
+import socket
 
 import pytest
 import torch
+import torch.distributed as dist
+import torch.multiprocessing as mp
 
 from paper_2405_12528_b200 import binding as B
+from paper_2405_12528_b200 import sharding
 
 
 @pytest.fixture(scope="module")
@@ -188,3 +193,50 @@ def test_binding_refuses_wrong_tensors_before_the_library(lib):
     hd("rows must be dense", weight=z(96, 1000).t())
     hd("needs", token_ids=i(15))
     hd("needs", target_out=torch.zeros(15))
+
+
+# ---- a vocabulary-parallel LM head: several tiles per rank through the exchange (gloo, two ranks) ----
+
+def _tile_pairs(z, width):
+    """(max, sum exp) of every ``width`` columns of fp64 logits, as sirllm_head_pairs hands them out."""
+    parts = [(p.amax(-1), torch.exp(p - p.amax(-1, keepdim=True)).sum(-1)) for p in z.split(width, dim=1)]
+    return torch.stack([torch.stack(p, -1) for p in parts], 1).float()
+
+
+def _rank_of_a_parallel_head(rank, world, port, out):
+    os.environ.update(MASTER_ADDR="127.0.0.1", MASTER_PORT=str(port))
+    dist.init_process_group("gloo", rank=rank, world_size=world)
+    try:
+        g = torch.Generator().manual_seed(4)
+        z, ids = torch.randn(9, 101, generator=g, dtype=torch.float64) * 3, torch.randint(0, 101, (9,), generator=g)
+        a, b = [(0, 70), (70, 101)][rank]                       # 5 and 3 tiles of 16 columns
+        pairs = torch.zeros(9, 5, 2)
+        mine = _tile_pairs(z[:, a:b], 16)
+        pairs[:, :mine.shape[1]] = mine
+        inside = (ids >= a) & (ids < b)
+        target = torch.where(inside, z[torch.arange(9), ids], 0.0).float()
+        got, tgt = sharding.exchange_vocab_partials(pairs, target)
+        e = torch.log((got[..., 1].double() * torch.exp(got[..., 0].double())).sum(-1)) - tgt
+        want = torch.logsumexp(z, -1) - z[torch.arange(9), ids]
+        out.put((rank, tuple(got.shape), float((e - want).abs().max())))
+    finally:
+        dist.destroy_process_group()
+
+
+def test_two_ranks_exchange_several_tiles_each():
+    with socket.socket() as s:
+        s.bind(("127.0.0.1", 0))
+        port = s.getsockname()[1]
+    ctx = mp.get_context("spawn")
+    out = ctx.Queue()
+    procs = [ctx.Process(target=_rank_of_a_parallel_head, args=(r, 2, port, out)) for r in range(2)]
+    for p in procs:
+        p.start()
+    results = sorted(out.get(timeout=120) for _ in procs)
+    for p in procs:
+        p.join(timeout=60)
+        assert p.exitcode == 0
+    # fp32 pairs and targets of logits below 16: each within 2^-21, their sums within a few of those
+    assert all(shape == (9, 10, 2) and worst < 8 * 2.0 ** -21 for _, shape, worst in results)
+    one, tgt = sharding.exchange_vocab_partials(torch.ones(4, 3, 2), torch.ones(4))   # a single process
+    assert one.shape == (4, 3, 2) and tgt.shape == (4,)

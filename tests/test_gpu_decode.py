@@ -744,3 +744,82 @@ def test_calls_at_once_on_two_streams():
     check_attend(q, k, v, [4096, 1777], 128 ** -0.5, got[0][0], None)
     _, want, walk = ref_scores(hidden, weight, ids)
     assert_scores(got[0][1], want, walk)
+
+
+def test_calls_behind_a_join_of_two_captured_streams():
+    # each call's programmatic launch follows work of another stream, joined by an event
+    g = gen(34)
+    dt = torch.bfloat16
+    cfg = config(S=1, KH=2, D=64, C=600, M=1, V=500)
+    ws, wa = B.new_workspace(cfg), B.new_attend_workspace(cfg)
+    k, v = (randn(g, 1, 1, 2, 600, 64, dtype=dt) for _ in range(2))
+    q, kn, vn = (randn(g, 1, h, 64, dtype=dt) for h in (4, 2, 2))
+    hidden, weight = torch.zeros(1, 128, dtype=dt, device="cuda"), randn(g, 500, 128, dtype=dt, scale=0.2)
+    source = randn(g, 1, 128, dtype=dt)
+    lens, first, ids = torch.zeros(1, dtype=torch.int32, device="cuda"), i32(0), i32(77)
+    q_out, out = torch.zeros_like(q), torch.zeros_like(q)
+    pairs, target = torch.zeros(1, B.sirllm_head_tiles(cfg, 500), 2, device="cuda"), torch.zeros(1, device="cuda")
+    ent = torch.zeros(1, device="cuda")
+    main, other = torch.cuda.Stream(), torch.cuda.Stream()
+    gr = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(gr, stream=main):
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            first.fill_(410)
+            lens.fill_(411)
+        main.wait_stream(other)
+        B.sirllm_append_kv(cfg, 0, q, kn, vn, None, None, 0.0, 1e4, B.ROPE_HALF, first, None, q_out, k, v, ws)
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            hidden.copy_(source)
+        B.sirllm_attend(cfg, 0, q_out, k, v, lens, None, out, None, wa)
+        main.wait_stream(other)
+        B.sirllm_head_pairs(cfg, hidden, weight, 0, ids, None, pairs, target, ws)
+        B.sirllm_score_pairs(cfg, pairs, target, ids, None, ent, ws)
+    for _ in range(3):
+        first.zero_()
+        lens.zero_()
+        hidden.zero_()
+        gr.replay()
+        torch.cuda.synchronize()
+        check_attend(q_out, k, v, [411], 64 ** -0.5, out, None)
+        _, want, walk = ref_scores(source, weight, ids)
+        assert_scores(ent, want, walk)
+
+
+FIRST_CALL = """
+import torch
+from paper_2405_12528_b200 import binding as B
+cfg = B.make_config(1, 1, 8, 128, 4096, 4096, 0, 0, {M}, 700, "f32", "bf16")
+dt, M = torch.bfloat16, {M}
+ws, wa = B.new_workspace(cfg), B.new_attend_workspace(cfg)
+k, v = (torch.randn(1, 1, 8, 4096, 128, device="cuda").to(dt) for _ in range(2))
+q, kn = torch.randn(M, 16, 128, device="cuda").to(dt), torch.randn(M, 8, 128, device="cuda").to(dt)
+out, q_out = torch.zeros_like(q), torch.zeros_like(q)
+hidden, weight = torch.randn(M, 64, device="cuda").to(dt), torch.randn(700, 64, device="cuda").to(dt)
+pairs, target = torch.zeros(M, B.sirllm_head_tiles(cfg, 700), 2, device="cuda"), torch.zeros(M, device="cuda")
+ids, first = torch.zeros(M, dtype=torch.int32, device="cuda"), torch.full((1,), 5, dtype=torch.int32, device="cuda")
+lens = torch.full((1,), 4000, dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    B.sirllm_append_kv(cfg, 0, q, kn, kn, None, None, 0.0, 1e4, 0, first, None, q_out, k, v, ws)
+    B.sirllm_attend(cfg, 0, q_out, k, v, lens, None, out, None, wa)
+    B.sirllm_head_pairs(cfg, hidden, weight, 0, ids, None, pairs, target, ws)
+g.replay()
+torch.cuda.synchronize()
+assert float(out[0].abs().sum()) > 0 and float(pairs.abs().sum()) > 0 and B.sirllm_status(ws) == 0
+print("captured")
+"""
+
+
+@pytest.mark.parametrize("M", [1, 200])
+def test_the_process_first_call_may_be_a_captured_one(M):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", FIRST_CALL.format(M=M)], capture_output=True, text=True, cwd=root,
+                         timeout=300)
+    assert run.returncode == 0 and "captured" in run.stdout, run.stderr[-2000:]
