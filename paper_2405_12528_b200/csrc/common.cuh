@@ -199,6 +199,7 @@ struct HeadParams {
     int32_t row_blocks;                      // blocks of rows of this launch
     int32_t n_parts, n_tiles, part_tiles, tile_cols, half_cols;
     int32_t a_bytes, b_bytes, load_bytes, stage_bytes, stages;  // a box of each, a stage of boxes
+    uint32_t div_mul, div_shift1, div_shift2;                   // division by max_new
 };
 
 // How the LM head's product is cut: column ranges ("parts", one pair per row each) of part_tiles

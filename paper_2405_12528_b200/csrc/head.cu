@@ -170,13 +170,40 @@ __device__ __forceinline__ void cta_or_pair_sync() {
         __syncthreads();
 }
 
+// a / max_new for 0 <= a < 2^31: multiplication by the rounded-up reciprocal (Granlund and Montgomery)
+__device__ __forceinline__ int stream_of(const HeadParams& p, int a) {
+    const uint32_t t = __umulhi(p.div_mul, (uint32_t)a);
+    return (int)((t + (((uint32_t)a - t) >> p.div_shift1)) >> p.div_shift2);
+}
 // whether a row holds a token to score: t < n_new[s]
 __device__ __forceinline__ bool row_scored(const HeadParams& p, int row) {
     if (row >= p.rows) return false;
     if (p.n_new == nullptr) return true;
-    const int s = row / p.max_new;
+    const int s = stream_of(p, row);
     return row - s * p.max_new < p.n_new[s];
 }
+
+// A CTA's (or pair's) way through the work: row blocks fastest, then parts.
+struct Work {
+    int block, part;             // index into the list of active blocks; part
+    int blocks, block_step, part_step, parts;
+    __device__ __forceinline__ Work(int first, int step, int blocks, int parts) : blocks(blocks), parts(parts) {
+        const int n = blocks > 0 ? blocks : 1;
+        part = blocks > 0 ? first / n : parts;
+        block = first - first / n * n;
+        part_step = step / n;
+        block_step = step - part_step * n;
+    }
+    __device__ __forceinline__ bool more() const { return part < parts; }
+    __device__ __forceinline__ void next() {
+        part += part_step;
+        block += block_step;
+        if (block >= blocks) {
+            block -= blocks;
+            ++part;
+        }
+    }
+};
 
 template <int kCtas>
 __global__ void __launch_bounds__(kHeadThreads, 1)
@@ -237,8 +264,7 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_base;
     const int blocks = n_active;
-    const int n_work = blocks * p.n_parts;  // the launcher keeps it below 2^30
-    const int w0 = blockIdx.x / kCtas, w_step = gridDim.x / kCtas;
+    const Work work(blockIdx.x / kCtas, gridDim.x / kCtas, blocks, p.n_parts);
     const int steps = (p.d_model + kBoxes * kHeadDepth - 1) / (kBoxes * kHeadDepth);
     const int chunks = (steps + kChunkSteps - 1) / kChunkSteps;
     // tiles of a part that hold a column
@@ -268,10 +294,9 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
             auto feed = [&]() -> bool {
                 int stage = 0;
                 uint32_t phase = 0;
-                for (int w = w0; w < n_work; w += w_step) {
-                    const int row = p.row0 + active[w % blocks] * kBlockRows + rank * kHeadRows;
-                    const int part = w / blocks;
-                    const int n_tiles = tiles_of(part);
+                for (Work w = work; w.more(); w.next()) {
+                    const int row = p.row0 + active[w.block] * kBlockRows + rank * kHeadRows;
+                    const int part = w.part, n_tiles = tiles_of(part);
                     for (int t = 0; t < n_tiles; ++t) {
                         const int col = (part * p.part_tiles + t) * p.tile_cols + rank * (p.tile_cols / kCtas);
                         for (int k = 0; k < steps; ++k) {
@@ -317,8 +342,8 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
                 const uint32_t a_box = p.a_bytes >> 4, b_box = p.b_bytes >> 4, next = p.stage_bytes >> 4;
                 int stage = 0, buf = 0;
                 uint32_t phase = 0, buf_phase = 0, at = 0;
-                for (int w = w0; w < n_work; w += w_step) {
-                    const int n_chunks = tiles_of(w / blocks) * chunks;
+                for (Work w = work; w.more(); w.next()) {
+                    const int n_chunks = tiles_of(w.part) * chunks;
                     int left = steps;
                     for (int c = 0; c < n_chunks; ++c) {
                         if (!wait(&acc_empty[buf], buf_phase ^ 1u)) return;
@@ -368,19 +393,33 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
         int buf = 0, turn = 0;
         uint32_t buf_phase = 0;
         bool ok = true;
-        // the row of a piece of work, whether it is scored, and its target's column within the range
-        auto row_of = [&](int w) { return p.row0 + active[w % blocks] * kBlockRows + rank * kHeadRows + r; };
-        auto scored = [&](int w) { return w < n_work && row_scored(p, row_of(w)); };
-        auto target_of = [&](int w, bool on) { return on ? (int64_t)p.token_ids[row_of(w)] - p.col0 : (int64_t)-1; };
-        bool next_on = scored(w0);
-        int64_t next_at = target_of(w0, next_on);
-        for (int w = w0; w < n_work; w += w_step) {
-            const int row = row_of(w), part = w / blocks;
+        // What the row of a piece of work is about: asked for a piece ahead, and only looked at when
+        // that piece's turn comes.
+        struct Row {
+            int row, t, n_new, id;
+        };
+        auto row_of = [&](const Work& w) {
+            Row x = {0, 0, 0, -1};
+            if (w.more()) {
+                x.row = p.row0 + active[w.block] * kBlockRows + rank * kHeadRows + r;
+                if (x.row < p.rows) {
+                    const int s = stream_of(p, x.row);
+                    x.t = x.row - s * p.max_new;
+                    x.n_new = p.n_new ? p.n_new[s] : p.max_new;
+                    x.id = p.token_ids[x.row];
+                }
+            }
+            return x;
+        };
+        Work ahead = work;
+        Row next = row_of(ahead);
+        for (Work w = work; w.more(); w.next()) {
+            const int row = next.row, part = w.part;
             const int n_tiles = tiles_of(part);
-            const bool on = next_on;
-            const int64_t at = next_at;
-            next_on = scored(w + w_step);  // asked for now, needed after this piece's arithmetic
-            next_at = target_of(w + w_step, next_on);
+            const bool on = next.t < next.n_new;              // a row to score
+            const int64_t at = (int64_t)next.id - p.col0;     // its target's column, if within the range
+            ahead.next();
+            next = row_of(ahead);
             // sum of exp(z) so far = sum * 2^ref, ref = m * log2 e rounded once
             float m = kNoLogit, ref = kNoLogit * kLog2e, sum = 0.f;
             for (int t = 0; t < n_tiles && ok; ++t) {
@@ -389,10 +428,7 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
 #pragma unroll
                 for (int i = 0; i < kHeadMaxCols / 2; ++i) z[i] = 0.f;
                 for (int c = 0; c < chunks; ++c) {
-                    // one lane waits (32 would poll 32 times), then every lane looks for itself
-                    if (lane == 0) ok = wait(&acc_full[buf], buf_phase);
-                    ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
-                    ok = __all_sync(0xFFFFFFFFu, ok && wait(&acc_full[buf], buf_phase));
+                    ok = __all_sync(0xFFFFFFFFu, wait(&acc_full[buf], buf_phase));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -581,14 +617,19 @@ cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hi
     // an instruction reads 128 rows of A from a stage's start; the ring leaves room for that at its end
     q.stages = (kHeadRing - (kARoom - q.a_bytes)) / q.stage_bytes;
     if (q.stages > kHeadMaxStages) q.stages = kHeadMaxStages;
+    {
+        const uint32_t d = (uint32_t)p.max_new;
+        int l = 0;
+        while (((uint64_t)1 << l) < d) ++l;
+        q.div_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
+        q.div_shift1 = l < 1 ? l : 1;
+        q.div_shift2 = l > 0 ? l - 1 : 0;
+    }
     const int64_t block_rows = (int64_t)kHeadRows * t.ctas;
     const int64_t all_blocks = ceil_div(p.rows, block_rows);
-    int64_t at_once = ((int64_t)1 << 30) / t.n_parts;  // row blocks of a launch: its work is counted in 32 bits
-    if (at_once < 1) at_once = 1;
-    if (at_once > kHeadRowBlocks) at_once = kHeadRowBlocks;
-    for (int64_t b = 0; b < all_blocks; b += at_once) {
+    for (int64_t b = 0; b < all_blocks; b += kHeadRowBlocks) {
         q.row0 = (int32_t)(b * block_rows);
-        q.row_blocks = (int32_t)(all_blocks - b < at_once ? all_blocks - b : at_once);
+        q.row_blocks = (int32_t)(all_blocks - b < kHeadRowBlocks ? all_blocks - b : kHeadRowBlocks);
         const int64_t work = (int64_t)q.row_blocks * q.n_parts, fit = dp.n_sm / t.ctas;
         const unsigned grid = (unsigned)((work < fit ? work : fit) * t.ctas);
         e = t.ctas == 2 ? launch<2>(q, grid, dp, map_a, map_b, st) : launch<1>(q, grid, dp, map_a, map_b, st);
