@@ -42,6 +42,9 @@ constexpr int kKeys = 16;  // slots per tile
 // how many SMs at that rate make up HBM's.
 constexpr float kJoinBytes = 640 * 1024, kClusterBytes = 220 * 1024;
 constexpr float kBusySms = 58.f;
+// What the end of a unit costs a CTA (about 2 us), in bytes of its share of HBM and at most in tiles.
+constexpr float kUnitBytes = 96 * 1024;
+constexpr int kUnitTiles = 40;
 constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
@@ -135,7 +138,7 @@ __device__ __forceinline__ int live_slots(const AttendParams& p, int s) {
 // A CTA's way through the work, segment by segment.  Two ways: along its stretch of the line of
 // tiles, or (whole_units) from unit to unit, `step` units apart.
 struct Walk {
-    int left;       // tiles of the stretch from this segment's first on; whole units: 1 until the end
+    int left;       // positions of the stretch from this segment's first on; whole units: 1 until the end
     int unit0;      // line position of the unit's first tile; whole units: the unit's number
     int s, unit;    // stream; unit within the stream (K/V head, block of query heads)
     int len;        // live slots of the stream
@@ -164,19 +167,20 @@ struct Walk {
         t0 = 0;
         set_end();
     }
-    __device__ __forceinline__ void next(const AttendParams& p) {
+    // `gap`: positions behind a unit's tiles that stand for what its end costs
+    __device__ __forceinline__ void next(const AttendParams& p, const int& gap) {
         if (step > 0) {
             unit0 += step;
             find_unit(p);
             return;
         }
-        left -= t1 - t0;
+        left -= tiles() + gap - t0;
         if (left <= 0) return;
-        unit0 += tiles();
+        unit0 += tiles() + gap;
         t0 = 0;
         if (++unit == p.units) {
             unit = 0;
-            for (len = 0; len == 0;) {  // tiles are left, so a stream with slots follows
+            for (len = 0; len == 0;) {  // positions are left, so a stream with slots follows
                 if (++s >= p.n_streams) {  // (unless the lengths changed under the call)
                     left = 0;
                     return;
@@ -202,7 +206,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     float* cta_o = reinterpret_cast<float*>(smem + kWarps * kStages * 2 * kTileBytes);  // [head][head_dim]
     float* merge = cta_o + kHeads * kDim;  // [warp][kPass][kDim]
     __shared__ int scan[kWarps];
-    __shared__ int longest[kWarps];
+    __shared__ int longest[kWarps], counted[kWarps], gap_all;
     __shared__ Walk first;
     __shared__ float stat_m[kWarps][kHeads], stat_l[kWarps][kHeads];
     __shared__ float part_w[kHeads];
@@ -216,14 +220,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     // ---- the line of tiles, this CTA's stretch of it -------------------------------------
     const int slice = (p.n_streams + kThreads - 1) / kThreads;
     const int s_lo = min(p.n_streams, tid * slice), s_hi = min(p.n_streams, s_lo + slice);
-    int mine = 0;
-    int long_unit = 0;
+    const float tile_bytes = (float)(kKeys * 4 * p.head_dim);
+    const int gap = min((int)(kUnitBytes / tile_bytes), kUnitTiles);
+    int mine = 0, live = 0, long_unit = 0;
     for (int s = s_lo; s < s_hi; ++s) {
         const int T = (live_slots(p, s) + kKeys - 1) / kKeys;
-        mine += T * p.units;
+        if (T == 0) continue;
+        mine += (T + gap) * p.units;
+        ++live;
         long_unit = max(long_unit, T);
     }
     long_unit = __reduce_max_sync(0xFFFFFFFFu, long_unit);
+    live = __reduce_add_sync(0xFFFFFFFFu, live);
     int before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -233,13 +241,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     if (lane == 31) {
         scan[warp] = before;
         longest[warp] = long_unit;
+        counted[warp] = live;
     }
     __syncthreads();
-    int total = 0, warps_before = 0;  // below 2^31: the caches of so many tiles fit no device
+    int line = 0, warps_before = 0;  // below 2^31: the caches of so many tiles fit no device
+    live = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) warps_before += scan[w];
-        total += scan[w];
+        line += scan[w];
+        live += counted[w];
         long_unit = max(long_unit, longest[w]);
     }
     before += warps_before - mine;  // tiles in front of this thread's streams
@@ -250,17 +261,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     // busiest SM takes in (at 110 GB/s alone, 80 GB/s among many): what HBM takes for all of them
     // (1/kBusySms of the tiles), what the busiest has left when the others are done, and what ends
     // a unit.
-    const float tile_bytes = (float)(kKeys * 4 * p.head_dim);
+    const int total = line - live * p.units * gap;  // tiles
     const float part_tiles = 4.f * (float)(min(kHeads, p.group) * p.head_dim * 4) / tile_bytes;
     // (1): a few very long units are cut into fewer parts than there are SMs: with `per` tiles in a
     // part and long_unit / per parts to join, the sum of both is least at the root
-    const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, max((int)sqrtf((float)long_unit * part_tiles), 1));
+    const int per = max((line + (int)gridDim.x - 1) / (int)gridDim.x, max((int)sqrtf((float)long_unit * part_tiles), 1));
     const int n_units = p.n_streams * p.units;
     const float hbm = (float)total / kBusySms;
     auto estimate = [&](int size) {
         const int groups = gridDim.x / size;
-        const float dealt = (float)((n_units + groups - 1) / groups) * (float)((long_unit + size - 1) / size);
-        return fmaxf(dealt * (4.f / 3.f), hbm + dealt - (float)total / (float)(min(n_units, groups) * size));
+        const float units = (float)((n_units + groups - 1) / groups), tiles = (float)((long_unit + size - 1) / size);
+        return fmaxf(units * (tiles * (4.f / 3.f) + gap),
+                     hbm + units * tiles - (float)total / (float)(min(n_units, groups) * size));
     };
     float least = fmaxf((float)per * (4.f / 3.f), hbm) + kJoinBytes / tile_bytes +
                   ((float)long_unit / (float)per + 1.f) * part_tiles;
@@ -278,8 +290,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     const int rank = team > 1 ? (int)cluster_rank() : 0;
     // the warp's first tile of a segment and its way to the next
     const int lead = rank * kWarps + warp, stride = team * kWarps;
-    const int r0 = total / per >= (int)blockIdx.x ? (int)blockIdx.x * per : total;  // (no overflow)
-    const int r1 = min(total, r0 + min(per, total - r0));
+    const int r0 = line / per >= (int)blockIdx.x ? (int)blockIdx.x * per : line;  // (no overflow)
+    const int r1 = r0 + min(per, line - r0);
+    if (tid == 0) gap_all = gap;
     if (whole_units) {
         if (tid == 0) {
             first.step = gridDim.x / team;
@@ -291,7 +304,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         int s = s_lo, len = 0, T = 0;
         for (; s < s_hi; ++s) {
             len = live_slots(p, s);
-            T = (len + kKeys - 1) / kKeys;
+            T = len > 0 ? (len + kKeys - 1) / kKeys + gap : 0;  // a unit's positions
             if (r0 < at + T * p.units) break;
             at += T * p.units;
         }
@@ -304,6 +317,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             first.unit0 = at + first.unit * T;
             first.t0 = r0 - first.unit0;
             first.set_end();
+            if (first.t0 >= first.tiles()) first.next(p, gap);  // begins behind a unit's last tile
         }
     }
     // streams without slots: nothing to weigh, the result is zero and its log-sum -inf; a length
@@ -321,7 +335,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         }
     }
     __syncthreads();
-    if (!whole_units && r0 >= total) return;
+    if (!whole_units && r0 >= line) return;
 
     // ---- the warp's ring ------------------------------------------------------------------
     const uint32_t ring0 = smem_u32(ring) + warp * kStages * 2 * kTileBytes;
@@ -332,7 +346,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     const bool chunk_on = chunk * 8 < p.head_dim;
     auto load_next = [&](int stage) {  // the warp's next tile, if there is one, into a stage; one group
         while (ahead.more() && ahead_tile >= ahead.t1) {
-            ahead.next(p);
+            ahead.next(p, gap_all);
             ahead_tile = ahead.t0 + lead;
         }
         if (ahead.more()) {
@@ -360,7 +374,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 
     // ---- the units ------------------------------------------------------------------------
     const int hc = 2 * (lane & 3);  // this lane's two heads within a block of 8
-    for (Walk w = first; w.more(); w.next(p)) {
+    for (Walk w = first; w.more(); w.next(p, gap_all)) {
         const int g = w.unit / p.blocks, block = w.unit - g * p.blocks;
         const int head0 = g * p.group + block * kHeads;            // first query head of the unit
         const int heads = min(kHeads, p.group - block * kHeads);   // query heads it really has
