@@ -417,6 +417,7 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
             const int row = next.row, part = w.part;
             const int n_tiles = tiles_of(part);
             const bool on = next.t < next.n_new;              // a row to score
+            const bool any = __any_sync(0xFFFFFFFFu, on);     // else this warp's lanes are left alone
             const int64_t at = (int64_t)next.id - p.col0;     // its target's column, if within the range
             ahead.next();
             next = row_of(ahead);
@@ -431,12 +432,14 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
                     ok = __all_sync(0xFFFFFFFFu, wait(&acc_full[buf], buf_phase));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (any) {
 #pragma unroll
-                    for (int j = 0; j < kHeadMaxCols / 32; ++j) {
-                        float v[16];
-                        tmem_load16(v, lanes + buf * kHeadMaxCols + j * 16);
+                        for (int j = 0; j < kHeadMaxCols / 32; ++j) {
+                            float v[16];
+                            tmem_load16(v, lanes + buf * kHeadMaxCols + j * 16);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) z[j * 16 + i] += v[i];
+                            for (int i = 0; i < 16; ++i) z[j * 16 + i] += v[i];
+                        }
                     }
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
@@ -446,6 +449,7 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
                     if (buf == 0) buf_phase ^= 1u;
                 }
                 if (!ok) break;
+                if (!any) continue;
                 const int64_t col = ((int64_t)part * p.part_tiles + t) * p.tile_cols + col_first;
                 const int cols = (int)max((int64_t)0, min((int64_t)width, p.n_cols - col));
                 if (cols < kHeadMaxCols / 2) {
