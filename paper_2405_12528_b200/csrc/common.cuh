@@ -199,13 +199,15 @@ struct HeadParams {
     int32_t row_blocks;                      // blocks of rows of this launch
     int32_t n_parts, n_tiles, part_tiles, tile_cols, half_cols;
     int32_t a_bytes, b_bytes, load_bytes, stage_bytes, stages;  // a box of each, a stage of boxes
+    int32_t few_cols, part_cols, tail_cols;                     // the few-rows form
     uint32_t div_mul, div_shift1, div_shift2;                   // division by max_new
 };
 
 // How the LM head's product is cut: column ranges ("parts", one pair per row each) of part_tiles
 // tiles of tile_cols columns, computed by one CTA or a pair of CTAs.
 struct HeadTiling {
-    int32_t ctas, n_parts, part_tiles, tile_cols;
+    int32_t ctas;  // 0: the form for few rows
+    int32_t n_parts, part_tiles, tile_cols, part_cols;
     int32_t half_cols;  // columns of a tile that the first of a row's two threads reduces
 };
 

@@ -7,15 +7,18 @@
 //
 // 2 * rows * columns * d operations on the tensor cores against columns * d * 2 bytes of weight:
 // many rows are bound by tcgen05 (and by what feeds it), up to about a hundred rows by reading
-// the weight once.  Two forms of one kernel, both persistent:
+// the weight once.  Three forms, all persistent:
 //   kCtas = 2  more than 128 rows.  A pair of CTAs (cta_group::2) multiplies 256 rows by up to 256
 //              columns; each CTA loads its own 128 rows and half of the columns, so an SM takes in
 //              64 bytes per clock of tensor work where a single CTA's 128 x 256 tile needs 96 -
 //              more than L2 delivers.  Tiles go rows fastest: the CTAs at work share weight tiles
 //              in L2 and the weight leaves HBM once.
-//   kCtas = 1  up to 128 rows.  Every CTA streams an equal range of weight rows past the one block
-//              of hidden rows (only as many of them as there are, so that the ring's space goes
-//              to the weight) and keeps one running pair per row for its whole range.
+//   kCtas = 1  65 to 128 rows.  Every CTA streams an equal range of weight rows past the one block
+//              of hidden rows and keeps one running pair per row for its whole range.
+//   few rows   up to 64.  As before, but with the operands exchanged: 128 weight rows on the lanes,
+//              16 to 64 hidden rows on the columns.  Padding one row to 128 costs no time by itself,
+//              but the energy of 128: a decode loop of 64 rows ran into the power cap (1000 W,
+//              1.16 GHz) and took 195 us a step where the first ones took 172.
 // Warp roles: one lane feeds a ring of TMA loads (128 elements of d per stage, 128-byte swizzle),
 // one lane issues tcgen05.mma, eight warps take the accumulators out of TMEM, which holds two
 // of them - one is read while the other is multiplied into.
@@ -498,6 +501,273 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
     if (tid == 0 && gave_up) atomicOr(p.status, SIRLLM_STATUS_TIMEOUT);
 }
 
+__device__ __forceinline__ void tmem_load8(float (&v)[8], uint32_t addr) {
+    uint32_t r[8];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// Up to kFewRows rows: z^T = weight * hidden^T, 128 vocabulary columns on the lanes and p.few_cols
+// (16, 32, 48 or 64) rows on the columns of an accumulator.  A reducing thread keeps the running
+// pairs of half of the rows over its lane's columns of the whole part; the 128 lanes are joined once,
+// at the part's end, by shuffles.  The last tile of a part loads only the columns that the part has
+// left (map_t); what else its lanes multiply is not looked at.
+constexpr int kFewRows = 64;
+constexpr int64_t kFewShare = 32;  // columns of a part, at least
+__global__ void __launch_bounds__(kHeadThreads, 1)
+head_few_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_h, const __grid_constant__ CUtensorMap map_w,
+                const __grid_constant__ CUtensorMap map_t) {
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t full[kHeadMaxStages], empty[kHeadMaxStages], acc_full[2], acc_empty[2], drained;
+    __shared__ float2 quarters[4][kFewRows];  // a row's pair over 32 lanes
+    __shared__ int want[kFewRows];            // a row's target column within the part, -1 if elsewhere
+    __shared__ int scored[kFewRows];
+    __shared__ uint32_t tmem_base;
+    __shared__ volatile int gave_up;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    constexpr int kTile = kHeadRows;          // vocabulary columns of a tile
+
+    if (tid == 0) {
+        for (int i = 0; i < kHeadMaxStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&acc_full[i], 1);
+            mbar_init(&acc_empty[i], kHeadReducers / 32);
+        }
+        mbar_init(&drained, 1);
+        mbar_init_fence();
+        gave_up = 0;
+    }
+    if (warp == 1) tmem_alloc<1>(&tmem_base);
+    grid_dependency_wait();  // as in head_kernel
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_base;
+    const int steps = (p.d_model + kBoxes * kHeadDepth - 1) / (kBoxes * kHeadDepth);
+    const int chunks = (steps + kChunkSteps - 1) / kChunkSteps;
+
+    // A wait that runs out raises the flag and every role leaves; the others see it or run out too.
+    auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+        for (uint32_t i = 0; i < kNapLimit; ++i) {
+            if (mbar_nap(bar, parity)) return true;
+            if (gave_up) return false;
+        }
+        gave_up = 1;
+        return false;
+    };
+
+    if (warp == 0) {
+        const bool issuer = lane == 0;
+        int issued = 0;
+        auto feed = [&]() -> bool {
+            int stage = 0;
+            uint32_t phase = 0;
+            for (int part = blockIdx.x; part < p.n_parts; part += gridDim.x) {
+                for (int t = 0; t < p.part_tiles; ++t) {
+                    const bool tail = t == p.part_tiles - 1;
+                    const int col = part * p.part_cols + t * kTile;
+                    const uint32_t bytes = p.load_bytes - (tail ? kBoxes * (kTile - p.tail_cols) * kHeadDepth * 2 : 0);
+                    for (int k = 0; k < steps; ++k) {
+                        if (!wait(&empty[stage], phase ^ 1u)) return false;
+                        if (issuer) {
+                            const uint32_t a = tiles + stage * p.stage_bytes, b = a + kBoxes * kARoom;
+                            mbar_expect_tx(&full[stage], bytes);
+#pragma unroll
+                            for (int i = 0; i < kBoxes; ++i) {
+                                const int depth = (k * kBoxes + i) * kHeadDepth;
+                                tma_load_2d<1>(a + i * kARoom, tail ? &map_t : &map_w, depth, col, smem_u32(&full[stage]));
+                                tma_load_2d<1>(b + i * p.b_bytes, &map_h, depth, 0, smem_u32(&full[stage]));
+                            }
+                        }
+                        if (issued < p.stages) ++issued;
+                        if (++stage == p.stages) {
+                            stage = 0;
+                            phase ^= 1u;
+                        }
+                    }
+                }
+            }
+            return true;
+        };
+        if (!feed() && issuer) {  // gave up: let the loads in flight land
+            for (int i = 0; i < issued; ++i)
+                for (uint32_t parity = 0; parity < 2; ++parity) mbar_wait_bounded(&full[i], parity, 1u << 14);
+        }
+    } else if (warp == 1) {
+        const bool issuer = lane == 0;
+        auto multiply = [&]() {
+            const uint32_t idesc = (1u << 4) | ((uint32_t)p.bf16 << 7) | ((uint32_t)p.bf16 << 10) |
+                                   ((uint32_t)(p.few_cols >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+            const uint32_t a_first = operand_lo(tiles), b_first = operand_lo(tiles + kBoxes * kARoom);
+            const uint32_t b_box = p.b_bytes >> 4, next = p.stage_bytes >> 4;
+            int stage = 0, buf = 0;
+            uint32_t phase = 0, buf_phase = 0, at = 0;
+            for (int part = blockIdx.x; part < p.n_parts; part += gridDim.x) {
+                int left = steps;
+                for (int c = 0; c < p.part_tiles * chunks; ++c) {
+                    if (!wait(&acc_empty[buf], buf_phase ^ 1u)) return;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t acc = tmem + buf * kFewRows;
+                    const int n = min(left, kChunkSteps);
+                    left = left == n ? steps : left - n;
+                    for (int k = 0; k < n; ++k) {
+                        if (!wait(&full[stage], phase)) return;
+                        if (issuer) {
+#pragma unroll
+                            for (int i = 0; i < kBoxes; ++i)
+#pragma unroll
+                                for (int j = 0; j < kHeadDepth / 16; ++j)
+                                    mma_f16<1>(acc, a_first + at + i * (kARoom >> 4) + 2 * j,
+                                               b_first + at + i * b_box + 2 * j, idesc, (k | i | j) != 0);
+                            mma_commit<1>(&empty[stage]);
+                        }
+                        at += next;
+                        if (++stage == p.stages) {
+                            stage = 0;
+                            at = 0;
+                            phase ^= 1u;
+                        }
+                    }
+                    if (issuer) mma_commit<1>(&acc_full[buf]);
+                    buf ^= 1;
+                    if (buf == 0) buf_phase ^= 1u;
+                }
+            }
+        };
+        multiply();
+        if (issuer) {
+            mma_commit<1>(&drained);  // products still under way use shared memory and TMEM
+            if (!mbar_wait_bounded(&drained, 0, kMbarSpinLimit)) gave_up = 1;
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2, me = tid - 128;
+        const int r = quarter * 32 + lane;                   // the tile's column of this lane
+        const int mine = p.few_cols >> 1, base = half * mine;  // this thread's rows
+        const uint32_t lanes = tmem + ((uint32_t)quarter << 21) + base;
+        int buf = 0;
+        uint32_t buf_phase = 0;
+        bool ok = true;
+        for (int part = blockIdx.x; part < p.n_parts; part += gridDim.x) {
+            const int64_t first = (int64_t)part * p.part_cols;
+            if (me < kFewRows) {
+                bool on = false;
+                int64_t at = -1;
+                if (row_scored(p, me)) {
+                    on = true;
+                    at = (int64_t)p.token_ids[me] - p.col0;
+                    if (part == 0 && (at < 0 || at >= p.n_cols)) p.target_out[me] = 0.f;  // the token is elsewhere
+                    if (at >= p.n_cols) at = -1;
+                    at = at >= first && at < first + p.part_cols ? at - first : -1;
+                }
+                scored[me] = on;
+                want[me] = (int)at;
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(kHeadReducers) : "memory");
+            float m[kFewRows / 2], s[kFewRows / 2];
+#pragma unroll
+            for (int i = 0; i < kFewRows / 2; ++i) {
+                m[i] = kNoLogit;
+                s[i] = 0.f;
+            }
+            for (int t = 0; t < p.part_tiles && ok; ++t) {
+                float z[kFewRows / 2];
+#pragma unroll
+                for (int i = 0; i < kFewRows / 2; ++i) z[i] = 0.f;
+                for (int c = 0; c < chunks; ++c) {
+                    if (!(ok = __all_sync(0xFFFFFFFFu, wait(&acc_full[buf], buf_phase)))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < kFewRows / 16; ++j) {
+                        if (j * 8 < mine) {
+                            float v[8];
+                            tmem_load8(v, lanes + buf * kFewRows + j * 8);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) z[j * 8 + i] += v[i];
+                        }
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(smem_u32(&acc_empty[buf]));
+                    buf ^= 1;
+                    if (buf == 0) buf_phase ^= 1u;
+                }
+                if (!ok) break;
+                // rows whose target is one of this tile's columns: the lane that has it writes it
+                const int at = lane < mine ? want[base + lane] - t * kTile : -1;
+                for (uint32_t hit = __ballot_sync(0xFFFFFFFFu, at >= 0 && at < kTile && want[base + lane] >= 0); hit != 0;
+                     hit &= hit - 1) {
+                    const int i = __ffs(hit) - 1;
+                    if (__shfl_sync(0xFFFFFFFFu, at, i) == r) {
+                        float target = 0.f;
+#pragma unroll
+                        for (int x = 0; x < kFewRows / 2; ++x)
+                            if (x == i) target = z[x];
+                        p.target_out[base + i] = target;
+                    }
+                }
+                const int cols = t == p.part_tiles - 1 ? p.tail_cols : kTile;
+                if (r < cols && first + t * kTile + r < p.n_cols) {
+#pragma unroll
+                    for (int j = 0; j < kFewRows / 16; ++j) {
+                        if (j * 8 < mine) {
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) {
+                                const int i = j * 8 + x;
+                                const float top = fmaxf(m[i], z[i]);
+                                const float f = ex2_approx((fminf(m[i], z[i]) - top) * kLog2e);
+                                s[i] = z[i] > m[i] ? fmaf(s[i], f, 1.f) : s[i] + f;
+                                m[i] = top;
+                            }
+                        }
+                    }
+                }
+            }
+            // 32 lanes into one, then the four quarters
+#pragma unroll
+            for (int j = 0; j < kFewRows / 16; ++j) {
+                if (j * 8 < mine) {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        const int i = j * 8 + x;
+                        float top = m[i];
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                        float sum = s[i] * ex2_approx((m[i] - top) * kLog2e);
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                        if (lane == x) quarters[quarter][base + i] = make_float2(top, sum);
+                    }
+                }
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(kHeadReducers) : "memory");
+            if (me < p.few_cols && scored[me] && ok) {
+                float top = kNoLogit, sum = 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) top = fmaxf(top, quarters[q][me].x);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum += quarters[q][me].y * ex2_approx((quarters[q][me].x - top) * kLog2e);
+                // a part whose logits are all -inf counts for nothing: (0, 0)
+                p.pairs_out[(int64_t)me * p.pair_stride + part] = sum == 0.f ? make_float2(0.f, 0.f) : make_float2(top, sum);
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(kHeadReducers) : "memory");  // before the tables are filled again
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1) tmem_free<1>(tmem);
+    if (tid == 0 && gave_up) atomicOr(p.status, SIRLLM_STATUS_TIMEOUT);
+}
+
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -556,6 +826,16 @@ cudaError_t launch(const HeadParams& p, unsigned grid, const DeviceProps& dp, co
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// What stream_of multiplies and shifts by.
+void division(HeadParams* q) {
+    const uint32_t d = (uint32_t)q->max_new;
+    int l = 0;
+    while (((uint64_t)1 << l) < d) ++l;
+    q->div_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
+    q->div_shift1 = l < 1 ? l : 1;
+    q->div_shift2 = l > 0 ? l - 1 : 0;
+}
+
 }  // namespace
 
 // The cut depends on the sizes alone (callers size their pairs by it), for the 148 SMs of a B200;
@@ -563,6 +843,19 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 HeadTiling head_tiling(int64_t rows, int64_t n_cols) {
     constexpr int64_t kSms = 148;
     HeadTiling t;
+    if (rows <= kFewRows) {
+        // Reading the weight bounds the call, so its columns are dealt out evenly, one range per SM, in
+        // tiles of 128 of which the last is loaded as far as it goes.
+        t.ctas = 0;
+        int64_t share = ceil_div(ceil_div(n_cols, kSms), 8) * 8;
+        if (share < kFewShare) share = kFewShare;
+        t.part_cols = (int32_t)share;
+        t.tile_cols = kHeadRows;
+        t.part_tiles = (int32_t)ceil_div(share, kHeadRows);
+        t.half_cols = 0;
+        t.n_parts = (int32_t)ceil_div(n_cols, share);
+        return t;
+    }
     if (rows <= kHeadRows) {
         // One block of rows: reading the weight bounds the call, so its columns are dealt out evenly,
         // one range per SM, each cut into equal tiles.
@@ -588,7 +881,8 @@ HeadTiling head_tiling(int64_t rows, int64_t n_cols) {
         }
         t.half_cols = t.tile_cols / 2;
     }
-    t.n_parts = (int32_t)ceil_div(n_cols, (int64_t)t.part_tiles * t.tile_cols);
+    t.part_cols = t.part_tiles * t.tile_cols;
+    t.n_parts = (int32_t)ceil_div(n_cols, t.part_cols);
     return t;
 }
 
@@ -601,6 +895,38 @@ cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hi
     if (e != cudaSuccess) return e;
     EncodeTiled encode;
     if ((e = encoder(&encode)) != cudaSuccess) return e;
+    if (t.ctas == 0) {
+        HeadParams q = p;
+        q.few_cols = (int32_t)ceil_div(p.rows, 16) * 16;
+        q.n_parts = t.n_parts;
+        q.part_tiles = t.part_tiles;
+        q.part_cols = t.part_cols;
+        q.tail_cols = t.part_cols - (t.part_tiles - 1) * kHeadRows;
+        q.b_bytes = q.few_cols * kHeadDepth * 2;
+        q.load_bytes = kBoxes * (kARoom + q.b_bytes);
+        q.stage_bytes = q.load_bytes;
+        q.stages = kHeadRing / q.stage_bytes;
+        if (q.stages > kHeadMaxStages) q.stages = kHeadMaxStages;
+        division(&q);
+        CUtensorMap map_h, map_w, map_t;
+        if ((e = row_map(encode, &map_h, hidden, p.rows, p.d_model, hidden_stride, q.few_cols, p.bf16)) != cudaSuccess ||
+            (e = row_map(encode, &map_w, weight, p.n_cols, p.d_model, weight_stride, kHeadRows, p.bf16)) != cudaSuccess ||
+            (e = row_map(encode, &map_t, weight, p.n_cols, p.d_model, weight_stride, q.tail_cols, p.bf16)) != cudaSuccess)
+            return e;
+        static unsigned char few_allowed[kMaxDevices];
+        if ((e = allow_max_dynamic_smem((const void*)head_few_kernel, dp, few_allowed)) != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(q.n_parts < dp.n_sm ? q.n_parts : dp.n_sm));
+        cfg.blockDim = dim3(kHeadThreads);
+        cfg.dynamicSmemBytes = kHeadSmem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, head_few_kernel, q, map_h, map_w, map_t);
+    }
     const int a_rows = t.ctas == 2 ? kHeadRows : (int)ceil_div(p.rows, 8) * 8;
     const int b_rows = t.tile_cols / t.ctas;
     CUtensorMap map_a, map_b;
@@ -621,14 +947,7 @@ cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hi
     // an instruction reads 128 rows of A from a stage's start; the ring leaves room for that at its end
     q.stages = (kHeadRing - (kARoom - q.a_bytes)) / q.stage_bytes;
     if (q.stages > kHeadMaxStages) q.stages = kHeadMaxStages;
-    {
-        const uint32_t d = (uint32_t)p.max_new;
-        int l = 0;
-        while (((uint64_t)1 << l) < d) ++l;
-        q.div_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
-        q.div_shift1 = l < 1 ? l : 1;
-        q.div_shift2 = l > 0 ? l - 1 : 0;
-    }
+    division(&q);
     const int64_t block_rows = (int64_t)kHeadRows * t.ctas;
     const int64_t all_blocks = ceil_div(p.rows, block_rows);
     for (int64_t b = 0; b < all_blocks; b += kHeadRowBlocks) {

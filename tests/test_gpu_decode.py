@@ -428,6 +428,7 @@ def assert_scores(got, want, walk):
 HEAD = [  # rows, width, vocabulary
     (1, 8, 1), (1, 64, 31), (3, 72, 33), (1, 4096, 32000), (5, 1000, 257), (127, 136, 500), (128, 64, 3000),
     (129, 200, 1000), (300, 64, 50257), (64, 512, 40001), (2, 7, 100), (33, 1, 50), (640, 256, 2049),
+    (16, 72, 18944), (17, 264, 19000), (48, 128, 37889), (65, 64, 19000), (64, 2056, 777), (100, 1100, 20000),
 ]
 
 
@@ -453,7 +454,7 @@ def test_head_scores_against_64_bits(dt, rows, width, vocab):
 
 
 @pytest.mark.parametrize("S,M,lens", [(3, 100, [0, 100, 1]), (40, 7, None), (2, 300, [130, 0]), (300, 1, None),
-                                      (5, 64, [0, 0, 0, 0, 0])])
+                                      (5, 64, [0, 0, 0, 0, 0]), (4, 9, [0, 9, 3, 1]), (64, 1, None), (2, 50, [3, 50])])
 def test_head_ragged_rows_leave_the_rest_alone(S, M, lens):
     g = gen(S)
     W, V = 192, 777
@@ -505,9 +506,10 @@ def test_head_more_rows_than_one_launch_takes():
     assert B.sirllm_status(ws) == 0
 
 
-def test_head_column_ranges_add_up_to_the_whole():
+@pytest.mark.parametrize("rows", [150, 100, 20])
+def test_head_column_ranges_add_up_to_the_whole(rows):
     g = gen(21)
-    rows, W, V = 150, 320, 5000
+    W, V = 320, 5000
     cfg = config(C=rows, M=rows, V=V)
     ws = B.new_workspace(cfg)
     hidden = randn(g, rows, W, dtype=torch.bfloat16)
@@ -530,9 +532,10 @@ def test_head_column_ranges_add_up_to_the_whole():
     assert_scores(ent, want, walk)
 
 
-def test_head_bad_ids_are_flagged_by_the_score_and_masked_columns_count_for_nothing():
+@pytest.mark.parametrize("rows", [10, 70, 200])
+def test_head_bad_ids_are_flagged_by_the_score_and_masked_columns_count_for_nothing(rows):
     g = gen(22)
-    rows, W, V = 10, 64, 700
+    W, V = 64, 700
     cfg = config(C=rows, M=rows, V=V)
     hidden = randn(g, rows, W, dtype=torch.float16).abs()
     weight = randn(g, V, W, dtype=torch.float16, scale=0.2)
@@ -549,9 +552,10 @@ def test_head_bad_ids_are_flagged_by_the_score_and_masked_columns_count_for_noth
     assert not pairs.isnan().any()
 
 
-def test_head_of_large_logits():
+@pytest.mark.parametrize("rows", [20, 120, 200])
+def test_head_of_large_logits(rows):
     g = gen(23)
-    rows, W, V = 20, 128, 2000
+    W, V = 128, 2000
     cfg = config(C=rows, M=rows, V=V)
     hidden = randn(g, rows, W, dtype=torch.bfloat16, scale=30)
     weight = randn(g, V, W, dtype=torch.bfloat16, scale=3)             # logits of +-1000 and more
@@ -561,9 +565,10 @@ def test_head_of_large_logits():
     assert_scores(ent, want, walk)
 
 
-def test_head_replayed_from_a_graph_on_another_stream():
+@pytest.mark.parametrize("rows", [7, 70, 300])
+def test_head_replayed_from_a_graph_on_another_stream(rows):
     g = gen(24)
-    rows, W, V = 70, 256, 4000
+    W, V = 256, 4000
     cfg = config(C=rows, M=rows, V=V)
     hidden = randn(g, rows, W, dtype=torch.bfloat16)
     weight = randn(g, V, W, dtype=torch.bfloat16, scale=0.1)
