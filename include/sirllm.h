@@ -343,8 +343,9 @@ int sirllm_attend(const sirllm_config *cfg, int32_t layer, const void *q, int32_
  * vocabulary whose weight rows the caller holds:
  *     pairs_out[row][i] = (max, sum exp(z - max)) over tile i of the columns, (0, 0) if all are -inf
  *     target_out[row]   = z[row][token_ids[row]] if that column lies in the range, else 0
- * sirllm_head_tiles() gives the number of tiles (0 for an invalid configuration or range); hand it
- * to sirllm_score_pairs or sirllm_step_pairs as n_tiles.  Under a vocabulary-parallel head every
+ * sirllm_head_tiles() gives the number of tiles (0 for an invalid configuration or range), which
+ * depends on n_streams * max_new and n_cols alone; hand it to sirllm_score_pairs or
+ * sirllm_step_pairs as n_tiles.  Under a vocabulary-parallel head every
  * rank calls this for its columns; the ranks gather the pairs and add up the targets.
  * Logits must be finite or -inf as in sirllm_score.  Rows at or beyond n_new[s] are left untouched.
  *   hidden    [n_streams*max_new] rows of d_model elements, hidden_row_stride apart

@@ -824,6 +824,9 @@ cudaError_t launch(const HeadParams& p, unsigned grid, const DeviceProps& dp, co
     return cudaLaunchKernelEx(&cfg, head_kernel<kCtas>, p, a, b);
 }
 
+// What a tile costs besides its columns, in columns (the reduction takes 128 a thread, used or not).
+constexpr int64_t kTileEnd = 64;
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // What stream_of multiplies and shifts by.
@@ -873,7 +876,7 @@ HeadTiling head_tiling(int64_t rows, int64_t n_cols) {
         int64_t best = 0;
         t.tile_cols = kHeadMaxCols;
         for (int64_t c = kHeadMaxCols; c >= 64; c -= 32) {
-            const int64_t cost = ceil_div(blocks * ceil_div(n_cols, c), kSms / 2) * (c + 16);
+            const int64_t cost = ceil_div(blocks * ceil_div(n_cols, c), kSms / 2) * (c + kTileEnd);
             if (best == 0 || cost * 33 < best * 32) {
                 best = cost;
                 t.tile_cols = (int32_t)c;
