@@ -8,8 +8,8 @@
 // tiles of all (stream, K/V head) units in one line and an equal stretch per CTA - whatever the
 // lengths are, the CTAs read the same amount, and a unit that spans CTAs leaves partial results
 // (max, sum, weighted rows) in the workspace, joined by the CTA that finishes last, by ticket -
-// or whole units per CTA, or per cluster of CTAs joined through shared memory.  Joins add in a
-// fixed order, so results do not depend on timing.  Inside a CTA every warp streams its own tiles through its own ring of cp.async stages and
+// or whole units per CTA, per cluster of CTAs joined through shared memory, or per warp.  Joins
+// add in a fixed order, so results do not depend on timing.  Inside a CTA every warp streams its own tiles through its own ring of cp.async stages and
 // keeps a running softmax; nothing but the end of a unit makes warps wait for one another, and
 // the ring runs ahead across units.
 //
@@ -24,7 +24,10 @@
 // maximum exceeds by less than 2^8, so fp16 cannot overflow), and the result.
 // Measured, bf16, heads of 128: 64 streams x 32 heads x 900 - 1280 slots 171 us (1.03 of the copy
 // rate, part from L2), 16 x 32 heads x 2048 slots 86 us (0.96), one stream x 8 heads x 12287 slots
-// 16.3 us (0.48: launch, reading the length and the join are 7 us of it, and 64 SMs read).
+// 15.9 us (0.49: launch, reading the length and the join are 7 us of it, and 64 SMs read).
+// What the ways to deal out the work bring: 64 x 32 heads x 100 slots 41 us by CTAs, 22 by warps; one
+// stream x 8 heads x 2048 slots 17 us by equal shares, 9 by clusters; 22 streams of 1 - 1862 slots x
+// 32 heads of 64 108 us by CTAs, 45 by equal shares.
 #include <atomic>
 
 #include <cuda_bf16.h>
@@ -45,6 +48,9 @@ constexpr float kBusySms = 58.f;
 // What the end of a unit costs a CTA (about 2 us), in bytes of its share of HBM and at most in tiles.
 constexpr float kUnitBytes = 96 * 1024;
 constexpr int kUnitTiles = 40;
+// The same for a single warp (about 0.9 us), and the longest units, in tiles, that are given to one.
+constexpr float kSoloBytes = 96 * 1024;
+constexpr int kSoloLongest = 32;
 constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
@@ -254,10 +260,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         long_unit = max(long_unit, longest[w]);
     }
     before += warps_before - mine;  // tiles in front of this thread's streams
-    // Three ways to deal out the work.  (1) An equal share of the line per CTA; units that CTAs share
+    // Four ways to deal out the work.  (1) An equal share of the line per CTA; units that CTAs share
     // are joined through memory.  (2) Whole units in turn to the CTAs: nothing to join, but no
     // balance between units of different length.  (3) As (2) to the clusters, a unit's tiles in turn
-    // to the cluster's CTAs, joined through shared memory.  The estimate is in tiles that the
+    // to the cluster's CTAs, joined through shared memory.  (4) Whole units in turn to the single
+    // warps, which then wait for nobody: for many short units.  The estimate is in tiles that the
     // busiest SM takes in (at 110 GB/s alone, 80 GB/s among many): what HBM takes for all of them
     // (1/kBusySms of the tiles), what the busiest has left when the others are done, and what ends
     // a unit.
@@ -266,34 +273,47 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     // (1): a few very long units are cut into fewer parts than there are SMs: with `per` tiles in a
     // part and long_unit / per parts to join, the sum of both is least at the root
     const int per = max((line + (int)gridDim.x - 1) / (int)gridDim.x, max((int)sqrtf((float)long_unit * part_tiles), 1));
-    const int n_units = p.n_streams * p.units;
-    const float hbm = (float)total / kBusySms;
-    auto estimate = [&](int size) {
-        const int groups = gridDim.x / size;
-        const float units = (float)((n_units + groups - 1) / groups), tiles = (float)((long_unit + size - 1) / size);
-        return fmaxf(units * (tiles * (4.f / 3.f) + gap),
-                     hbm + units * tiles - (float)total / (float)(min(n_units, groups) * size));
+    const float hbm = (float)total * (1.f / kBusySms);
+    auto estimate = [&](const AttendDeal& d, int log2_size) {
+        const float tiles = (float)((long_unit + (1 << log2_size) - 1) >> log2_size);
+        return fmaxf(d.units * (tiles * (4.f / 3.f) + gap), hbm + d.units * tiles - (float)total * d.per_busy);
     };
     float least = fmaxf((float)per * (4.f / 3.f), hbm) + kJoinBytes / tile_bytes +
-                  ((float)long_unit / (float)per + 1.f) * part_tiles;
+                  (__fdividef((float)long_unit, (float)per) + 1.f) * part_tiles;
     bool whole_units = false;
     int team = 1;  // CTAs that share a unit
-    const float alone = estimate(1);
+    const float alone = estimate(p.alone, 0);
     if (alone <= least) {
         whole_units = true;
         least = alone;
     }
-    if (p.cluster > 1 && estimate(p.cluster) + kClusterBytes / tile_bytes < least) {
+    if (p.cluster > 1) {
+        const float together = estimate(p.together, p.cluster_log2) + kClusterBytes / tile_bytes;
+        if (together < least) {
+            whole_units = true;
+            team = p.cluster;
+            least = together;
+        }
+    }
+    // What a tile takes a single warp: 0.9 us of latency over the stages of its ring, 0.15 us of work.
+    constexpr float kSoloTile = (0.9f / (kStages - 1) + 0.15f) * 110e3f;  // bytes, as above
+    const float solo_tiles =
+        p.solo_units * ((float)long_unit * fmaxf((float)kWarps, kSoloTile / tile_bytes) + kSoloBytes / tile_bytes);
+    // (long units and wide heads measured slower this way whatever the estimate)
+    const bool solo = kWarps == 8 && long_unit <= kSoloLongest && fmaxf(solo_tiles, hbm) < least;
+    if (solo) {
         whole_units = true;
-        team = p.cluster;
+        team = 1;
     }
     const int rank = team > 1 ? (int)cluster_rank() : 0;
     // the warp's first tile of a segment and its way to the next
-    const int lead = rank * kWarps + warp, stride = team * kWarps;
+    const int lead = solo ? 0 : rank * kWarps + warp, stride = solo ? 1 : team * kWarps;
     const int r0 = line / per >= (int)blockIdx.x ? (int)blockIdx.x * per : line;  // (no overflow)
     const int r1 = r0 + min(per, line - r0);
     if (tid == 0) gap_all = gap;
-    if (whole_units) {
+    if (solo) {
+        // every warp finds its own first unit below
+    } else if (whole_units) {
         if (tid == 0) {
             first.step = gridDim.x / team;
             first.unit0 = blockIdx.x / team;
@@ -339,7 +359,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 
     // ---- the warp's ring ------------------------------------------------------------------
     const uint32_t ring0 = smem_u32(ring) + warp * kStages * 2 * kTileBytes;
-    Walk ahead = first;                 // what the loads have reached
+    Walk start = first;
+    if (solo) {
+        start.step = gridDim.x * kWarps;
+        start.unit0 = warp * gridDim.x + blockIdx.x;  // over the SMs first
+        start.find_unit(p);
+    }
+    Walk ahead = start;                 // what the loads have reached
     int ahead_tile = ahead.t0 + lead;
     constexpr int kRowsAtOnce = 32 / kChunks;  // rows that one load instruction of the warp covers
     const int chunk = lane % kChunks, row_in = lane / kChunks;
@@ -374,7 +400,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 
     // ---- the units ------------------------------------------------------------------------
     const int hc = 2 * (lane & 3);  // this lane's two heads within a block of 8
-    for (Walk w = first; w.more(); w.next(p, gap_all)) {
+    for (Walk w = start; w.more(); w.next(p, gap_all)) {
         const int g = w.unit / p.blocks, block = w.unit - g * p.blocks;
         const int head0 = g * p.group + block * kHeads;            // first query head of the unit
         const int heads = min(kHeads, p.group - block * kHeads);   // query heads it really has
@@ -479,18 +505,61 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             }
             stage = stage == kStages - 1 ? 0 : stage + 1;
         }
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], x);
+        if (solo) {
+            // ---- the warp has the whole unit: four heads at a time through its part of the buffer ------
+            float* rows = merge + warp * kPass * kDim;
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int h = n * 8 + hc + i;
+                    if (lane < 4 && h < heads && p.lse != nullptr)
+                        p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (m[n][i] + log2f(l[n][i])) * (float)kLn2;
+                }
+#pragma unroll
+            for (int q = 0; q < kHeads / kPass; ++q) {
+                if (q * kPass >= heads) break;
+                const int n = q >> 1;
+                if (((lane & 3) >> 1) == (q & 1)) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float f = 1.0f / l[n][i];
+                        float* row = rows + ((hc & 3) + i) * kDim + (lane >> 2);
+#pragma unroll
+                        for (int d = 0; d < kDim / 16; ++d) {
+                            row[d * 16] = o[n][d][i] * f;
+                            row[d * 16 + 8] = o[n][d][i + 2] * f;
+                        }
+                    }
+                }
+                __syncwarp();
+                const int last = min(kPass, heads - q * kPass);
+                for (int h = 0; h < last; ++h)
+                    for (int e = 2 * lane; e < p.head_dim; e += 64) {
+                        const float2 v = *reinterpret_cast<const float2*>(&rows[h * kDim + e]);
+                        *reinterpret_cast<uint32_t*>(p.out + (int64_t)w.s * p.out_stride +
+                                                     (int64_t)(head0 + q * kPass + h) * p.head_dim + e) =
+                            pack16<kBf16>(v.x, v.y);
+                    }
+                __syncwarp();
+            }
+            continue;
+        }
         // ---- the warps' sums into one ------------------------------------------------------
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-#pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], x);
+            for (int i = 0; i < 2; ++i)
                 if (lane < 4) {
                     stat_m[warp][n * 8 + hc + i] = m[n][i];
                     stat_l[warp][n * 8 + hc + i] = l[n][i];
                 }
-            }
         __syncthreads();
         const bool shared_unit = team > 1;  // with the cluster's other CTAs
         const bool whole = w.t0 == 0 && w.t1 == w.tiles() && !shared_unit;
@@ -749,6 +818,18 @@ cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st
             break;
         }
     }
+    // what the kernel's choice needs of these numbers
+    auto deal = [&](int size) {
+        const int64_t groups = grid / size;
+        AttendDeal d;
+        d.units = (float)((n_units + groups - 1) / groups);
+        d.per_busy = 1.0f / (float)((n_units < groups ? n_units : groups) * size);
+        return d;
+    };
+    q.alone = deal(1);
+    q.together = deal(q.cluster);
+    q.solo_units = (float)((n_units + (int64_t)grid * kWarps - 1) / ((int64_t)grid * kWarps));
+    q.cluster_log2 = q.cluster == 8 ? 3 : q.cluster == 4 ? 2 : q.cluster == 2 ? 1 : 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(kWarps * 32);

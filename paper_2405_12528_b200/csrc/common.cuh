@@ -169,6 +169,11 @@ struct AttendLayout {
     size_t tickets_off, part_ml_off, part_o_off, zeroed, total;
 };
 
+// Units dealt out in turn: to how many the busiest CTA (or cluster) comes, and 1 / CTAs with work.
+struct AttendDeal {
+    float units, per_busy;
+};
+
 struct AttendParams {
     const char *q, *k, *v;
     const int32_t* kv_len;
@@ -184,7 +189,10 @@ struct AttendParams {
     int32_t group, blocks, units;            // query heads per K/V head; blocks of them; units per stream
     int32_t planes_per_stream, layer_plane;
     int32_t part_heads;
-    int32_t cluster;                         // CTAs of a cluster, set by the launcher
+    // set by the launcher
+    int32_t cluster, cluster_log2;           // CTAs of a cluster
+    AttendDeal alone, together;              // to CTAs, to clusters
+    float solo_units;                        // the busiest warp's, dealt out to warps
 };
 
 struct HeadParams {

@@ -271,6 +271,15 @@ def test_attend_many_streams_of_all_lengths():
     attend_case(700, 4, 2, 64, 300, lens.tolist(), seed=8, fill=math.inf)
 
 
+@pytest.mark.parametrize("D,group", [(64, 1), (128, 1), (128, 4), (96, 8), (128, 11), (40, 3)])
+@pytest.mark.parametrize("longest", [20, 300, 512])
+def test_attend_many_short_units(D, group, longest):
+    S, KH = 180, 8                                                      # more units than warps
+    lens = [(37 * s) % (longest + 1) for s in range(S)]
+    attend_case(S, KH * group, KH, D, longest, lens, kv="f16" if D == 96 else "bf16", seed=D + group, fill=math.nan)
+    attend_case(S, KH * group, KH, D, longest, [longest] * S, seed=D)
+
+
 def test_attend_only_the_last_stream_has_slots():
     attend_case(600, 2, 1, 64, 40, [0] * 599 + [33], seed=9)
     attend_case(5, 2, 1, 128, 40, [0] * 5, seed=9)
