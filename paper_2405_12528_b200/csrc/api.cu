@@ -747,7 +747,8 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
     const int unit = attend_unit_heads(p.group, p.head_dim);
     p.blocks = (p.group + unit - 1) / unit;
     p.units = cfg->n_kv_heads * p.blocks;
-    if ((int64_t)cfg->n_streams * p.units > 0x3FFFFFFF) return SIRLLM_ERR_TOO_LARGE;  // counted in 32 bits
+    // positions are counted in 32 bits: up to 41 per unit besides the tiles that fit a device's memory
+    if ((int64_t)cfg->n_streams * p.units > 0x1FFFFFF) return SIRLLM_ERR_TOO_LARGE;
     p.planes_per_stream = cfg->n_layers * cfg->n_kv_heads;
     p.layer_plane = layer * cfg->n_kv_heads;
     p.part_heads = kAttendPartHeads;

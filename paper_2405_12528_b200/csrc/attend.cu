@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         counted[warp] = live;
     }
     __syncthreads();
-    int line = 0, warps_before = 0;  // below 2^31: the caches of so many tiles fit no device
+    int line = 0, warps_before = 0;  // below 2^31: few enough units, and no device holds so many tiles
     live = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {

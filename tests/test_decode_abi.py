@@ -83,6 +83,11 @@ def test_attend_refusals(lib, want, kw):
     assert attend(lib, **kw) == want
 
 
+def test_attend_refuses_more_units_than_it_counts(lib):
+    big = cfg(n_streams=2**24, n_layers=1, n_kv_heads=2, head_dim=8, capacity=1, budget=1, n_sink=0, n_recent=0, max_new=1)
+    assert attend(lib, big, n_heads=2, qs=16, os=16) == B.ERR_TOO_LARGE
+
+
 def test_attend_refuses_heads_wider_than_its_registers(lib):
     wide = cfg(head_dim=264)
     assert attend(lib, wide, qs=2048, os=2048) == B.ERR_TOO_LARGE
