@@ -327,9 +327,10 @@ int sirllm_append_kv(const sirllm_config *cfg, int32_t layer, const void *q, int
  *             disjoint parts of a context can be joined
  *   ws        its own kind of workspace: sirllm_attend_workspace_bytes() bytes, 256-byte aligned,
  *             set up once with sirllm_attend_workspace_init(); sirllm_status() reads its status
- *   head_dim  at most SIRLLM_MAX_ATTEND_HEAD_DIM, and fewer than 2^25 blocks of 8 query heads that
- *             share a K/V head (n_streams * n_kv_heads * ceil(n_heads / n_kv_heads / 8)), else
- *             SIRLLM_ERR_TOO_LARGE
+ *   sizes     head_dim at most SIRLLM_MAX_ATTEND_HEAD_DIM; blocks of query heads that share a K/V head
+ *             (n_streams * n_kv_heads * ceil(n_heads / n_kv_heads / b), b = 16 where more than 8 share
+ *             one and head_dim <= 128, else 8) fewer than 2^25, and fewer than 2^31 - 256 when
+ *             multiplied by ceil(capacity / 16) + 40; else SIRLLM_ERR_TOO_LARGE
  */
 size_t sirllm_attend_workspace_bytes(const sirllm_config *cfg);
 int sirllm_attend_workspace_init(const sirllm_config *cfg, void *ws, void *cuda_stream);

@@ -747,8 +747,11 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
     const int unit = attend_unit_heads(p.group, p.head_dim);
     p.blocks = (p.group + unit - 1) / unit;
     p.units = cfg->n_kv_heads * p.blocks;
-    // positions are counted in 32 bits: up to 41 per unit besides the tiles that fit a device's memory
-    if ((int64_t)cfg->n_streams * p.units > 0x1FFFFFF) return SIRLLM_ERR_TOO_LARGE;
+    // Positions are counted in 32 bits, and rounded up to the CTAs.  The units of one K/V head have its
+    // tiles each, so query heads alone can make them many.
+    const int64_t all_units = (int64_t)cfg->n_streams * p.units;
+    const int64_t most_tiles = (cfg->capacity + kAttendTileSlots - 1) / kAttendTileSlots + kAttendUnitTiles;
+    if (all_units > 0x1FFFFFF || all_units * most_tiles > 0x7FFFFFFF - kAttendMaxCtas) return SIRLLM_ERR_TOO_LARGE;
     p.planes_per_stream = cfg->n_layers * cfg->n_kv_heads;
     p.layer_plane = layer * cfg->n_kv_heads;
     p.part_heads = kAttendPartHeads;

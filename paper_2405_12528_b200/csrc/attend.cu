@@ -39,15 +39,14 @@ namespace sirllm {
 
 namespace {
 
-constexpr int kKeys = 16;  // slots per tile
+constexpr int kKeys = kAttendTileSlots;
 // What an SM reads in the time that joining a unit's parts takes, through memory (6 us at the 110 GB/s
 // that one SM takes in, and for each part's rows four times their bytes) and within a cluster (2 us), and
 // how many SMs at that rate make up HBM's.
 constexpr float kJoinBytes = 640 * 1024, kClusterBytes = 220 * 1024;
 constexpr float kBusySms = 58.f;
-// What the end of a unit costs a CTA (about 2 us), in bytes of its share of HBM and at most in tiles.
+// What the end of a unit costs a CTA (about 2 us), in bytes of its share of HBM, at most kAttendUnitTiles.
 constexpr float kUnitBytes = 96 * 1024;
-constexpr int kUnitTiles = 40;
 // The same for a single warp (about 0.9 us), and the longest units, in tiles, that are given to one.
 constexpr float kSoloBytes = 96 * 1024;
 constexpr int kSoloLongest = 32;
@@ -227,7 +226,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     const int slice = (p.n_streams + kThreads - 1) / kThreads;
     const int s_lo = min(p.n_streams, tid * slice), s_hi = min(p.n_streams, s_lo + slice);
     const float tile_bytes = (float)(kKeys * 4 * p.head_dim);
-    const int gap = min((int)(kUnitBytes / tile_bytes), kUnitTiles);
+    const int gap = min((int)(kUnitBytes / tile_bytes), kAttendUnitTiles);
     int mine = 0, live = 0, long_unit = 0;
     for (int s = s_lo; s < s_hi; ++s) {
         const int T = (live_slots(p, s) + kKeys - 1) / kKeys;
@@ -250,7 +249,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         counted[warp] = live;
     }
     __syncthreads();
-    int line = 0, warps_before = 0;  // below 2^31: few enough units, and no device holds so many tiles
+    int line = 0, warps_before = 0;  // below 2^31 - kAttendMaxCtas: a call with more is refused
     live = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {

@@ -159,6 +159,8 @@ struct AppendParams {
 
 constexpr int kAttendMaxCtas = 256;   // CTAs of an attention call, at most
 constexpr int kAttendPartHeads = 16;  // query heads of a unit, at most
+constexpr int kAttendTileSlots = 16;  // slots per tile
+constexpr int kAttendUnitTiles = 40;  // positions behind a unit's tiles that stand for what its end costs, at most
 
 // ---- workspace of the attention call ------------------------------------------------------
 //   [0, 256)                     header: int32 status word

@@ -88,6 +88,22 @@ def test_attend_refuses_more_units_than_it_counts(lib):
     assert attend(lib, big, n_heads=2, qs=16, os=16) == B.ERR_TOO_LARGE
 
 
+@pytest.mark.parametrize("streams,heads,dim,capacity", [
+    (64, 196608, 8, 49152),         # 786432 units x (3072 tiles + 40): 2447376384 positions
+    (1024, 10816, 8, 49152),        # 2154201088
+    (1, 5600000, 256, 49152),       # wide heads: units of 8
+    (2**18, 2032, 8, 400),          # 33.3 million units (below 2^25) of 25 tiles
+])
+def test_attend_refuses_more_positions_than_it_counts(lib, streams, heads, dim, capacity):
+    # query heads that share a K/V head multiply the work without any memory for the cache
+    big = cfg(n_streams=streams, n_layers=1, n_kv_heads=1, head_dim=dim, capacity=capacity, budget=capacity, n_sink=0,
+              n_recent=0, max_new=1)
+    units = streams * -(-heads // (16 if dim <= 128 else 8))
+    wide = heads * dim
+    refused = units * (-(-capacity // 16) + 40) > 2**31 - 1 - 256
+    assert refused and attend(lib, big, n_heads=heads, qs=wide, os=wide) == B.ERR_TOO_LARGE
+
+
 def test_attend_refuses_heads_wider_than_its_registers(lib):
     wide = cfg(head_dim=264)
     assert attend(lib, wide, qs=2048, os=2048) == B.ERR_TOO_LARGE
