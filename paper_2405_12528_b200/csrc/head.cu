@@ -382,8 +382,6 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
                 multiply();
                 if (issuer) mma_commit<kCtas>(&drained);
             }
-            // products still under way use both CTAs' shared memory and TMEM
-            if (issuer && !mbar_wait_bounded(&drained, 0, kMbarSpinLimit)) gave_up = 1;
         }
     } else {  // sums of the chunks, then the reduction: a thread has half of a tile's columns of one row
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kReduceRegs));
@@ -495,6 +493,16 @@ head_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_a, const
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    // Products still under way use both CTAs' shared memory and TMEM.  Waited for here, where every
+    // role of this CTA is done and they are due at once: the bound is for one step, not for the call.
+    if (warp == 1) {
+        if (lane == 0) {
+            bool done = false;
+            for (uint32_t i = 0; i < kNapLimit && !done; ++i) done = mbar_nap(&drained, 0);
+            if (!done) gave_up = 1;
+        }
+        __syncwarp();
+    }
     cta_or_pair_sync<kCtas>();  // neither CTA's memory goes while the other may still use it
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 1) tmem_free<kCtas>(tmem);

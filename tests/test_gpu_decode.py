@@ -515,6 +515,26 @@ def test_head_more_rows_than_one_launch_takes():
     assert B.sirllm_status(ws) == 0
 
 
+def test_head_launch_that_takes_longer_than_any_one_wait():
+    # 3.4e15 operations in one launch: 2 s and more.  No wait inside may be bounded over the whole of it
+    # (2^20 polls of a barrier at 1.5 us each are 1.55 s).
+    if torch.cuda.mem_get_info()[0] < 60e9:
+        pytest.skip("needs 60 GB of device memory")
+    g = gen(27)
+    S, M, W, V = 32, 32768, 8192, 200000
+    cfg = config(S=S, C=M, M=M, V=V)
+    hidden = torch.empty(S * M, W, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    weight = torch.empty(V, W, dtype=torch.bfloat16, device="cuda").normal_(0, 2 / math.sqrt(W), generator=g)
+    ids = torch.randint(0, V, (S * M,), generator=g, device="cuda", dtype=torch.int32)
+    pairs, target, ent, ws = head_scores(cfg, hidden, weight, ids, None)
+    assert B.sirllm_status(ws) == 0
+    assert (pairs[..., 1] >= 1 - 1e-6).all()
+    rows = torch.arange(0, S * M, S * M // 61, device="cuda")           # both CTAs' rows, first block to last
+    rows[-1] = S * M - 1
+    _, want, walk = ref_scores(hidden[rows], weight, ids[rows])
+    assert_scores(ent[rows], want, walk)
+
+
 @pytest.mark.parametrize("rows", [150, 100, 20])
 def test_head_column_ranges_add_up_to_the_whole(rows):
     g = gen(21)
