@@ -20,8 +20,10 @@
 // wants 128 rows of queries or 64+ of K per instruction and a round trip through TMEM for the
 // probabilities, and has nothing to give where HBM is the bound.
 // fp32: scores, running maximum and sum, output sums, the join.  Rounded to 16 bits: the
-// probabilities on their way into the second product (relative to a reference that the true
-// maximum exceeds by less than 2^8, so fp16 cannot overflow), and the result.
+// probabilities on their way into the second product, and the result.  The probabilities are taken
+// relative to a reference; the true maximum stands between 2^0 and 2^8 of it with bf16, between 2^11
+// and 2^15 with fp16, which cannot overflow then, and where what underflows (half a step of 2^-24 a
+// slot) is below 2^-36 of the maximum: 49152 faint slots beside a dominant one lose 7e-7 of V.
 // Measured, bf16, heads of 128: 64 streams x 32 heads x 900 - 1280 slots 171 us (1.03 of the copy
 // rate, part from L2), 16 x 32 heads x 2048 slots 86 us (0.96), one stream x 8 heads x 12287 slots
 // 15.9 us (0.49: launch, reading the length and the join are 7 us of it, and 64 SMs read).
@@ -51,6 +53,12 @@ constexpr float kUnitBytes = 96 * 1024;
 constexpr float kSoloBytes = 96 * 1024;
 constexpr int kSoloLongest = 32;
 constexpr int kMaxCluster = 8;
+// Powers of two between the reference of the probabilities and the largest: where it is set, and
+// where it has to move.
+template <bool kBf16>
+constexpr float kSetBelow = kBf16 ? 0.f : 11.f;
+template <bool kBf16>
+constexpr float kMoveAt = kBf16 ? 8.f : 15.f;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0)
@@ -458,10 +466,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     z[n][i] = (i < 2 ? in0 : in1) ? z[n][i] * p.scale_log2 : __uint_as_float(0xFF800000u);
-                    raise |= z[n][i] > m[n][i & 1] + 8.f;
+                    raise |= z[n][i] > m[n][i & 1] + kMoveAt<kBf16>;
                 }
             }
-            // The reference moves only when a score passes it by more than 2^8; the sums stay exact.
+            // The reference moves only when a score passes it by more than that; the sums stay exact.
             if (__any_sync(0xFFFFFFFFu, raise)) {
 #pragma unroll
                 for (int n = 0; n < kTiles; ++n)
@@ -470,7 +478,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                         float top = fmaxf(z[n][i], z[n][i + 2]);
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-                        const float up = fmaxf(m[n][i], top);
+                        const float up = fmaxf(m[n][i], top - kSetBelow<kBf16>);
                         const float f = ex2_approx(m[n][i] - up);
                         m[n][i] = up;
                         l[n][i] *= f;

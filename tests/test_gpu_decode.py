@@ -316,6 +316,33 @@ def test_attend_scores_that_keep_rising_and_falling():
         check_attend(q, k, v, [C], 1.0, out, lse)
 
 
+@pytest.mark.parametrize("kv", ["bf16", "f16"])
+@pytest.mark.parametrize("S,H,D,at", [(1, 1, 64, 0), (1, 4, 128, 49151), (1, 12, 128, 30000), (1, 2, 256, 17),
+                                      (160, 1, 64, 0)])   # the last: thousands of slots per warp
+@pytest.mark.parametrize("faint", [22.0, 25.5, 30.0])
+def test_attend_one_dominant_slot_and_many_faint_ones(kv, S, H, D, at, faint):
+    # The faint slots' weights are 2^-faint of the dominant one's, whose V row is zero.  Rounded to 16
+    # bits relative to a reference 2^11 or more below the maximum, an fp16 weight is off by u or by half a
+    # subnormal step, 2^-25: 2^-36 of the maximum per slot (bf16 has fp32's range).
+    g = gen(17)
+    C, dt = 49152, DT[kv]
+    cfg = config(S=S, D=D, C=C, kv=kv)
+    q = torch.zeros(S, H, D, dtype=dt, device="cuda")
+    q[..., 0] = 1.0
+    k = torch.zeros(S, 1, 1, C, D, dtype=dt, device="cuda")
+    k[..., at, 0] = 1.0
+    v = (1 + randn(g, 1, 1, 1, C, D, scale=0.2)).to(dt).expand(S, 1, 1, C, D).contiguous()
+    v[..., at, :] = 0.0
+    scale = faint * math.log(2)
+    out, lse = torch.empty_like(q), torch.empty(S, H, device="cuda")
+    B.sirllm_attend(cfg, 0, q, k, v, i32(*[C] * S), scale, out, lse, B.new_attend_workspace(cfg))
+    want, l, tol, tol_l = ref_attend(q[0], k[0, 0], v[0, 0], C, scale)
+    tol = tol + 2.0 ** -36 * v[0].double().abs().sum(-2).amax()
+    d = (out.double() - want).abs()
+    assert (d <= tol).all(), f"worst {float((d / tol).max()):.2f} x tol"
+    assert ((lse.double() - l).abs() <= tol_l).all()
+
+
 def test_attend_infinite_scores_follow_the_formula():
     cfg = config(D=64, C=64, kv="bf16")
     ws = B.new_attend_workspace(cfg)
