@@ -354,7 +354,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         if (n < 0 || n > p.capacity) {
             if (tid == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
         } else if (n == 0) {
-            for (int i = tid; i < p.n_heads * p.head_dim; i += kThreads)
+            // (a row of up to 2^31 - 1 elements: the index of the step behind it does not fit an int)
+            for (uint32_t i = tid; i < (uint32_t)p.n_heads * p.head_dim; i += kThreads)
                 p.out[(int64_t)s * p.out_stride + i] = 0;
             if (p.lse != nullptr)
                 for (int i = tid; i < p.n_heads; i += kThreads)

@@ -394,6 +394,23 @@ def test_attend_offsets_past_32_bits():
     check_attend(q, k[:, L - 1:], v[:, L - 1:], [C], D ** -0.5, out, lse)
 
 
+def test_attend_an_empty_stream_of_the_widest_row():
+    # 2^28 - 1 heads of 8: 2147483640 elements, 8 below 2^31
+    if torch.cuda.mem_get_info()[0] < 20e9:
+        pytest.skip("needs 20 GB of device memory")
+    H, D = 2**28 - 1, 8
+    cfg = config(D=D, C=1)
+    q = torch.empty(1, H, D, dtype=torch.bfloat16, device="cuda")
+    wide = torch.full((1, H + 64, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    out, lse = wide[:, 32:32 + H], torch.full((1, H), 7.0, device="cuda")
+    k, v = (torch.zeros(1, 1, 1, 1, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ws = B.new_attend_workspace(cfg)
+    B.sirllm_attend(cfg, 0, q, k, v, i32(0), None, out, lse, ws)
+    assert B.sirllm_status(ws) == 0
+    assert int(torch.count_nonzero(out)) == 0 and bool((lse == -math.inf).all())
+    assert (wide[:, :32] == 7).all() and (wide[:, 32 + H:] == 7).all()
+
+
 def test_attend_is_reproducible_and_leaves_its_workspace_ready():
     lens = [1, 800, 0, 3333, 64, 4095, 17]
     cfg, q, k, v, out, lse, ws = attend_case(7, 8, 2, 128, 4096, lens, seed=15)
