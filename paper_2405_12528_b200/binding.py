@@ -204,7 +204,8 @@ def _dev(t, dtype=None, name="tensor", numel: int = 0) -> _Arg:
 class Prepared:
     """A call whose arguments were checked and marshalled once (see :func:`prepared`): calling
     it again costs one ctypes call.  It keeps its tensors alive and reads the current CUDA
-    stream at every call; it must be called with the device it was prepared on current."""
+    stream at every call; it refuses to be called with another device current than the one it
+    was prepared on, where its pointers mean nothing."""
 
     def __init__(self, fn, cfg, args):
         self._fn, self._cfg = fn, Config.from_buffer_copy(cfg)
@@ -214,9 +215,13 @@ class Prepared:
         raw = [self._stream if isinstance(a, _CurrentStream) else a.ptr() if isinstance(a, _Arg) else a for a in args]
         self._args = [ctypes.byref(self._cfg)] + [
             t(a) if t in _PLAIN and not isinstance(a, t) else a for t, a in zip(fn.argtypes[1:], raw)]
-        self._device = torch.cuda.current_device()
+        self._device = _current_device()
 
     def __call__(self) -> None:
+        current = _current_device()
+        if current != self._device:
+            raise SirllmError(ERR_BAD_CONFIG, f"the call was prepared on cuda:{self._device}, the current device "
+                                              f"is cuda:{current}")
         self._stream.value = _raw_stream(self._device)
         rc = self._fn(*self._args)
         if rc != OK:
@@ -225,6 +230,12 @@ class Prepared:
 
 _PLAIN = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float,
           ctypes.c_double)
+
+
+def _current_device() -> int:
+    """The current device's index (torch's short way where this torch has it)."""
+    short = getattr(torch._C, "_cuda_getDevice", None)
+    return short() if short is not None else torch.cuda.current_device()
 
 
 def _raw_stream(device: int) -> int:

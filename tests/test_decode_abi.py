@@ -261,3 +261,30 @@ def test_two_ranks_exchange_several_tiles_each():
     assert all(shape == (9, 10, 2) and worst < 8 * 2.0 ** -21 for _, shape, worst in results)
     one, tgt = sharding.exchange_vocab_partials(torch.ones(4, 3, 2), torch.ones(4))   # a single process
     assert one.shape == (4, 3, 2) and tgt.shape == (4,)
+
+
+def test_a_prepared_call_is_refused_on_another_device(monkeypatch):
+    # its pointers are the first device's; the launch would go to the current one
+    made = []
+
+    class Call:
+        argtypes = [ctypes.POINTER(B.Config), ctypes.c_int32, ctypes.c_void_p]
+
+        def __call__(self, c, layer, stream):
+            made.append((layer.value, stream.value))
+            return B.OK
+
+    device = [1]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: device[0])
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: device[0], raising=False)
+    monkeypatch.setattr(B, "_raw_stream", lambda d: 0x40 + d)
+    call = B.Prepared(Call(), cfg(), (7, B._stream()))
+    call()
+    assert made == [(7, 0x41)]
+    device[0] = 0
+    with pytest.raises(B.SirllmError) as err:
+        call()
+    assert err.value.code == B.ERR_BAD_CONFIG and "cuda:1" in str(err.value) and made == [(7, 0x41)]
+    device[0] = 1
+    call()
+    assert len(made) == 2
