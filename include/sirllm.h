@@ -293,6 +293,7 @@ int sirllm_rerotate_keys(const sirllm_config *cfg, void *k, const int32_t *keep_
  * Angles are formed in fp64, everything else in fp32, and each element is rounded once, to the
  * K/V dtype; all tensors have that type.  Writing the rows is all the bookkeeping done here:
  * live_len is left to the round (sirllm_step reads the rows behind it).
+ * int32 and fp32 arrays of this call and of the ones below have to be 4-byte aligned.
  *   q, k_new, v_new   rows of n_heads / n_kv_heads / n_kv_heads heads of head_dim elements, rows
  *                     *_row_stride elements apart (slices of one projection's output are fine);
  *                     16-byte aligned, strides multiples of 8; head_dim % 16 == 0

@@ -655,7 +655,7 @@ int sirllm_append_kv(const sirllm_config* cfg, int32_t layer, const void* q, int
         if (x && misaligned(x, 16)) return SIRLLM_ERR_ALIGN;
     if (k_row_stride % 8 != 0 || v_row_stride % 8 != 0 || (q && (q_row_stride % 8 != 0 || q_out_row_stride % 8 != 0)))
         return SIRLLM_ERR_ALIGN;
-    if (misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
+    if (misaligned(first_slot, 4) || misaligned(n_new, 4) || misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
     AppendParams p;
     memset(&p, 0, sizeof p);
     p.q = (const char*)q;
@@ -722,7 +722,9 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
     const void* vectors[4] = {q, k, v, out};
     for (const void* x : vectors)
         if (misaligned(x, 16)) return SIRLLM_ERR_ALIGN;
-    if (q_row_stride % 8 != 0 || out_row_stride % 8 != 0 || misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
+    if (q_row_stride % 8 != 0 || out_row_stride % 8 != 0 || misaligned(kv_len, 4) || misaligned(lse, 4) ||
+        misaligned(ws, 256))
+        return SIRLLM_ERR_ALIGN;
     const AttendLayout L = attend_layout(*cfg);
     AttendParams p;
     memset(&p, 0, sizeof p);
@@ -780,7 +782,8 @@ int sirllm_head_pairs(const sirllm_config* cfg, const void* hidden, int64_t hidd
     const HeadTiling tiling = head_tiling((int64_t)cfg->n_streams * cfg->max_new, n_cols);
     if (pair_row_stride < tiling.n_parts) return SIRLLM_ERR_BAD_CONFIG;
     if (misaligned(hidden, 16) || misaligned(weight, 16) || hidden_row_stride % 8 != 0 || weight_row_stride % 8 != 0 ||
-        misaligned(pairs_out, 8) || misaligned(target_out, 4) || misaligned(ws, 256))
+        misaligned(pairs_out, 8) || misaligned(target_out, 4) || misaligned(token_ids, 4) || misaligned(n_new, 4) ||
+        misaligned(ws, 256))
         return SIRLLM_ERR_ALIGN;
     HeadParams p;
     memset(&p, 0, sizeof p);

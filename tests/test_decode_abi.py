@@ -216,6 +216,14 @@ def test_binding_refuses_wrong_tensors_before_the_library(lib):
     hd("needs", target_out=torch.zeros(15))
 
 
+@pytest.mark.parametrize("call,arg", [(append, "first"), (append, "n_new"), (attend, "kv_len"), (attend, "lse"),
+                                      (head, "ids"), (head, "n_new"), (head, "target")])
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_words_off_their_4_bytes_are_refused(lib, call, arg, off):
+    # the kernels would fault on them
+    assert call(lib, **{arg: P + off}) == B.ERR_ALIGN
+
+
 # ---- a vocabulary-parallel LM head: several tiles per rank through the exchange (gloo, two ranks) ----
 
 def _tile_pairs(z, width):
