@@ -232,16 +232,10 @@ _PLAIN = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctyp
           ctypes.c_double)
 
 
-def _current_device() -> int:
-    """The current device's index (torch's short way where this torch has it)."""
-    short = getattr(torch._C, "_cuda_getDevice", None)
-    return short() if short is not None else torch.cuda.current_device()
-
-
-def _raw_stream(device: int) -> int:
-    """Handle of the device's current stream (torch's short way where this torch has it)."""
-    short = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return short(device) if short is not None else torch.cuda.current_stream(device).cuda_stream
+# The current device's index, and the handle of a device's current stream: torch's short ways where
+# this torch has them.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 _preparing = threading.local()

@@ -283,8 +283,7 @@ def test_a_prepared_call_is_refused_on_another_device(monkeypatch):
             return B.OK
 
     device = [1]
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: device[0])
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: device[0], raising=False)
+    monkeypatch.setattr(B, "_current_device", lambda: device[0])
     monkeypatch.setattr(B, "_raw_stream", lambda d: 0x40 + d)
     call = B.Prepared(Call(), cfg(), (7, B._stream()))
     call()
