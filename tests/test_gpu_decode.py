@@ -2,8 +2,8 @@
 ``sirllm_append_kv``, ``sirllm_attend``, ``sirllm_head_pairs``, and a run of them together.
 
 Tolerances.  ``u`` is half a step of the 16-bit type.  append: fp32 arithmetic and one rounding:
-u * |want| plus 2e-6 of the pair's length (a dozen fp32 roundings of 2^-24, and an angle known to
-2^-26 of a turn).  attend: the weights of the second product are rounded to 16 bits (u of
+u * |want| plus 2e-6 of the pair's length (a dozen fp32 roundings of 2^-24, 7.2e-7, and sine and
+cosine off by 5.5e-7 together in their fast forms and 3e-7 for the angle in fp32).  attend: the weights of the second product are rounded to 16 bits (u of
 sum p|V|), the result once more (u of |out|), and an error dz of the scores moves the weights by
 2 dz; dz is D products and sums in fp32, 2^-23 D sum|q k| scale at the very most.  head: the
 framework's bound for scores, plus the random walk of d fp32 roundings."""
@@ -156,6 +156,35 @@ def test_append_that_does_not_fit_skips_the_stream_and_reports_it(first, n):
     # a stream without new tokens is not looked at
     B.sirllm_append_kv(cfg, 0, q, kn, vn, None, None, 1e-6, 1e4, B.ROPE_HALF, i32(first, 60), i32(0, 4), out, k, v, ws)
     assert B.sirllm_status(ws) == 0
+
+
+@pytest.mark.parametrize("layout", [B.ROPE_HALF, B.ROPE_INTERLEAVED])
+def test_append_angles_where_a_pair_nearly_cancels(layout):
+    # a pair (sin, cos) of its own angle turns to (0, 1): what is left of the first element shows the
+    # error of the angle, the sine and the cosine, far below the rounding of the 16-bit type.  Bound, of
+    # the pair's length: hypot(2^-21.19, 2^-21.41) for the fast cosine and sine; for the angle 2^-26 of a
+    # turn (its fraction in fp32), pi times the error of 2pi in fp32, half a step below 4 for their
+    # product; 2^-25 for the one product that is rounded by itself (at most half the length).
+    M, D = 49152, 128
+    cfg = config(D=D, C=M, M=M, kv="f16")
+    pos = torch.arange(M, device="cuda")
+    i = torch.arange(D // 2, device="cuda")
+    a, b = (i, i + D // 2) if layout == B.ROPE_HALF else (2 * i, 2 * i + 1)
+    ang = pos.to(F64)[:, None] * torch.pow(torch.tensor(1e4, dtype=F64, device="cuda"), -2.0 * i.to(F64) / D)
+    kn = torch.empty(M, 1, D, dtype=torch.float16, device="cuda")
+    kn[:, 0, a], kn[:, 0, b] = torch.sin(ang).half(), torch.cos(ang).half()
+    k, v = (torch.zeros(1, 1, 1, M, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    ws = B.new_workspace(cfg)
+    B.sirllm_append_kv(cfg, 0, None, kn, kn, None, None, 0.0, 1e4, layout, i32(0), None, None, k, v, ws)
+    want, length = ref_rope(kn.double(), None, pos, 0.0, 1e4, layout)
+    got = k[0, 0, 0, :, a].double()
+    want, length = want[:, 0, a], length[:, 0, a]
+    turn = float(torch.tensor(2 * math.pi, dtype=torch.float32))
+    angle = 2.0 ** -26 * 2 * math.pi + abs(turn / (2 * math.pi) - 1) * math.pi + 2.0 ** -23
+    bound = math.hypot(2 ** -21.19, 2 ** -21.41) + angle + 2.0 ** -25
+    tol = half_step(torch.float16) * want.abs() + bound * length + 2.0 ** -25
+    d = (got - want).abs()
+    assert (d <= tol).all(), f"worst {float((d / tol).max()):.3f} x tol"
 
 
 def test_append_equals_the_rerotated_key_of_another_slot():
