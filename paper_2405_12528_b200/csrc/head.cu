@@ -23,11 +23,14 @@
 // one lane issues tcgen05.mma, eight warps take the accumulators out of TMEM, which holds two
 // of them - one is read while the other is multiplied into.
 //
-// Precision: the tensor core's fp32 accumulator truncates; measured, its sums run short by 1e-9 of
-// the logit per element of d (4e-6 at d = 4096, a bias that does not average out).  So d is cut
-// into chunks of kChunkSteps stages: a chunk is summed in TMEM, the chunks in registers with
-// rounded additions (128 columns of one row per thread); 9e-7 remain at any d.  Nothing is rounded
-// to 16 bits.
+// Precision: the tensor core truncates as it adds, a bias that does not average out and grows with the
+// number of additions.  So d is cut into chunks of kChunkSteps stages: a chunk is summed in TMEM, the
+// chunks in registers with rounded additions (128 columns of one row per thread), and the bias stays
+// that of 1024 elements at any d (measured at 1024 to 16384, the same in all three forms): ordinary
+// logits run short by 9e-7 of themselves (fp16 1.2e-6), terms of one sign by 2.2e-6 (fp16 6.1e-6, whose products
+// have more bits to lose); unchunked it was 4e-6 for ordinary logits at d = 4096.  The scores of such logits are
+// as close to 64 bits as those of plain fp32 products and sums: 8e-7 of their norm at d = 4096 (plain 1e-6),
+// 8e-7 at 16384 (plain 2.7e-6).  Nothing is rounded to 16 bits.
 //
 // Measured, bf16: 2048 rows x 37888 columns x 4096 in 371 us (1715 TFLOP/s, 1.03 of cuBLAS's measured
 // burst), 4096 x 128256 x 4096 back to back 2.9 - 3.1 ms (1.00 - 1.06 of its rate under the power cap);

@@ -667,6 +667,31 @@ def test_head_of_large_logits(rows):
     assert_scores(ent, want, walk)
 
 
+@pytest.mark.parametrize("rows", [40, 100, 300])
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_head_sums_lean_no_further_at_a_larger_width(rows, dt):
+    # Terms of one sign, so that a truncated addition always errs the same way.  A chunk of 1024 elements
+    # is 64 additions of 16 products each.  Addition j takes 17 terms in units of the sum so far's last
+    # place and cuts each short by less than one of them, 2^-23 j/64 of the chunk's sum: over j = 1 .. 64
+    # less than 17 * 65/2 * 2^-23 of it.  The chunks' rounded additions do not lean to a side, so the mean
+    # error of a wider sum is that of a chunk; one chunk over 4096 or 8192 would lean 4 or 8 times as
+    # far.  The mean over 40 rows is known to well within a quarter (one row scatters by that much).
+    off = {}
+    for width in (1024, 4096, 8192):
+        g = gen(rows + width)
+        V = 2000
+        cfg = config(C=rows, M=rows, V=V)
+        hidden = randn(g, rows, width).abs().to(DT[dt])
+        weight = (randn(g, V, width).abs() / 64).to(DT[dt])
+        ids = torch.randint(0, V, (rows,), generator=g, device="cuda", dtype=torch.int32)
+        _, target, _, _ = head_scores(cfg, hidden, weight, ids, None)
+        z = (hidden.double() * weight.double()[ids.long()]).sum(-1)
+        off[width] = float(((target.double() - z) / z).mean())
+    assert abs(off[1024]) < 17 * 65 / 2 * 2.0 ** -23
+    for width in (4096, 8192):
+        assert abs(off[width] - off[1024]) < 0.25 * abs(off[1024]) + 2.0 ** -24, off
+
+
 @pytest.mark.parametrize("rows", [7, 70, 300])
 def test_head_replayed_from_a_graph_on_another_stream(rows):
     g = gen(24)
