@@ -293,7 +293,7 @@ int sirllm_rerotate_keys(const sirllm_config *cfg, void *k, const int32_t *keep_
  * Angles are formed in fp64, everything else in fp32, and each element is rounded once, to the
  * K/V dtype; all tensors have that type.  Writing the rows is all the bookkeeping done here:
  * live_len is left to the round (sirllm_step reads the rows behind it).
- * int32 and fp32 arrays of this call and of the ones below have to be 4-byte aligned.
+ * int32 and fp32 arrays of this call, sirllm_attend and sirllm_head_pairs are 4-byte aligned.
  *   q, k_new, v_new   rows of n_heads / n_kv_heads / n_kv_heads heads of head_dim elements, rows
  *                     *_row_stride elements apart (slices of one projection's output are fine);
  *                     16-byte aligned, strides multiples of 8; head_dim % 16 == 0
@@ -327,7 +327,8 @@ int sirllm_append_kv(const sirllm_config *cfg, int32_t layer, const void *q, int
  *   lse       fp32 [n_streams][n_heads] (natural logarithm) or NULL.  With it results over
  *             disjoint parts of a context can be joined
  *   ws        its own kind of workspace: sirllm_attend_workspace_bytes() bytes, 256-byte aligned,
- *             set up once with sirllm_attend_workspace_init(); sirllm_status() reads its status
+ *             set up once with sirllm_attend_workspace_init(); sirllm_status() reads its status.
+ *             Calls that can overlap on the GPU (two streams, two graphs) need one each
  *   sizes     head_dim at most SIRLLM_MAX_ATTEND_HEAD_DIM; blocks of query heads that share a K/V head
  *             (n_streams * n_kv_heads * ceil(n_heads / n_kv_heads / b), b = 16 where more than 8 share
  *             one and head_dim <= 128, else 8) fewer than 2^25, and fewer than 2^31 - 256 when

@@ -9,9 +9,9 @@
 // lengths are, the CTAs read the same amount, and a unit that spans CTAs leaves partial results
 // (max, sum, weighted rows) in the workspace, joined by the CTA that finishes last, by ticket -
 // or whole units per CTA, per cluster of CTAs joined through shared memory, or per warp.  Joins
-// add in a fixed order, so results do not depend on timing.  Inside a CTA every warp streams its own tiles through its own ring of cp.async stages and
-// keeps a running softmax; nothing but the end of a unit makes warps wait for one another, and
-// the ring runs ahead across units.
+// add in a fixed order, so results do not depend on timing.  Inside a CTA every warp streams its
+// own tiles through its own ring of cp.async stages and keeps a running softmax; nothing but the end
+// of a unit makes warps wait for one another, and the ring runs ahead across units.
 //
 // The products run on mma.sync (m16n8k16) with K and V as the LEFT operand: z^T = K q^T puts 16
 // slots on the rows and 8 query heads on the columns, out^T = V^T p^T 16 elements on the rows.
@@ -24,7 +24,9 @@
 // relative to a reference; the true maximum stands between 2^0 and 2^8 of it with bf16, between 2^11
 // and 2^15 with fp16, which cannot overflow then, and where what underflows (half a step of 2^-24 a
 // slot) is below 2^-36 of the maximum: 49152 faint slots beside a dominant one lose 7e-7 of V.
-// Measured, bf16, heads of 128: 64 streams x 32 heads x 900 - 1280 slots 171 us (1.03 of the copy
+// Results are 2.3e-3 (bf16) and 2.8e-4 (fp16) of their norm from 64 bits, of which the one rounding at the
+// end alone makes 1.7e-3 and 2.1e-4.
+// Measured, bf16, heads of 128: 64 streams x 32 heads x 900 - 1280 slots 172 us (1.03 of the copy
 // rate, part from L2), 16 x 32 heads x 2048 slots 86 us (0.96), one stream x 8 heads x 12287 slots
 // 15.9 us (0.49: launch, reading the length and the join are 7 us of it, and 64 SMs read).
 // What the ways to deal out the work bring: 64 x 32 heads x 100 slots 41 us by CTAs, 22 by warps; one
@@ -306,7 +308,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     constexpr float kSoloTile = (0.9f / (kStages - 1) + 0.15f) * 110e3f;  // bytes, as above
     const float solo_tiles =
         p.solo_units * ((float)long_unit * fmaxf((float)kWarps, kSoloTile / tile_bytes) + kSoloBytes / tile_bytes);
-    // (long units and wide heads measured slower this way whatever the estimate)
+    // Single warps take units of up to 512 slots.  Up to there they measured faster than the other ways or 6 %
+    // slower at worst (streams x heads of 128 x slots: 64 x 32 x 1 - 512 77 -> 57 us, 192 x 32 x 256 162 ->
+    // 137, 192 x 32 x 512 242 -> 256).  With longer units the estimate does not tell even lengths, which lose
+    // (192 x 32 x 1024 454 -> 498 us; heads of 64, 64 x 32 x 2048 158 -> 174), from ragged ones, which may gain
+    // (64 x 32 x 1 - 768 100 -> 78).  Heads above 128, with four warps to a CTA, keep to the other ways: the
+    // estimate is too kind there (heads of 256, 64 x 32 x 1 - 2048 351 -> 442 us), though short units would
+    // gain (192 x 32 x 64 161 -> 85).
     const bool solo = kWarps == 8 && long_unit <= kSoloLongest && fmaxf(solo_tiles, hbm) < least;
     if (solo) {
         whole_units = true;

@@ -33,8 +33,10 @@
 // 8e-7 at 16384 (plain 2.7e-6).  Nothing is rounded to 16 bits.
 //
 // Measured, bf16: 2048 rows x 37888 columns x 4096 in 371 us (1715 TFLOP/s, 1.03 of cuBLAS's measured
-// burst), 4096 x 128256 x 4096 back to back 2.9 - 3.1 ms (1.00 - 1.06 of its rate under the power cap);
-// 64 rows x 128256 x 4096 in 158 us (6.6 TB/s, 1.03 of the copy rate), 1 x 32000 x 4096 in 46 us (0.88).
+// burst), 4096 x 128256 x 4096 back to back 2.8 - 3.1 ms (1.00 - 1.11 of its rate under the power cap).
+// 128256 x 4096 in a loop of 400 calls: 1 row 157 us (6.7 TB/s, 1.04 of the copy rate), 64 rows 164 us (0.99;
+// 174 with the board at its power cap), 65 185 us, 100 188 us, 128 201 us, 129 236 us, 256 260 us.
+// 32000 x 4096: 1 row 44.5 us (0.91), 64 46.9, 65 48.6, 100 50.4, 129 58.0, 256 60.1.
 #include <atomic>
 
 #include <cuda.h>
