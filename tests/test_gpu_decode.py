@@ -140,6 +140,37 @@ def test_append_without_lengths_without_queries_and_in_place():
     assert k[0, 0, :, 12:].abs().sum() > 0 and k[0, 0, :, :12].abs().sum() == 0
 
 
+@pytest.mark.parametrize("kv", ["bf16", "f16"])
+@pytest.mark.parametrize("norms", [False, True])
+@pytest.mark.parametrize("S,M,H,KH,D", [(1, 1, 32, 8, 128), (3, 5, 6, 2, 80), (2, 300, 5, 1, 512)])
+def test_append_rows_of_every_tensor_at_a_distance_of_their_own(kv, norms, S, M, H, KH, D):
+    g, dt, C = gen(6), DT[kv], 310
+    cfg = config(S=S, KH=KH, D=D, C=C, M=M, kv=kv)
+    wide = [randn(g, S * M + 2, h, D, dtype=dt) for h in (H + 3, KH + 1, KH + 5)]
+    q, kn, vn = wide[0][:S * M, 2:2 + H], wide[1][:S * M, 1:], wide[2][:S * M, 3:3 + KH]
+    wq, wk = (randn(g, D, dtype=dt), randn(g, D, dtype=dt)) if norms else (None, None)
+    out = randn(g, S * M + 1, H + 4, D, dtype=dt)
+    before, q_out = out.clone(), out[:, 1:1 + H]
+    k, v = (torch.zeros(S, 1, KH, C, D, dtype=dt, device="cuda") for _ in range(2))
+    ws = B.new_workspace(cfg)
+    first = [3 + s for s in range(S)]
+    B.sirllm_append_kv(cfg, 0, q, kn, vn, wq, wk, 1e-6, 1e4, B.ROPE_HALF, i32(*first), None, q_out, k, v, ws)
+    assert B.sirllm_status(ws) == 0
+    for s in range(S):
+        r, f = slice(s * M, s * M + M), first[s]
+        pos = torch.arange(f, f + M, device="cuda")
+        assert_turned(q_out[r], *ref_rope(q[r].double(), wq, pos, 1e-6, 1e4, B.ROPE_HALF))
+        want, length = ref_rope(kn[r].double(), wk, pos, 1e-6, 1e4, B.ROPE_HALF)
+        assert_turned(k[s, 0, :, f:f + M], want.transpose(0, 1), length.transpose(0, 1))
+        assert same_bits(v[s, 0, :, f:f + M], vn[r].transpose(0, 1))
+    assert same_bits(out[:, :1], before[:, :1]) and same_bits(out[:, 1 + H:], before[:, 1 + H:])
+    assert same_bits(out[S * M:], before[S * M:])
+    # in place, in rows that are wider than their heads
+    turned, tail = q_out[:S * M].clone(), wide[0][S * M:].clone()
+    B.sirllm_append_kv(cfg, 0, q, kn, vn, wq, wk, 1e-6, 1e4, B.ROPE_HALF, i32(*first), None, q, k, v, ws)
+    assert same_bits(q, turned) and same_bits(wide[0][S * M:], tail)
+
+
 @pytest.mark.parametrize("first,n", [(-1, 1), (61, 4), (64, 1), (2**31 - 1, 1)])
 def test_append_that_does_not_fit_skips_the_stream_and_reports_it(first, n):
     g = gen(4)
