@@ -14,8 +14,8 @@
 // fp32.  The angle in [-pi, pi] is then off by 3.0e-7 at most (the fraction rounded to fp32 9.4e-8, the
 // constant 2pi 8.7e-8, their product 1.2e-7), the fast cosine and sine by their documented 2^-21.19
 // and 2^-21.41: each carries up to 7.2e-7 wherever the token sits, a seven hundredth of a rounding to
-// fp16.  (Measured where a pair cancels, all angles of 49152 positions: 4.3e-7 of the pair's length.)  Sums, norm and rotation are fp32; each element is
-// rounded once, to the cache's type.
+// fp16.  (Measured where a pair cancels, all angles of 49152 positions: 4.3e-7 of the pair's length.)
+// Sums, norm and rotation are fp32; each element is rounded once, to the cache's type.
 // Measured, 4096 tokens x 48 heads x 128 bf16 (50 MB in, 50 MB out): 20.9 us with norms (0.75 of the
 // copy rate), 18.1 us without; 16384 tokens with norms 68.5 us (0.91); one token 2.4 us.  What is
 // left at 4096 tokens is the start and the last, partly filled wave of blocks.

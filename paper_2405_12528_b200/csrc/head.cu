@@ -28,9 +28,9 @@
 // chunks in registers with rounded additions (128 columns of one row per thread), and the bias stays
 // that of 1024 elements at any d (measured at 1024 to 16384, the same in all three forms): ordinary
 // logits run short by 9e-7 of themselves (fp16 1.2e-6), terms of one sign by 2.2e-6 (fp16 6.1e-6, whose products
-// have more bits to lose); unchunked it was 4e-6 for ordinary logits at d = 4096.  The scores of such logits are
-// as close to 64 bits as those of plain fp32 products and sums: 8e-7 of their norm at d = 4096 (plain 1e-6),
-// 8e-7 at 16384 (plain 2.7e-6).  Nothing is rounded to 16 bits.
+// have more bits to lose); unchunked it was 4e-6 for ordinary logits at d = 4096.  Scores are 2e-7 to 1e-6 of
+// their norm from 64 bits at d = 1000 to 16384; those of plain fp32 products and sums 4e-8 to 1e-6 up to
+// 4096, 2.7e-6 at 16384.  Nothing is rounded to 16 bits.
 //
 // Measured, bf16: 2048 rows x 37888 columns x 4096 in 371 us (1715 TFLOP/s, 1.03 of cuBLAS's measured
 // burst), 4096 x 128256 x 4096 back to back 2.8 - 3.1 ms (1.00 - 1.11 of its rate under the power cap).
