@@ -323,7 +323,7 @@ int sirllm_append_kv(const sirllm_config *cfg, int32_t layer, const void *q, int
  * lse as they were.  Results do not depend on the timing of the GPU.
  *   q, out    [n_streams] rows of n_heads * head_dim elements of the K/V dtype, *_row_stride
  *             elements apart, 16-byte aligned, strides multiples of 8; out must not overlap an input
- *   n_heads   a multiple of n_kv_heads
+ *   n_heads   a multiple of n_kv_heads;  scale finite, times log2 e too
  *   lse       fp32 [n_streams][n_heads] (natural logarithm) or NULL.  With it results over
  *             disjoint parts of a context can be joined
  *   ws        its own kind of workspace: sirllm_attend_workspace_bytes() bytes, 256-byte aligned,

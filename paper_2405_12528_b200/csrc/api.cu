@@ -716,7 +716,7 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
     if (!q || !k || !v || !kv_len || !out || !ws) return SIRLLM_ERR_NULL;
     const int64_t width = (int64_t)n_heads * cfg->head_dim;
     if (layer < 0 || layer >= cfg->n_layers || n_heads < 1 || n_heads % cfg->n_kv_heads != 0 || width > 0x7FFFFFFF ||
-        !std::isfinite(scale) || q_row_stride < width || out_row_stride < width)
+        !std::isfinite(scale * kLog2e) || q_row_stride < width || out_row_stride < width)
         return SIRLLM_ERR_BAD_CONFIG;
     if (cfg->head_dim > SIRLLM_MAX_ATTEND_HEAD_DIM) return SIRLLM_ERR_TOO_LARGE;
     const void* vectors[4] = {q, k, v, out};

@@ -83,6 +83,12 @@ def test_attend_refusals(lib, want, kw):
     assert attend(lib, **kw) == want
 
 
+@pytest.mark.parametrize("scale", [3e38, -2.4e38])
+def test_attend_refuses_a_scale_that_overflows_in_units_of_log2(lib, scale):
+    # scores are kept times log2 e: a score of 0 would become NaN
+    assert attend(lib, scale=scale) == B.ERR_BAD_CONFIG
+
+
 def test_attend_refuses_more_units_than_it_counts(lib):
     big = cfg(n_streams=2**24, n_layers=1, n_kv_heads=2, head_dim=8, capacity=1, budget=1, n_sink=0, n_recent=0, max_new=1)
     assert attend(lib, big, n_heads=2, qs=16, os=16) == B.ERR_TOO_LARGE
