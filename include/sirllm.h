@@ -62,6 +62,8 @@ extern "C" {
 #define SIRLLM_STATUS_TIMEOUT 4     /* a bounded device-side wait gave up; results are unreliable */
 #define SIRLLM_STATUS_BAD_KEEP 8    /* a caller-supplied keep list is not strictly ascending within
                                        [0, capacity); that stream was not compacted */
+#define SIRLLM_STATUS_BAD_SOURCE 16 /* sirllm_reorder_streams: a source outside its group; that stream
+                                       was left as it was */
 
 /* comparison policies of Section 4.1.1 for sirllm_keep_policy */
 #define SIRLLM_POLICY_STREAM 1
@@ -79,6 +81,10 @@ extern "C" {
 #define SIRLLM_MAX_HEAD_DIM 512
 /* Largest `head_dim` of sirllm_attend (one unit's queries and sums are held in registers). */
 #define SIRLLM_MAX_ATTEND_HEAD_DIM 256
+/* Largest groups of streams: beams of sirllm_beam_select (and its candidates), streams of
+ * sirllm_reorder_streams. */
+#define SIRLLM_MAX_BEAMS 64
+#define SIRLLM_MAX_GROUP 256
 
 typedef struct sirllm_config {
     int32_t n_streams;   /* independent dialogue streams, >= 1 */
@@ -339,6 +345,84 @@ int sirllm_attend_workspace_init(const sirllm_config *cfg, void *ws, void *cuda_
 int sirllm_attend(const sirllm_config *cfg, int32_t layer, const void *q, int32_t n_heads, int64_t q_row_stride,
                   const void *k, const void *v, const int32_t *kv_len, float scale, void *out,
                   int64_t out_row_stride, float *lse, void *ws, void *cuda_stream);
+
+/*
+ * sirllm_attend for streams whose first slots are the same (the beams of one prompt, dialogues behind
+ * one system prompt): streams g*group .. g*group+group-1 are group g, and its first shared_len[g] slots
+ * are held once, in the planes of its first stream.  Slot j of stream s is, in every formula of
+ * sirllm_attend,
+ *     K[g*group][layer][.][j]  for j < shared_len[g],      K[s][layer][.][j]  from there on
+ * (and V likewise), so slots stay positions and sirllm_append_kv needs no offset.  What the other
+ * streams' planes hold below shared_len is not read.  kv_len[s] counts the shared slots; it may be
+ * smaller than shared_len.  shared_len outside [0, capacity] raises SIRLLM_STATUS_OVERFLOW and leaves
+ * the group's out and lse as they were.
+ *   group       divides n_streams;  shared_len int32 [n_streams / group]
+ *   ws          a workspace of its own kind, for this group and n_heads: sirllm_attend_shared_workspace_bytes()
+ *               bytes (0 for an invalid combination); the rules of sirllm_attend's hold for it
+ * All other arguments, limits and results as in sirllm_attend.
+ */
+size_t sirllm_attend_shared_workspace_bytes(const sirllm_config *cfg, int32_t group, int32_t n_heads);
+int sirllm_attend_shared_workspace_init(const sirllm_config *cfg, int32_t group, int32_t n_heads, void *ws,
+                                        void *cuda_stream);
+int sirllm_attend_shared(const sirllm_config *cfg, int32_t layer, int32_t group, const int32_t *shared_len,
+                         const void *q, int32_t n_heads, int64_t q_row_stride, const void *k, const void *v,
+                         const int32_t *kv_len, float scale, void *out, int64_t out_row_stride, float *lse, void *ws,
+                         void *cuda_stream);
+
+/*
+ * Selection among the beams of a search, one beam per stream: streams g*group .. g*group+group-1 are the
+ * beams of group g.  With z = logits row s (one row per stream, whatever max_new is) and e_s(v) =
+ * -log softmax(z)[v], the Token Entropy that token v would have, a candidate is
+ *     (s, v) with score totals[s] - e_s(v)   for every token v with a logit above -inf
+ * and, if ended[s] is not 0, the one candidate (s, end_token) with score totals[s] and entropy 0.  The
+ * n_out best candidates of the group go out, higher score first (compared in fp64; within a stream by
+ * logit); equal -> the lower stream, then the lower token.  Candidate j of group g stands at
+ * [g*n_out + j]:
+ *     source = s    token_ids = v    totals_out = its score    entropy = e_s(v)
+ *     ended_out = 1 if ended[s] is not 0 or v is end_token, else 0
+ * If there are fewer, the rest is  source -1, token -1, total -inf, entropy 0, ended 0:  such a stream
+ * holds no beam; a stream with total -inf gives no candidates and its logits are not read.  (Start: total 0
+ * for a group's first stream, -inf for the others.)  source feeds sirllm_reorder_streams, token_ids the
+ * next step, entropy the entropy cache.
+ *   places      not 0 (n_out == group): the best candidate of every stream stands in that stream's own
+ *               place, the others, in order, in the free places: no stream is then both overwritten and
+ *               still needed, and sirllm_reorder_streams moves as little as possible
+ *   logits      [n_streams] rows, logits_row_stride apart, of the logits type; finite or -inf
+ *   totals      fp32 [n_streams];  ended int32 [n_streams] or NULL (none has);  end_token in [0, vocab) or -1 (none)
+ *   outputs     [n_streams / group * n_out]; entropy and ended_out may be NULL.  Where n_out == group,
+ *               totals_out may be totals itself and ended_out may be ended itself; else nothing overlaps
+ *   limits      group and n_out at most SIRLLM_MAX_BEAMS, else SIRLLM_ERR_TOO_LARGE
+ *   ws          its own kind of workspace: sirllm_beam_workspace_bytes() bytes, 256-byte aligned, set up once
+ *               with sirllm_beam_workspace_init(); calls that can overlap on the GPU need one each
+ */
+size_t sirllm_beam_workspace_bytes(const sirllm_config *cfg);
+int sirllm_beam_workspace_init(const sirllm_config *cfg, void *ws, void *cuda_stream);
+int sirllm_beam_select(const sirllm_config *cfg, const void *logits, int32_t group, int32_t n_out,
+                       const float *totals, const int32_t *ended, int32_t end_token, int32_t places,
+                       float *totals_out, int32_t *source, int32_t *token_ids, float *entropy, int32_t *ended_out,
+                       void *ws, void *cuda_stream);
+
+/*
+ * Streams that go on from other streams of their group, in place (the survivors of a beam search; a
+ * prompt handed to all of its beams; the winner handed back).  For every stream s with source[s] other
+ * than s and -1, all sources being read before any is overwritten:
+ *     K, V [s][p][j] <- [source[s]][p][j]   for all planes p,  shared_len[g] <= j < live_len[source[s]]
+ *     scores[s][j], serial[s][j] <- those of source[s]         for the same slots j
+ *     live_len[s] <- live_len[source[s]]
+ * Everything else stays as it was.  Results do not depend on the timing of the GPU.
+ *   group       divides n_streams, at most SIRLLM_MAX_GROUP (else SIRLLM_ERR_TOO_LARGE)
+ *   source      int32 [n_streams], streams of the same group, or -1.  One outside the group raises
+ *               SIRLLM_STATUS_BAD_SOURCE and leaves its stream as it was
+ *   shared_len  int32 [n_streams / group] or NULL (0): slots that need no copy, being the same in all streams
+ *               of the group or read from the first one (sirllm_attend_shared)
+ *   scores, serial, k, v   each may be NULL: then it is not moved
+ * A source's length or a shared_len outside [0, capacity] raises SIRLLM_STATUS_OVERFLOW and leaves the
+ * stream, or the group, as it was.  SIRLLM_STATUS_TIMEOUT (a device-side wait gave up) leaves the
+ * streams that were to change undefined.
+ */
+int sirllm_reorder_streams(const sirllm_config *cfg, int32_t group, const int32_t *source, const int32_t *shared_len,
+                           float *scores, int64_t *serial, int32_t *live_len, void *k, void *v, void *ws,
+                           void *cuda_stream);
 
 /*
  * The producer of sirllm_score_pairs' input: the LM head's product, reduced tile by tile as it is

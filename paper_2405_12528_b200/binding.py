@@ -19,9 +19,10 @@ _LIB_PATH = os.path.join(_HERE, "libsirllm.so")
 
 F32, BF16, F16 = 0, 1, 2
 OK, ERR_NULL, ERR_BAD_CONFIG, ERR_ALIGN, ERR_CUDA, ERR_TOO_LARGE = 0, -1, -2, -3, -4, -5
-STATUS_TOKEN_RANGE, STATUS_OVERFLOW, STATUS_TIMEOUT, STATUS_BAD_KEEP = 1, 2, 4, 8
+STATUS_TOKEN_RANGE, STATUS_OVERFLOW, STATUS_TIMEOUT, STATUS_BAD_KEEP, STATUS_BAD_SOURCE = 1, 2, 4, 8, 16
 MAX_CAPACITY = 49152
 MAX_ATTEND_HEAD_DIM = 256
+MAX_BEAMS, MAX_GROUP = 64, 256
 POLICY_STREAM, POLICY_RANDOM, POLICY_INTERVAL = 1, 2, 3
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 
@@ -29,6 +30,8 @@ EXPORTS = ["sirllm_workspace_bytes", "sirllm_workspace_init", "sirllm_score", "s
            "sirllm_score_partial",
            "sirllm_score_pairs", "sirllm_step_pairs", "sirllm_decay_select", "sirllm_keep_policy", "sirllm_rerotate_keys",
            "sirllm_append_kv", "sirllm_attend_workspace_bytes", "sirllm_attend_workspace_init", "sirllm_attend",
+           "sirllm_attend_shared_workspace_bytes", "sirllm_attend_shared_workspace_init", "sirllm_attend_shared",
+           "sirllm_beam_workspace_bytes", "sirllm_beam_workspace_init", "sirllm_beam_select", "sirllm_reorder_streams",
            "sirllm_head_tiles", "sirllm_head_pairs",
            "sirllm_compact_kv", "sirllm_step", "sirllm_step_phases", "sirllm_step_host",
            "sirllm_selftest_bounded_wait", "sirllm_status", "sirllm_strerror",
@@ -125,6 +128,20 @@ def lib():
         L.sirllm_attend_workspace_init.argtypes = [cfgp, vp, vp]
         L.sirllm_attend.restype = ctypes.c_int
         L.sirllm_attend.argtypes = [cfgp, i32, vp, i32, i64, vp, vp, vp, f32, vp, i64, vp, vp, vp]
+        L.sirllm_attend_shared_workspace_bytes.restype = ctypes.c_size_t
+        L.sirllm_attend_shared_workspace_bytes.argtypes = [cfgp, i32, i32]
+        L.sirllm_attend_shared_workspace_init.restype = ctypes.c_int
+        L.sirllm_attend_shared_workspace_init.argtypes = [cfgp, i32, i32, vp, vp]
+        L.sirllm_attend_shared.restype = ctypes.c_int
+        L.sirllm_attend_shared.argtypes = [cfgp, i32, i32, vp, vp, i32, i64, vp, vp, vp, f32, vp, i64, vp, vp, vp]
+        L.sirllm_beam_workspace_bytes.restype = ctypes.c_size_t
+        L.sirllm_beam_workspace_bytes.argtypes = [cfgp]
+        L.sirllm_beam_workspace_init.restype = ctypes.c_int
+        L.sirllm_beam_workspace_init.argtypes = [cfgp, vp, vp]
+        L.sirllm_beam_select.restype = ctypes.c_int
+        L.sirllm_beam_select.argtypes = [cfgp, vp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.sirllm_reorder_streams.restype = ctypes.c_int
+        L.sirllm_reorder_streams.argtypes = [cfgp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.sirllm_head_tiles.restype = i32
         L.sirllm_head_tiles.argtypes = [cfgp, i64]
         L.sirllm_head_pairs.restype = ctypes.c_int
@@ -317,9 +334,9 @@ class _LogitsArg(_Arg):
     """A logits matrix [>= rows, vocab] whose rows are logits_row_stride elements apart
     (a column slice of a wider buffer is fine: only the last dimension must be dense)."""
 
-    def __init__(self, cfg, t, name="logits", host=False):
+    def __init__(self, cfg, t, name="logits", host=False, rows=None):
         super().__init__(t, None, name, 0, host)
-        self.cfg = cfg
+        self.cfg, self.rows = cfg, _rows(cfg) if rows is None else rows
 
     def check_shape(self):
         cfg, t = self.cfg, self.t
@@ -327,7 +344,7 @@ class _LogitsArg(_Arg):
             return
         if _DTYPE_CODE.get(t.dtype) != cfg.logits_dtype:
             raise SirllmError(ERR_BAD_CONFIG, f"{self.name} dtype {t.dtype} does not match the config")
-        rows = _rows(cfg)
+        rows = self.rows
         if t.dim() != 2 or t.shape[1] != cfg.vocab or t.shape[0] < rows:
             raise SirllmError(ERR_BAD_CONFIG, f"{self.name} has shape {tuple(t.shape)}, the "
                                               f"configuration needs [>= {rows}, {cfg.vocab}]")
@@ -605,6 +622,91 @@ def sirllm_attend(cfg: Config, layer: int, q, k, v, kv_len, scale: Optional[floa
     _call(lib().sirllm_attend, cfg, int(layer), qa, qa.heads, qa.row_stride, _kv(cfg, k, "k"), _kv(cfg, v, "v"),
           _dev(kv_len, torch.int32, "kv_len", S), cfg.head_dim ** -0.5 if scale is None else float(scale), oa,
           oa.row_stride, _dev(lse, torch.float32, "lse", S * qa.heads), _attend_ws(cfg, ws), _stream())
+
+
+def _groups(cfg: Config, group: int) -> int:
+    if int(group) < 1 or cfg.n_streams % int(group) != 0:
+        raise SirllmError(ERR_BAD_CONFIG, f"{cfg.n_streams} streams do not divide into groups of {group}")
+    return cfg.n_streams // int(group)
+
+
+def sirllm_attend_shared_workspace_bytes(cfg: Config, group: int, n_heads: int) -> int:
+    return lib().sirllm_attend_shared_workspace_bytes(ctypes.byref(cfg), int(group), int(n_heads))
+
+
+def new_attend_shared_workspace(cfg: Config, group: int, n_heads: int, device="cuda") -> torch.Tensor:
+    """Allocates (with torch) and initialises a workspace for :func:`sirllm_attend_shared`."""
+    n = sirllm_attend_shared_workspace_bytes(cfg, group, n_heads)
+    if n == 0:
+        raise SirllmError(ERR_BAD_CONFIG, "invalid configuration")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    sirllm_attend_shared_workspace_init(cfg, group, n_heads, ws)
+    return ws
+
+
+def sirllm_attend_shared_workspace_init(cfg: Config, group: int, n_heads: int, ws: torch.Tensor) -> None:
+    _call(lib().sirllm_attend_shared_workspace_init, cfg, int(group), int(n_heads),
+          _dev(ws, torch.uint8, "ws", sirllm_attend_shared_workspace_bytes(cfg, group, n_heads)), _stream())
+
+
+def sirllm_attend_shared(cfg: Config, layer: int, group: int, shared_len, q, k, v, kv_len, scale: Optional[float], out,
+                         lse, ws) -> None:
+    """:func:`sirllm_attend` for groups of ``group`` consecutive streams whose first ``shared_len[g]`` slots
+    are held once, in the planes of the group's first stream.  ``ws`` from :func:`new_attend_shared_workspace`."""
+    S, groups = cfg.n_streams, _groups(cfg, group)
+    qa = _HeadsArg(cfg, q, "q", S)
+    qa.check_shape()
+    oa = _HeadsArg(cfg, out, "out", S, qa.heads if q is not None else None)
+    oa.check_shape()
+    _call(lib().sirllm_attend_shared, cfg, int(layer), int(group), _dev(shared_len, torch.int32, "shared_len", groups), qa,
+          qa.heads, qa.row_stride, _kv(cfg, k, "k"), _kv(cfg, v, "v"), _dev(kv_len, torch.int32, "kv_len", S),
+          cfg.head_dim ** -0.5 if scale is None else float(scale), oa, oa.row_stride,
+          _dev(lse, torch.float32, "lse", S * qa.heads),
+          _dev(ws, torch.uint8, "ws", sirllm_attend_shared_workspace_bytes(cfg, group, qa.heads)), _stream())
+
+
+def sirllm_beam_workspace_bytes(cfg: Config) -> int:
+    return lib().sirllm_beam_workspace_bytes(ctypes.byref(cfg))
+
+
+def new_beam_workspace(cfg: Config, device="cuda") -> torch.Tensor:
+    """Allocates (with torch) and initialises a workspace for :func:`sirllm_beam_select`."""
+    n = sirllm_beam_workspace_bytes(cfg)
+    if n == 0:
+        raise SirllmError(ERR_BAD_CONFIG, "invalid configuration")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    sirllm_beam_workspace_init(cfg, ws)
+    return ws
+
+
+def sirllm_beam_workspace_init(cfg: Config, ws: torch.Tensor) -> None:
+    _call(lib().sirllm_beam_workspace_init, cfg, _dev(ws, torch.uint8, "ws", sirllm_beam_workspace_bytes(cfg)), _stream())
+
+
+def sirllm_beam_select(cfg: Config, logits, group: int, n_out: int, totals, ended, end_token: int, places: bool,
+                       totals_out, source, token_ids, entropy, ended_out, ws) -> None:
+    """The ``n_out`` best continuations of every group of ``group`` beams (one beam per stream): ``logits``
+    ``[n_streams, vocab]``, ``totals`` fp32 and ``ended`` int32 (or None) ``[n_streams]``; outputs
+    ``[n_streams / group * n_out]``, ``entropy`` and ``ended_out`` may be None.  ``ws`` from
+    :func:`new_beam_workspace`."""
+    S, n = cfg.n_streams, _groups(cfg, group) * max(int(n_out), 0)
+    _call(lib().sirllm_beam_select, cfg, _LogitsArg(cfg, logits, rows=S), int(group), int(n_out),
+          _dev(totals, torch.float32, "totals", S), _dev(ended, torch.int32, "ended", S), int(end_token),
+          int(bool(places)), _dev(totals_out, torch.float32, "totals_out", n), _dev(source, torch.int32, "source", n),
+          _dev(token_ids, torch.int32, "token_ids", n), _dev(entropy, torch.float32, "entropy", n),
+          _dev(ended_out, torch.int32, "ended_out", n),
+          _dev(ws, torch.uint8, "ws", sirllm_beam_workspace_bytes(cfg)), _stream())
+
+
+def sirllm_reorder_streams(cfg: Config, group: int, source, shared_len, scores, serial, live_len, k, v, ws) -> None:
+    """Stream ``s`` goes on from stream ``source[s]`` of its group (-1: it stays): K/V rows, scores, tags and
+    length, in place, from slot ``shared_len[g]`` (None: 0) on."""
+    S, groups = cfg.n_streams, _groups(cfg, group)
+    per_slot = S * cfg.capacity
+    _call(lib().sirllm_reorder_streams, cfg, int(group), _dev(source, torch.int32, "source", S),
+          _dev(shared_len, torch.int32, "shared_len", groups), _dev(scores, torch.float32, "scores", per_slot),
+          _dev(serial, torch.int64, "serial", per_slot), _dev(live_len, torch.int32, "live_len", S),
+          _kv(cfg, k, "k"), _kv(cfg, v, "v"), _ws(cfg, ws), _stream())
 
 
 class _MatrixArg(_Arg):

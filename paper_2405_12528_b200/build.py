@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsirllm.so")
 SOURCES = ["api.cu", "score.cu", "select.cu", "compact.cu", "policy.cu", "rope.cu", "append.cu",
-           "attend.cu", "head.cu"]
+           "attend.cu", "head.cu", "beam.cu", "reorder.cu"]
 
 
 def _stale() -> bool:
@@ -26,7 +26,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "--fmad=true", "-I", os.path.join(ROOT, "include"),
+           "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "--fmad=true", "-I", os.path.join(ROOT, "include"),
            "-I", CSRC, "-o", LIB]
     if verbose:
         cmd += ["-Xptxas", "-v"]

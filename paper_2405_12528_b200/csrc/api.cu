@@ -105,6 +105,8 @@ WorkspaceLayout workspace_layout(const sirllm_config& c) {
     off = align_up(off + (size_t)c.n_streams * 4, 256);
     L.partials_off = off;
     off = align_up(off + (size_t)c.n_streams * c.max_new * L.n_part * sizeof(float2), 256);
+    L.reorder_tickets_off = off;
+    off = align_up(off + (size_t)c.n_streams * 4, 256);
     L.total = off;
     return L;
 }
@@ -117,6 +119,29 @@ AttendLayout attend_layout(const sirllm_config& c) {
     L.zeroed = L.part_ml_off;
     L.part_o_off = align_up(L.part_ml_off + parts * sizeof(float2), 256);
     L.total = align_up(L.part_o_off + parts * c.head_dim * sizeof(float), 256);
+    return L;
+}
+
+// Chunks of 32 KB of a row, or of 16, 8, 4 KB where that leaves fewer than two for every SM.
+static BeamTiling beam_tiling(const sirllm_config& c) {
+    const int64_t per = 16 / logits_elem_bytes(c.logits_dtype);
+    BeamTiling t;
+    for (t.vecs = 8;; t.vecs /= 2) {
+        const int64_t chunk = (int64_t)t.vecs * kBeamThreads * per;
+        t.parts = (c.vocab + per - 1 + chunk - 1) / chunk;  // a row may begin anywhere within a vector
+        if (t.vecs == 1 || t.parts * c.n_streams >= 296) return t;
+    }
+}
+
+static BeamLayout beam_layout(const sirllm_config& c) {
+    BeamLayout L;
+    L.tiling = beam_tiling(c);
+    const size_t chunks = (size_t)c.n_streams * L.tiling.parts;
+    L.tickets_off = 256;
+    L.pairs_off = align_up(L.tickets_off + (size_t)c.n_streams * 4, 256);
+    L.zeroed = L.pairs_off;
+    L.cands_off = align_up(L.pairs_off + chunks * sizeof(float2), 256);
+    L.total = align_up(L.cands_off + chunks * kBeamMaxOut * 8, 256);
     return L;
 }
 
@@ -708,13 +733,15 @@ int sirllm_attend_workspace_init(const sirllm_config* cfg, void* ws, void* cuda_
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "cudaMemsetAsync");
 }
 
-int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_t n_heads, int64_t q_row_stride,
-                  const void* k, const void* v, const int32_t* kv_len, float scale, void* out,
-                  int64_t out_row_stride, float* lse, void* ws, void* cuda_stream) {
+// `shared_len`: null in calls of sirllm_attend
+static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, const int32_t* shared_len, const void* q,
+                       int32_t n_heads, int64_t q_row_stride, const void* k, const void* v, const int32_t* kv_len,
+                       float scale, void* out, int64_t out_row_stride, float* lse, void* ws, void* cuda_stream) {
     int rc = validate_config(cfg);
     if (rc != SIRLLM_OK) return rc;
     if (!q || !k || !v || !kv_len || !out || !ws) return SIRLLM_ERR_NULL;
     const int64_t width = (int64_t)n_heads * cfg->head_dim;
+    if (group < 1 || cfg->n_streams % group != 0) return SIRLLM_ERR_BAD_CONFIG;
     if (layer < 0 || layer >= cfg->n_layers || n_heads < 1 || n_heads % cfg->n_kv_heads != 0 || width > 0x7FFFFFFF ||
         !std::isfinite(scale * kLog2e) || q_row_stride < width || out_row_stride < width)
         return SIRLLM_ERR_BAD_CONFIG;
@@ -723,7 +750,7 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
     for (const void* x : vectors)
         if (misaligned(x, 16)) return SIRLLM_ERR_ALIGN;
     if (q_row_stride % 8 != 0 || out_row_stride % 8 != 0 || misaligned(kv_len, 4) || misaligned(lse, 4) ||
-        misaligned(ws, 256))
+        misaligned(shared_len, 4) || misaligned(ws, 256))
         return SIRLLM_ERR_ALIGN;
     const AttendLayout L = attend_layout(*cfg);
     AttendParams p;
@@ -757,8 +784,136 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
     p.planes_per_stream = cfg->n_layers * cfg->n_kv_heads;
     p.layer_plane = layer * cfg->n_kv_heads;
     p.part_heads = kAttendPartHeads;
+    p.shared_len = shared_len;
+    p.stream_group = group;
     cudaError_t e = launch_attend(p, cfg->kv_dtype == SIRLLM_BF16, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "attend");
+}
+
+int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_t n_heads, int64_t q_row_stride,
+                  const void* k, const void* v, const int32_t* kv_len, float scale, void* out,
+                  int64_t out_row_stride, float* lse, void* ws, void* cuda_stream) {
+    return attend_impl(cfg, layer, 1, nullptr, q, n_heads, q_row_stride, k, v, kv_len, scale, out, out_row_stride, lse, ws,
+                       cuda_stream);
+}
+
+size_t sirllm_attend_shared_workspace_bytes(const sirllm_config* cfg, int32_t group, int32_t n_heads) {
+    if (group < 1 || n_heads < 1 || validate_config(cfg) != SIRLLM_OK || cfg->n_streams % group != 0 ||
+        n_heads % cfg->n_kv_heads != 0)
+        return 0;
+    return sirllm_attend_workspace_bytes(cfg);
+}
+
+int sirllm_attend_shared_workspace_init(const sirllm_config* cfg, int32_t group, int32_t n_heads, void* ws,
+                                        void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (ws == nullptr) return SIRLLM_ERR_NULL;
+    if (group < 1 || cfg->n_streams % group != 0 || n_heads < 1 || n_heads % cfg->n_kv_heads != 0)
+        return SIRLLM_ERR_BAD_CONFIG;
+    return sirllm_attend_workspace_init(cfg, ws, cuda_stream);
+}
+
+int sirllm_attend_shared(const sirllm_config* cfg, int32_t layer, int32_t group, const int32_t* shared_len,
+                         const void* q, int32_t n_heads, int64_t q_row_stride, const void* k, const void* v,
+                         const int32_t* kv_len, float scale, void* out, int64_t out_row_stride, float* lse, void* ws,
+                         void* cuda_stream) {
+    if (cfg != nullptr && shared_len == nullptr) return SIRLLM_ERR_NULL;
+    return attend_impl(cfg, layer, group, shared_len, q, n_heads, q_row_stride, k, v, kv_len, scale, out, out_row_stride,
+                       lse, ws, cuda_stream);
+}
+
+size_t sirllm_beam_workspace_bytes(const sirllm_config* cfg) {
+    if (validate_config(cfg) != SIRLLM_OK) return 0;
+    return beam_layout(*cfg).total;
+}
+
+int sirllm_beam_workspace_init(const sirllm_config* cfg, void* ws, void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (ws == nullptr) return SIRLLM_ERR_NULL;
+    if (misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
+    // the candidates are written before they are read; status word and tickets must start at zero
+    cudaError_t e = cudaMemsetAsync(ws, 0, beam_layout(*cfg).zeroed, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "cudaMemsetAsync");
+}
+
+int sirllm_beam_select(const sirllm_config* cfg, const void* logits, int32_t group, int32_t n_out,
+                       const float* totals, const int32_t* ended, int32_t end_token, int32_t places,
+                       float* totals_out, int32_t* source, int32_t* token_ids, float* entropy, int32_t* ended_out,
+                       void* ws, void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (!logits || !totals || !totals_out || !source || !token_ids || !ws) return SIRLLM_ERR_NULL;
+    if (group < 1 || cfg->n_streams % group != 0 || n_out < 1 || (places && n_out != group) || end_token < -1 ||
+        end_token >= cfg->vocab)
+        return SIRLLM_ERR_BAD_CONFIG;
+    if (group > SIRLLM_MAX_BEAMS || n_out > SIRLLM_MAX_BEAMS) return SIRLLM_ERR_TOO_LARGE;
+    if (n_out != group && (totals_out == totals || (ended && ended_out == ended))) return SIRLLM_ERR_BAD_CONFIG;
+    const BeamLayout L = beam_layout(*cfg);
+    if (L.tiling.parts * cfg->n_streams > 0x7FFFFFFF || (int64_t)L.tiling.parts * group * n_out > 0x7FFFFFFF)
+        return SIRLLM_ERR_TOO_LARGE;
+    if ((rc = check_logits(*cfg, logits)) != SIRLLM_OK) return rc;
+    const void* words[7] = {totals, ended, totals_out, source, token_ids, entropy, ended_out};
+    for (const void* x : words)
+        if (misaligned(x, 4)) return SIRLLM_ERR_ALIGN;
+    if (misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
+    BeamParams p;
+    memset(&p, 0, sizeof p);
+    p.logits = logits;
+    p.totals = totals;
+    p.ended = ended;
+    p.totals_out = totals_out;
+    p.source = source;
+    p.token_ids = token_ids;
+    p.entropy = entropy;
+    p.ended_out = ended_out;
+    p.tickets = (int32_t*)((char*)ws + L.tickets_off);
+    p.pairs = (float2*)((char*)ws + L.pairs_off);
+    p.cands = (unsigned long long*)((char*)ws + L.cands_off);
+    p.vocab = cfg->vocab;
+    p.row_stride = cfg->logits_row_stride;
+    p.n_streams = cfg->n_streams;
+    p.group = group;
+    p.n_out = n_out;
+    p.end_token = end_token;
+    p.places = places != 0;
+    p.parts = (int32_t)L.tiling.parts;
+    p.vecs = L.tiling.vecs;
+    p.logits_dtype = cfg->logits_dtype;
+    cudaError_t e = launch_beam(p, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "beam_select");
+}
+
+int sirllm_reorder_streams(const sirllm_config* cfg, int32_t group, const int32_t* source, const int32_t* shared_len,
+                           float* scores, int64_t* serial, int32_t* live_len, void* k, void* v, void* ws,
+                           void* cuda_stream) {
+    int rc = validate_config(cfg);
+    if (rc != SIRLLM_OK) return rc;
+    if (!source || !live_len || !ws) return SIRLLM_ERR_NULL;
+    if (group < 1 || cfg->n_streams % group != 0) return SIRLLM_ERR_BAD_CONFIG;
+    if (group > SIRLLM_MAX_GROUP) return SIRLLM_ERR_TOO_LARGE;
+    if (misaligned(k, 16) || misaligned(v, 16) || misaligned(source, 4) || misaligned(shared_len, 4) ||
+        misaligned(live_len, 4) || misaligned(scores, 4) || misaligned(serial, 8) || misaligned(ws, 256))
+        return SIRLLM_ERR_ALIGN;
+    ReorderParams p;
+    memset(&p, 0, sizeof p);
+    p.source = source;
+    p.shared_len = shared_len;
+    p.live_len = live_len;
+    p.scores = scores;
+    p.serial = serial;
+    p.k = (char*)k;
+    p.v = (char*)v;
+    p.status = (int32_t*)ws;
+    p.tickets = (int32_t*)((char*)ws + workspace_layout(*cfg).reorder_tickets_off);
+    p.n_streams = cfg->n_streams;
+    p.group = group;
+    p.capacity = cfg->capacity;
+    p.row_bytes = cfg->head_dim * 2;
+    p.planes = cfg->n_layers * cfg->n_kv_heads;
+    cudaError_t e = launch_reorder(p, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "reorder_streams");
 }
 
 int32_t sirllm_head_tiles(const sirllm_config* cfg, int64_t n_cols) {

@@ -150,8 +150,22 @@ __device__ __forceinline__ int live_slots(const AttendParams& p, int s) {
     return n < 0 || n > p.capacity ? 0 : n;
 }
 
+// Where streams share slots: whether the group's count of them can be used, and the slots of a stream
+// that are read here (all of them).
+template <bool kShared>
+__device__ __forceinline__ bool group_ok(const AttendParams& p, int s) {
+    if (!kShared) return true;
+    const int n = p.shared_len[s / p.stream_group];
+    return n >= 0 && n <= p.capacity;
+}
+template <bool kShared>
+__device__ __forceinline__ int unit_slots(const AttendParams& p, int s) {
+    return group_ok<kShared>(p, s) ? live_slots(p, s) : 0;
+}
+
 // A CTA's way through the work, segment by segment.  Two ways: along its stretch of the line of
 // tiles, or (whole_units) from unit to unit, `step` units apart.
+template <bool kShared>
 struct Walk {
     int left;       // positions of the stretch from this segment's first on; whole units: 1 until the end
     int unit0;      // line position of the unit's first tile; whole units: the unit's number
@@ -159,7 +173,18 @@ struct Walk {
     int len;        // live slots of the stream
     int t0, t1;     // this segment's tiles of the unit
     int step;       // 0: along the line
+    int shared;     // kShared: slots below this one are those of the stream `lead`
+    int lead;
 
+    // the stream s: its slots, and where they are
+    __device__ __forceinline__ void look_up(const AttendParams& p) {
+        len = unit_slots<kShared>(p, s);
+        if (kShared) {
+            const int g = s / p.stream_group;
+            lead = g * p.stream_group;
+            shared = p.shared_len[g];
+        }
+    }
     __device__ __forceinline__ bool more() const { return left > 0; }
     __device__ __forceinline__ int tiles() const { return (len + kKeys - 1) / kKeys; }
     __device__ __forceinline__ void set_end() {
@@ -173,7 +198,7 @@ struct Walk {
         for (; unit0 < n_units; unit0 += step) {
             s = unit0 / p.units;
             unit = unit0 - s * p.units;
-            len = live_slots(p, s);
+            look_up(p);
             if (len > 0) {
                 left = 1;
                 break;
@@ -200,7 +225,7 @@ struct Walk {
                     left = 0;
                     return;
                 }
-                len = live_slots(p, s);
+                look_up(p);
             }
         }
         set_end();
@@ -209,7 +234,8 @@ struct Walk {
 
 // kDim: head_dim rounded up to 64, 128 or 256 (the columns behind head_dim are zeros in shared
 // memory); kTiles: blocks of 8 query heads that a unit carries.
-template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages>
+// kShared: the streams of a group share their first slots, which are read from the group's first stream.
+template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, bool kShared>
 __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendParams p) {
     constexpr int kThreads = kWarps * 32;
     constexpr int kChunks = kDim / 8;               // 16-byte vectors of a row
@@ -222,7 +248,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     float* merge = cta_o + kHeads * kDim;  // [warp][kPass][kDim]
     __shared__ int scan[kWarps];
     __shared__ int longest[kWarps], counted[kWarps], gap_all;
-    __shared__ Walk first;
+    __shared__ Walk<kShared> first;
     __shared__ float stat_m[kWarps][kHeads], stat_l[kWarps][kHeads];
     __shared__ float part_w[kHeads];
     __shared__ __align__(8) float2 cta_ml[kHeads];
@@ -239,7 +265,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     const int gap = min((int)(kUnitBytes / tile_bytes), kAttendUnitTiles);
     int mine = 0, live = 0, long_unit = 0;
     for (int s = s_lo; s < s_hi; ++s) {
-        const int T = (live_slots(p, s) + kKeys - 1) / kKeys;
+        const int T = (unit_slots<kShared>(p, s) + kKeys - 1) / kKeys;
         if (T == 0) continue;
         mine += (T + gap) * p.units;
         ++live;
@@ -338,7 +364,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         int at = before;
         int s = s_lo, len = 0, T = 0;
         for (; s < s_hi; ++s) {
-            len = live_slots(p, s);
+            len = unit_slots<kShared>(p, s);
             T = len > 0 ? (len + kKeys - 1) / kKeys + gap : 0;  // a unit's positions
             if (r0 < at + T * p.units) break;
             at += T * p.units;
@@ -347,7 +373,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         first.left = s < s_hi ? r1 - r0 : 0;
         if (s < s_hi) {
             first.s = s;
-            first.len = len;
+            first.look_up(p);
             first.unit = (r0 - at) / T;
             first.unit0 = at + first.unit * T;
             first.t0 = r0 - first.unit0;
@@ -359,7 +385,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     // outside the planes is reported and its rows are left alone
     for (int s = blockIdx.x; s < p.n_streams; s += gridDim.x) {
         const int n = p.kv_len[s];
-        if (n < 0 || n > p.capacity) {
+        if (n < 0 || n > p.capacity || !group_ok<kShared>(p, s)) {
             if (tid == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
         } else if (n == 0) {
             // (a row of up to 2^31 - 1 elements: the index of the step behind it does not fit an int)
@@ -375,13 +401,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 
     // ---- the warp's ring ------------------------------------------------------------------
     const uint32_t ring0 = smem_u32(ring) + warp * kStages * 2 * kTileBytes;
-    Walk start = first;
+    Walk<kShared> start = first;
     if (solo) {
         start.step = gridDim.x * kWarps;
         start.unit0 = warp * gridDim.x + blockIdx.x;  // over the SMs first
         start.find_unit(p);
     }
-    Walk ahead = start;                 // what the loads have reached
+    Walk<kShared> ahead = start;                 // what the loads have reached
     int ahead_tile = ahead.t0 + lead;
     constexpr int kRowsAtOnce = 32 / kChunks;  // rows that one load instruction of the warp covers
     const int chunk = lane % kChunks, row_in = lane / kChunks;
@@ -396,12 +422,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             const int64_t plane = (int64_t)ahead.s * p.planes_per_stream + p.layer_plane + g;
             const int key0 = ahead_tile * kKeys;
             const int64_t off = ((plane * p.capacity + key0) * p.head_dim + (chunk_on ? chunk * 8 : 0)) * 2;
+            // from this stream's planes to those of the stream that holds the shared slots
+            const int64_t to_lead = kShared ? (int64_t)(ahead.lead - ahead.s) * p.planes_per_stream * p.capacity *
+                                                  p.head_dim * 2
+                                            : 0;
             const uint32_t dst0 = ring0 + stage * 2 * kTileBytes;
 #pragma unroll
             for (int i = 0; i < kKeys / kRowsAtOnce; ++i) {
                 const int r = i * kRowsAtOnce + row_in;
                 const bool valid = chunk_on && key0 + r < ahead.len;
-                const int64_t o = valid ? off + (int64_t)r * p.head_dim * 2 : off;
+                int64_t o = valid ? off + (int64_t)r * p.head_dim * 2 : off;
+                if (kShared && key0 + r < ahead.shared) o += to_lead;
                 const uint32_t d = dst0 + r * (kDim * 2) + ((chunk ^ (r & 7)) << 4);
                 cp_async16(d, p.k + o, valid);
                 cp_async16(d + kTileBytes, p.v + o, valid);
@@ -416,7 +447,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 
     // ---- the units ------------------------------------------------------------------------
     const int hc = 2 * (lane & 3);  // this lane's two heads within a block of 8
-    for (Walk w = start; w.more(); w.next(p, gap_all)) {
+    for (Walk<kShared> w = start; w.more(); w.next(p, gap_all)) {
         const int g = w.unit / p.blocks, block = w.unit - g * p.blocks;
         const int head0 = g * p.group + block * kHeads;            // first query head of the unit
         const int heads = min(kHeads, p.group - block * kHeads);   // query heads it really has
@@ -792,10 +823,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     cp_wait<0>();
 }
 
-template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages>
+template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, bool kShared>
 cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
     static unsigned char allowed[kMaxDevices];
-    auto kernel = attend_kernel<kBf16, kDim, kTiles, kWarps, kStages>;
+    auto kernel = attend_kernel<kBf16, kDim, kTiles, kWarps, kStages, kShared>;
     cudaError_t e = allow_max_dynamic_smem((const void*)kernel, dp, allowed);
     if (e != cudaSuccess) return e;
     // the ring, a CTA's sums, and a buffer that takes [warp][4 heads][kDim] sums or [part][head] weights
@@ -862,24 +893,25 @@ cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st
     return cudaLaunchKernelEx(&cfg, kernel, q);
 }
 
-template <bool kBf16>
+template <bool kBf16, bool kShared>
 cudaError_t launch_dim(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
     const bool wide = attend_unit_heads(p.group, p.head_dim) == 16;
     if (p.head_dim <= 64)
-        return wide ? launch<kBf16, 64, 2, 8, 6>(p, dp, st) : launch<kBf16, 64, 1, 8, 6>(p, dp, st);
+        return wide ? launch<kBf16, 64, 2, 8, 6, kShared>(p, dp, st) : launch<kBf16, 64, 1, 8, 6, kShared>(p, dp, st);
     if (p.head_dim <= 128)
-        return wide ? launch<kBf16, 128, 2, 8, 3>(p, dp, st) : launch<kBf16, 128, 1, 8, 3>(p, dp, st);
-    return launch<kBf16, 256, 1, 4, 3>(p, dp, st);
+        return wide ? launch<kBf16, 128, 2, 8, 3, kShared>(p, dp, st) : launch<kBf16, 128, 1, 8, 3, kShared>(p, dp, st);
+    return launch<kBf16, 256, 1, 4, 3, kShared>(p, dp, st);
 }
 
 }  // namespace
 
 cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st) {
-    TraceRange trace("sirllm:attend");
+    TraceRange trace(p.shared_len != nullptr ? "sirllm:attend_shared" : "sirllm:attend");
     DeviceProps dp;
     cudaError_t e = device_props(&dp);
     if (e != cudaSuccess) return e;
-    return bf16 ? launch_dim<true>(p, dp, st) : launch_dim<false>(p, dp, st);
+    if (p.shared_len != nullptr) return bf16 ? launch_dim<true, true>(p, dp, st) : launch_dim<false, true>(p, dp, st);
+    return bf16 ? launch_dim<true, false>(p, dp, st) : launch_dim<false, false>(p, dp, st);
 }
 
 }  // namespace sirllm

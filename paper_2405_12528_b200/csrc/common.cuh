@@ -21,6 +21,7 @@ namespace sirllm {
 //   policy_ranks[n_streams][capacity]     synthetic scores of the comparison policies, ones[n_streams]
 //   tickets[n_streams*max_new]            arrivals per logits row (the last CTA finishes the row)
 //   partials[n_streams*max_new][n_part]   (scaled max, sum) pair per CTA of a multi-CTA row
+//   reorder_tickets[n_streams]            arrivals per group of streams (the last CTA sets the lengths)
 struct WorkspaceLayout {
     size_t plane_progress_off;
     size_t first_moved_off;
@@ -31,6 +32,7 @@ struct WorkspaceLayout {
     size_t policy_ranks_off;
     size_t policy_ones_off;
     size_t partials_off;
+    size_t reorder_tickets_off;
     size_t total;
     int32_t n_part;  // CTAs (kScoreCtaVecs vectors each) per logits row
 };
@@ -191,6 +193,9 @@ struct AttendParams {
     int32_t group, blocks, units;            // query heads per K/V head; blocks of them; units per stream
     int32_t planes_per_stream, layer_plane;
     int32_t part_heads;
+    // slots shared by the streams of a group (null: none are); set in calls of sirllm_attend_shared only
+    const int32_t* shared_len;
+    int32_t stream_group;
     // set by the launcher
     int32_t cluster, cluster_log2;           // CTAs of a cluster
     AttendDeal alone, together;              // to CTAs, to clusters
@@ -219,6 +224,50 @@ struct HeadTiling {
     int32_t ctas;  // 0: the form for few rows
     int32_t n_parts, part_tiles, tile_cols, part_cols;
     int32_t half_cols;  // columns of a tile that the first of a row's two threads reduces
+};
+
+// ---- selection among beams ---------------------------------------------------------------
+constexpr int kBeamThreads = 256;
+constexpr int kBeamMaxGroup = SIRLLM_MAX_BEAMS;
+constexpr int kBeamMaxOut = SIRLLM_MAX_BEAMS;
+// How the rows are cut: `parts` chunks of vecs * kBeamThreads 16-byte vectors each.
+struct BeamTiling {
+    int32_t vecs;
+    int64_t parts;
+};
+// ---- its workspace ------------------------------------------------------------------------
+//   [0, 256)                      header: int32 status word
+//   tickets[n_streams]            arrivals per group
+//   pairs[n_streams][parts]       (max, sum exp) of a chunk
+//   cands[n_streams][parts][64]   a chunk's best logits, order key << 32 | ~token
+struct BeamLayout {
+    size_t tickets_off, pairs_off, cands_off, zeroed, total;
+    BeamTiling tiling;
+};
+struct BeamParams {
+    const void* logits;
+    const float* totals;
+    const int32_t* ended;            // nullable
+    float* totals_out;
+    int32_t *source, *token_ids;
+    float* entropy;                  // nullable
+    int32_t* ended_out;              // nullable
+    int32_t* tickets;
+    float2* pairs;
+    unsigned long long* cands;
+    int64_t vocab, row_stride;
+    int32_t n_streams, group, n_out, end_token, places, parts, vecs, logits_dtype;
+};
+
+struct ReorderParams {
+    const int32_t *source, *shared_len;  // shared_len nullable
+    int32_t* live_len;
+    float* scores;                   // nullable
+    int64_t* serial;                 // nullable
+    char *k, *v;                     // nullable
+    int32_t *status, *tickets;
+    int32_t n_streams, group, capacity, row_bytes, planes;  // planes of a stream, of one tensor
+    int32_t ctas;                    // per group, set by the launcher
 };
 
 struct CompactParams {
@@ -259,6 +308,8 @@ cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st);
 HeadTiling head_tiling(int64_t rows, int64_t n_cols);
 cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hidden, int64_t hidden_stride,
                         const void* weight, int64_t weight_stride, cudaStream_t st);
+cudaError_t launch_beam(const BeamParams& p, cudaStream_t st);
+cudaError_t launch_reorder(const ReorderParams& p, cudaStream_t st);
 cudaError_t launch_compact_plan(const CompactParams& p, int n_streams, int32_t* first_moved,
                                 cudaStream_t st);
 cudaError_t launch_compact(const CompactParams& p, cudaStream_t st, bool overlap);
