@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsirllm.so")
 SOURCES = ["api.cu", "score.cu", "select.cu", "compact.cu", "policy.cu", "rope.cu", "append.cu",
-           "attend.cu", "head.cu", "beam.cu", "reorder.cu"]
+           "attend.cu", "head.cu", "beam.cu", "reorder.cu", "prefix.cu"]
 
 
 def _stale() -> bool:

@@ -133,6 +133,29 @@ static BeamTiling beam_tiling(const sirllm_config& c) {
     }
 }
 
+// attend's own, then what the shared slots give
+struct AttendSharedLayout {
+    AttendLayout own;
+    PrefixPlan plan;   // no pointers yet
+    bool on;
+    size_t line_off, part_ml_off, part_o_off, total;
+};
+static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t group, int32_t n_heads) {
+    AttendSharedLayout L;
+    L.own = attend_layout(c);
+    L.on = prefix_plan(c, group, n_heads, &L.plan);
+    L.line_off = L.own.total;
+    L.part_ml_off = L.part_o_off = L.total = L.line_off;
+    if (L.on) {
+        const size_t groups = c.n_streams / group;
+        const size_t places = groups * c.n_kv_heads * L.plan.units + kAttendMaxCtas, rows = places * L.plan.rows;
+        L.part_ml_off = align_up(L.line_off + (1 + groups) * 4, 256);
+        L.part_o_off = align_up(L.part_ml_off + rows * sizeof(float2), 256);
+        L.total = align_up(L.part_o_off + rows * c.head_dim * sizeof(float), 256);
+    }
+    return L;
+}
+
 static BeamLayout beam_layout(const sirllm_config& c) {
     BeamLayout L;
     L.tiling = beam_tiling(c);
@@ -786,6 +809,32 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
     p.part_heads = kAttendPartHeads;
     p.shared_len = shared_len;
     p.stream_group = group;
+    if (shared_len != nullptr) {
+        const AttendSharedLayout S = attend_shared_layout(*cfg, group, n_heads);
+        if (S.on) {
+            p.prefix = S.plan;
+            p.prefix.line = (int32_t*)((char*)ws + S.line_off);
+            p.prefix.part_ml = (float2*)((char*)ws + S.part_ml_off);
+            p.prefix.part_o = (float*)((char*)ws + S.part_o_off);
+            PrefixParams x;
+            memset(&x, 0, sizeof x);
+            x.plan = p.prefix;
+            x.shared_len = shared_len;
+            x.status = p.status;
+            x.scale_log2 = p.scale_log2;
+            x.n_groups = cfg->n_streams / group;
+            x.stream_group = group;
+            x.heads = p.group;
+            x.n_kv_heads = cfg->n_kv_heads;
+            x.head_dim = cfg->head_dim;
+            x.capacity = cfg->capacity;
+            x.planes_per_stream = p.planes_per_stream;
+            x.layer_plane = p.layer_plane;
+            x.bf16 = cfg->kv_dtype == SIRLLM_BF16;
+            cudaError_t e = launch_prefix(x, q, q_row_stride, cfg->n_streams, k, v, (cudaStream_t)cuda_stream);
+            if (e != cudaSuccess) return cuda_fail(e, "attend_shared");
+        }
+    }
     cudaError_t e = launch_attend(p, cfg->kv_dtype == SIRLLM_BF16, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "attend");
 }
@@ -799,9 +848,9 @@ int sirllm_attend(const sirllm_config* cfg, int32_t layer, const void* q, int32_
 
 size_t sirllm_attend_shared_workspace_bytes(const sirllm_config* cfg, int32_t group, int32_t n_heads) {
     if (group < 1 || n_heads < 1 || validate_config(cfg) != SIRLLM_OK || cfg->n_streams % group != 0 ||
-        n_heads % cfg->n_kv_heads != 0)
+        n_heads % cfg->n_kv_heads != 0 || cfg->head_dim > SIRLLM_MAX_ATTEND_HEAD_DIM)
         return 0;
-    return sirllm_attend_workspace_bytes(cfg);
+    return attend_shared_layout(*cfg, group, n_heads).total;
 }
 
 int sirllm_attend_shared_workspace_init(const sirllm_config* cfg, int32_t group, int32_t n_heads, void* ws,

@@ -151,16 +151,26 @@ __device__ __forceinline__ int live_slots(const AttendParams& p, int s) {
 }
 
 // Where streams share slots: whether the group's count of them can be used, and the slots of a stream
-// that are read here (all of them).
+// that are read here.
 template <bool kShared>
 __device__ __forceinline__ bool group_ok(const AttendParams& p, int s) {
     if (!kShared) return true;
     const int n = p.shared_len[s / p.stream_group];
     return n >= 0 && n <= p.capacity;
 }
+// The first of the stream's slots that is read here: those in front of it were computed for the whole
+// group, unless the stream ends among them.
+template <bool kShared>
+__device__ __forceinline__ int first_slot(const AttendParams& p, int s, int live) {
+    if (!kShared || p.prefix.part_o == nullptr) return 0;
+    const int n = prefix_slots(p.shared_len[s / p.stream_group]);
+    return live > n ? n : 0;
+}
 template <bool kShared>
 __device__ __forceinline__ int unit_slots(const AttendParams& p, int s) {
-    return group_ok<kShared>(p, s) ? live_slots(p, s) : 0;
+    if (!group_ok<kShared>(p, s)) return 0;
+    const int n = live_slots(p, s);
+    return n - first_slot<kShared>(p, s, n);
 }
 
 // A CTA's way through the work, segment by segment.  Two ways: along its stretch of the line of
@@ -173,8 +183,8 @@ struct Walk {
     int len;        // live slots of the stream
     int t0, t1;     // this segment's tiles of the unit
     int step;       // 0: along the line
-    int shared;     // kShared: slots below this one are those of the stream `lead`
-    int lead;
+    int base;       // kShared: the unit's first slot; slots below `shared` are those of the stream `lead`
+    int shared, lead;
 
     // the stream s: its slots, and where they are
     __device__ __forceinline__ void look_up(const AttendParams& p) {
@@ -183,6 +193,7 @@ struct Walk {
             const int g = s / p.stream_group;
             lead = g * p.stream_group;
             shared = p.shared_len[g];
+            base = first_slot<kShared>(p, s, live_slots(p, s));
         }
     }
     __device__ __forceinline__ bool more() const { return left > 0; }
@@ -421,7 +432,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             const int g = ahead.unit / p.blocks;
             const int64_t plane = (int64_t)ahead.s * p.planes_per_stream + p.layer_plane + g;
             const int key0 = ahead_tile * kKeys;
-            const int64_t off = ((plane * p.capacity + key0) * p.head_dim + (chunk_on ? chunk * 8 : 0)) * 2;
+            const int slot0 = kShared ? ahead.base + key0 : key0;
+            const int64_t off = ((plane * p.capacity + slot0) * p.head_dim + (chunk_on ? chunk * 8 : 0)) * 2;
             // from this stream's planes to those of the stream that holds the shared slots
             const int64_t to_lead = kShared ? (int64_t)(ahead.lead - ahead.s) * p.planes_per_stream * p.capacity *
                                                   p.head_dim * 2
@@ -432,7 +444,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 const int r = i * kRowsAtOnce + row_in;
                 const bool valid = chunk_on && key0 + r < ahead.len;
                 int64_t o = valid ? off + (int64_t)r * p.head_dim * 2 : off;
-                if (kShared && key0 + r < ahead.shared) o += to_lead;
+                if (kShared && slot0 + r < ahead.shared) o += to_lead;
                 const uint32_t d = dst0 + r * (kDim * 2) + ((chunk ^ (r & 7)) << 4);
                 cp_async16(d, p.k + o, valid);
                 cp_async16(d + kTileBytes, p.v + o, valid);
@@ -475,6 +487,41 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 for (int i = 0; i < 4; ++i) o[n][d][i] = 0.f;
             m[n][0] = m[n][1] = kNegHuge;
             l[n][0] = l[n][1] = 0.f;
+        }
+        if (kShared && w.base > 0 && w.t0 == 0) {
+            // ---- what the group's slots in front of the unit's gave, a part at a time per warp -----------
+            const PrefixPlan& x = p.prefix;
+            const int local = w.s - w.lead, in_block = local / x.block_streams;
+            const int u = g * x.units + (x.pair ? in_block >> 1 : 0);             // unit of the group
+            const int tiles = w.base / kPrefixTile, per = x.line[0], group_no = w.s / p.stream_group;
+            const int at = x.line[1 + group_no] + u * tiles;
+            const int64_t unit0 = (int64_t)group_no * (p.units / p.blocks) * x.units + u;
+            const int row = (local - in_block * x.block_streams) * p.group + block * kHeads +
+                            (x.pair ? (in_block & 1) * kPrefixRows : 0);
+            for (int c = at / per + lead; c <= (at + tiles - 1) / per; c += stride) {
+                const int64_t place = (unit0 + c) * x.rows + row;
+                const float2* ml = x.part_ml + place;
+                const float* po = x.part_o + place * p.head_dim;
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int h = n * 8 + hc + i;
+                        const float2 y = h < heads ? __ldcg(&ml[h]) : make_float2(kNegHuge, 0.f);
+                        const float up = fmaxf(m[n][i], y.x);
+                        const float f = ex2_approx(m[n][i] - up), fy = ex2_approx(y.x - up);
+                        m[n][i] = up;
+                        l[n][i] = l[n][i] * f + (lane < 4 ? y.y * fy : 0.f);
+#pragma unroll
+                        for (int d = 0; d < kDim / 16; ++d)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const int e = d * 16 + j * 8 + (lane >> 2);
+                                const float v = h < heads && e < p.head_dim ? __ldcg(&po[h * p.head_dim + e]) : 0.f;
+                                o[n][d][i + 2 * j] = o[n][d][i + 2 * j] * f + v * fy;
+                            }
+                    }
+            }
         }
         for (int tile = w.t0 + lead; tile < w.t1; tile += stride) {
             cp_wait<kStages - 2>();

@@ -178,6 +178,37 @@ struct AttendDeal {
     float units, per_busy;
 };
 
+// ---- slots shared by a group of streams, computed once for all of them ----------------------
+// The streams' query heads that share a K/V head are the rows: row r of a block is head r % heads of its
+// stream r / heads.  A unit is one block of up to 128 rows, or two (pair), of one K/V head of a group;
+// its tiles of 128 slots stand in one line with the other units', cut into equal stretches for the CTAs.
+// The part of unit u (of all groups) that CTA c computes is in place u + c.
+constexpr int kPrefixTile = 128;
+constexpr int kPrefixRows = 128;   // rows of a block, at most
+struct PrefixPlan {
+    float* part_o;            // [place][rows][head_dim], relative to 2^reference; null: not in use
+    float2* part_ml;          // [place][rows] (reference in units of log2, sum)
+    int32_t* line;            // [0]: tiles per CTA; [1 + g]: first tile of group g in the line
+    int32_t block_streams;    // streams of a block
+    int32_t blocks;           // blocks of a group
+    int32_t pair;             // two blocks to a unit
+    int32_t units;            // units of a K/V head of a group
+    int32_t rows;             // rows of a place
+};
+// Slots of a group that go this way: whole tiles, of prefixes of two tiles and more.
+__host__ __device__ inline int prefix_slots(int shared) { return shared >= 2 * kPrefixTile ? shared & ~(kPrefixTile - 1) : 0; }
+
+struct PrefixParams {
+    PrefixPlan plan;
+    const int32_t* shared_len;
+    int32_t* status;
+    float scale_log2;
+    int32_t n_groups, stream_group, heads, n_kv_heads, head_dim, capacity;
+    int32_t planes_per_stream, layer_plane, bf16;
+    // set by the launcher
+    int32_t panels, stages, stage_bytes, q_box_bytes;
+};
+
 struct AttendParams {
     const char *q, *k, *v;
     const int32_t* kv_len;
@@ -196,6 +227,7 @@ struct AttendParams {
     // slots shared by the streams of a group (null: none are); set in calls of sirllm_attend_shared only
     const int32_t* shared_len;
     int32_t stream_group;
+    PrefixPlan prefix;
     // set by the launcher
     int32_t cluster, cluster_log2;           // CTAs of a cluster
     AttendDeal alone, together;              // to CTAs, to clusters
@@ -304,6 +336,11 @@ cudaError_t launch_append(const AppendParams& p, bool bf16, cudaStream_t st);
 // query heads of a unit: 16 where more than 8 share a K/V head, so that K and V are read once for
 // them - unless the head is so wide that two blocks' queries and sums do not fit the registers
 inline int attend_unit_heads(int group, int head_dim) { return group > 8 && head_dim <= 128 ? 16 : 8; }
+// Whether the shared slots of groups of `stream_group` streams with `heads` query heads per K/V head go
+// to the kernel that computes them once for all (else every stream reads them for itself), and how.
+bool prefix_plan(const sirllm_config& c, int32_t stream_group, int32_t n_heads, PrefixPlan* plan);
+cudaError_t launch_prefix(const PrefixParams& p, const void* q, int64_t q_stride, int32_t n_streams, const void* k,
+                          const void* v, cudaStream_t st);
 cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st);
 HeadTiling head_tiling(int64_t rows, int64_t n_cols);
 cudaError_t launch_head(const HeadParams& p, const HeadTiling& t, const void* hidden, int64_t hidden_stride,

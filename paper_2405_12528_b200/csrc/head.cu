@@ -37,11 +37,7 @@
 // 128256 x 4096 in a loop of 400 calls: 1 row 157 us (6.7 TB/s, 1.04 of the copy rate), 64 rows 164 us (0.99;
 // 174 with the board at its power cap), 65 185 us, 100 188 us, 128 201 us, 129 236 us, 256 260 us.
 // 32000 x 4096: 1 row 44.5 us (0.91), 64 46.9, 65 48.6, 100 50.4, 129 58.0, 256 60.1.
-#include <atomic>
-
-#include <cuda.h>
-
-#include "common.cuh"
+#include "tcgen05.cuh"
 
 namespace sirllm {
 
@@ -65,111 +61,8 @@ constexpr int kHeadRowBlocks = 4096; // row blocks per launch (the list of block
 constexpr int kARoom = kHeadRows * kHeadDepth * 2;  // what an instruction reads of A, loaded or not
 constexpr int kHeadRing = 212 * 1024;
 constexpr size_t kHeadSmem = 1024 + kHeadRing;
-constexpr uint32_t kNapNs = 20000, kNapLimit = 1u << 17;  // a wait gives up after seconds
 constexpr float kNoLogit = -2.0e38f;  // below any running maximum; times log2 e it is still finite
 
-template <int kCtas>
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    if (kCtas == 2)  // the barrier may be the pair's other CTA's
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, "
-            "%4}], [%2];" ::"r"(dst),
-            "l"(map), "r"(bar), "r"(x), "r"(y)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::
-                "r"(dst),
-            "l"(map), "r"(bar), "r"(x), "r"(y)
-            : "memory");
-}
-// Polls of a barrier go through shared memory, which the tensor core needs for its operands: a
-// waiting thread sleeps in the poll (up to kNapNs) instead of spinning.
-__device__ __forceinline__ bool mbar_nap(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity), "r"(kNapNs)
-        : "memory");
-    return ok != 0;
-}
-// the address of a shared variable in the pair's first CTA
-__device__ __forceinline__ uint32_t in_first_cta(const void* p) {
-    uint32_t a;
-    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
-    return a;
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// Shared-memory operand of tcgen05.mma, K-major rows of 128 bytes with the 128-byte swizzle: the
-// low word holds the address / 16, the high word says that groups of 8 rows are 1024 bytes apart.
-__device__ __forceinline__ uint32_t operand_lo(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
-constexpr uint32_t kOperandHi = (1024u >> 4) | (1u << 14) | (2u << 29);
-template <int kCtas>
-__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, bool accumulate) {
-    if (kCtas == 2)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-            "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
-            "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
-            "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)accumulate), "r"(kOperandHi)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-            "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
-            "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)accumulate), "r"(kOperandHi)
-            : "memory");
-}
-// signals the barrier (in both CTAs of a pair) once the products issued so far are done
-template <int kCtas>
-__device__ __forceinline__ void mma_commit(uint64_t* bar) {
-    if (kCtas == 2)
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
-                smem_u32(bar)),
-            "h"((uint16_t)3)
-            : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-                     : "memory");
-}
-template <int kCtas>
-__device__ __forceinline__ void tmem_alloc(uint32_t* where) {
-    if (kCtas == 2) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(512u)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(512u)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-}
-template <int kCtas>
-__device__ __forceinline__ void tmem_free(uint32_t tmem) {
-    if (kCtas == 2)
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
-    else
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
-}
-__device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t addr) {
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
 template <int kCtas>
 __device__ __forceinline__ void cta_or_pair_sync() {
     if (kCtas == 2)
@@ -779,25 +672,6 @@ head_few_kernel(const HeadParams p, const __grid_constant__ CUtensorMap map_h, c
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 1) tmem_free<1>(tmem);
     if (tid == 0 && gave_up) atomicOr(p.status, SIRLLM_STATUS_TIMEOUT);
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's encoder, looked up once per process (the library does not link against the driver).
-cudaError_t encoder(EncodeTiled* out) {
-    static std::atomic<void*> known{nullptr};
-    void* fn = known.load(std::memory_order_acquire);
-    if (fn == nullptr) {
-        cudaDriverEntryPointQueryResult found;
-        cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
-        if (e != cudaSuccess) return e;
-        if (found != cudaDriverEntryPointSuccess || fn == nullptr) return cudaErrorNotSupported;
-        known.store(fn, std::memory_order_release);
-    }
-    *out = reinterpret_cast<EncodeTiled>(fn);
-    return cudaSuccess;
 }
 
 // Rows of `width` 16-bit elements, `stride` elements apart, read in boxes of box_rows x 64.

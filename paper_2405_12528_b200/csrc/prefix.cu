@@ -1,0 +1,602 @@
+// Attention of one new token per stream over the slots that a group of streams shares, computed once
+// for the whole group (sirllm_attend_shared): the query heads of all streams of the group that share a
+// K/V head are the rows of one product,
+//     S = Q K^T [rows x slots],   P = 2^(scale log2e S - reference),   O = P V,
+// and every row's (reference, sum of P, O) over a stretch of the slots goes to the workspace, where
+// attend_kernel takes it up as the start of the stream's own slots.
+//
+// Read once for up to 256 rows, K and V cost 4 * rows operations per element: HBM's bound up to about 250
+// rows, the tensor core's beyond.  tcgen05 for both products: 128 rows on the lanes, S and O in tensor
+// memory; P goes back there as the left operand of the second product, V is its right operand as it
+// lies in memory ([slot][element], rows of the product along the columns of V).
+// One persistent CTA per SM takes an equal stretch of the line of all units' tiles (128 slots).  Two lanes of
+// work (S, P, O each) keep the tensor core and the exponentials busy at once: with more than 128 rows
+// they are two blocks of rows over the same tiles, else the even and the odd tiles of one block, whose
+// results are joined at the end of the stretch.  Warp 0 loads (TMA, a ring of K and V tiles), warp 1
+// issues the products, four warps per lane own one row per thread.
+// The reference moves only when a score passes it by more than 2^8 (bf16; fp16: the weights stand 2^11 to
+// 2^15 above the reference, see attend_kernel), so O is rarely rescaled.  Sums, references and O are
+// fp32; P is rounded to 16 bits on its way into the second product.
+// Whole tiles only: what is left of the shared slots (fewer than 128) attend_kernel reads itself, so
+// nothing here is masked and no slot behind the shared ones is read.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "tcgen05.cuh"
+
+namespace sirllm {
+
+namespace {
+
+constexpr int kThreads = 384;       // loads, products, two idle warps, 2 x 4 warps of rows
+constexpr int kRowThreads = 256;
+// registers: 168 a thread at launch (64512 for 384 threads); 128 * 72 + 256 * 216 = 64512
+constexpr int kFeedRegs = 72, kRowRegs = 216;
+static_assert(128 * kFeedRegs + kRowThreads * kRowRegs <= kThreads * 168, "more registers than the launch has");
+constexpr int kMaxStages = 10;
+constexpr int kPanelBytes = 128 * 128;  // 64 elements of 128 rows or slots, 128-byte swizzle
+constexpr int kSmemRoom = 224 * 1024;
+constexpr uint32_t kScoreCol = 0, kOutCol = 256, kLaneCols = 128;  // tensor memory: S (and P) and O of the two lanes
+
+template <bool kBf16>
+constexpr float kSetBelow = kBf16 ? 0.f : 11.f;
+template <bool kBf16>
+constexpr float kMoveAt = kBf16 ? 8.f : 15.f;
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+            dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::
+            "r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+// Right operand with the product's columns contiguous: panels of 64 columns kPanelBytes apart, groups of
+// 8 slots 1024 bytes apart.
+__device__ __forceinline__ uint32_t columns_lo(uint32_t addr) {
+    return ((addr & 0x3FFFFu) >> 4) | ((uint32_t)(kPanelBytes >> 4) << 16);
+}
+// left operand from tensor memory
+__device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b_lo), "r"(idesc), "r"((uint32_t)accumulate), "r"(kOperandHi)
+        : "memory");
+}
+// 32 columns, without waiting
+__device__ __forceinline__ void tmem_ask32(uint32_t (&r)[32], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_give32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    uint32_t out;
+    if (kBf16)
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(out) : "f"(hi), "f"(lo));
+    return out;
+}
+
+__device__ __forceinline__ int group_tiles(const PrefixParams& p, int g) {
+    const int n = p.shared_len[g];
+    return n < 0 || n > p.capacity ? 0 : prefix_slots(n) / kPrefixTile;
+}
+
+// A CTA's way along its stretch of the line, unit by unit.
+struct Stretch {
+    int left;         // tiles of the stretch from here on
+    int g, u;         // group, unit of the group
+    int t0, tiles;    // first tile here, tiles of a unit of this group
+    __device__ __forceinline__ int count() const { return min(left, tiles - t0); }
+    __device__ __forceinline__ void next(const PrefixParams& p) {
+        left -= count();
+        t0 = 0;
+        if (left > 0 && ++u == p.n_kv_heads * p.plan.units) {
+            u = 0;
+            for (tiles = 0; tiles == 0;) {
+                if (++g >= p.n_groups) {  // (the lengths changed under the call)
+                    left = 0;
+                    return;
+                }
+                tiles = group_tiles(p, g);
+            }
+        }
+    }
+};
+
+// kPair: two blocks of rows over the same tiles; else one block, its even and its odd tiles.
+template <bool kBf16, bool kPair>
+__global__ void __launch_bounds__(kThreads, 1)
+prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+              const __grid_constant__ CUtensorMap map_v) {
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages];
+    __shared__ __align__(8) uint64_t q_full[2], q_empty[2];     // the two buffers of queries
+    __shared__ __align__(8) uint64_t s_full[2], p_full[2], o_full[2], o_empty, drained;
+    __shared__ float2 stats[kPrefixRows];
+    __shared__ Stretch first;
+    __shared__ uint32_t tmem_base;
+    __shared__ volatile int gave_up;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t q_at = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_bytes = p.panels * kPanelBytes;             // a buffer of queries
+    const uint32_t ring = q_at + 2 * q_bytes;
+
+    if (tid == 0) {
+        for (int i = 0; i < kMaxStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], 4);
+            mbar_init(&o_full[i], 1);
+        }
+        mbar_init(&o_empty, kRowThreads / 32);
+        mbar_init(&drained, 1);
+        mbar_init_fence();
+        gave_up = 0;
+    }
+    if (warp == 1) tmem_alloc<1>(&tmem_base);
+    grid_dependency_wait();
+    if (warp == 2) {
+        // the line: its length, this CTA's stretch, and (the first CTA) where every group begins
+        const int per_group = p.n_kv_heads * p.plan.units;
+        int total = 0;
+        for (int g0 = 0; g0 < p.n_groups; g0 += 32)
+            total += __reduce_add_sync(0xFFFFFFFFu, g0 + lane < p.n_groups ? group_tiles(p, g0 + lane) * per_group : 0);
+        const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 2);
+        if (blockIdx.x == 0 && lane == 0) p.plan.line[0] = per;
+        const int begin = (int)min((int64_t)blockIdx.x * per, (int64_t)total);
+        Stretch w;
+        w.left = min(per, total - begin);
+        int before = 0;
+        for (int g0 = 0; g0 < p.n_groups && (before <= begin || blockIdx.x == 0); g0 += 32) {
+            const int g = g0 + lane;
+            const int T = g < p.n_groups ? group_tiles(p, g) : 0;
+            int upto = T * per_group;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            const int start = before + upto - T * per_group;
+            if (blockIdx.x == 0 && g < p.n_groups) p.plan.line[1 + g] = start;
+            if (w.left > 0 && T > 0 && begin >= start && begin < before + upto) {  // one lane, once
+                w.g = g;
+                w.u = (begin - start) / T;
+                w.t0 = begin - start - w.u * T;
+                w.tiles = T;
+                first = w;
+            }
+            before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+        }
+        if (w.left <= 0 && lane == 0) {
+            w.left = 0;
+            first = w;
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    grid_launch_dependents();
+    const uint32_t tmem = tmem_base;
+
+    // A wait that runs out raises the flag and every role leaves; the others see it or run out too.
+    auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+        for (uint32_t i = 0; i < kNapLimit; ++i) {
+            if (mbar_nap(bar, parity)) return true;
+            if (gave_up) return false;
+        }
+        gave_up = 1;
+        return false;
+    };
+    constexpr int kTilesAtOnce = kPair ? 1 : 2;  // tiles that the two lanes take together
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFeedRegs));
+        const bool issuer = lane == 0;
+        if (warp == 0) {  // ---- loads
+            int stage = 0, issued = 0;
+            uint32_t phase = 0;
+            uint32_t q_phase = 0;
+            int buf = 0, q_asked = 0;
+            auto feed = [&]() -> bool {
+                for (Stretch w = first; w.left > 0; w.next(p)) {
+                    const int kv_head = w.u / p.plan.units, block0 = kPair ? (w.u - kv_head * p.plan.units) * 2 : 0;
+                    // queries: both blocks, or the one block into the buffers in turn
+                    for (int b = 0; b < (kPair ? 2 : 1); ++b) {
+                        const int q_buf = kPair ? b : buf;
+                        if (!wait(&q_empty[q_buf], q_phase ^ 1u)) return false;
+                        if (issuer) {
+                            mbar_expect_tx(&q_full[q_buf], p.q_box_bytes * p.panels);
+                            for (int i = 0; i < p.panels; ++i)
+                                tma_load_4d(q_at + q_buf * q_bytes + i * kPanelBytes, &map_q, i * 64, 0, kv_head,
+                                            w.g * p.stream_group + (block0 + b) * p.plan.block_streams,
+                                            smem_u32(&q_full[q_buf]));
+                        }
+                        ++q_asked;
+                    }
+                    if (kPair || buf == 1) q_phase ^= 1u;
+                    buf ^= 1;
+                    const int plane = w.g * p.stream_group * p.planes_per_stream + p.layer_plane + kv_head;
+                    for (int t = 0; t < w.count(); ++t)
+                        for (int kv = 0; kv < 2; ++kv) {
+                            if (!wait(&empty[stage], phase ^ 1u)) return false;
+                            if (issuer) {
+                                mbar_expect_tx(&full[stage], p.stage_bytes);
+                                for (int i = 0; i < p.panels; ++i)
+                                    tma_load_3d(ring + stage * p.stage_bytes + i * kPanelBytes, kv == 0 ? &map_k : &map_v,
+                                                i * 64, (w.t0 + t) * kPrefixTile, plane, smem_u32(&full[stage]));
+                            }
+                            if (issued < p.stages) ++issued;
+                            if (++stage == p.stages) {
+                                stage = 0;
+                                phase ^= 1u;
+                            }
+                        }
+                }
+                return true;
+            };
+            if (!feed() && issuer) {  // gave up: let the loads in flight land
+                for (int i = 0; i < issued; ++i)
+                    for (uint32_t parity = 0; parity < 2; ++parity) mbar_wait_bounded(&full[i], parity, 1u << 14);
+                for (int i = 0; i < 2 && i < q_asked; ++i)
+                    for (uint32_t parity = 0; parity < 2; ++parity) mbar_wait_bounded(&q_full[i], parity, 1u << 14);
+            }
+        } else if (warp == 1) {  // ---- products
+            auto multiply = [&]() {
+                const uint32_t type = (1u << 4) | ((uint32_t)kBf16 << 7) | ((uint32_t)kBf16 << 10) | (8u << 24);  // 128 rows
+                const uint32_t s_desc = type | (16u << 17);                                       // 128 slots
+                const int out_cols = (p.head_dim + 15) / 16 * 16;
+                const uint32_t o_desc = type | (1u << 16) | ((uint32_t)(out_cols >> 3) << 17);    // V: columns contiguous
+                const int q_steps = (p.head_dim + 15) / 16;
+                // job n is tile n / 2 of lane n % 2 (pair), or tile n of lane n % 2; its K and V are two stages
+                int k_stage = 0, v_stage = 1;
+                uint32_t k_phase = 0, v_phase = 0, p_phase[2] = {0, 0}, q_phase = 0, o_phase = 0;
+                int buf = 0;
+                bool begun = false;
+                auto step = [&](int& stage, uint32_t& phase) {
+                    stage += 2;
+                    if (stage >= p.stages) {
+                        stage -= p.stages;
+                        phase ^= 1u;
+                    }
+                };
+                for (Stretch w = first; w.left > 0; w.next(p)) {
+                    const int tiles = w.count(), jobs = kPair ? 2 * tiles : tiles;
+                    auto scores = [&](int n) -> bool {  // S of job n
+                        const int ln = n & 1;
+                        if (kPair ? n < 2 : n == 0) {
+                            if (!wait(&q_full[kPair ? ln : buf], q_phase)) return false;
+                        }
+                        if (!kPair || ln == 0) {
+                            if (!wait(&full[k_stage], k_phase)) return false;
+                        }
+                        tmem_fence_after();
+                        if (issuer) {
+                            const uint32_t a = operand_lo(q_at + (kPair ? ln : buf) * q_bytes);
+                            const uint32_t b = operand_lo(ring + k_stage * p.stage_bytes);
+                            for (int i = 0; i < q_steps; ++i) {
+                                const uint32_t off = (uint32_t)(i >> 2) * (kPanelBytes >> 4) + (uint32_t)(i & 3) * 2;
+                                mma_f16<1>(tmem + kScoreCol + ln * kLaneCols, a + off, b + off, s_desc, i > 0);
+                            }
+                            if (!kPair || ln == 1) mma_commit<1>(&empty[k_stage]);
+                            if (kPair ? n >= jobs - 2 : n == jobs - 1) mma_commit<1>(&q_empty[kPair ? ln : buf]);
+                            mma_commit<1>(&s_full[ln]);
+                        }
+                        if (!kPair || ln == 1) step(k_stage, k_phase);
+                        return true;
+                    };
+                    for (int n = 0; n < 2 && n < jobs; ++n)
+                        if (!scores(n)) return;
+                    if (begun && !wait(&o_empty, o_phase)) return;  // the last unit's results have been read
+                    if (begun) o_phase ^= 1u;
+                    begun = true;
+                    for (int n = 0; n < jobs; ++n) {
+                        const int ln = n & 1;
+                        if (!wait(&p_full[ln], p_phase[ln])) return;
+                        p_phase[ln] ^= 1u;
+                        if (!kPair || ln == 0) {
+                            if (!wait(&full[v_stage], v_phase)) return;
+                        }
+                        tmem_fence_after();
+                        if (issuer) {
+                            const uint32_t b = columns_lo(ring + v_stage * p.stage_bytes);
+#pragma unroll
+                            for (int i = 0; i < kPrefixTile / 16; ++i)
+                                mma_f16_tmem(tmem + kOutCol + ln * kLaneCols, tmem + kScoreCol + ln * kLaneCols + i * 8,
+                                             b + i * (2048 >> 4), o_desc, n > 1 || i > 0);
+                            if (!kPair || ln == 1) mma_commit<1>(&empty[v_stage]);
+                            if (n + 2 >= jobs) mma_commit<1>(&o_full[ln]);
+                        }
+                        if (!kPair || ln == 1) step(v_stage, v_phase);
+                        if (n + 2 < jobs && !scores(n + 2)) return;
+                    }
+                    if (kPair || buf == 1) q_phase ^= 1u;
+                    buf ^= 1;
+                }
+            };
+            multiply();
+            if (issuer) mma_commit<1>(&drained);
+        }
+    } else {  // ---- one row of a lane per thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegs));
+        const int quarter = warp & 3, ln = (warp - 4) >> 2, row = quarter * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
+        const uint32_t s_at = lanes + kScoreCol + ln * kLaneCols, o_at = lanes + kOutCol + ln * kLaneCols;
+        uint32_t s_phase = 0, o_phase[2] = {0, 0};
+        const float scale = p.scale_log2;
+        bool ok = true;
+        // (a warp that gave up goes on to meet the others at their barriers)
+        for (Stretch w = first; w.left > 0; w.next(p)) {
+            const int kv_head = w.u / p.plan.units, block0 = kPair ? (w.u - kv_head * p.plan.units) * 2 : 0;
+            const int block = block0 + (kPair ? ln : 0);
+            const int used = max(0, min(p.plan.block_streams, p.stream_group - block * p.plan.block_streams)) * p.heads;
+            const bool any = quarter * 32 < used;   // rows of this warp that are somebody's
+            const int tiles = w.count();
+            float m = kNegHuge, l = 0.f;
+            bool fresh = true;
+            for (int t = kPair ? 0 : ln; t < tiles && ok; t += kTilesAtOnce, fresh = false) {
+                ok = __all_sync(0xFFFFFFFFu, wait(&s_full[ln], s_phase));
+                if (!ok) break;
+                s_phase ^= 1u;
+                tmem_fence_after();
+                if (any) {
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tmem_ask32(s[i], s_at + i * 32);
+                    tmem_wait_loads();
+                    float top[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        top[i] = __uint_as_float(s[i][0]) * scale;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float z = __uint_as_float(s[i][j]) * scale;
+                            s[i][j] = __float_as_uint(z);
+                            top[i] = fmaxf(top[i], z);
+                        }
+                    }
+                    const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                    if (__any_sync(0xFFFFFFFFu, high > m + kMoveAt<kBf16>)) {
+                        const float up = fmaxf(m, high - kSetBelow<kBf16>);
+                        const float f = ex2_approx(m - up);
+                        m = up;
+                        l *= f;
+                        if (!fresh) {  // the products so far are done: S came after them
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if (i * 32 >= p.head_dim) break;
+                                uint32_t o[32];
+                                tmem_ask32(o, o_at + i * 32);
+                                tmem_wait_loads();
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                tmem_give32(o_at + i * 32, o);
+                            }
+                        }
+                    }
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float e = ex2_approx(__uint_as_float(s[i][j]) - m);
+                            s[i][j] = __float_as_uint(e);
+                            sum[j & 3] += e;
+                        }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t w16[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const int e = i * 64 + 2 * j;
+                            w16[j] = pack16<kBf16>(__uint_as_float(s[e >> 5][e & 31]), __uint_as_float(s[e >> 5][(e & 31) + 1]));
+                        }
+                        tmem_give32(s_at + i * 32, w16);
+                    }
+                    tmem_wait_stores();
+                }
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[ln]);
+            }
+            // ---- the unit's part -----------------------------------------------------------------
+            const int lanes_used = kPair || tiles > 1 ? 2 : 1;
+            const int64_t place =
+                ((int64_t)w.g * p.n_kv_heads * p.plan.units + w.u + blockIdx.x) * p.plan.rows + row + (kPair ? ln * kPrefixRows : 0);
+            for (int x = 0; x < 2; ++x)
+                if (x < lanes_used && (!kPair || x == ln) && ok) {
+                    ok = __all_sync(0xFFFFFFFFu, wait(&o_full[x], o_phase[x]));
+                    o_phase[x] ^= 1u;
+                }
+            tmem_fence_after();
+            float* dst = p.plan.part_o + place * p.head_dim;
+            if (kPair) {
+                if (any && ok) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (i * 32 >= p.head_dim) break;
+                        uint32_t o[32];
+                        tmem_ask32(o, o_at + i * 32);
+                        tmem_wait_loads();
+                        if (row < used) {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4)
+                                if (i * 32 + j < p.head_dim)
+                                    *reinterpret_cast<uint4*>(dst + i * 32 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                        }
+                    }
+                    if (row < used) p.plan.part_ml[place] = make_float2(m, l);
+                }
+            } else {
+                // the even and the odd tiles into one; each of a row's two threads takes half of the columns
+                if (ln == 1) stats[row] = make_float2(m, l);
+                asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
+                float2 f;
+                if (ln == 0) {
+                    const float2 odd = stats[row];
+                    const float up = fmaxf(m, odd.x);
+                    f = make_float2(ex2_approx(m - up), ex2_approx(odd.x - up));
+                    stats[row] = f;
+                    if (row < used && ok) p.plan.part_ml[place] = make_float2(up, l * f.x + odd.y * f.y);
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
+                if (ln == 1) f = stats[row];
+                if (any && ok) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int col = ln * 64 + i * 32;
+                        if (col >= p.head_dim) break;
+                        uint32_t o[32], q[32];
+                        tmem_ask32(o, lanes + kOutCol + col);
+                        tmem_ask32(q, lanes + kOutCol + kLaneCols + col);
+                        tmem_wait_loads();
+                        if (row < used) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                float v = __uint_as_float(o[j]) * f.x;
+                                if (lanes_used == 2) v = fmaf(__uint_as_float(q[j]), f.y, v);
+                                o[j] = __float_as_uint(v);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4)
+                                if (col + j < p.head_dim)
+                                    *reinterpret_cast<uint4*>(dst + col + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                        }
+                    }
+                }
+            }
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&o_empty);
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    // products still under way use shared memory and tensor memory
+    if (warp == 1) {
+        if (lane == 0) {
+            bool done = false;
+            for (uint32_t i = 0; i < kNapLimit && !done; ++i) done = mbar_nap(&drained, 0);
+            if (!done) gave_up = 1;
+        }
+        __syncwarp();
+    }
+    __syncthreads();
+    tmem_fence_after();
+    if (warp == 1) tmem_free<1>(tmem);
+    if (tid == 0 && gave_up) atomicOr(p.status, SIRLLM_STATUS_TIMEOUT);
+}
+
+template <bool kBf16, bool kPair>
+cudaError_t launch(const PrefixParams& p, const DeviceProps& dp, const CUtensorMap& q, const CUtensorMap& k,
+                   const CUtensorMap& v, cudaStream_t st) {
+    static unsigned char allowed[kMaxDevices];
+    auto kernel = prefix_kernel<kBf16, kPair>;
+    cudaError_t e = allow_max_dynamic_smem((const void*)kernel, dp, allowed);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(dp.n_sm < kAttendMaxCtas ? dp.n_sm : kAttendMaxCtas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = 1024 + (size_t)p.panels * kPanelBytes * 2 + (size_t)p.stages * p.stage_bytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p, q, k, v);
+}
+
+}  // namespace
+
+bool prefix_plan(const sirllm_config& c, int32_t stream_group, int32_t n_heads, PrefixPlan* plan) {
+    const int heads = n_heads / c.n_kv_heads;
+    if (heads > kPrefixRows || c.head_dim > 128 || (int64_t)stream_group * heads <= 16) return false;
+    *plan = PrefixPlan{};
+    plan->block_streams = stream_group < kPrefixRows / heads ? stream_group : kPrefixRows / heads;
+    plan->blocks = (stream_group + plan->block_streams - 1) / plan->block_streams;
+    plan->pair = plan->blocks > 1;
+    plan->units = (plan->blocks + 1) / 2;
+    plan->rows = plan->pair ? 2 * kPrefixRows : plan->block_streams * heads;
+    // tiles are counted in 32 bits
+    const int64_t tiles = (int64_t)(c.n_streams / stream_group) * c.n_kv_heads * plan->units * (c.capacity / kPrefixTile + 1);
+    return tiles < 0x7FFFFFFF - 2 * kAttendMaxCtas;
+}
+
+cudaError_t launch_prefix(const PrefixParams& p, const void* q, int64_t q_stride, int32_t n_streams, const void* k,
+                          const void* v, cudaStream_t st) {
+    TraceRange trace("sirllm:attend_shared prefix");
+    DeviceProps dp;
+    cudaError_t e = device_props(&dp);
+    if (e != cudaSuccess) return e;
+    EncodeTiled encode;
+    if ((e = encoder(&encode)) != cudaSuccess) return e;
+    const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    CUtensorMap map_q, map_k, map_v;
+    {
+        const cuuint64_t dims[4] = {(cuuint64_t)p.head_dim, (cuuint64_t)p.heads, (cuuint64_t)p.n_kv_heads, (cuuint64_t)n_streams};
+        const cuuint64_t strides[3] = {(cuuint64_t)p.head_dim * 2, (cuuint64_t)p.heads * p.head_dim * 2, (cuuint64_t)q_stride * 2};
+        const cuuint32_t box[4] = {64, (cuuint32_t)p.heads, 1, (cuuint32_t)p.plan.block_streams};
+        if (encode(&map_q, type, 4, const_cast<void*>(q), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    for (int i = 0; i < 2; ++i) {
+        const cuuint64_t dims[3] = {(cuuint64_t)p.head_dim, (cuuint64_t)p.capacity, (cuuint64_t)n_streams * p.planes_per_stream};
+        const cuuint64_t strides[2] = {(cuuint64_t)p.head_dim * 2, (cuuint64_t)p.capacity * p.head_dim * 2};
+        const cuuint32_t box[3] = {64, (cuuint32_t)kPrefixTile, 1};
+        if (encode(i == 0 ? &map_k : &map_v, type, 3, const_cast<void*>(i == 0 ? k : v), dims, strides, box, ones,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    PrefixParams x = p;
+    x.panels = (p.head_dim + 63) / 64;
+    x.q_box_bytes = p.plan.block_streams * p.heads * 128;
+    x.stage_bytes = x.panels * kPanelBytes;
+    x.stages = (kSmemRoom - 2 * x.panels * kPanelBytes) / x.stage_bytes;
+    if (x.stages > kMaxStages) x.stages = kMaxStages;
+    if (p.plan.pair)
+        return p.bf16 ? launch<true, true>(x, dp, map_q, map_k, map_v, st) : launch<false, true>(x, dp, map_q, map_k, map_v, st);
+    return p.bf16 ? launch<true, false>(x, dp, map_q, map_k, map_v, st) : launch<false, false>(x, dp, map_q, map_k, map_v, st);
+}
+
+}  // namespace sirllm
