@@ -133,26 +133,43 @@ static BeamTiling beam_tiling(const sirllm_config& c) {
     }
 }
 
-// attend's own, then what the shared slots give
+// How sirllm_attend_shared goes about a call, and its workspace: attend's own, then the parts.
+enum { kSharedRead, kSharedUnits, kSharedProduct };
 struct AttendSharedLayout {
     AttendLayout own;
     PrefixPlan plan;   // no pointers yet
-    bool on;
-    size_t line_off, part_ml_off, part_o_off, total;
+    int how;
+    size_t line_off, part_ml_off, part_o_off, own_ml_off, own_o_off, total;
 };
 static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t group, int32_t n_heads) {
     AttendSharedLayout L;
     L.own = attend_layout(c);
-    L.on = prefix_plan(c, group, n_heads, &L.plan);
-    L.line_off = L.own.total;
-    L.part_ml_off = L.part_o_off = L.total = L.line_off;
-    if (L.on) {
-        const size_t groups = c.n_streams / group;
-        const size_t places = groups * c.n_kv_heads * L.plan.units + kAttendMaxCtas, rows = places * L.plan.rows;
-        L.part_ml_off = align_up(L.line_off + (1 + groups) * 4, 256);
-        L.part_o_off = align_up(L.part_ml_off + rows * sizeof(float2), 256);
-        L.total = align_up(L.part_o_off + rows * c.head_dim * sizeof(float), 256);
+    const int64_t rows = (int64_t)group * (n_heads / c.n_kv_heads);   // query heads of a group that share a K/V head
+    // Few rows and little to read (a stream's shared slots as often as there are streams, at most): every
+    // stream reads them itself, in one launch.
+    const int64_t most = (int64_t)c.n_streams * c.n_kv_heads * c.capacity * c.head_dim * 4;
+    L.how = kSharedRead;
+    if (group > 1 && most > kSharedReadBytes) {
+        if (rows <= attend_unit_heads((int)rows, c.head_dim))
+            L.how = kSharedUnits;
+        else if (prefix_plan(c, group, n_heads, &L.plan))
+            L.how = kSharedProduct;
     }
+    L.line_off = L.own.total;
+    L.part_ml_off = L.part_o_off = L.own_ml_off = L.own_o_off = L.total = L.line_off;
+    if (L.how == kSharedRead) return L;
+    const size_t groups = c.n_streams / group, heads = (size_t)c.n_streams * n_heads;
+    size_t off = L.line_off;
+    if (L.how == kSharedProduct) {
+        const size_t places = groups * c.n_kv_heads * L.plan.units + kAttendMaxCtas, part_rows = places * L.plan.rows;
+        L.part_ml_off = align_up(off + (1 + groups) * 4, 256);
+        L.part_o_off = align_up(L.part_ml_off + part_rows * sizeof(float2), 256);
+        off = align_up(L.part_o_off + part_rows * c.head_dim * sizeof(float), 256);
+    }
+    const size_t own = L.how == kSharedUnits ? 2 * heads : heads;
+    L.own_ml_off = off;
+    L.own_o_off = align_up(off + own * sizeof(float2), 256);
+    L.total = align_up(L.own_o_off + own * c.head_dim * sizeof(float), 256);
     return L;
 }
 
@@ -809,9 +826,23 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
     p.part_heads = kAttendPartHeads;
     p.shared_len = shared_len;
     p.stream_group = group;
+    p.walk = cfg->n_streams;
     if (shared_len != nullptr) {
         const AttendSharedLayout S = attend_shared_layout(*cfg, group, n_heads);
-        if (S.on) {
+        if (S.how != kSharedRead) {
+            if ((int64_t)cfg->n_streams * n_heads > 0x7FFFFFFF) return SIRLLM_ERR_TOO_LARGE;
+            p.own_ml = (float2*)((char*)ws + S.own_ml_off);
+            p.own_o = (float*)((char*)ws + S.own_o_off);
+        }
+        if (S.how == kSharedUnits) {
+            p.lead_units = cfg->n_streams / group;
+            p.walk += p.lead_units;
+            p.blocks = 1;
+            p.units = cfg->n_kv_heads;
+            const int64_t walk_units = (int64_t)p.walk * p.units;
+            if (walk_units > 0x1FFFFFF || walk_units * most_tiles > 0x7FFFFFFF - kAttendMaxCtas) return SIRLLM_ERR_TOO_LARGE;
+        }
+        if (S.how == kSharedProduct) {
             p.prefix = S.plan;
             p.prefix.line = (int32_t*)((char*)ws + S.line_off);
             p.prefix.part_ml = (float2*)((char*)ws + S.part_ml_off);

@@ -150,52 +150,60 @@ __device__ __forceinline__ int live_slots(const AttendParams& p, int s) {
     return n < 0 || n > p.capacity ? 0 : n;
 }
 
-// Where streams share slots: whether the group's count of them can be used, and the slots of a stream
-// that are read here.
-template <bool kShared>
-__device__ __forceinline__ bool group_ok(const AttendParams& p, int s) {
-    if (!kShared) return true;
-    const int n = p.shared_len[s / p.stream_group];
+// How a kernel is used.  kPlain: sirllm_attend.  kLead: the streams of a group share their first slots,
+// and every stream reads them from the group's first stream.  kParts: the shared slots are computed once
+// for the group; what this kernel computes - every stream's own slots and, where a group has few query
+// heads per K/V head, the shared slots as a unit of all its streams' heads - goes out in parts that
+// join_kernel puts together.
+enum { kPlain, kLead, kParts };
+
+__device__ __forceinline__ bool group_ok(const AttendParams& p, int g) {
+    const int n = p.shared_len[g];
     return n >= 0 && n <= p.capacity;
 }
-// The first of the stream's slots that is read here: those in front of it were computed for the whole
-// group, unless the stream ends among them.
-template <bool kShared>
-__device__ __forceinline__ int first_slot(const AttendParams& p, int s, int live) {
-    if (!kShared || p.prefix.part_o == nullptr) return 0;
-    const int n = prefix_slots(p.shared_len[s / p.stream_group]);
+// The first slot of stream s that is its own work in kParts: those in front of it are computed for the
+// whole group, unless the stream ends among them.
+__device__ __forceinline__ int first_slot(const AttendParams& p, int shared, int live) {
+    const int n = p.lead_units > 0 ? shared : prefix_slots(shared);
     return live > n ? n : 0;
 }
-template <bool kShared>
-__device__ __forceinline__ int unit_slots(const AttendParams& p, int s) {
-    if (!group_ok<kShared>(p, s)) return 0;
+// slots of walk member i: a group's shared ones (i < lead_units), else those of stream i - lead_units
+template <int kUse>
+__device__ __forceinline__ int unit_slots(const AttendParams& p, int i) {
+    if (kUse == kPlain) return live_slots(p, i);
+    const int s = i - p.lead_units;
+    const int g = s < 0 ? i : s / p.stream_group;
+    if (!group_ok(p, g)) return 0;
+    if (s < 0) return p.shared_len[g];
     const int n = live_slots(p, s);
-    return n - first_slot<kShared>(p, s, n);
+    return kUse == kLead ? n : n - first_slot(p, p.shared_len[g], n);
 }
 
 // A CTA's way through the work, segment by segment.  Two ways: along its stretch of the line of
 // tiles, or (whole_units) from unit to unit, `step` units apart.
-template <bool kShared>
+template <int kUse>
 struct Walk {
     int left;       // positions of the stretch from this segment's first on; whole units: 1 until the end
     int unit0;      // line position of the unit's first tile; whole units: the unit's number
-    int s, unit;    // stream; unit within the stream (K/V head, block of query heads)
+    int s, unit;    // stream (member of the walk); unit within it (K/V head, block of query heads)
     int len;        // live slots of the stream
     int t0, t1;     // this segment's tiles of the unit
     int step;       // 0: along the line
-    int base;       // kShared: the unit's first slot; slots below `shared` are those of the stream `lead`
-    int shared, lead;
+    // kLead, kParts: the stream whose planes are read (-1: a group's shared slots), the unit's first slot;
+    // slots below `shared` are those of the stream `lead`
+    int stream, base, shared, lead;
 
-    // the stream s: its slots, and where they are
+    // the walk's member s: its slots, and where they are
     __device__ __forceinline__ void look_up(const AttendParams& p) {
-        len = unit_slots<kShared>(p, s);
-        if (kShared) {
-            const int g = s / p.stream_group;
-            lead = g * p.stream_group;
-            shared = p.shared_len[g];
-            base = first_slot<kShared>(p, s, live_slots(p, s));
-        }
+        len = unit_slots<kUse>(p, s);
+        if (kUse == kPlain) return;
+        stream = s - p.lead_units;
+        const int g = stream < 0 ? s : stream / p.stream_group;
+        lead = g * p.stream_group;
+        shared = stream < 0 ? 0 : p.shared_len[g];
+        base = kUse == kParts && stream >= 0 ? first_slot(p, shared, live_slots(p, stream)) : 0;
     }
+
     __device__ __forceinline__ bool more() const { return left > 0; }
     __device__ __forceinline__ int tiles() const { return (len + kKeys - 1) / kKeys; }
     __device__ __forceinline__ void set_end() {
@@ -204,7 +212,7 @@ struct Walk {
     }
     // from the unit numbered unit0, the first one with slots, in steps
     __device__ __forceinline__ void find_unit(const AttendParams& p) {
-        const int n_units = p.n_streams * p.units;
+        const int n_units = p.walk * p.units;
         left = 0;
         for (; unit0 < n_units; unit0 += step) {
             s = unit0 / p.units;
@@ -232,7 +240,7 @@ struct Walk {
         if (++unit == p.units) {
             unit = 0;
             for (len = 0; len == 0;) {  // positions are left, so a stream with slots follows
-                if (++s >= p.n_streams) {  // (unless the lengths changed under the call)
+                if (++s >= p.walk) {  // (unless the lengths changed under the call)
                     left = 0;
                     return;
                 }
@@ -245,8 +253,7 @@ struct Walk {
 
 // kDim: head_dim rounded up to 64, 128 or 256 (the columns behind head_dim are zeros in shared
 // memory); kTiles: blocks of 8 query heads that a unit carries.
-// kShared: the streams of a group share their first slots, which are read from the group's first stream.
-template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, bool kShared>
+template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, int kUse>
 __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendParams p) {
     constexpr int kThreads = kWarps * 32;
     constexpr int kChunks = kDim / 8;               // 16-byte vectors of a row
@@ -259,24 +266,26 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     float* merge = cta_o + kHeads * kDim;  // [warp][kPass][kDim]
     __shared__ int scan[kWarps];
     __shared__ int longest[kWarps], counted[kWarps], gap_all;
-    __shared__ Walk<kShared> first;
+    __shared__ Walk<kUse> first;
     __shared__ float stat_m[kWarps][kHeads], stat_l[kWarps][kHeads];
     __shared__ float part_w[kHeads];
     __shared__ __align__(8) float2 cta_ml[kHeads];
     __shared__ int last_one;
     __shared__ float4 team_sum[kThreads];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    grid_dependency_wait();
+    // Behind the kernel that computes the shared slots nothing of that kernel is read here: it has waited
+    // for what came before it, and is waited for at the end.
+    if (kUse != kParts || p.lead_units > 0) grid_dependency_wait();
     grid_launch_dependents();
 
     // ---- the line of tiles, this CTA's stretch of it -------------------------------------
-    const int slice = (p.n_streams + kThreads - 1) / kThreads;
-    const int s_lo = min(p.n_streams, tid * slice), s_hi = min(p.n_streams, s_lo + slice);
+    const int slice = (p.walk + kThreads - 1) / kThreads;
+    const int s_lo = min(p.walk, tid * slice), s_hi = min(p.walk, s_lo + slice);
     const float tile_bytes = (float)(kKeys * 4 * p.head_dim);
     const int gap = min((int)(kUnitBytes / tile_bytes), kAttendUnitTiles);
     int mine = 0, live = 0, long_unit = 0;
     for (int s = s_lo; s < s_hi; ++s) {
-        const int T = (unit_slots<kShared>(p, s) + kKeys - 1) / kKeys;
+        const int T = (unit_slots<kUse>(p, s) + kKeys - 1) / kKeys;
         if (T == 0) continue;
         mine += (T + gap) * p.units;
         ++live;
@@ -375,7 +384,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         int at = before;
         int s = s_lo, len = 0, T = 0;
         for (; s < s_hi; ++s) {
-            len = unit_slots<kShared>(p, s);
+            len = unit_slots<kUse>(p, s);
             T = len > 0 ? (len + kKeys - 1) / kKeys + gap : 0;  // a unit's positions
             if (r0 < at + T * p.units) break;
             at += T * p.units;
@@ -394,9 +403,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     }
     // streams without slots: nothing to weigh, the result is zero and its log-sum -inf; a length
     // outside the planes is reported and its rows are left alone
-    for (int s = blockIdx.x; s < p.n_streams; s += gridDim.x) {
+    // (kParts: left to join_kernel)
+    for (int s = blockIdx.x; s < p.n_streams && kUse != kParts; s += gridDim.x) {
         const int n = p.kv_len[s];
-        if (n < 0 || n > p.capacity || !group_ok<kShared>(p, s)) {
+        if (n < 0 || n > p.capacity || (kUse == kLead && !group_ok(p, s / p.stream_group))) {
             if (tid == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
         } else if (n == 0) {
             // (a row of up to 2^31 - 1 elements: the index of the step behind it does not fit an int)
@@ -408,17 +418,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         }
     }
     __syncthreads();
-    if (!whole_units && r0 >= line) return;
+    if (!whole_units && r0 >= line) {
+        if (kUse == kParts && p.lead_units == 0) grid_dependency_wait();
+        return;
+    }
 
     // ---- the warp's ring ------------------------------------------------------------------
     const uint32_t ring0 = smem_u32(ring) + warp * kStages * 2 * kTileBytes;
-    Walk<kShared> start = first;
+    Walk<kUse> start = first;
     if (solo) {
         start.step = gridDim.x * kWarps;
         start.unit0 = warp * gridDim.x + blockIdx.x;  // over the SMs first
         start.find_unit(p);
     }
-    Walk<kShared> ahead = start;                 // what the loads have reached
+    Walk<kUse> ahead = start;                 // what the loads have reached
     int ahead_tile = ahead.t0 + lead;
     constexpr int kRowsAtOnce = 32 / kChunks;  // rows that one load instruction of the warp covers
     const int chunk = lane % kChunks, row_in = lane / kChunks;
@@ -430,21 +443,21 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         }
         if (ahead.more()) {
             const int g = ahead.unit / p.blocks;
-            const int64_t plane = (int64_t)ahead.s * p.planes_per_stream + p.layer_plane + g;
+            const int from = kUse == kPlain ? ahead.s : ahead.stream < 0 ? ahead.lead : ahead.stream;
+            const int64_t plane = (int64_t)from * p.planes_per_stream + p.layer_plane + g;
             const int key0 = ahead_tile * kKeys;
-            const int slot0 = kShared ? ahead.base + key0 : key0;
+            const int slot0 = kUse != kPlain ? ahead.base + key0 : key0;
             const int64_t off = ((plane * p.capacity + slot0) * p.head_dim + (chunk_on ? chunk * 8 : 0)) * 2;
             // from this stream's planes to those of the stream that holds the shared slots
-            const int64_t to_lead = kShared ? (int64_t)(ahead.lead - ahead.s) * p.planes_per_stream * p.capacity *
-                                                  p.head_dim * 2
-                                            : 0;
+            const int64_t to_lead =
+                kUse != kPlain ? (int64_t)(ahead.lead - from) * p.planes_per_stream * p.capacity * p.head_dim * 2 : 0;
             const uint32_t dst0 = ring0 + stage * 2 * kTileBytes;
 #pragma unroll
             for (int i = 0; i < kKeys / kRowsAtOnce; ++i) {
                 const int r = i * kRowsAtOnce + row_in;
                 const bool valid = chunk_on && key0 + r < ahead.len;
                 int64_t o = valid ? off + (int64_t)r * p.head_dim * 2 : off;
-                if (kShared && slot0 + r < ahead.shared) o += to_lead;
+                if (kUse != kPlain && slot0 + r < ahead.shared) o += to_lead;
                 const uint32_t d = dst0 + r * (kDim * 2) + ((chunk ^ (r & 7)) << 4);
                 cp_async16(d, p.k + o, valid);
                 cp_async16(d + kTileBytes, p.v + o, valid);
@@ -459,20 +472,35 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 
     // ---- the units ------------------------------------------------------------------------
     const int hc = 2 * (lane & 3);  // this lane's two heads within a block of 8
-    for (Walk<kShared> w = start; w.more(); w.next(p, gap_all)) {
+    for (Walk<kUse> w = start; w.more(); w.next(p, gap_all)) {
         const int g = w.unit / p.blocks, block = w.unit - g * p.blocks;
         const int head0 = g * p.group + block * kHeads;            // first query head of the unit
-        const int heads = min(kHeads, p.group - block * kHeads);   // query heads it really has
+        const bool of_group = kUse == kParts && w.stream < 0;      // all streams' heads: group * heads rows, one block
+        const int heads = min(kHeads, (of_group ? p.stream_group * p.group : p.group) - block * kHeads);  // it really has
+        // head h of the unit among all streams' heads
+        auto row_of_head = [&](int h) -> int64_t {
+            if (kUse == kPlain) return (int64_t)w.s * p.n_heads + head0 + h;
+            if (!of_group) return (int64_t)w.stream * p.n_heads + head0 + h;
+            const int local = h / p.group;
+            return (int64_t)(w.lead + local) * p.n_heads + g * p.group + (h - local * p.group);
+        };
+        // kParts: where the head's part goes
+        auto part_of_head = [&](int h) { return row_of_head(h) + (of_group ? (int64_t)p.n_streams * p.n_heads : 0); };
         // queries as the right operand: lane holds elements 2(lane%4), +1 (and +8, +9) of head lane/4
         uint32_t qf[kTiles][kDim / 16][2];
-        const char* qrow = p.q + ((int64_t)w.s * p.q_stride + (int64_t)head0 * p.head_dim) * 2;
+        const char* qrow = p.q + ((int64_t)(kUse == kPlain ? w.s : w.stream) * p.q_stride + (int64_t)head0 * p.head_dim) * 2;
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
             const int h = n * 8 + (lane >> 2);
+            const char* qhead = qrow + (int64_t)h * p.head_dim * 2;
+            if (of_group) {
+                const int local = h / p.group;
+                qhead = p.q + ((w.lead + local) * p.q_stride + (int64_t)(g * p.group + h - local * p.group) * p.head_dim) * 2;
+            }
 #pragma unroll
             for (int ks = 0; ks < kDim / 16; ++ks) {
                 const int e = ks * 16 + hc;
-                const char* src = qrow + ((int64_t)h * p.head_dim + e) * 2;
+                const char* src = qhead + e * 2;
                 qf[n][ks][0] = h < heads && e < p.head_dim ? *reinterpret_cast<const uint32_t*>(src) : 0u;
                 qf[n][ks][1] = h < heads && e + 8 < p.head_dim ? *reinterpret_cast<const uint32_t*>(src + 16) : 0u;
             }
@@ -487,41 +515,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 for (int i = 0; i < 4; ++i) o[n][d][i] = 0.f;
             m[n][0] = m[n][1] = kNegHuge;
             l[n][0] = l[n][1] = 0.f;
-        }
-        if (kShared && w.base > 0 && w.t0 == 0) {
-            // ---- what the group's slots in front of the unit's gave, a part at a time per warp -----------
-            const PrefixPlan& x = p.prefix;
-            const int local = w.s - w.lead, in_block = local / x.block_streams;
-            const int u = g * x.units + (x.pair ? in_block >> 1 : 0);             // unit of the group
-            const int tiles = w.base / kPrefixTile, per = x.line[0], group_no = w.s / p.stream_group;
-            const int at = x.line[1 + group_no] + u * tiles;
-            const int64_t unit0 = (int64_t)group_no * (p.units / p.blocks) * x.units + u;
-            const int row = (local - in_block * x.block_streams) * p.group + block * kHeads +
-                            (x.pair ? (in_block & 1) * kPrefixRows : 0);
-            for (int c = at / per + lead; c <= (at + tiles - 1) / per; c += stride) {
-                const int64_t place = (unit0 + c) * x.rows + row;
-                const float2* ml = x.part_ml + place;
-                const float* po = x.part_o + place * p.head_dim;
-#pragma unroll
-                for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int h = n * 8 + hc + i;
-                        const float2 y = h < heads ? __ldcg(&ml[h]) : make_float2(kNegHuge, 0.f);
-                        const float up = fmaxf(m[n][i], y.x);
-                        const float f = ex2_approx(m[n][i] - up), fy = ex2_approx(y.x - up);
-                        m[n][i] = up;
-                        l[n][i] = l[n][i] * f + (lane < 4 ? y.y * fy : 0.f);
-#pragma unroll
-                        for (int d = 0; d < kDim / 16; ++d)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                const int e = d * 16 + j * 8 + (lane >> 2);
-                                const float v = h < heads && e < p.head_dim ? __ldcg(&po[h * p.head_dim + e]) : 0.f;
-                                o[n][d][i + 2 * j] = o[n][d][i + 2 * j] * f + v * fy;
-                            }
-                    }
-            }
         }
         for (int tile = w.t0 + lead; tile < w.t1; tile += stride) {
             cp_wait<kStages - 2>();
@@ -605,6 +598,24 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], x);
+        // A finished head's results: four (or two, or one) of its elements, times 1 / sum - or, in kParts, as they
+        // are - and its log-sum, or reference and sum.
+        auto factor = [&](float sum) { return kUse == kParts ? 1.0f : 1.0f / sum; };
+        auto put_sum = [&](int h, float ref, float sum) {
+            if (kUse == kParts)
+                p.own_ml[part_of_head(h)] = make_float2(ref, sum);
+            else if (p.lse != nullptr)
+                p.lse[row_of_head(h)] = (ref + log2f(sum)) * (float)kLn2;
+        };
+        auto out_at = [&](int h, int e) {
+            return p.out + (int64_t)(kUse == kPlain ? w.s : w.stream) * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e;
+        };
+        auto put4 = [&](int h, int e, const float4& v, float f) {
+            if (kUse == kParts)
+                *reinterpret_cast<float4*>(p.own_o + part_of_head(h) * p.head_dim + e) = v;
+            else
+                *reinterpret_cast<uint2*>(out_at(h, e)) = make_uint2(pack16<kBf16>(v.x * f, v.y * f), pack16<kBf16>(v.z * f, v.w * f));
+        };
         if (solo) {
             // ---- the warp has the whole unit: four heads at a time through its part of the buffer ------
             float* rows = merge + warp * kPass * kDim;
@@ -613,8 +624,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int h = n * 8 + hc + i;
-                    if (lane < 4 && h < heads && p.lse != nullptr)
-                        p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (m[n][i] + log2f(l[n][i])) * (float)kLn2;
+                    if (lane < 4 && h < heads) put_sum(h, m[n][i], l[n][i]);
                 }
 #pragma unroll
             for (int q = 0; q < kHeads / kPass; ++q) {
@@ -623,7 +633,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 if (((lane & 3) >> 1) == (q & 1)) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float f = 1.0f / l[n][i];
+                        const float f = factor(l[n][i]);
                         float* row = rows + ((hc & 3) + i) * kDim + (lane >> 2);
 #pragma unroll
                         for (int d = 0; d < kDim / 16; ++d) {
@@ -637,9 +647,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 for (int h = 0; h < last; ++h)
                     for (int e = 2 * lane; e < p.head_dim; e += 64) {
                         const float2 v = *reinterpret_cast<const float2*>(&rows[h * kDim + e]);
-                        *reinterpret_cast<uint32_t*>(p.out + (int64_t)w.s * p.out_stride +
-                                                     (int64_t)(head0 + q * kPass + h) * p.head_dim + e) =
-                            pack16<kBf16>(v.x, v.y);
+                        if (kUse == kParts)
+                            *reinterpret_cast<float2*>(p.own_o + part_of_head(q * kPass + h) * p.head_dim + e) = v;
+                        else
+                            *reinterpret_cast<uint32_t*>(out_at(q * kPass + h, e)) = pack16<kBf16>(v.x, v.y);
                     }
                 __syncwarp();
             }
@@ -678,9 +689,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 #pragma unroll
             for (int x = 0; x < kWarps; ++x) sum += stat_l[x][tid] * ex2_approx(stat_m[x][tid] - t);
             if (whole) {
-                part_w[tid] = 1.0f / sum;
-                if (p.lse != nullptr)
-                    p.lse[(int64_t)w.s * p.n_heads + head0 + tid] = (t + log2f(sum)) * (float)kLn2;
+                part_w[tid] = factor(sum);
+                put_sum(tid, t, sum);
             } else if (shared_unit) {
                 cta_ml[tid] = make_float2(t, sum);
             } else {
@@ -710,9 +720,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 float sum = 0.f;
 #pragma unroll
                 for (int y = 0; y < kWarps; ++y) sum += merge[y * kPass * kDim + x];
-                if (whole)
-                    p.out[(int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e] =
-                        round16<kBf16>(sum * part_w[h]);
+                if (whole && kUse == kParts)
+                    p.own_o[part_of_head(h) * p.head_dim + e] = sum;
+                else if (whole)
+                    *out_at(h, e) = round16<kBf16>(sum * part_w[h]);
                 else if (shared_unit)
                     cta_o[h * p.head_dim + e] = sum;
                 else
@@ -751,11 +762,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                     acc.z = fmaf(v[c].z, f, acc.z);
                     acc.w = fmaf(v[c].w, f, acc.w);
                 }
-                const float f = 1.0f / sum;
-                *reinterpret_cast<uint2*>(p.out + (int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e) =
-                    make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
-                if (e == 0 && p.lse != nullptr)
-                    p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (t + log2f(sum)) * (float)kLn2;
+                put4(h, e, acc, factor(sum));
+                if (e == 0) put_sum(h, t, sum);
             }
             cluster_sync();  // the others have read this CTA's sums
             continue;
@@ -817,9 +825,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 #pragma unroll
             for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
             if (lane == 0) {
-                part_w[h] = 1.0f / sum;
-                if (p.lse != nullptr)
-                    p.lse[(int64_t)w.s * p.n_heads + head0 + h] = (t + log2f(sum)) * (float)kLn2;
+                part_w[h] = factor(sum);
+                put_sum(h, t, sum);
             }
         }
         __syncthreads();
@@ -858,22 +865,113 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                     }
                 }
             }
-            if (busy && mine == 0) {
-                const float f = part_w[h];
-                const uint2 packed = make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
-                *reinterpret_cast<uint2*>(p.out + (int64_t)w.s * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e) =
-                    packed;
-            }
+            if (busy && mine == 0) put4(h, e, acc, part_w[h]);
         }
         __syncthreads();  // the merge buffer and last_one are used again by the next unit
     }
     cp_wait<0>();
+    if (kUse == kParts && p.lead_units == 0) grid_dependency_wait();
 }
 
-template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, bool kShared>
+// The parts of every stream's heads into the result: what the group's shared slots gave (several parts from
+// prefix_kernel, one from attend_kernel) and what the stream's own gave.  A warp per head and stream.
+template <bool kBf16>
+__global__ void __launch_bounds__(128) join_kernel(const AttendParams p) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const int64_t rows = (int64_t)p.n_streams * p.n_heads;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const int s = (int)(row / p.n_heads), head = (int)(row - (int64_t)s * p.n_heads);
+    const int g = s / p.stream_group, n = p.kv_len[s], shared = p.shared_len[g];
+    uint16_t* const out = p.out + (int64_t)s * p.out_stride + (int64_t)head * p.head_dim;
+    if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
+        if (lane == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
+        return;
+    }
+    if (n == 0) {
+        for (int e = lane * 8; e < p.head_dim; e += 256) *reinterpret_cast<uint4*>(out + e) = make_uint4(0, 0, 0, 0);
+        if (lane == 0 && p.lse != nullptr) p.lse[row] = __uint_as_float(0xFF800000u);
+        return;
+    }
+    // part 0: the stream's own slots; parts 1 .. : the group's
+    const int base = first_slot(p, shared, n);
+    int parts = 1;
+    int64_t first = 0, step = 0;
+    const float2* ml = nullptr;
+    const float* po = nullptr;
+    if (base > 0) {
+        if (p.lead_units > 0) {
+            parts = 2;
+            first = rows + row;
+            ml = p.own_ml;
+            po = p.own_o;
+        } else {
+            const PrefixPlan& x = p.prefix;
+            const int kv_head = head / p.group, local = s - g * p.stream_group, in_block = local / x.block_streams;
+            const int u = kv_head * x.units + (x.pair ? in_block >> 1 : 0);   // unit of the group
+            const int tiles = base / kPrefixTile, per = x.line[0], at = x.line[1 + g] + u * tiles;
+            const int c = at / per;
+            parts = 2 + (at + tiles - 1) / per - c;
+            const int64_t unit = (int64_t)g * (p.n_heads / p.group) * x.units + u;
+            first = (unit + c) * x.rows + (local - in_block * x.block_streams) * p.group + head - kv_head * p.group +
+                    (x.pair ? (in_block & 1) * kPrefixRows : 0);
+            step = x.rows;
+            ml = x.part_ml;
+            po = x.part_o;
+        }
+    }
+    auto place = [&](int i) { return first + (i - 1) * step; };
+    float m = kNegHuge, l = 0.f;
+    float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int i0 = 0; i0 < parts; i0 += 32) {
+        const int i = i0 + lane;
+        const float2 mine = i >= parts ? make_float2(kNegHuge, 0.f) : __ldcg(i == 0 ? &p.own_ml[row] : &ml[place(i)]);
+        float up = mine.x;
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, x));
+        up = fmaxf(up, m);
+        const float f = ex2_approx(m - up), fi = ex2_approx(mine.x - up);
+        float sum = mine.y * fi;
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+        l = l * f + sum;
+        m = up;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int e = (j * 32 + lane) * 4;
+            acc[j] = make_float4(acc[j].x * f, acc[j].y * f, acc[j].z * f, acc[j].w * f);
+            if (j * 128 >= p.head_dim) break;
+#pragma unroll 8
+            for (int k = 0; k < min(32, parts - i0); ++k) {
+                const float w = __shfl_sync(0xFFFFFFFFu, fi, k);
+                if (e < p.head_dim) {
+                    const float* from = i0 + k == 0 ? p.own_o + row * p.head_dim : po + place(i0 + k) * p.head_dim;
+                    const float4 v = __ldcg(reinterpret_cast<const float4*>(from + e));
+                    acc[j].x = fmaf(v.x, w, acc[j].x);
+                    acc[j].y = fmaf(v.y, w, acc[j].y);
+                    acc[j].z = fmaf(v.z, w, acc[j].z);
+                    acc[j].w = fmaf(v.w, w, acc[j].w);
+                }
+            }
+        }
+    }
+    const float f = 1.0f / l;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int e = (j * 32 + lane) * 4;
+        if (e < p.head_dim)
+            *reinterpret_cast<uint2*>(out + e) =
+                make_uint2(pack16<kBf16>(acc[j].x * f, acc[j].y * f), pack16<kBf16>(acc[j].z * f, acc[j].w * f));
+    }
+    if (lane == 0 && p.lse != nullptr) p.lse[row] = (m + log2f(l)) * (float)kLn2;
+}
+
+template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, int kUse>
 cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
     static unsigned char allowed[kMaxDevices];
-    auto kernel = attend_kernel<kBf16, kDim, kTiles, kWarps, kStages, kShared>;
+    auto kernel = attend_kernel<kBf16, kDim, kTiles, kWarps, kStages, kUse>;
     cudaError_t e = allow_max_dynamic_smem((const void*)kernel, dp, allowed);
     if (e != cudaSuccess) return e;
     // the ring, a CTA's sums, and a buffer that takes [warp][4 heads][kDim] sums or [part][head] weights
@@ -881,7 +979,7 @@ cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st
     const size_t smem = (size_t)kWarps * kStages * 2 * kKeys * kDim * 2 + (size_t)kTiles * 8 * kDim * 4 +
                         (sums > weights ? sums : weights);
     // the largest clusters of which the device holds one per unit
-    const int64_t n_units = (int64_t)p.n_streams * p.units;
+    const int64_t n_units = (int64_t)p.walk * p.units;
     AttendParams q = p;
     q.cluster = 1;
     int grid = dp.n_sm < kAttendMaxCtas ? dp.n_sm : kAttendMaxCtas;
@@ -940,14 +1038,32 @@ cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st
     return cudaLaunchKernelEx(&cfg, kernel, q);
 }
 
-template <bool kBf16, bool kShared>
+template <bool kBf16, int kUse>
 cudaError_t launch_dim(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
-    const bool wide = attend_unit_heads(p.group, p.head_dim) == 16;
+    const bool wide = attend_unit_heads(p.lead_units > 0 ? p.stream_group * p.group : p.group, p.head_dim) == 16;
     if (p.head_dim <= 64)
-        return wide ? launch<kBf16, 64, 2, 8, 6, kShared>(p, dp, st) : launch<kBf16, 64, 1, 8, 6, kShared>(p, dp, st);
+        return wide ? launch<kBf16, 64, 2, 8, 6, kUse>(p, dp, st) : launch<kBf16, 64, 1, 8, 6, kUse>(p, dp, st);
     if (p.head_dim <= 128)
-        return wide ? launch<kBf16, 128, 2, 8, 3, kShared>(p, dp, st) : launch<kBf16, 128, 1, 8, 3, kShared>(p, dp, st);
-    return launch<kBf16, 256, 1, 4, 3, kShared>(p, dp, st);
+        return wide ? launch<kBf16, 128, 2, 8, 3, kUse>(p, dp, st) : launch<kBf16, 128, 1, 8, 3, kUse>(p, dp, st);
+    return launch<kBf16, 256, 1, 4, 3, kUse>(p, dp, st);
+}
+
+template <bool kBf16>
+cudaError_t launch_use(const AttendParams& p, const DeviceProps& dp, cudaStream_t st) {
+    if (p.shared_len == nullptr) return launch_dim<kBf16, kPlain>(p, dp, st);
+    if (p.own_o == nullptr) return launch_dim<kBf16, kLead>(p, dp, st);
+    cudaError_t e = launch_dim<kBf16, kParts>(p, dp, st);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(((int64_t)p.n_streams * p.n_heads + 3) / 4));
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, join_kernel<kBf16>, p);
 }
 
 }  // namespace
@@ -957,8 +1073,7 @@ cudaError_t launch_attend(const AttendParams& p, bool bf16, cudaStream_t st) {
     DeviceProps dp;
     cudaError_t e = device_props(&dp);
     if (e != cudaSuccess) return e;
-    if (p.shared_len != nullptr) return bf16 ? launch_dim<true, true>(p, dp, st) : launch_dim<false, true>(p, dp, st);
-    return bf16 ? launch_dim<true, false>(p, dp, st) : launch_dim<false, false>(p, dp, st);
+    return bf16 ? launch_use<true>(p, dp, st) : launch_use<false>(p, dp, st);
 }
 
 }  // namespace sirllm

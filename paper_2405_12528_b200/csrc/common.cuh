@@ -183,6 +183,7 @@ struct AttendDeal {
 // stream r / heads.  A unit is one block of up to 128 rows, or two (pair), of one K/V head of a group;
 // its tiles of 128 slots stand in one line with the other units', cut into equal stretches for the CTAs.
 // The part of unit u (of all groups) that CTA c computes is in place u + c.
+constexpr int64_t kSharedReadBytes = 8 << 20;
 constexpr int kPrefixTile = 128;
 constexpr int kPrefixRows = 128;   // rows of a block, at most
 struct PrefixPlan {
@@ -206,7 +207,7 @@ struct PrefixParams {
     int32_t n_groups, stream_group, heads, n_kv_heads, head_dim, capacity;
     int32_t planes_per_stream, layer_plane, bf16;
     // set by the launcher
-    int32_t panels, stages, stage_bytes, q_box_bytes;
+    int32_t q_box_bytes;
 };
 
 struct AttendParams {
@@ -228,6 +229,12 @@ struct AttendParams {
     const int32_t* shared_len;
     int32_t stream_group;
     PrefixPlan prefix;
+    // where the shared slots are computed once for the group (else null): every stream's heads' parts
+    // [2][n_streams * n_heads], of its own slots and of the shared ones
+    float* own_o;                            // [...][head_dim]
+    float2* own_ml;
+    int32_t lead_units;                      // groups whose shared slots are units of this kernel: all or none
+    int32_t walk;                            // what the kernel walks through: lead_units + n_streams
     // set by the launcher
     int32_t cluster, cluster_log2;           // CTAs of a cluster
     AttendDeal alone, together;              // to CTAs, to clusters

@@ -33,21 +33,25 @@ constexpr int kRowThreads = 256;
 // registers: 168 a thread at launch (64512 for 384 threads); 128 * 72 + 256 * 216 = 64512
 constexpr int kFeedRegs = 72, kRowRegs = 216;
 static_assert(128 * kFeedRegs + kRowThreads * kRowRegs <= kThreads * 168, "more registers than the launch has");
-constexpr int kMaxStages = 10;
 constexpr int kPanelBytes = 128 * 128;  // 64 elements of 128 rows or slots, 128-byte swizzle
 constexpr int kSmemRoom = 224 * 1024;
+template <int kPanels>
+constexpr int kStagesOf = kPanels == 1 ? 10 : (kSmemRoom - 2 * kPanels * kPanelBytes) / (kPanels * kPanelBytes);
 constexpr uint32_t kScoreCol = 0, kOutCol = 256, kLaneCols = 128;  // tensor memory: S (and P) and O of the two lanes
+
+constexpr float kLowest = -3.4028235e38f;
 
 template <bool kBf16>
 constexpr float kSetBelow = kBf16 ? 0.f : 11.f;
 template <bool kBf16>
 constexpr float kMoveAt = kBf16 ? 8.f : 15.f;
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar,
+                                            uint64_t policy) {
     asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-            dst),
-        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], "
+        "[%2], %6;" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "l"(policy)
         : "memory");
 }
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
@@ -57,10 +61,19 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
         "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 // Right operand with the product's columns contiguous: panels of 64 columns kPanelBytes apart, groups of
 // 8 slots 1024 bytes apart.
 __device__ __forceinline__ uint32_t columns_lo(uint32_t addr) {
     return ((addr & 0x3FFFFu) >> 4) | ((uint32_t)(kPanelBytes >> 4) << 16);
+}
+// one lane of the warp, the same every time; the compiler knows that it is one
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
 }
 // left operand from tensor memory
 __device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, bool accumulate) {
@@ -98,6 +111,29 @@ __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fenc
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// two fp32 values side by side in one register pair
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+// eight values, one sector of memory
+__device__ __forceinline__ void store8(float* at, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
 }
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
@@ -137,25 +173,28 @@ struct Stretch {
 };
 
 // kPair: two blocks of rows over the same tiles; else one block, its even and its odd tiles.
-template <bool kBf16, bool kPair>
+// kPanels: panels of 64 elements of a head.
+template <bool kBf16, bool kPair, int kPanels>
 __global__ void __launch_bounds__(kThreads, 1)
 prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
               const __grid_constant__ CUtensorMap map_v) {
+    constexpr int kStageBytes = kPanels * kPanelBytes;
+    constexpr int kStages = kStagesOf<kPanels>;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages];
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages];
     __shared__ __align__(8) uint64_t q_full[2], q_empty[2];     // the two buffers of queries
-    __shared__ __align__(8) uint64_t s_full[2], p_full[2], o_full[2], o_empty, drained;
+    __shared__ __align__(8) uint64_t s_full[2], p_full[2][2], o_full[2], o_empty, drained;
     __shared__ float2 stats[kPrefixRows];
     __shared__ Stretch first;
     __shared__ uint32_t tmem_base;
     __shared__ volatile int gave_up;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t q_at = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t q_bytes = p.panels * kPanelBytes;             // a buffer of queries
+    const uint32_t q_bytes = kPanels * kPanelBytes;              // a buffer of queries
     const uint32_t ring = q_at + 2 * q_bytes;
 
     if (tid == 0) {
-        for (int i = 0; i < kMaxStages; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
@@ -163,7 +202,8 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
             mbar_init(&q_full[i], 1);
             mbar_init(&q_empty[i], 1);
             mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], 4);
+            mbar_init(&p_full[i][0], 4);
+            mbar_init(&p_full[i][1], 4);
             mbar_init(&o_full[i], 1);
         }
         mbar_init(&o_empty, kRowThreads / 32);
@@ -172,12 +212,18 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
         gave_up = 0;
     }
     if (warp == 1) tmem_alloc<1>(&tmem_base);
+    if (tid == 0) {
+        prefetch_map(&map_q);
+        prefetch_map(&map_k);
+        prefetch_map(&map_v);
+    }
     grid_dependency_wait();
     if (warp == 2) {
         // the line: its length, this CTA's stretch, and (the first CTA) where every group begins
         const int per_group = p.n_kv_heads * p.plan.units;
-        int total = 0;
-        for (int g0 = 0; g0 < p.n_groups; g0 += 32)
+        const int T0 = lane < p.n_groups ? group_tiles(p, lane) : 0;
+        int total = __reduce_add_sync(0xFFFFFFFFu, T0 * per_group);
+        for (int g0 = 32; g0 < p.n_groups; g0 += 32)
             total += __reduce_add_sync(0xFFFFFFFFu, g0 + lane < p.n_groups ? group_tiles(p, g0 + lane) * per_group : 0);
         const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 2);
         if (blockIdx.x == 0 && lane == 0) p.plan.line[0] = per;
@@ -187,7 +233,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
         int before = 0;
         for (int g0 = 0; g0 < p.n_groups && (before <= begin || blockIdx.x == 0); g0 += 32) {
             const int g = g0 + lane;
-            const int T = g < p.n_groups ? group_tiles(p, g) : 0;
+            const int T = g0 == 0 ? T0 : g < p.n_groups ? group_tiles(p, g) : 0;
             int upto = T * per_group;
             for (int o = 1; o < 32; o <<= 1) {
                 const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
@@ -217,8 +263,8 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
 
     // A wait that runs out raises the flag and every role leaves; the others see it or run out too.
     auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-        for (uint32_t i = 0; i < kNapLimit; ++i) {
-            if (mbar_nap(bar, parity)) return true;
+        for (uint32_t i = 0; i < kSpinLimit; ++i) {
+            if (mbar_try_wait(bar, parity)) return true;
             if (gave_up) return false;
         }
         gave_up = 1;
@@ -228,8 +274,15 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFeedRegs));
-        const bool issuer = lane == 0;
         if (warp == 0) {  // ---- loads
+            const bool issuer = elect_one();
+            // K and V that only one CTA reads shall not push other things out of L2 (this kernel's
+            // instructions among them: fetching them from HBM costs microseconds at every start)
+            uint64_t policy;
+            if (p.plan.units == 1)
+                asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+            else
+                asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
             int stage = 0, issued = 0;
             uint32_t phase = 0;
             uint32_t q_phase = 0;
@@ -242,8 +295,8 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                         const int q_buf = kPair ? b : buf;
                         if (!wait(&q_empty[q_buf], q_phase ^ 1u)) return false;
                         if (issuer) {
-                            mbar_expect_tx(&q_full[q_buf], p.q_box_bytes * p.panels);
-                            for (int i = 0; i < p.panels; ++i)
+                            mbar_expect_tx(&q_full[q_buf], p.q_box_bytes * kPanels);
+                            for (int i = 0; i < kPanels; ++i)
                                 tma_load_4d(q_at + q_buf * q_bytes + i * kPanelBytes, &map_q, i * 64, 0, kv_head,
                                             w.g * p.stream_group + (block0 + b) * p.plan.block_streams,
                                             smem_u32(&q_full[q_buf]));
@@ -257,13 +310,13 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                         for (int kv = 0; kv < 2; ++kv) {
                             if (!wait(&empty[stage], phase ^ 1u)) return false;
                             if (issuer) {
-                                mbar_expect_tx(&full[stage], p.stage_bytes);
-                                for (int i = 0; i < p.panels; ++i)
-                                    tma_load_3d(ring + stage * p.stage_bytes + i * kPanelBytes, kv == 0 ? &map_k : &map_v,
-                                                i * 64, (w.t0 + t) * kPrefixTile, plane, smem_u32(&full[stage]));
+                                mbar_expect_tx(&full[stage], kStageBytes);
+                                for (int i = 0; i < kPanels; ++i)
+                                    tma_load_3d(ring + stage * kStageBytes + i * kPanelBytes, kv == 0 ? &map_k : &map_v,
+                                                i * 64, (w.t0 + t) * kPrefixTile, plane, smem_u32(&full[stage]), policy);
                             }
-                            if (issued < p.stages) ++issued;
-                            if (++stage == p.stages) {
+                            if (issued < kStages) ++issued;
+                            if (++stage == kStages) {
                                 stage = 0;
                                 phase ^= 1u;
                             }
@@ -283,7 +336,6 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                 const uint32_t s_desc = type | (16u << 17);                                       // 128 slots
                 const int out_cols = (p.head_dim + 15) / 16 * 16;
                 const uint32_t o_desc = type | (1u << 16) | ((uint32_t)(out_cols >> 3) << 17);    // V: columns contiguous
-                const int q_steps = (p.head_dim + 15) / 16;
                 // job n is tile n / 2 of lane n % 2 (pair), or tile n of lane n % 2; its K and V are two stages
                 int k_stage = 0, v_stage = 1;
                 uint32_t k_phase = 0, v_phase = 0, p_phase[2] = {0, 0}, q_phase = 0, o_phase = 0;
@@ -291,8 +343,8 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                 bool begun = false;
                 auto step = [&](int& stage, uint32_t& phase) {
                     stage += 2;
-                    if (stage >= p.stages) {
-                        stage -= p.stages;
+                    if (stage >= kStages) {
+                        stage -= kStages;
                         phase ^= 1u;
                     }
                 };
@@ -307,12 +359,14 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                             if (!wait(&full[k_stage], k_phase)) return false;
                         }
                         tmem_fence_after();
-                        if (issuer) {
-                            const uint32_t a = operand_lo(q_at + (kPair ? ln : buf) * q_bytes);
-                            const uint32_t b = operand_lo(ring + k_stage * p.stage_bytes);
-                            for (int i = 0; i < q_steps; ++i) {
+                        const uint32_t a = operand_lo(q_at + (kPair ? ln : buf) * q_bytes);
+                        const uint32_t b = operand_lo(ring + k_stage * kStageBytes);
+                        const uint32_t d = tmem + kScoreCol + ln * kLaneCols;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int i = 0; i < kPanels * 4; ++i) {  // (what lies behind head_dim is zeros)
                                 const uint32_t off = (uint32_t)(i >> 2) * (kPanelBytes >> 4) + (uint32_t)(i & 3) * 2;
-                                mma_f16<1>(tmem + kScoreCol + ln * kLaneCols, a + off, b + off, s_desc, i > 0);
+                                mma_f16<1>(d, a + off, b + off, s_desc, i > 0);
                             }
                             if (!kPair || ln == 1) mma_commit<1>(&empty[k_stage]);
                             if (kPair ? n >= jobs - 2 : n == jobs - 1) mma_commit<1>(&q_empty[kPair ? ln : buf]);
@@ -328,21 +382,27 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                     begun = true;
                     for (int n = 0; n < jobs; ++n) {
                         const int ln = n & 1;
-                        if (!wait(&p_full[ln], p_phase[ln])) return;
-                        p_phase[ln] ^= 1u;
-                        if (!kPair || ln == 0) {
-                            if (!wait(&full[v_stage], v_phase)) return;
-                        }
-                        tmem_fence_after();
-                        if (issuer) {
-                            const uint32_t b = columns_lo(ring + v_stage * p.stage_bytes);
+                        const uint32_t b = columns_lo(ring + v_stage * kStageBytes);
+                        const uint32_t d = tmem + kOutCol + ln * kLaneCols, a = tmem + kScoreCol + ln * kLaneCols;
+                        const bool more = n > 1;
 #pragma unroll
-                            for (int i = 0; i < kPrefixTile / 16; ++i)
-                                mma_f16_tmem(tmem + kOutCol + ln * kLaneCols, tmem + kScoreCol + ln * kLaneCols + i * 8,
-                                             b + i * (2048 >> 4), o_desc, n > 1 || i > 0);
-                            if (!kPair || ln == 1) mma_commit<1>(&empty[v_stage]);
-                            if (n + 2 >= jobs) mma_commit<1>(&o_full[ln]);
+                        for (int half = 0; half < 2; ++half) {
+                            if (!wait(&p_full[ln][half], p_phase[ln])) return;
+                            if (half == 0 && (!kPair || ln == 0)) {
+                                if (!wait(&full[v_stage], v_phase)) return;
+                            }
+                            tmem_fence_after();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int i = half * 4; i < half * 4 + 4; ++i)
+                                    mma_f16_tmem(d, a + i * 8, b + i * (2048 >> 4), o_desc, i > 0 || more);
+                                if (half == 1) {
+                                    if (!kPair || ln == 1) mma_commit<1>(&empty[v_stage]);
+                                    if (n + 2 >= jobs) mma_commit<1>(&o_full[ln]);
+                                }
+                            }
                         }
+                        p_phase[ln] ^= 1u;
                         if (!kPair || ln == 1) step(v_stage, v_phase);
                         if (n + 2 < jobs && !scores(n + 2)) return;
                     }
@@ -351,7 +411,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                 }
             };
             multiply();
-            if (issuer) mma_commit<1>(&drained);
+            if (elect_one()) mma_commit<1>(&drained);
         }
     } else {  // ---- one row of a lane per thread
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegs));
@@ -360,6 +420,8 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
         const uint32_t s_at = lanes + kScoreCol + ln * kLaneCols, o_at = lanes + kOutCol + ln * kLaneCols;
         uint32_t s_phase = 0, o_phase[2] = {0, 0};
         const float scale = p.scale_log2;
+        const uint32_t flip = scale < 0.f ? 0x80000000u : 0u;  // the largest score is the smallest product then
+        
         bool ok = true;
         // (a warp that gave up goes on to meet the others at their barriers)
         for (Stretch w = first; w.left > 0; w.next(p)) {
@@ -370,71 +432,76 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
             const int tiles = w.count();
             float m = kNegHuge, l = 0.f;
             bool fresh = true;
+            // Twice over a row's scores, 64 columns at a time, in loops: what is not in the instruction cache
+            // comes in at 250 cycles and more per 8 instructions (unrolled over the row, the first tile of a
+            // call took 2 us more; in steps of 32 columns the others 0.3 us more).
             for (int t = kPair ? 0 : ln; t < tiles && ok; t += kTilesAtOnce, fresh = false) {
                 ok = __all_sync(0xFFFFFFFFu, wait(&s_full[ln], s_phase));
                 if (!ok) break;
                 s_phase ^= 1u;
                 tmem_fence_after();
                 if (any) {
-                    uint32_t s[4][32];
+                    float top[4] = {kLowest, kLowest, kLowest, kLowest};
+#pragma unroll 1
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t s[2][32];
+                        tmem_ask32(s[0], s_at + i * 64);
+                        tmem_ask32(s[1], s_at + i * 64 + 32);
+                        tmem_wait_loads();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ask32(s[i], s_at + i * 32);
-                    tmem_wait_loads();
-                    float top[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        top[i] = __uint_as_float(s[i][0]) * scale;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float z = __uint_as_float(s[i][j]) * scale;
-                            s[i][j] = __float_as_uint(z);
-                            top[i] = fmaxf(top[i], z);
-                        }
+                        for (int j = 0; j < 64; j += 2)
+                            top[(j >> 1) & 3] = fmaxf(fmaxf(top[(j >> 1) & 3], __uint_as_float(s[j >> 5][j & 31] ^ flip)),
+                                                      __uint_as_float(s[j >> 5][(j & 31) + 1] ^ flip));
                     }
-                    const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                    const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(scale);
                     if (__any_sync(0xFFFFFFFFu, high > m + kMoveAt<kBf16>)) {
                         const float up = fmaxf(m, high - kSetBelow<kBf16>);
                         const float f = ex2_approx(m - up);
                         m = up;
                         l *= f;
-                        if (!fresh) {  // the products so far are done: S came after them
+                        // the products so far are done: S came after them
+#pragma unroll 1
+                        for (int i = 0; !fresh && i * 32 < p.head_dim; ++i) {
+                            uint32_t o[32];
+                            tmem_ask32(o, o_at + i * 32);
+                            tmem_wait_loads();
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (i * 32 >= p.head_dim) break;
-                                uint32_t o[32];
-                                tmem_ask32(o, o_at + i * 32);
-                                tmem_wait_loads();
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                tmem_give32(o_at + i * 32, o);
-                            }
+                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                            tmem_give32(o_at + i * 32, o);
                         }
                     }
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float e = ex2_approx(__uint_as_float(s[i][j]) - m);
-                            s[i][j] = __float_as_uint(e);
-                            sum[j & 3] += e;
-                        }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
+                    const uint64_t scale2 = pack2(scale, scale), minus2 = pack2(-m, -m);
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll 1
                     for (int i = 0; i < 2; ++i) {
-                        uint32_t w16[32];
+                        uint32_t s[2][32], w16[32];
+                        tmem_ask32(s[0], s_at + i * 64);
+                        tmem_ask32(s[1], s_at + i * 64 + 32);
+                        tmem_wait_loads();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const int e = i * 64 + 2 * j;
-                            w16[j] = pack16<kBf16>(__uint_as_float(s[e >> 5][e & 31]), __uint_as_float(s[e >> 5][(e & 31) + 1]));
+                        for (int j = 0; j < 64; j += 2) {
+                            float e0, e1;
+                            unpack2(fma2(pack2(__uint_as_float(s[j >> 5][j & 31]), __uint_as_float(s[j >> 5][(j & 31) + 1])),
+                                         scale2, minus2), e0, e1);
+                            e0 = ex2_approx(e0);
+                            e1 = ex2_approx(e1);
+                            sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], pack2(e0, e1));
+                            w16[j >> 1] = pack16<kBf16>(e0, e1);
                         }
-                        tmem_give32(s_at + i * 32, w16);
+                        tmem_give32(s_at + i * 32, w16);  // half of the weights, over scores that have been read
+                        tmem_wait_stores();
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_full[ln][i]);
                     }
-                    tmem_wait_stores();
+                    float s0, s1;
+                    unpack2(add2(sum[0], sum[1]), s0, s1);
+                    l += s0 + s1;
+                } else {
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane < 2) mbar_arrive(&p_full[ln][lane]);
                 }
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[ln]);
             }
             // ---- the unit's part -----------------------------------------------------------------
             const int lanes_used = kPair || tiles > 1 ? 2 : 1;
@@ -449,17 +516,15 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
             float* dst = p.plan.part_o + place * p.head_dim;
             if (kPair) {
                 if (any && ok) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (i * 32 >= p.head_dim) break;
+#pragma unroll 1
+                    for (int i = 0; i * 32 < p.head_dim; ++i) {
                         uint32_t o[32];
                         tmem_ask32(o, o_at + i * 32);
                         tmem_wait_loads();
                         if (row < used) {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 4)
-                                if (i * 32 + j < p.head_dim)
-                                    *reinterpret_cast<uint4*>(dst + i * 32 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                            for (int j = 0; j < 32; j += 8)
+                                if (i * 32 + j < p.head_dim) store8(dst + i * 32 + j, o + j);
                         }
                     }
                     if (row < used) p.plan.part_ml[place] = make_float2(m, l);
@@ -479,7 +544,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                 asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
                 if (ln == 1) f = stats[row];
                 if (any && ok) {
-#pragma unroll
+#pragma unroll 1
                     for (int i = 0; i < 2; ++i) {
                         const int col = ln * 64 + i * 32;
                         if (col >= p.head_dim) break;
@@ -495,9 +560,8 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                                 o[j] = __float_as_uint(v);
                             }
 #pragma unroll
-                            for (int j = 0; j < 32; j += 4)
-                                if (col + j < p.head_dim)
-                                    *reinterpret_cast<uint4*>(dst + col + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                            for (int j = 0; j < 32; j += 8)
+                                if (col + j < p.head_dim) store8(dst + col + j, o + j);
                         }
                     }
                 }
@@ -524,17 +588,17 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
     if (tid == 0 && gave_up) atomicOr(p.status, SIRLLM_STATUS_TIMEOUT);
 }
 
-template <bool kBf16, bool kPair>
-cudaError_t launch(const PrefixParams& p, const DeviceProps& dp, const CUtensorMap& q, const CUtensorMap& k,
+template <bool kBf16, bool kPair, int kPanels>
+cudaError_t launch_one(const PrefixParams& p, const DeviceProps& dp, const CUtensorMap& q, const CUtensorMap& k,
                    const CUtensorMap& v, cudaStream_t st) {
     static unsigned char allowed[kMaxDevices];
-    auto kernel = prefix_kernel<kBf16, kPair>;
+    auto kernel = prefix_kernel<kBf16, kPair, kPanels>;
     cudaError_t e = allow_max_dynamic_smem((const void*)kernel, dp, allowed);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(dp.n_sm < kAttendMaxCtas ? dp.n_sm : kAttendMaxCtas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = 1024 + (size_t)p.panels * kPanelBytes * 2 + (size_t)p.stages * p.stage_bytes;
+    cfg.dynamicSmemBytes = 1024 + (size_t)(2 + kStagesOf<kPanels>) * kPanels * kPanelBytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -542,6 +606,12 @@ cudaError_t launch(const PrefixParams& p, const DeviceProps& dp, const CUtensorM
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, p, q, k, v);
+}
+
+template <bool kBf16, bool kPair>
+cudaError_t launch(const PrefixParams& p, const DeviceProps& dp, const CUtensorMap& q, const CUtensorMap& k,
+                   const CUtensorMap& v, cudaStream_t st) {
+    return p.head_dim <= 64 ? launch_one<kBf16, kPair, 1>(p, dp, q, k, v, st) : launch_one<kBf16, kPair, 2>(p, dp, q, k, v, st);
 }
 
 }  // namespace
@@ -589,11 +659,7 @@ cudaError_t launch_prefix(const PrefixParams& p, const void* q, int64_t q_stride
             return cudaErrorInvalidValue;
     }
     PrefixParams x = p;
-    x.panels = (p.head_dim + 63) / 64;
     x.q_box_bytes = p.plan.block_streams * p.heads * 128;
-    x.stage_bytes = x.panels * kPanelBytes;
-    x.stages = (kSmemRoom - 2 * x.panels * kPanelBytes) / x.stage_bytes;
-    if (x.stages > kMaxStages) x.stages = kMaxStages;
     if (p.plan.pair)
         return p.bf16 ? launch<true, true>(x, dp, map_q, map_k, map_v, st) : launch<false, true>(x, dp, map_q, map_k, map_v, st);
     return p.bf16 ? launch<true, false>(x, dp, map_q, map_k, map_v, st) : launch<false, false>(x, dp, map_q, map_k, map_v, st);
