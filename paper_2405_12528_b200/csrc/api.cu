@@ -139,7 +139,8 @@ struct AttendSharedLayout {
     AttendLayout own;
     PrefixPlan plan;   // no pointers yet
     int how;
-    size_t line_off, part_ml_off, part_o_off, own_ml_off, own_o_off, total;
+    int32_t blocks, part_rows;   // blocks of query heads of a K/V head, query heads of one
+    size_t line_off, part_ml_off, part_o_off, part_line_off, own_ml_off, own_o_off, total;
 };
 static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t group, int32_t n_heads) {
     AttendSharedLayout L;
@@ -158,7 +159,7 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
     L.line_off = L.own.total;
     L.part_ml_off = L.part_o_off = L.own_ml_off = L.own_o_off = L.total = L.line_off;
     if (L.how == kSharedRead) return L;
-    const size_t groups = c.n_streams / group, heads = (size_t)c.n_streams * n_heads;
+    const size_t groups = c.n_streams / group;
     size_t off = L.line_off;
     if (L.how == kSharedProduct) {
         const size_t places = groups * c.n_kv_heads * L.plan.units + kAttendMaxCtas, part_rows = places * L.plan.rows;
@@ -166,9 +167,14 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
         L.part_o_off = align_up(L.part_ml_off + part_rows * sizeof(float2), 256);
         off = align_up(L.part_o_off + part_rows * c.head_dim * sizeof(float), 256);
     }
-    const size_t own = L.how == kSharedUnits ? 2 * heads : heads;
-    L.own_ml_off = off;
-    L.own_o_off = align_up(off + own * sizeof(float2), 256);
+    const int heads = n_heads / c.n_kv_heads, unit = attend_unit_heads(heads, c.head_dim);
+    L.blocks = L.how == kSharedUnits ? 1 : (heads + unit - 1) / unit;
+    L.part_rows = L.how == kSharedUnits ? (int32_t)rows : heads < unit ? heads : unit;
+    const size_t members = (L.how == kSharedUnits ? groups : 0) + c.n_streams;
+    const size_t own = (members * c.n_kv_heads * L.blocks + kAttendMaxCtas * kAttendMaxWarps) * L.part_rows;
+    L.part_line_off = off;
+    L.own_ml_off = align_up(off + (1 + members) * 4, 256);
+    L.own_o_off = align_up(L.own_ml_off + own * sizeof(float2), 256);
     L.total = align_up(L.own_o_off + own * c.head_dim * sizeof(float), 256);
     return L;
 }
@@ -833,12 +839,14 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
             if ((int64_t)cfg->n_streams * n_heads > 0x7FFFFFFF) return SIRLLM_ERR_TOO_LARGE;
             p.own_ml = (float2*)((char*)ws + S.own_ml_off);
             p.own_o = (float*)((char*)ws + S.own_o_off);
+            p.part_line = (int32_t*)((char*)ws + S.part_line_off);
+            p.part_rows = S.part_rows;
+            p.blocks = S.blocks;
+            p.units = cfg->n_kv_heads * S.blocks;
         }
         if (S.how == kSharedUnits) {
             p.lead_units = cfg->n_streams / group;
             p.walk += p.lead_units;
-            p.blocks = 1;
-            p.units = cfg->n_kv_heads;
             const int64_t walk_units = (int64_t)p.walk * p.units;
             if (walk_units > 0x1FFFFFF || walk_units * most_tiles > 0x7FFFFFFF - kAttendMaxCtas) return SIRLLM_ERR_TOO_LARGE;
         }

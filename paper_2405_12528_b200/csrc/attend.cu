@@ -55,6 +55,9 @@ constexpr float kUnitBytes = 96 * 1024;
 constexpr float kSoloBytes = 96 * 1024;
 constexpr int kSoloLongest = 32;
 constexpr int kMaxCluster = 8;
+// kParts: the least a warp takes, in tiles, and what the end of a unit counts there.
+constexpr int kPartLeast = 2;
+__device__ __forceinline__ int part_gap(int head_dim) { return head_dim > 64 ? 2 : 4; }
 // Powers of two between the reference of the probabilities and the largest: where it is set, and
 // where it has to move.
 template <bool kBf16>
@@ -266,7 +269,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     float* merge = cta_o + kHeads * kDim;  // [warp][kPass][kDim]
     __shared__ int scan[kWarps];
     __shared__ int longest[kWarps], counted[kWarps], gap_all;
-    __shared__ Walk<kUse> first;
+    __shared__ Walk<kUse> first, first_of[kUse == kParts ? kWarps : 1];
     __shared__ float stat_m[kWarps][kHeads], stat_l[kWarps][kHeads];
     __shared__ float part_w[kHeads];
     __shared__ __align__(8) float2 cta_ml[kHeads];
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     const int slice = (p.walk + kThreads - 1) / kThreads;
     const int s_lo = min(p.walk, tid * slice), s_hi = min(p.walk, s_lo + slice);
     const float tile_bytes = (float)(kKeys * 4 * p.head_dim);
-    const int gap = min((int)(kUnitBytes / tile_bytes), kAttendUnitTiles);
+    const int gap = kUse == kParts ? part_gap(p.head_dim) : min((int)(kUnitBytes / tile_bytes), kAttendUnitTiles);
     int mine = 0, live = 0, long_unit = 0;
     for (int s = s_lo; s < s_hi; ++s) {
         const int T = (unit_slots<kUse>(p, s) + kKeys - 1) / kKeys;
@@ -315,6 +318,38 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         long_unit = max(long_unit, longest[w]);
     }
     before += warps_before - mine;  // tiles in front of this thread's streams
+    // kParts: an equal stretch of the line per WARP, consecutive ones on different SMs; every stretch of a
+    // unit gives a part, so no warp waits for another.
+    const int warp_no = warp * (int)gridDim.x + (int)blockIdx.x;
+    if (kUse == kParts) {
+        const int n_warps = (int)gridDim.x * kWarps;
+        const int per = max((line + n_warps - 1) / n_warps, kPartLeast);
+        if (tid < kWarps) first_of[tid].left = 0;
+        __syncthreads();
+        if (blockIdx.x == 0 && tid == 0) p.part_line[0] = per;
+        int at = before;
+        for (int s = s_lo; s < s_hi; ++s) {
+            const int len = unit_slots<kUse>(p, s);
+            const int T = len > 0 ? (len + kKeys - 1) / kKeys + gap : 0, end = at + T * p.units;
+            if (blockIdx.x == 0) p.part_line[1 + s] = at;
+            for (int w = 0; w < kWarps && T > 0; ++w) {
+                const int no = w * (int)gridDim.x + (int)blockIdx.x;
+                const int r0 = line / per >= no ? no * per : line;  // (no overflow)
+                if (r0 < at || r0 >= end) continue;
+                Walk<kUse>& f = first_of[w];
+                f.step = 0;
+                f.left = min(per, line - r0);
+                f.s = s;
+                f.look_up(p);
+                f.unit = (r0 - at) / T;
+                f.unit0 = at + f.unit * T;
+                f.t0 = r0 - f.unit0;
+                f.set_end();
+                if (f.t0 >= f.tiles()) f.next(p, gap);  // begins behind a unit's last tile
+            }
+            at = end;
+        }
+    }
     // Four ways to deal out the work.  (1) An equal share of the line per CTA; units that CTAs share
     // are joined through memory.  (2) Whole units in turn to the CTAs: nothing to join, but no
     // balance between units of different length.  (3) As (2) to the clusters, a unit's tiles in turn
@@ -361,7 +396,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     // (64 x 32 x 1 - 768 100 -> 78).  Heads above 128, with four warps to a CTA, keep to the other ways: the
     // estimate is too kind there (heads of 256, 64 x 32 x 1 - 2048 351 -> 442 us), though short units would
     // gain (192 x 32 x 64 161 -> 85).
-    const bool solo = kWarps == 8 && long_unit <= kSoloLongest && fmaxf(solo_tiles, hbm) < least;
+    const bool solo = kUse == kParts || kWarps == 8 && long_unit <= kSoloLongest && fmaxf(solo_tiles, hbm) < least;
     if (solo) {
         whole_units = true;
         team = 1;
@@ -418,15 +453,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         }
     }
     __syncthreads();
-    if (!whole_units && r0 >= line) {
-        if (kUse == kParts && p.lead_units == 0) grid_dependency_wait();
-        return;
-    }
+    if (!whole_units && r0 >= line) return;
 
     // ---- the warp's ring ------------------------------------------------------------------
     const uint32_t ring0 = smem_u32(ring) + warp * kStages * 2 * kTileBytes;
-    Walk<kUse> start = first;
-    if (solo) {
+    Walk<kUse> start = kUse == kParts ? first_of[warp] : first;
+    if (solo && kUse != kParts) {
         start.step = gridDim.x * kWarps;
         start.unit0 = warp * gridDim.x + blockIdx.x;  // over the SMs first
         start.find_unit(p);
@@ -477,15 +509,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         const int head0 = g * p.group + block * kHeads;            // first query head of the unit
         const bool of_group = kUse == kParts && w.stream < 0;      // all streams' heads: group * heads rows, one block
         const int heads = min(kHeads, (of_group ? p.stream_group * p.group : p.group) - block * kHeads);  // it really has
-        // head h of the unit among all streams' heads
-        auto row_of_head = [&](int h) -> int64_t {
-            if (kUse == kPlain) return (int64_t)w.s * p.n_heads + head0 + h;
-            if (!of_group) return (int64_t)w.stream * p.n_heads + head0 + h;
-            const int local = h / p.group;
-            return (int64_t)(w.lead + local) * p.n_heads + g * p.group + (h - local * p.group);
-        };
-        // kParts: where the head's part goes
-        auto part_of_head = [&](int h) { return row_of_head(h) + (of_group ? (int64_t)p.n_streams * p.n_heads : 0); };
+        // kParts: the place of the warp's part of the unit
+        const int64_t place = ((int64_t)w.s * p.units + w.unit + warp_no) * p.part_rows;
         // queries as the right operand: lane holds elements 2(lane%4), +1 (and +8, +9) of head lane/4
         uint32_t qf[kTiles][kDim / 16][2];
         const char* qrow = p.q + ((int64_t)(kUse == kPlain ? w.s : w.stream) * p.q_stride + (int64_t)head0 * p.head_dim) * 2;
@@ -598,23 +623,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], x);
-        // A finished head's results: four (or two, or one) of its elements, times 1 / sum - or, in kParts, as they
-        // are - and its log-sum, or reference and sum.
+        // A finished head's results: elements times 1 / sum and the log-sum; in kParts elements as they are,
+        // reference and sum.
         auto factor = [&](float sum) { return kUse == kParts ? 1.0f : 1.0f / sum; };
         auto put_sum = [&](int h, float ref, float sum) {
             if (kUse == kParts)
-                p.own_ml[part_of_head(h)] = make_float2(ref, sum);
+                p.own_ml[place + h] = make_float2(ref, sum);
             else if (p.lse != nullptr)
-                p.lse[row_of_head(h)] = (ref + log2f(sum)) * (float)kLn2;
+                p.lse[(int64_t)(kUse == kPlain ? w.s : w.stream) * p.n_heads + head0 + h] = (ref + log2f(sum)) * (float)kLn2;
         };
         auto out_at = [&](int h, int e) {
             return p.out + (int64_t)(kUse == kPlain ? w.s : w.stream) * p.out_stride + (int64_t)(head0 + h) * p.head_dim + e;
         };
         auto put4 = [&](int h, int e, const float4& v, float f) {
-            if (kUse == kParts)
-                *reinterpret_cast<float4*>(p.own_o + part_of_head(h) * p.head_dim + e) = v;
-            else
-                *reinterpret_cast<uint2*>(out_at(h, e)) = make_uint2(pack16<kBf16>(v.x * f, v.y * f), pack16<kBf16>(v.z * f, v.w * f));
+            *reinterpret_cast<uint2*>(out_at(h, e)) = make_uint2(pack16<kBf16>(v.x * f, v.y * f), pack16<kBf16>(v.z * f, v.w * f));
         };
         if (solo) {
             // ---- the warp has the whole unit: four heads at a time through its part of the buffer ------
@@ -648,7 +670,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                     for (int e = 2 * lane; e < p.head_dim; e += 64) {
                         const float2 v = *reinterpret_cast<const float2*>(&rows[h * kDim + e]);
                         if (kUse == kParts)
-                            *reinterpret_cast<float2*>(p.own_o + part_of_head(q * kPass + h) * p.head_dim + e) = v;
+                            *reinterpret_cast<float2*>(p.own_o + (place + q * kPass + h) * p.head_dim + e) = v;
                         else
                             *reinterpret_cast<uint32_t*>(out_at(q * kPass + h, e)) = pack16<kBf16>(v.x, v.y);
                     }
@@ -656,6 +678,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             }
             continue;
         }
+        if (kUse == kParts) continue;  // (not reached)
         // ---- the warps' sums into one ------------------------------------------------------
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
@@ -720,9 +743,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 float sum = 0.f;
 #pragma unroll
                 for (int y = 0; y < kWarps; ++y) sum += merge[y * kPass * kDim + x];
-                if (whole && kUse == kParts)
-                    p.own_o[part_of_head(h) * p.head_dim + e] = sum;
-                else if (whole)
+                if (whole)
                     *out_at(h, e) = round16<kBf16>(sum * part_w[h]);
                 else if (shared_unit)
                     cta_o[h * p.head_dim + e] = sum;
@@ -895,39 +916,46 @@ __global__ void __launch_bounds__(128) join_kernel(const AttendParams p) {
         if (lane == 0 && p.lse != nullptr) p.lse[row] = __uint_as_float(0xFF800000u);
         return;
     }
-    // part 0: the stream's own slots; parts 1 .. : the group's
+    // the stream's own parts, then the group's
+    const int kv_head = head / p.group, local = s - g * p.stream_group;
     const int base = first_slot(p, shared, n);
-    int parts = 1;
-    int64_t first = 0, step = 0;
-    const float2* ml = nullptr;
-    const float* po = nullptr;
-    if (base > 0) {
-        if (p.lead_units > 0) {
-            parts = 2;
-            first = rows + row;
-            ml = p.own_ml;
-            po = p.own_o;
-        } else {
-            const PrefixPlan& x = p.prefix;
-            const int kv_head = head / p.group, local = s - g * p.stream_group, in_block = local / x.block_streams;
-            const int u = kv_head * x.units + (x.pair ? in_block >> 1 : 0);   // unit of the group
-            const int tiles = base / kPrefixTile, per = x.line[0], at = x.line[1 + g] + u * tiles;
-            const int c = at / per;
-            parts = 2 + (at + tiles - 1) / per - c;
-            const int64_t unit = (int64_t)g * (p.n_heads / p.group) * x.units + u;
-            first = (unit + c) * x.rows + (local - in_block * x.block_streams) * p.group + head - kv_head * p.group +
-                    (x.pair ? (in_block & 1) * kPrefixRows : 0);
-            step = x.rows;
-            ml = x.part_ml;
-            po = x.part_o;
-        }
+    const int gap = part_gap(p.head_dim), part_per = p.part_line[0];
+    auto count = [](int at, int tiles, int per) { return (at + tiles - 1) / per - at / per + 1; };
+    int own = 0, parts = 0;
+    int64_t own_first, lead_first = 0, lead_step = p.part_rows;
+    const float2* lead_ml = p.own_ml;
+    const float* lead_o = p.own_o;
+    {
+        const int member = p.lead_units + s, tiles = (n - base + kKeys - 1) / kKeys;
+        const int hq = head - kv_head * p.group, block = hq / p.part_rows, unit = kv_head * p.blocks + block;
+        const int at = p.part_line[1 + member] + unit * (tiles + gap);
+        own = parts = count(at, tiles, part_per);
+        own_first = ((int64_t)member * p.units + unit + at / part_per) * p.part_rows + hq - block * p.part_rows;
     }
-    auto place = [&](int i) { return first + (i - 1) * step; };
+    if (base > 0 && p.lead_units > 0) {
+        const int tiles = (shared + kKeys - 1) / kKeys;
+        const int at = p.part_line[1 + g] + kv_head * (tiles + gap);
+        parts += count(at, tiles, part_per);
+        lead_first = ((int64_t)g * p.units + kv_head + at / part_per) * p.part_rows + local * p.group + head - kv_head * p.group;
+    } else if (base > 0) {
+        const PrefixPlan& x = p.prefix;
+        const int in_block = local / x.block_streams;
+        const int u = kv_head * x.units + (x.pair ? in_block >> 1 : 0);   // unit of the group
+        const int tiles = base / kPrefixTile, per = x.line[0], at = x.line[1 + g] + u * tiles;
+        parts += count(at, tiles, per);
+        lead_first = ((int64_t)g * (p.n_heads / p.group) * x.units + u + at / per) * x.rows +
+                     (local - in_block * x.block_streams) * p.group + head - kv_head * p.group +
+                     (x.pair ? (in_block & 1) * kPrefixRows : 0);
+        lead_step = x.rows;
+        lead_ml = x.part_ml;
+        lead_o = x.part_o;
+    }
+    auto place = [&](int i) { return i < own ? own_first + (int64_t)i * p.part_rows : lead_first + (int64_t)(i - own) * lead_step; };
     float m = kNegHuge, l = 0.f;
     float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
     for (int i0 = 0; i0 < parts; i0 += 32) {
         const int i = i0 + lane;
-        const float2 mine = i >= parts ? make_float2(kNegHuge, 0.f) : __ldcg(i == 0 ? &p.own_ml[row] : &ml[place(i)]);
+        const float2 mine = i >= parts ? make_float2(kNegHuge, 0.f) : __ldcg((i < own ? p.own_ml : lead_ml) + place(i));
         float up = mine.x;
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, x));
@@ -947,7 +975,7 @@ __global__ void __launch_bounds__(128) join_kernel(const AttendParams p) {
             for (int k = 0; k < min(32, parts - i0); ++k) {
                 const float w = __shfl_sync(0xFFFFFFFFu, fi, k);
                 if (e < p.head_dim) {
-                    const float* from = i0 + k == 0 ? p.own_o + row * p.head_dim : po + place(i0 + k) * p.head_dim;
+                    const float* from = (i0 + k < own ? p.own_o : lead_o) + place(i0 + k) * p.head_dim;
                     const float4 v = __ldcg(reinterpret_cast<const float4*>(from + e));
                     acc[j].x = fmaf(v.x, w, acc[j].x);
                     acc[j].y = fmaf(v.y, w, acc[j].y);

@@ -161,6 +161,7 @@ struct AppendParams {
 
 constexpr int kAttendMaxCtas = 256;   // CTAs of an attention call, at most
 constexpr int kAttendPartHeads = 16;  // query heads of a unit, at most
+constexpr int kAttendMaxWarps = 8;    // warps of a CTA, at most
 constexpr int kAttendTileSlots = 16;  // slots per tile
 constexpr int kAttendUnitTiles = 40;  // positions behind a unit's tiles that stand for what its end costs, at most
 
@@ -229,10 +230,12 @@ struct AttendParams {
     const int32_t* shared_len;
     int32_t stream_group;
     PrefixPlan prefix;
-    // where the shared slots are computed once for the group (else null): every stream's heads' parts
-    // [2][n_streams * n_heads], of its own slots and of the shared ones
-    float* own_o;                            // [...][head_dim]
-    float2* own_ml;
+    // where the shared slots are computed once for the group (else null): the parts that the warps leave,
+    // the one of unit u (of all members of the walk) and warp w in place u + w
+    float* own_o;                            // [place][part_rows][head_dim], relative to 2^reference
+    float2* own_ml;                          // [place][part_rows] (reference in units of log2, sum)
+    int32_t* part_line;                      // [0]: positions per warp; [1 + i]: where member i's units begin
+    int32_t part_rows;                       // query heads of a unit, at most
     int32_t lead_units;                      // groups whose shared slots are units of this kernel: all or none
     int32_t walk;                            // what the kernel walks through: lead_units + n_streams
     // set by the launcher
