@@ -140,7 +140,7 @@ struct AttendSharedLayout {
     PrefixPlan plan;   // no pointers yet
     int how;
     int32_t blocks, part_rows;   // blocks of query heads of a K/V head, query heads of one
-    size_t line_off, part_ml_off, part_o_off, part_line_off, own_ml_off, own_o_off, total;
+    size_t parts_off, part_ml_off, part_o_off, own_parts_off, own_ml_off, own_o_off, total;
 };
 static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t group, int32_t n_heads) {
     AttendSharedLayout L;
@@ -156,14 +156,14 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
         else if (prefix_plan(c, group, n_heads, &L.plan))
             L.how = kSharedProduct;
     }
-    L.line_off = L.own.total;
-    L.part_ml_off = L.part_o_off = L.own_ml_off = L.own_o_off = L.total = L.line_off;
+    L.parts_off = L.own.total;
+    L.part_ml_off = L.part_o_off = L.own_parts_off = L.own_ml_off = L.own_o_off = L.total = L.parts_off;
     if (L.how == kSharedRead) return L;
     const size_t groups = c.n_streams / group;
-    size_t off = L.line_off;
+    size_t off = L.parts_off;
     if (L.how == kSharedProduct) {
         const size_t places = groups * c.n_kv_heads * L.plan.units + kAttendMaxCtas, part_rows = places * L.plan.rows;
-        L.part_ml_off = align_up(off + (1 + groups) * 4, 256);
+        L.part_ml_off = align_up(off + groups * c.n_kv_heads * L.plan.units * sizeof(int2), 256);
         L.part_o_off = align_up(L.part_ml_off + part_rows * sizeof(float2), 256);
         off = align_up(L.part_o_off + part_rows * c.head_dim * sizeof(float), 256);
     }
@@ -171,9 +171,9 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
     L.blocks = L.how == kSharedUnits ? 1 : (heads + unit - 1) / unit;
     L.part_rows = L.how == kSharedUnits ? (int32_t)rows : heads < unit ? heads : unit;
     const size_t members = (L.how == kSharedUnits ? groups : 0) + c.n_streams;
-    const size_t own = (members * c.n_kv_heads * L.blocks + kAttendMaxCtas * kAttendMaxWarps) * L.part_rows;
-    L.part_line_off = off;
-    L.own_ml_off = align_up(off + (1 + members) * 4, 256);
+    const size_t units = members * c.n_kv_heads * L.blocks, own = (units + kAttendMaxCtas * kAttendMaxWarps) * L.part_rows;
+    L.own_parts_off = off;
+    L.own_ml_off = align_up(off + units * sizeof(int2), 256);
     L.own_o_off = align_up(L.own_ml_off + own * sizeof(float2), 256);
     L.total = align_up(L.own_o_off + own * c.head_dim * sizeof(float), 256);
     return L;
@@ -836,10 +836,10 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
     if (shared_len != nullptr) {
         const AttendSharedLayout S = attend_shared_layout(*cfg, group, n_heads);
         if (S.how != kSharedRead) {
-            if ((int64_t)cfg->n_streams * n_heads > 0x7FFFFFFF) return SIRLLM_ERR_TOO_LARGE;
+            if (cfg->n_kv_heads > 65535) return SIRLLM_ERR_TOO_LARGE;  // (a grid's second dimension)
             p.own_ml = (float2*)((char*)ws + S.own_ml_off);
             p.own_o = (float*)((char*)ws + S.own_o_off);
-            p.part_line = (int32_t*)((char*)ws + S.part_line_off);
+            p.own_parts = (int2*)((char*)ws + S.own_parts_off);
             p.part_rows = S.part_rows;
             p.blocks = S.blocks;
             p.units = cfg->n_kv_heads * S.blocks;
@@ -852,7 +852,7 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
         }
         if (S.how == kSharedProduct) {
             p.prefix = S.plan;
-            p.prefix.line = (int32_t*)((char*)ws + S.line_off);
+            p.prefix.parts = (int2*)((char*)ws + S.parts_off);
             p.prefix.part_ml = (float2*)((char*)ws + S.part_ml_off);
             p.prefix.part_o = (float*)((char*)ws + S.part_o_off);
             PrefixParams x;

@@ -57,6 +57,7 @@ constexpr int kSoloLongest = 32;
 constexpr int kMaxCluster = 8;
 // kParts: the least a warp takes, in tiles, and what the end of a unit counts there.
 constexpr int kPartLeast = 2;
+constexpr int kJoinWarps = 4;
 __device__ __forceinline__ int part_gap(int head_dim) { return head_dim > 64 ? 2 : 4; }
 // Powers of two between the reference of the probabilities and the largest: where it is set, and
 // where it has to move.
@@ -321,17 +322,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     // kParts: an equal stretch of the line per WARP, consecutive ones on different SMs; every stretch of a
     // unit gives a part, so no warp waits for another.
     const int warp_no = warp * (int)gridDim.x + (int)blockIdx.x;
+    int part_per = 0;
     if (kUse == kParts) {
         const int n_warps = (int)gridDim.x * kWarps;
-        const int per = max((line + n_warps - 1) / n_warps, kPartLeast);
+        const int per = part_per = max((line + n_warps - 1) / n_warps, kPartLeast);
         if (tid < kWarps) first_of[tid].left = 0;
         __syncthreads();
-        if (blockIdx.x == 0 && tid == 0) p.part_line[0] = per;
         int at = before;
         for (int s = s_lo; s < s_hi; ++s) {
             const int len = unit_slots<kUse>(p, s);
             const int T = len > 0 ? (len + kKeys - 1) / kKeys + gap : 0, end = at + T * p.units;
-            if (blockIdx.x == 0) p.part_line[1 + s] = at;
             for (int w = 0; w < kWarps && T > 0; ++w) {
                 const int no = w * (int)gridDim.x + (int)blockIdx.x;
                 const int r0 = line / per >= no ? no * per : line;  // (no overflow)
@@ -509,6 +509,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         const int head0 = g * p.group + block * kHeads;            // first query head of the unit
         const bool of_group = kUse == kParts && w.stream < 0;      // all streams' heads: group * heads rows, one block
         const int heads = min(kHeads, (of_group ? p.stream_group * p.group : p.group) - block * kHeads);  // it really has
+        if (kUse == kParts && w.t0 == 0 && lane == 0)  // where the unit's parts are, for join_kernel
+            p.own_parts[(int64_t)w.s * p.units + w.unit] = make_int2(warp_no, (w.unit0 + w.tiles() - 1) / part_per - warp_no + 1);
         // kParts: the place of the warp's part of the unit
         const int64_t place = ((int64_t)w.s * p.units + w.unit + warp_no) * p.part_rows;
         // queries as the right operand: lane holds elements 2(lane%4), +1 (and +8, +9) of head lane/4
@@ -894,106 +896,88 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     if (kUse == kParts && p.lead_units == 0) grid_dependency_wait();
 }
 
-// The parts of every stream's heads into the result: what the group's shared slots gave (several parts from
-// prefix_kernel, one from attend_kernel) and what the stream's own gave.  A warp per head and stream.
+// The parts of every stream's heads into the result: those of the stream's own slots, then those of the
+// group's.  A block per stream, K/V head and 128 elements, a warp per query head, four elements per lane.
+// (What is executed once costs its way from L2 into the instruction cache, 250 cycles per 8 instructions:
+// with divisions for the places of the parts, and unrolled, this took 13 us instead of 5.)
 template <bool kBf16>
-__global__ void __launch_bounds__(128) join_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const AttendParams p) {
+    const int lane = threadIdx.x & 31, s = blockIdx.x, kv_head = blockIdx.y, e = (int)blockIdx.z * 128 + lane * 4;
+    const int g = s / p.stream_group, local = s - g * p.stream_group, kv_heads = gridDim.y;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    const int64_t rows = (int64_t)p.n_streams * p.n_heads;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (row >= rows) return;
-    const int s = (int)(row / p.n_heads), head = (int)(row - (int64_t)s * p.n_heads);
-    const int g = s / p.stream_group, n = p.kv_len[s], shared = p.shared_len[g];
-    uint16_t* const out = p.out + (int64_t)s * p.out_stride + (int64_t)head * p.head_dim;
+    const int n = p.kv_len[s], shared = p.shared_len[g];
     if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
-        if (lane == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
+        if (threadIdx.x == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
         return;
     }
-    if (n == 0) {
-        for (int e = lane * 8; e < p.head_dim; e += 256) *reinterpret_cast<uint4*>(out + e) = make_uint4(0, 0, 0, 0);
-        if (lane == 0 && p.lse != nullptr) p.lse[row] = __uint_as_float(0xFF800000u);
-        return;
+    const bool with_lead = first_slot(p, shared, n) > 0, on = e < p.head_dim;
+    const bool product = p.lead_units == 0;
+    int lead_unit = g * kv_heads + kv_head, in_block = 0;
+    if (product && p.prefix.pair) {
+        in_block = local / p.prefix.block_streams;
+        lead_unit = lead_unit * p.prefix.units + (in_block >> 1);
     }
-    // the stream's own parts, then the group's
-    const int kv_head = head / p.group, local = s - g * p.stream_group;
-    const int base = first_slot(p, shared, n);
-    const int gap = part_gap(p.head_dim), part_per = p.part_line[0];
-    auto count = [](int at, int tiles, int per) { return (at + tiles - 1) / per - at / per + 1; };
-    int own = 0, parts = 0;
-    int64_t own_first, lead_first = 0, lead_step = p.part_rows;
-    const float2* lead_ml = p.own_ml;
-    const float* lead_o = p.own_o;
-    {
-        const int member = p.lead_units + s, tiles = (n - base + kKeys - 1) / kKeys;
-        const int hq = head - kv_head * p.group, block = hq / p.part_rows, unit = kv_head * p.blocks + block;
-        const int at = p.part_line[1 + member] + unit * (tiles + gap);
-        own = parts = count(at, tiles, part_per);
-        own_first = ((int64_t)member * p.units + unit + at / part_per) * p.part_rows + hq - block * p.part_rows;
-    }
-    if (base > 0 && p.lead_units > 0) {
-        const int tiles = (shared + kKeys - 1) / kKeys;
-        const int at = p.part_line[1 + g] + kv_head * (tiles + gap);
-        parts += count(at, tiles, part_per);
-        lead_first = ((int64_t)g * p.units + kv_head + at / part_per) * p.part_rows + local * p.group + head - kv_head * p.group;
-    } else if (base > 0) {
-        const PrefixPlan& x = p.prefix;
-        const int in_block = local / x.block_streams;
-        const int u = kv_head * x.units + (x.pair ? in_block >> 1 : 0);   // unit of the group
-        const int tiles = base / kPrefixTile, per = x.line[0], at = x.line[1 + g] + u * tiles;
-        parts += count(at, tiles, per);
-        lead_first = ((int64_t)g * (p.n_heads / p.group) * x.units + u + at / per) * x.rows +
-                     (local - in_block * x.block_streams) * p.group + head - kv_head * p.group +
-                     (x.pair ? (in_block & 1) * kPrefixRows : 0);
-        lead_step = x.rows;
-        lead_ml = x.part_ml;
-        lead_o = x.part_o;
-    }
-    auto place = [&](int i) { return i < own ? own_first + (int64_t)i * p.part_rows : lead_first + (int64_t)(i - own) * lead_step; };
-    float m = kNegHuge, l = 0.f;
-    float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    for (int i0 = 0; i0 < parts; i0 += 32) {
-        const int i = i0 + lane;
-        const float2 mine = i >= parts ? make_float2(kNegHuge, 0.f) : __ldcg((i < own ? p.own_ml : lead_ml) + place(i));
-        float up = mine.x;
+    const int2 lead = !with_lead ? make_int2(0, 0) : __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
+    for (int hq = threadIdx.x >> 5; hq < p.group; hq += kJoinWarps) {
+        const int64_t head = kv_head * p.group + hq;
+        const int block = hq >= p.part_rows ? hq / p.part_rows : 0;
+        const int64_t unit = (int64_t)(p.lead_units + s) * p.units + kv_head * p.blocks + block;
+        const int2 own = n == 0 ? make_int2(0, 0) : __ldcg(p.own_parts + unit);
+        const int parts = own.y + lead.y, lead_row = (local - in_block * p.prefix.block_streams) * p.group + hq;
+        // from part i - own.y on: rows of the group's
+        const int64_t own_at = (unit + own.x) * p.part_rows + hq - block * p.part_rows;
+        const int64_t lead_at = product ? ((int64_t)lead_unit + lead.x) * p.prefix.rows + lead_row + (in_block & 1) * kPrefixRows
+                                        : ((int64_t)g * p.units + kv_head + lead.x) * p.part_rows + lead_row;
+        const int lead_step = product ? p.prefix.rows : p.part_rows;
+        const float2* const lead_ml = product ? p.prefix.part_ml : p.own_ml;
+        const float* const lead_o = product ? p.prefix.part_o : p.own_o;
+        float m = kNegHuge, l = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int i0 = 0; i0 < parts; i0 += 32) {
+            const int i = i0 + lane;
+            const bool is_own = i < own.y;
+            const int64_t at = is_own ? own_at + (int64_t)i * p.part_rows : lead_at + (int64_t)(i - own.y) * lead_step;
+            const float2 mine = i >= parts ? make_float2(kNegHuge, 0.f) : __ldcg((is_own ? p.own_ml : lead_ml) + at);
+            const unsigned long long from = (unsigned long long)((is_own ? p.own_o : lead_o) + at * p.head_dim);
+            float up = mine.x;
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, x));
-        up = fmaxf(up, m);
-        const float f = ex2_approx(m - up), fi = ex2_approx(mine.x - up);
-        float sum = mine.y * fi;
+            for (int x = 16; x > 0; x >>= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, x));
+            up = fmaxf(up, m);
+            const float f = ex2_approx(m - up), fi = ex2_approx(mine.x - up);
+            l = fmaf(l, f, mine.y * fi);  // this lane's parts
+            m = up;
+            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+            const int last = min(32, parts - i0);
+#pragma unroll 1
+            for (int k0 = 0; k0 < last; k0 += 4) {
+                float4 v[4];
+                float w[4];
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-        l = l * f + sum;
-        m = up;
+                for (int k = 0; k < 4; ++k) {  // (a lane behind the last part has weight 0)
+                    const unsigned long long a = __shfl_sync(0xFFFFFFFFu, from, k0 + k);
+                    w[k] = __shfl_sync(0xFFFFFFFFu, fi, k0 + k);
+                    v[k] = on && k0 + k < last ? __ldcg(reinterpret_cast<const float4*>(a) + (e >> 2)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int e = (j * 32 + lane) * 4;
-            acc[j] = make_float4(acc[j].x * f, acc[j].y * f, acc[j].z * f, acc[j].w * f);
-            if (j * 128 >= p.head_dim) break;
-#pragma unroll 8
-            for (int k = 0; k < min(32, parts - i0); ++k) {
-                const float w = __shfl_sync(0xFFFFFFFFu, fi, k);
-                if (e < p.head_dim) {
-                    const float* from = (i0 + k < own ? p.own_o : lead_o) + place(i0 + k) * p.head_dim;
-                    const float4 v = __ldcg(reinterpret_cast<const float4*>(from + e));
-                    acc[j].x = fmaf(v.x, w, acc[j].x);
-                    acc[j].y = fmaf(v.y, w, acc[j].y);
-                    acc[j].z = fmaf(v.z, w, acc[j].z);
-                    acc[j].w = fmaf(v.w, w, acc[j].w);
+                for (int k = 0; k < 4; ++k) {
+                    acc.x = fmaf(v[k].x, w[k], acc.x);
+                    acc.y = fmaf(v[k].y, w[k], acc.y);
+                    acc.z = fmaf(v[k].z, w[k], acc.z);
+                    acc.w = fmaf(v[k].w, w[k], acc.w);
                 }
             }
         }
-    }
-    const float f = 1.0f / l;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int e = (j * 32 + lane) * 4;
-        if (e < p.head_dim)
-            *reinterpret_cast<uint2*>(out + e) =
-                make_uint2(pack16<kBf16>(acc[j].x * f, acc[j].y * f), pack16<kBf16>(acc[j].z * f, acc[j].w * f));
+        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
+        const float f = n == 0 ? 0.f : 1.0f / l;
+        if (on)
+            *reinterpret_cast<uint2*>(p.out + (int64_t)s * p.out_stride + head * p.head_dim + e) =
+                make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
+        if (lane == 0 && blockIdx.z == 0 && p.lse != nullptr)
+            p.lse[(int64_t)s * p.n_heads + head] = n == 0 ? __uint_as_float(0xFF800000u) : (m + log2f(l)) * (float)kLn2;
     }
-    if (lane == 0 && p.lse != nullptr) p.lse[row] = (m + log2f(l)) * (float)kLn2;
 }
 
 template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, int kUse>
@@ -1083,8 +1067,8 @@ cudaError_t launch_use(const AttendParams& p, const DeviceProps& dp, cudaStream_
     cudaError_t e = launch_dim<kBf16, kParts>(p, dp, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(((int64_t)p.n_streams * p.n_heads + 3) / 4));
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3(p.n_streams, p.n_heads / p.group, (p.head_dim + 127) / 128);
+    cfg.blockDim = dim3(kJoinWarps * 32);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

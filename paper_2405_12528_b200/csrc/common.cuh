@@ -190,7 +190,7 @@ constexpr int kPrefixRows = 128;   // rows of a block, at most
 struct PrefixPlan {
     float* part_o;            // [place][rows][head_dim], relative to 2^reference; null: not in use
     float2* part_ml;          // [place][rows] (reference in units of log2, sum)
-    int32_t* line;            // [0]: tiles per CTA; [1 + g]: first tile of group g in the line
+    int2* parts;              // [unit] its first part's CTA, how many parts
     int32_t block_streams;    // streams of a block
     int32_t blocks;           // blocks of a group
     int32_t pair;             // two blocks to a unit
@@ -234,7 +234,7 @@ struct AttendParams {
     // the one of unit u (of all members of the walk) and warp w in place u + w
     float* own_o;                            // [place][part_rows][head_dim], relative to 2^reference
     float2* own_ml;                          // [place][part_rows] (reference in units of log2, sum)
-    int32_t* part_line;                      // [0]: positions per warp; [1 + i]: where member i's units begin
+    int2* own_parts;                         // [unit] its first part's warp, how many parts
     int32_t part_rows;                       // query heads of a unit, at most
     int32_t lead_units;                      // groups whose shared slots are units of this kernel: all or none
     int32_t walk;                            // what the kernel walks through: lead_units + n_streams

@@ -186,6 +186,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
     __shared__ __align__(8) uint64_t s_full[2], p_full[2][2], o_full[2], o_empty, drained;
     __shared__ float2 stats[kPrefixRows];
     __shared__ Stretch first;
+    __shared__ int tiles_per_cta;
     __shared__ uint32_t tmem_base;
     __shared__ volatile int gave_up;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -219,19 +220,18 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
     }
     grid_dependency_wait();
     if (warp == 2) {
-        // the line: its length, this CTA's stretch, and (the first CTA) where every group begins
+        // the line: its length, and this CTA's stretch
         const int per_group = p.n_kv_heads * p.plan.units;
         const int T0 = lane < p.n_groups ? group_tiles(p, lane) : 0;
         int total = __reduce_add_sync(0xFFFFFFFFu, T0 * per_group);
         for (int g0 = 32; g0 < p.n_groups; g0 += 32)
             total += __reduce_add_sync(0xFFFFFFFFu, g0 + lane < p.n_groups ? group_tiles(p, g0 + lane) * per_group : 0);
         const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 2);
-        if (blockIdx.x == 0 && lane == 0) p.plan.line[0] = per;
         const int begin = (int)min((int64_t)blockIdx.x * per, (int64_t)total);
         Stretch w;
         w.left = min(per, total - begin);
         int before = 0;
-        for (int g0 = 0; g0 < p.n_groups && (before <= begin || blockIdx.x == 0); g0 += 32) {
+        for (int g0 = 0; g0 < p.n_groups && before <= begin; g0 += 32) {
             const int g = g0 + lane;
             const int T = g0 == 0 ? T0 : g < p.n_groups ? group_tiles(p, g) : 0;
             int upto = T * per_group;
@@ -240,7 +240,6 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                 if (lane >= o) upto += v;
             }
             const int start = before + upto - T * per_group;
-            if (blockIdx.x == 0 && g < p.n_groups) p.plan.line[1 + g] = start;
             if (w.left > 0 && T > 0 && begin >= start && begin < before + upto) {  // one lane, once
                 w.g = g;
                 w.u = (begin - start) / T;
@@ -250,6 +249,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
             }
             before += __shfl_sync(0xFFFFFFFFu, upto, 31);
         }
+        if (lane == 0) tiles_per_cta = per;
         if (w.left <= 0 && lane == 0) {
             w.left = 0;
             first = w;
@@ -512,6 +512,11 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                     ok = __all_sync(0xFFFFFFFFu, wait(&o_full[x], o_phase[x]));
                     o_phase[x] ^= 1u;
                 }
+            if (w.t0 == 0 && tid == kThreads - 1) {  // where the unit's parts are
+                const int behind = w.tiles - w.count();
+                p.plan.parts[w.g * p.n_kv_heads * p.plan.units + w.u] =
+                    make_int2(blockIdx.x, 1 + (behind + tiles_per_cta - 1) / tiles_per_cta);
+            }
             tmem_fence_after();
             float* dst = p.plan.part_o + place * p.head_dim;
             if (kPair) {
