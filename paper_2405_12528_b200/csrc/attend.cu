@@ -70,6 +70,11 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool v
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0)
                  : "memory");
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src),
+                 "r"(valid ? 16 : 0), "l"(policy)
+                 : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() {
@@ -468,6 +473,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     constexpr int kRowsAtOnce = 32 / kChunks;  // rows that one load instruction of the warp covers
     const int chunk = lane % kChunks, row_in = lane / kChunks;
     const bool chunk_on = chunk * 8 < p.head_dim;
+    // kParts: rows that are read once shall not push parts and instructions out of L2
+    uint64_t policy = 0;
+    if (kUse == kParts) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     auto load_next = [&](int stage) {  // the warp's next tile, if there is one, into a stage; one group
         while (ahead.more() && ahead_tile >= ahead.t1) {
             ahead.next(p, gap_all);
@@ -491,8 +499,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 int64_t o = valid ? off + (int64_t)r * p.head_dim * 2 : off;
                 if (kUse != kPlain && slot0 + r < ahead.shared) o += to_lead;
                 const uint32_t d = dst0 + r * (kDim * 2) + ((chunk ^ (r & 7)) << 4);
-                cp_async16(d, p.k + o, valid);
-                cp_async16(d + kTileBytes, p.v + o, valid);
+                if (kUse == kParts) {
+                    cp_async16(d, p.k + o, valid, policy);
+                    cp_async16(d + kTileBytes, p.v + o, valid, policy);
+                } else {
+                    cp_async16(d, p.k + o, valid);
+                    cp_async16(d + kTileBytes, p.v + o, valid);
+                }
             }
             ahead_tile += stride;
         }
