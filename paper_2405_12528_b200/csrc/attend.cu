@@ -911,35 +911,32 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 
 // The parts of every stream's heads into the result: those of the stream's own slots, then those of the
 // group's.  A block per stream, K/V head and 128 elements, a warp per query head, four elements per lane.
-// (What is executed once costs its way from L2 into the instruction cache, 250 cycles per 8 instructions:
-// with divisions for the places of the parts, and unrolled, this took 13 us instead of 5.)
+// (What is executed once costs its way from L2 into the instruction cache, 250 cycles and more per 8
+// instructions: with divisions for the places of the parts, and unrolled, this took 13 us.)
 template <bool kBf16>
 __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const AttendParams p) {
     const int lane = threadIdx.x & 31, s = blockIdx.x, kv_head = blockIdx.y, e = (int)blockIdx.z * 128 + lane * 4;
     const int g = s / p.stream_group, local = s - g * p.stream_group, kv_heads = gridDim.y;
-    grid_dependency_wait();
     grid_launch_dependents();
-    const int n = p.kv_len[s], shared = p.shared_len[g];
-    if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
-        if (threadIdx.x == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
-        return;
-    }
-    const bool with_lead = first_slot(p, shared, n) > 0, on = e < p.head_dim;
-    const bool product = p.lead_units == 0;
+    const bool on = e < p.head_dim, product = p.lead_units == 0;
     int lead_unit = g * kv_heads + kv_head, in_block = 0;
     if (product && p.prefix.pair) {
         in_block = local / p.prefix.block_streams;
         lead_unit = lead_unit * p.prefix.units + (in_block >> 1);
     }
-    const int2 lead = !with_lead ? make_int2(0, 0) : __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
+    // The first time round is a rehearsal, in the shadow of the kernel before: it writes nothing.
+    int n = 1;
+    int2 lead = make_int2(0, 0);
+    bool real = false;
+again:
     for (int hq = threadIdx.x >> 5; hq < p.group; hq += kJoinWarps) {
         const int64_t head = kv_head * p.group + hq;
         const int block = hq >= p.part_rows ? hq / p.part_rows : 0;
         const int64_t unit = (int64_t)(p.lead_units + s) * p.units + kv_head * p.blocks + block;
-        const int2 own = n == 0 ? make_int2(0, 0) : __ldcg(p.own_parts + unit);
+        const int2 own = n == 0 ? make_int2(0, 0) : real ? __ldcg(p.own_parts + unit) : make_int2(0, 1);
         const int parts = own.y + lead.y, lead_row = (local - in_block * p.prefix.block_streams) * p.group + hq;
         // from part i - own.y on: rows of the group's
-        const int64_t own_at = (unit + own.x) * p.part_rows + hq - block * p.part_rows;
+        const int64_t own_at = real ? (unit + own.x) * p.part_rows + hq - block * p.part_rows : 0;
         const int64_t lead_at = product ? ((int64_t)lead_unit + lead.x) * p.prefix.rows + lead_row + (in_block & 1) * kPrefixRows
                                         : ((int64_t)g * p.units + kv_head + lead.x) * p.part_rows + lead_row;
         const int lead_step = product ? p.prefix.rows : p.part_rows;
@@ -985,12 +982,23 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const AttendParam
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
         const float f = n == 0 ? 0.f : 1.0f / l;
-        if (on)
+        if (on && real)
             *reinterpret_cast<uint2*>(p.out + (int64_t)s * p.out_stride + head * p.head_dim + e) =
                 make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
-        if (lane == 0 && blockIdx.z == 0 && p.lse != nullptr)
+        if (lane == 0 && blockIdx.z == 0 && p.lse != nullptr && real)
             p.lse[(int64_t)s * p.n_heads + head] = n == 0 ? __uint_as_float(0xFF800000u) : (m + log2f(l)) * (float)kLn2;
     }
+    if (real) return;
+    grid_dependency_wait();
+    n = p.kv_len[s];
+    const int shared = p.shared_len[g];
+    if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
+        if (threadIdx.x == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
+        return;
+    }
+    if (first_slot(p, shared, n) > 0) lead = __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
+    real = true;
+    goto again;
 }
 
 template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, int kUse>
