@@ -21,6 +21,7 @@ namespace {
 constexpr int kThreads = kBeamThreads;
 constexpr int kWarps = kThreads / 32;
 constexpr int kList = 1024;
+constexpr int kFewOut = 8;
 
 // log2 e in two parts: the product's bias would show in lse (1.3e-8 of the distance to the maximum)
 constexpr float kLog2eHi = 1.4426950216293335f, kLog2eLo = 1.9259629e-8f;
@@ -42,7 +43,7 @@ __device__ __forceinline__ double from_key64(unsigned long long k) {
 // A bound that n of the threads' values reach, or the lowest value where too few threads have one
 // (`lowest` says that a thread has none); syncs.
 __device__ __forceinline__ float reach_by_warps(float mine, float warp_top, float lowest, int n, float (&tops)[kWarps],
-                                                float (&bounds)[kWarps], float& top) {
+                                                float (&bounds)[kWarps], float (&nths)[kWarps], float& top) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) tops[warp] = warp_top;
     __syncthreads();
@@ -53,23 +54,33 @@ __device__ __forceinline__ float reach_by_warps(float mine, float warp_top, floa
         with += tops[w] > lowest;
         top = fmaxf(top, tops[w]);
     }
-    // k-th largest of the warp
-    uint32_t key = key_of(mine), bound = 0;
+    // The k-th largest of the warp, k * warps >= n: the least of those is reached by n values.  And the n-th
+    // largest of the warp, for small n: the largest of those is, too.
+    uint32_t key = key_of(mine), bound = 0, nth = 0;
     if (warp_top > lowest) {
+        const int k = (n + with - 1) / with;
 #pragma unroll 1
-        for (int left = n; left > 0; left -= with) {
-            bound = __reduce_max_sync(0xFFFFFFFFu, key);
-            const uint32_t who = __ballot_sync(0xFFFFFFFFu, key == bound);
+        for (int i = 1; i <= max(k, n <= kFewOut ? n : 0); ++i) {
+            const uint32_t high = __reduce_max_sync(0xFFFFFFFFu, key);
+            if (i == k) bound = high;
+            nth = high;
+            const uint32_t who = __ballot_sync(0xFFFFFFFFu, key == high);
             if (lane == __ffs(who) - 1) key = 0;
         }
     }
     // (more than 32 rounds, or lanes without a value, end at or below the lowest)
-    if (lane == 0) bounds[warp] = warp_top > lowest ? (bound == 0 ? lowest : from_key(bound)) : __uint_as_float(0x7F800000u);
+    if (lane == 0) {
+        bounds[warp] = warp_top > lowest ? (bound == 0 ? lowest : from_key(bound)) : __uint_as_float(0x7F800000u);
+        nths[warp] = nth == 0 || n > kFewOut ? lowest : from_key(nth);
+    }
     __syncthreads();
-    float reach = bounds[0];
+    float reach = bounds[0], other = nths[0];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) reach = fminf(reach, bounds[w]);
-    return reach;
+    for (int w = 1; w < kWarps; ++w) {
+        reach = fminf(reach, bounds[w]);
+        other = fmaxf(other, nths[w]);
+    }
+    return fmaxf(reach, other);
 }
 // the n-th largest of the threads' values (n <= kThreads), the same for all; syncs
 __device__ __noinline__ float reach_by_threads(float mine, uint32_t* all, uint32_t* found, int n) {
@@ -128,12 +139,11 @@ __device__ __forceinline__ float largest(const uint4& v) {
 struct BeamShared {
     uint32_t maxima[kThreads];
     uint32_t bound;
-    float tops[kWarps], bounds[kWarps], sums[kWarps];
+    float tops[kWarps], bounds[kWarps], nths[kWarps], sums[kWarps];
     int listed, last_one;
-    union {
-        unsigned long long list[kList];
-        Found found[kList];
-    };
+    unsigned long long list[kList];    // a chunk's candidates; of a group's, the scores ...
+    unsigned long long list_at[kList]; // ... the places
+    float list_z[kList];               // ... and the logits
     unsigned long long best[kBeamMaxOut];
     unsigned long long warp_best[kWarps];
     Found warp_found[kWarps], chosen[kBeamMaxOut];
@@ -233,7 +243,7 @@ __device__ __forceinline__ void scan_chunk(const BeamParams& p, BeamShared& sh, 
     if (tid < kBeamMaxOut) sh.best[tid] = 0;  // no candidate
     float top;
     const float warp_top = from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(m)));
-    const float reach = reach_by_warps(m, warp_top, lowest, p.n_out, sh.tops, sh.bounds, top);
+    const float reach = reach_by_warps(m, warp_top, lowest, p.n_out, sh.tops, sh.bounds, sh.nths, top);
     const bool any = top > lowest;
     // element j of vector i, and its token
     auto value = [&](const uint4& v, int j) {
@@ -244,19 +254,29 @@ __device__ __forceinline__ void scan_chunk(const BeamParams& p, BeamShared& sh, 
     auto candidate = [&](float z, int i, int j) {
         return ((unsigned long long)key_of(z) << 32) | (0xFFFFFFFFu - (uint32_t)(e_first + i * kThreads * kPer + j));
     };
-    if (m >= reach && any) {
+    uint32_t hits = 0;  // vectors that reach it
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const float high = largest<kBf16>(raw[i]);
-            if (high >= reach && high > lowest) {
+    for (int i = 0; i < kVecs; ++i) {
+        const float high = largest<kBf16>(raw[i]);
+        hits |= (uint32_t)(high >= reach && high > lowest) << i;
+    }
+    // One copy of the code for all of them (unrolled, the instructions' way into the cache took 10 us): the
+    // few vectors are read again, from L2.
 #pragma unroll 1
-                for (int j = 0; j < kPer; ++j) {
-                    const float z = value(raw[i], j);
-                    if (z >= reach && z > lowest) {
-                        const int n = atomicAdd(&sh.listed, 1);
-                        if (n < kList) sh.list[n] = candidate(z, i, j);
-                    }
-                }
+    for (; hits != 0; hits &= hits - 1) {
+        const int i = __ffs(hits) - 1;
+        const int64_t e0 = e_first + i * kThreads * kPer;
+        uint4 v;
+        if (e0 >= 0 && e0 + kPer <= p.vocab)
+            v = __ldg(reinterpret_cast<const uint4*>(at + i * kThreads * 16));
+        else
+            v = edge_vector<kBf16>(at + i * kThreads * 16, e0, p.vocab);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const float z = value(v, j);
+            if (z >= reach && z > lowest) {
+                const int n = atomicAdd(&sh.listed, 1);
+                if (n < kList) sh.list[n] = candidate(z, i, j);
             }
         }
     }
@@ -371,7 +391,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
     }
     float top;
     float reach = reach_by_warps(mine, from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(mine))), none, p.n_out, sh.tops,
-                                 sh.bounds, top);
+                                 sh.bounds, sh.nths, top);
     if (tid < p.n_out) sh.chosen[tid].score = 0;
     int n;
 #pragma unroll 1
@@ -383,7 +403,11 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
                 candidate(i, f);
                 if (f.score == 0 || rounded(f.score) < reach) continue;
                 const int at = atomicAdd(&sh.listed, 1);
-                if (at < kList) sh.found[at] = f;
+                if (at < kList) {
+                    sh.list[at] = f.score;
+                    sh.list_at[at] = f.at;
+                    sh.list_z[at] = f.z;
+                }
             }
         }
         __syncthreads();
@@ -396,10 +420,15 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
     if (n <= kList) {
 #pragma unroll 1
         for (int i = tid; i < n; i += kThreads) {
-            const Found f = sh.found[i];
+            const unsigned long long score = sh.list[i], at = sh.list_at[i];
             int rank = 0;
-            for (int j = 0; j < n; ++j) rank += better(sh.found[j].score, sh.found[j].at, f.score, f.at);
-            if (rank < p.n_out) sh.chosen[rank] = f;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) {
+                const unsigned long long x = sh.list[j];
+                rank += x > score;
+                if (x == score) rank += sh.list_at[j] < at;
+            }
+            if (rank < p.n_out) sh.chosen[rank] = {score, at, sh.list_z[i]};
         }
     } else {
         unsigned long long last_score = ~0ull, last_at = 0;
