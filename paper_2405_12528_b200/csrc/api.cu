@@ -122,15 +122,19 @@ AttendLayout attend_layout(const sirllm_config& c) {
     return L;
 }
 
-// Chunks of 32 KB of a row, or of 16, 8, 4 KB where that leaves fewer than two for every SM.
+// Segments of a row, one warp each: as many trips of the lanes as leave one segment for every warp that
+// the GPU holds (148 SMs, 32 warps each; on another one only the balance differs), 64 at most.
 static BeamTiling beam_tiling(const sirllm_config& c) {
-    const int64_t per = 16 / logits_elem_bytes(c.logits_dtype);
+    const int64_t trip = kBeamTripBytes / logits_elem_bytes(c.logits_dtype), per = 16 / logits_elem_bytes(c.logits_dtype);
+    const int64_t row_trips = (c.vocab + per - 1 + trip - 1) / trip;  // a row may begin anywhere within a vector
     BeamTiling t;
-    for (t.vecs = 8;; t.vecs /= 2) {
-        const int64_t chunk = (int64_t)t.vecs * kBeamThreads * per;
-        t.parts = (c.vocab + per - 1 + chunk - 1) / chunk;  // a row may begin anywhere within a vector
-        if (t.vecs == 1 || t.parts * c.n_streams >= 296) return t;
-    }
+    int64_t trips = (row_trips * c.n_streams + 148 * 32 - 1) / (148 * 32);
+    if (trips > 64) trips = 64;
+    if (trips > row_trips) trips = row_trips;
+    t.trips = (int32_t)trips;
+    t.parts = (row_trips + trips - 1) / trips;
+    t.blocks = (int32_t)((c.vocab + per - 1 + 32 * per - 1) / (32 * per));
+    return t;
 }
 
 // How sirllm_attend_shared goes about a call, and its workspace: attend's own, then the parts.
@@ -182,12 +186,12 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
 static BeamLayout beam_layout(const sirllm_config& c) {
     BeamLayout L;
     L.tiling = beam_tiling(c);
-    const size_t chunks = (size_t)c.n_streams * L.tiling.parts;
+    const size_t segments = (size_t)c.n_streams * L.tiling.parts;
     L.tickets_off = 256;
     L.pairs_off = align_up(L.tickets_off + (size_t)c.n_streams * 4, 256);
     L.zeroed = L.pairs_off;
-    L.cands_off = align_up(L.pairs_off + chunks * sizeof(float2), 256);
-    L.total = align_up(L.cands_off + chunks * kBeamMaxOut * 8, 256);
+    L.block_max_off = align_up(L.pairs_off + segments * sizeof(float2), 256);
+    L.total = align_up(L.block_max_off + (size_t)c.n_streams * L.tiling.blocks * sizeof(float), 256);
     return L;
 }
 
@@ -921,7 +925,7 @@ int sirllm_beam_workspace_init(const sirllm_config* cfg, void* ws, void* cuda_st
     if (rc != SIRLLM_OK) return rc;
     if (ws == nullptr) return SIRLLM_ERR_NULL;
     if (misaligned(ws, 256)) return SIRLLM_ERR_ALIGN;
-    // the candidates are written before they are read; status word and tickets must start at zero
+    // the rest is written before it is read; status word and tickets must start at zero
     cudaError_t e = cudaMemsetAsync(ws, 0, beam_layout(*cfg).zeroed, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "cudaMemsetAsync");
 }
@@ -939,7 +943,7 @@ int sirllm_beam_select(const sirllm_config* cfg, const void* logits, int32_t gro
     if (group > SIRLLM_MAX_BEAMS || n_out > SIRLLM_MAX_BEAMS) return SIRLLM_ERR_TOO_LARGE;
     if (n_out != group && (totals_out == totals || (ended && ended_out == ended))) return SIRLLM_ERR_BAD_CONFIG;
     const BeamLayout L = beam_layout(*cfg);
-    if (L.tiling.parts * cfg->n_streams > 0x7FFFFFFF || (int64_t)L.tiling.parts * group * n_out > 0x7FFFFFFF)
+    if (L.tiling.parts * cfg->n_streams > 0x7FFFFFFF || (int64_t)L.tiling.blocks * group > 0x7FFFFFFF - kBeamThreads)
         return SIRLLM_ERR_TOO_LARGE;
     if ((rc = check_logits(*cfg, logits)) != SIRLLM_OK) return rc;
     const void* words[7] = {totals, ended, totals_out, source, token_ids, entropy, ended_out};
@@ -958,7 +962,7 @@ int sirllm_beam_select(const sirllm_config* cfg, const void* logits, int32_t gro
     p.ended_out = ended_out;
     p.tickets = (int32_t*)((char*)ws + L.tickets_off);
     p.pairs = (float2*)((char*)ws + L.pairs_off);
-    p.cands = (unsigned long long*)((char*)ws + L.cands_off);
+    p.block_max = (float*)((char*)ws + L.block_max_off);
     p.vocab = cfg->vocab;
     p.row_stride = cfg->logits_row_stride;
     p.n_streams = cfg->n_streams;
@@ -967,7 +971,8 @@ int sirllm_beam_select(const sirllm_config* cfg, const void* logits, int32_t gro
     p.end_token = end_token;
     p.places = places != 0;
     p.parts = (int32_t)L.tiling.parts;
-    p.vecs = L.tiling.vecs;
+    p.trips = L.tiling.trips;
+    p.blocks = L.tiling.blocks;
     p.logits_dtype = cfg->logits_dtype;
     cudaError_t e = launch_beam(p, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? SIRLLM_OK : cuda_fail(e, "beam_select");

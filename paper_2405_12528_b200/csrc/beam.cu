@@ -3,15 +3,20 @@
 // over the group's streams s and all tokens v, the n_out largest in order.  An ended beam is one
 // candidate, with its total.  Equal scores: the lower stream, then the lower token.
 //
-// The logits are read once and that is the bound: rows * V elements, a few bytes out.  A CTA takes
-// a chunk of one row (up to 32 KB, kept in registers), and gives (max, sum exp) and the chunk's n_out
-// best logits; the CTA that finishes a group last joins them: sums in fp64, candidates ranked by
-// their score in fp64.  Within a row the order of the logits is the order of the scores.
-// The n_out best of many values, twice: every thread knows the largest of its own.  The k-th largest of
-// every warp's, k * warps >= n_out, the least of them over the warps, is a bound that n_out values reach;
-// what reaches it is listed (a few times n_out) and the list is ranked by counting.  A list that
+// The logits are read once and that is the bound: rows * V elements, a few bytes out.  A warp streams a
+// segment of one row and keeps the running maximum and sum per lane; of every block of 512 bytes it leaves
+// the largest logit, and looks for no candidates.  The CTA whose warp finishes a group last joins its
+// segments (sums in fp64) and takes the n_out best BLOCKS of the group, by their largest logit's score and
+// then by place: they hold the n_out best candidates, for each of n_out better blocks would bring a
+// better candidate.  Only those few blocks are read again.  Scores are compared in fp64; within a row
+// the order of the logits is the order of the scores.
+// The n_out best of many: every thread knows the best of its own.  The k-th largest of every warp's,
+// k * warps >= n_out, the least of them over the warps, is a bound that n_out values reach (and so is the
+// largest of the warps' n_out-th); what reaches it is listed and ranked by counting.  A list that
 // overflows is made again with the n_out-th largest of all threads' as the bound, and if that overflows
-// too (thousands of equal logits) the best come out in n_out rounds of maximum: slow, and right.
+// too (thousands of equal scores) the best come out in n_out rounds of maximum: slow, and right.
+// On the way here, 512 x 128256 bf16: chunks of 32 KB per CTA, with barriers between loading, bounding,
+// listing and ranking, 61 us; warps that keep lists of their own while they stream, 83 us.
 #include "common.cuh"
 
 namespace sirllm {
@@ -21,7 +26,8 @@ namespace {
 constexpr int kThreads = kBeamThreads;
 constexpr int kWarps = kThreads / 32;
 constexpr int kList = 1024;
-constexpr int kFewOut = 8;
+constexpr int kStep = 4;   // vectors of a lane per trip: blocks of a trip
+static_assert(kStep * 512 == kBeamTripBytes, "a trip is kStep blocks");
 
 // log2 e in two parts: the product's bias would show in lse (1.3e-8 of the distance to the maximum)
 constexpr float kLog2eHi = 1.4426950216293335f, kLog2eLo = 1.9259629e-8f;
@@ -60,7 +66,7 @@ __device__ __forceinline__ float reach_by_warps(float mine, float warp_top, floa
     if (warp_top > lowest) {
         const int k = (n + with - 1) / with;
 #pragma unroll 1
-        for (int i = 1; i <= max(k, n <= kFewOut ? n : 0); ++i) {
+        for (int i = 1; i <= max(k, n <= 32 ? n : 0); ++i) {
             const uint32_t high = __reduce_max_sync(0xFFFFFFFFu, key);
             if (i == k) bound = high;
             nth = high;
@@ -71,7 +77,7 @@ __device__ __forceinline__ float reach_by_warps(float mine, float warp_top, floa
     // (more than 32 rounds, or lanes without a value, end at or below the lowest)
     if (lane == 0) {
         bounds[warp] = warp_top > lowest ? (bound == 0 ? lowest : from_key(bound)) : __uint_as_float(0x7F800000u);
-        nths[warp] = nth == 0 || n > kFewOut ? lowest : from_key(nth);
+        nths[warp] = nth == 0 || n > 32 ? lowest : from_key(nth);
     }
     __syncthreads();
     float reach = bounds[0], other = nths[0];
@@ -103,9 +109,12 @@ struct Found {                // one candidate of a group
     unsigned long long at;     // (row within the group) << 32 | token
     float z;                   // its logit
 };
-__device__ __forceinline__ bool better(unsigned long long sa, unsigned long long aa, unsigned long long sb,
-                                       unsigned long long ab) {
-    return sa > sb || (sa == sb && aa < ab);
+// Of equal scores: the lower stream, then the larger logit (a huge total hides it), then the lower token.
+__device__ __forceinline__ bool ahead(unsigned long long at_a, float za, unsigned long long at_b, float zb) {
+    return (at_a >> 32) == (at_b >> 32) && za != zb ? za > zb : at_a < at_b;
+}
+__device__ __forceinline__ bool better(const Found& a, const Found& b) {
+    return a.score > b.score || (a.score == b.score && ahead(a.at, a.z, b.at, b.z));
 }
 
 // 16 bytes of a row of which some elements lie outside [0, vocab): those count as -inf
@@ -137,194 +146,157 @@ __device__ __forceinline__ float largest(const uint4& v) {
 }
 
 struct BeamShared {
+    unsigned long long list[kList];    // what reaches the bound: scores,
+    unsigned long long list_at[kList]; // places
+    float list_z[kList];               // and logits
     uint32_t maxima[kThreads];
     uint32_t bound;
-    float tops[kWarps], bounds[kWarps], nths[kWarps], sums[kWarps];
-    int listed, last_one;
-    unsigned long long list[kList];    // a chunk's candidates; of a group's, the scores ...
-    unsigned long long list_at[kList]; // ... the places
-    float list_z[kList];               // ... and the logits
-    unsigned long long best[kBeamMaxOut];
-    unsigned long long warp_best[kWarps];
-    Found warp_found[kWarps], chosen[kBeamMaxOut];
+    float tops[kWarps], bounds[kWarps], nths[kWarps];
+    int listed, ended_groups[kWarps];
+    Found warp_found[kWarps], chosen[2][kBeamMaxOut];  // the best blocks, the best candidates
     // of a group's rows.  Score of a logit: total + ((z - top) - log sum), top the row's maximum: the
     // differences stay exact where a mask of the type's lowest value is all there is.  A row without
     // candidates has total -inf.
     double total_of[kBeamMaxGroup], log_of[kBeamMaxGroup];
-    float top_of[kBeamMaxGroup];
+    float top_of[kBeamMaxGroup], const_of[kBeamMaxGroup];  // const: total - log sum, -inf for a row without logits that count
+    int skew_of[kBeamMaxGroup];                            // elements between a row and its first block's start
+    __device__ __forceinline__ double score(unsigned long long at, float z) const {
+        const int r = (int)(at >> 32);
+        return ended_row[r] ? total_of[r] : total_of[r] + (((double)z - (double)top_of[r]) - log_of[r]);
+    }
+    int strip_row[kBeamMaxOut], strip_at[kBeamMaxOut];     // the best blocks: row (-1: none), first element
     unsigned char ended_row[kBeamMaxGroup];
     int first_of[kBeamMaxGroup];       // the first candidate of every row
     uint32_t placed[2], taken[2];      // candidates with a place of their own, places taken
 };
 
-// What the chunk's list could not hold: from the logits again.
+// One warp's segment of a row: p.trips trips of kStep vectors per lane.
 template <bool kBf16>
-__device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, int row, int64_t first, int length, float m) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const float lowest = __uint_as_float(0xFF800000u);
-    const int begin = first < 0 ? (int)-first : 0, end = (int)min((int64_t)length, p.vocab - first);
-    auto logit = [&](int i) {
-        const int64_t at = (int64_t)row * p.row_stride + first + i;
-        return kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p.logits)[at] << 16)
-                     : static_cast<const float*>(p.logits)[at];
-    };
-    auto candidate = [&](float z, int i) { return ((unsigned long long)key_of(z) << 32) | (0xFFFFFFFFu - (uint32_t)(first + i)); };
-    __syncthreads();
-    if (tid == 0) sh.listed = 0;
-    const float reach = reach_by_threads(m, sh.maxima, &sh.bound, p.n_out);
-    for (int i = begin + tid; i < end; i += kThreads) {
-        const float z = logit(i);
-        if (z >= reach && z > lowest) {
-            const int n = atomicAdd(&sh.listed, 1);
-            if (n < kList) sh.list[n] = candidate(z, i);
-        }
-    }
-    __syncthreads();
-    const int n = sh.listed;
-    if (n <= kList) {
-        for (int i = tid; i < n; i += kThreads) {
-            const unsigned long long mine = sh.list[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += sh.list[j] > mine;
-            if (rank < p.n_out) sh.best[rank] = mine;
-        }
-        return;
-    }
-    unsigned long long below = ~0ull;
-    for (int r = 0; r < p.n_out; ++r) {
-        unsigned long long mine = 0;
-        for (int i = begin + tid; i < end; i += kThreads) {
-            const float z = logit(i);
-            const unsigned long long c = candidate(z, i);
-            if (z > lowest && c < below && c > mine) mine = c;
-        }
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) {
-            const unsigned long long o = __shfl_xor_sync(0xFFFFFFFFu, mine, x);
-            if (o > mine) mine = o;
-        }
-        if (lane == 0) sh.warp_best[warp] = mine;
-        __syncthreads();
-        for (int w = 0; w < kWarps; ++w)
-            if (sh.warp_best[w] > mine) mine = sh.warp_best[w];
-        if (tid == 0) sh.best[r] = mine;
-        below = mine;
-        __syncthreads();
-    }
-}
-
-// kVecs 16-byte vectors of a row per thread
-template <bool kBf16, int kVecs>
-__device__ __forceinline__ void scan_chunk(const BeamParams& p, BeamShared& sh, int row, int part) {
+__device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int part) {
     constexpr int kPer = kBf16 ? 8 : 4;  // elements of a vector
     constexpr int kSize = kBf16 ? 2 : 4;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    // ---- the chunk, as aligned vectors; what lies outside the row counts as -inf ------------------
+    const int lane = threadIdx.x & 31;
+    // as aligned vectors; what lies outside the row counts as -inf
     const char* row_at = static_cast<const char*>(p.logits) + (int64_t)row * p.row_stride * kSize;
     const int skew = (int)(((uintptr_t)row_at & 15) / kSize);  // elements in front of the row
-    const int64_t e_first = (int64_t)part * kVecs * kThreads * kPer + tid * kPer - skew;  // this thread's first element
-    const char* at = row_at + e_first * kSize;
-    uint4 raw[kVecs];
+    const int first_block = part * p.trips * kStep;
+    const int trips = min(p.trips, (p.blocks - first_block + kStep - 1) / kStep);
+    int64_t e_next = ((int64_t)first_block * 32 + lane) * kPer - skew;  // first element of the lane's next vector
+    auto load = [&](uint4 (&v)[kStep]) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int64_t e0 = e_first + i * kThreads * kPer;
-        if (e0 >= 0 && e0 + kPer <= p.vocab)
-            asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                         : "=r"(raw[i].x), "=r"(raw[i].y), "=r"(raw[i].z), "=r"(raw[i].w)
-                         : "l"(at + i * kThreads * 16));
-        else
-            raw[i] = edge_vector<kBf16>(at + i * kThreads * 16, e0, p.vocab);
-    }
-    const float lowest = __uint_as_float(0xFF800000u);
-    float m = lowest;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) m = fmaxf(m, largest<kBf16>(raw[i]));
-    if (tid == 0) sh.listed = 0;
-    if (tid < kBeamMaxOut) sh.best[tid] = 0;  // no candidate
-    float top;
-    const float warp_top = from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(m)));
-    const float reach = reach_by_warps(m, warp_top, lowest, p.n_out, sh.tops, sh.bounds, sh.nths, top);
-    const bool any = top > lowest;
-    // element j of vector i, and its token
-    auto value = [&](const uint4& v, int j) {
+        for (int i = 0; i < kStep; ++i) {
+            const int64_t e0 = e_next + i * 32 * kPer;
+            const char* at = row_at + e0 * kSize;
+            if (e0 >= 0 && e0 + kPer <= p.vocab)
+                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                             : "l"(at));
+            else
+                v[i] = edge_vector<kBf16>(at, e0, p.vocab);
+        }
+        e_next += kStep * 32 * kPer;
+    };
+    auto value = [&](const uint4& v, int j) {  // element j
         const uint32_t w = (kBf16 ? j >> 1 : j) == 0 ? v.x : (kBf16 ? j >> 1 : j) == 1 ? v.y : (kBf16 ? j >> 1 : j) == 2 ? v.z : v.w;
         if (!kBf16) return __uint_as_float(w);
         return __uint_as_float((j & 1) ? (w & 0xFFFF0000u) : (w << 16));
     };
-    auto candidate = [&](float z, int i, int j) {
-        return ((unsigned long long)key_of(z) << 32) | (0xFFFFFFFFu - (uint32_t)(e_first + i * kThreads * kPer + j));
-    };
-    uint32_t hits = 0;  // vectors that reach it
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const float high = largest<kBf16>(raw[i]);
-        hits |= (uint32_t)(high >= reach && high > lowest) << i;
-    }
-    // One copy of the code for all of them (unrolled, the instructions' way into the cache took 10 us): the
-    // few vectors are read again, from L2.
+    float top = -3.4028235e38f, sum = 0.f;
+    float* block_max = p.block_max + (int64_t)row * p.blocks + first_block;
+    uint4 cur[kStep], next[kStep];
+    if (trips > 0) load(next);
 #pragma unroll 1
-    for (; hits != 0; hits &= hits - 1) {
-        const int i = __ffs(hits) - 1;
-        const int64_t e0 = e_first + i * kThreads * kPer;
-        uint4 v;
-        if (e0 >= 0 && e0 + kPer <= p.vocab)
-            v = __ldg(reinterpret_cast<const uint4*>(at + i * kThreads * 16));
-        else
-            v = edge_vector<kBf16>(at + i * kThreads * 16, e0, p.vocab);
+    for (int t = 0; t < trips; ++t) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const float z = value(v, j);
-            if (z >= reach && z > lowest) {
-                const int n = atomicAdd(&sh.listed, 1);
-                if (n < kList) sh.list[n] = candidate(z, i, j);
-            }
+        for (int i = 0; i < kStep; ++i) cur[i] = next[i];
+        if (t + 1 < trips) load(next);
+        float m = top;
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+            const float high = largest<kBf16>(cur[i]);
+            m = fmaxf(m, high);
+            const uint32_t key = __reduce_max_sync(0xFFFFFFFFu, key_of(high));
+            if (lane == i) mine = key;
         }
-    }
-    // ---- the sum ------------------------------------------------------------------------------
-    uint64_t sum2[2] = {0, 0};
-    if (any) {
+        if (lane < kStep && first_block + t * kStep + lane < p.blocks) block_max[t * kStep + lane] = from_key(mine);
+        sum *= exp_of(top - m);
+        top = m;
         const uint64_t minus_top = pack2(-top, -top), hi = pack2(kLog2eHi, kLog2eHi), lo = pack2(kLog2eLo, kLog2eLo);
+        uint64_t sum2[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i)
+        for (int i = 0; i < kStep; ++i)
 #pragma unroll
             for (int j = 0; j < kPer; j += 2) {
-                const uint64_t t = add2(pack2(value(raw[i], j), value(raw[i], j + 1)), minus_top);
+                const uint64_t d = add2(pack2(value(cur[i], j), value(cur[i], j + 1)), minus_top);
                 float a, b;
-                unpack2(fma2(t, lo, mul2(t, hi)), a, b);
+                unpack2(fma2(d, lo, mul2(d, hi)), a, b);
                 sum2[(j >> 1) & 1] = add2(sum2[(j >> 1) & 1], pack2(ex2_approx(a), ex2_approx(b)));
             }
+        float s0, s1;
+        unpack2(add2(sum2[0], sum2[1]), s0, s1);
+        sum += s0 + s1;
     }
-    float s0, s1;
-    unpack2(add2(sum2[0], sum2[1]), s0, s1);
-    float sum = s0 + s1;
+    const float all = from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(top)));
+    sum *= exp_of(top - all);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-    if (lane == 0) sh.sums[warp] = sum;
+    if (lane == 0) p.pairs[(int64_t)row * p.parts + part] = make_float2(all, sum);  // (a sum of 0: nothing but -inf)
+}
+
+// What the list could not hold, in rounds of maximum: blocks (level 0) or candidates (level 1).
+template <bool kBf16>
+__device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, int g, int level) {
+    constexpr int kBlock = kBf16 ? 256 : 128;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row0 = g * p.group;
+    const int strips = level == 0 ? p.group : p.n_out, length = level == 0 ? p.blocks : kBlock;
+    Found last = {~0ull, 0, 0.f};
     __syncthreads();
-    // ---- the chunk's best ----------------------------------------------------------------------
-    const int n = sh.listed;
-    if (n <= kList) {
-        for (int i = tid; i < n; i += kThreads) {
-            const unsigned long long mine = sh.list[i];
-            int rank = 0;
-#pragma unroll 4
-            for (int j = 0; j < n; ++j) rank += sh.list[j] > mine;
-            if (rank < p.n_out) sh.best[rank] = mine;
+    for (int round = 0; round < p.n_out; ++round) {
+        Found own = {0, ~0ull, 0.f};
+        auto offer = [&](int r, int b, float z) {
+            const unsigned long long at = ((unsigned long long)r << 32) | (uint32_t)b;
+            const Found f = {key64_of(sh.score(at, z)), at, z};
+            if (better(last, f) && better(f, own)) own = f;
+        };
+        for (int i = tid; i < strips * length; i += kThreads) {
+            const int strip = i / length, off = i - strip * length, r = level == 0 ? strip : sh.strip_row[strip];
+            if (r < 0 || sh.ended_row[r] || !(sh.total_of[r] > -INFINITY)) continue;
+            float z = __uint_as_float(0xFF800000u);
+            int b = off;
+            if (level == 0) {
+                z = __ldcg(&p.block_max[(int64_t)(row0 + r) * p.blocks + b]);
+            } else {
+                b = sh.strip_at[strip] + off - sh.skew_of[r];
+                const int64_t at = (int64_t)(row0 + r) * p.row_stride + b;
+                if (b >= 0 && b < p.vocab)
+                    z = kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p.logits)[at] << 16)
+                              : static_cast<const float*>(p.logits)[at];
+            }
+            if (z > -INFINITY) offer(r, b, z);
         }
-    } else {
-        best_of_many<kBf16>(p, sh, row, (int64_t)part * kVecs * kThreads * kPer - skew, kVecs * kThreads * kPer, m);
-    }
-    __syncthreads();
-    if (tid < p.n_out) p.cands[(int64_t)blockIdx.x * p.n_out + tid] = sh.best[tid];
-    if (tid == 0) {
-        float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) s += sh.sums[w];
-        p.pairs[blockIdx.x] = any ? make_float2(top, s) : make_float2(0.f, 0.f);
+        for (int r = tid; r < p.group; r += kThreads)
+            if (sh.ended_row[r] && sh.total_of[r] > -INFINITY) offer(r, 0, 0.f);
+        for (int x = 16; x > 0; x >>= 1) {
+            Found o;
+            o.score = __shfl_xor_sync(0xFFFFFFFFu, own.score, x);
+            o.at = __shfl_xor_sync(0xFFFFFFFFu, own.at, x);
+            o.z = __shfl_xor_sync(0xFFFFFFFFu, own.z, x);
+            if (better(o, own)) own = o;
+        }
+        if (lane == 0) sh.warp_found[warp] = own;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w)
+            if (better(sh.warp_found[w], own)) own = sh.warp_found[w];
+        if (tid == 0) sh.chosen[level][round] = own;
+        last = own;
+        __syncthreads();
+        if (own.score == 0) break;
     }
 }
 
 // the group's candidates, and what comes of them
+template <bool kBf16>
 __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int g) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row0 = g * p.group;
@@ -337,7 +309,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
             const float2* pairs = p.pairs + (int64_t)(row0 + r) * p.parts;
             for (int i = lane; i < p.parts; i += 32) {
                 const float2 v = __ldcg(&pairs[i]);
-                if (v.y > 0.f) {  // (running: a row of more than 32 chunks)
+                if (v.y > 0.f) {  // (running: a row of more than 32 segments)
                     const float up = fmaxf(top, v.x);
                     sum = sum * exp_of(top - up) + (double)v.y * exp_of(v.x - up);
                     top = up;
@@ -350,123 +322,141 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
             for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
         }
         if (lane == 0) {
+            const bool counts = top > -INFINITY && sum > 0.0;
+            const double log_sum = log(sum);
             sh.ended_row[r] = e;
-            sh.top_of[r] = top;
-            sh.log_of[r] = log(sum);
-            sh.total_of[r] = e || top > -INFINITY ? (double)t : -INFINITY;
+            sh.top_of[r] = counts ? top : 0.f;
+            sh.log_of[r] = log_sum;
+            sh.total_of[r] = e || counts ? (double)t : -INFINITY;
+            sh.const_of[r] = counts ? (float)((double)t - log_sum) : __uint_as_float(0xFF800000u);
+            const char* row_at = static_cast<const char*>(p.logits) + (int64_t)(row0 + r) * p.row_stride * (kBf16 ? 2 : 4);
+            sh.skew_of[r] = (int)(((uintptr_t)row_at & 15) / (kBf16 ? 2 : 4));
         }
     }
-    if (tid == 0) sh.listed = 0;
     __syncthreads();
-    const int per_row = p.parts * p.n_out, n_cands = p.group * per_row;
-    // candidate i: its score's key (0: none), place and logit
-    auto candidate = [&](int i, Found& f) {
-        const int r = i / per_row, c = i - r * per_row;
-        f.score = 0;
-        const double total = sh.total_of[r];
-        if (!(total > -INFINITY)) return;
-        if (sh.ended_row[r]) {
-            if (c != 0) return;
-            f.score = key64_of(total);
-            f.at = (unsigned long long)r << 32;
-            f.z = 0.f;
-            return;
+    // First the best blocks, then the best of their elements: strips of items, one per row or per block.
+    constexpr int kBlock = kBf16 ? 256 : 128;
+    const float none = __uint_as_float(0xFF800000u);   // no item
+#pragma unroll 1
+    for (int level = 0; level < 2; ++level) {
+        const int strips = level == 0 ? p.group : p.n_out, length = level == 0 ? p.blocks : kBlock;
+        if (level == 1) {
+            for (int c = tid; c < p.n_out; c += kThreads) {
+                const Found block = sh.chosen[0][c];
+                sh.strip_row[c] = block.score != 0 ? (int)(block.at >> 32) : -1;
+                sh.strip_at[c] = (int)(uint32_t)block.at * kBlock;
+            }
         }
-        const unsigned long long key = __ldcg(&p.cands[(int64_t)(row0 + r) * per_row + c]);
-        if (key == 0) return;
-        f.z = from_key((uint32_t)(key >> 32));
-        f.at = ((unsigned long long)r << 32) | (0xFFFFFFFFu - (uint32_t)key);
-        f.score = key64_of(total + (((double)f.z - (double)sh.top_of[r]) - sh.log_of[r]));
-    };
-    // The bound is taken among scores rounded to fp32 and no lower than its lowest (rounding keeps the
-    // order): -inf stands for no candidate.
-    const float none = __uint_as_float(0xFF800000u);
-    auto rounded = [](unsigned long long score) { return fmaxf((float)from_key64(score), -3.4028235e38f); };
-    float mine = none;
+        if (tid == 0) sh.listed = 0;
+        __syncthreads();
+        float mine = none, reach = none;
+        // Scores to fp32 accuracy with what they may be off by (the difference to the row's maximum, the row's
+        // constant and their sum are rounded once each): the bound is taken among the least they can be,
+        // and listed is what can reach it.
+        auto visit = [&](bool bound) {
+            int strip = 0, off = tid;
+            for (; off >= length; off -= length) ++strip;
 #pragma unroll 1
-    for (int i = tid; i < n_cands; i += kThreads) {
-        Found f;
-        candidate(i, f);
-        if (f.score != 0) mine = fmaxf(mine, rounded(f.score));
-    }
-    float top;
-    float reach = reach_by_warps(mine, from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(mine))), none, p.n_out, sh.tops,
-                                 sh.bounds, sh.nths, top);
-    if (tid < p.n_out) sh.chosen[tid].score = 0;
-    int n;
-#pragma unroll 1
-    for (int again = 0;; ++again) {
-        if (mine >= reach && mine > none) {
-#pragma unroll 1
-            for (int i = tid; i < n_cands; i += kThreads) {
-                Found f;
-                candidate(i, f);
-                if (f.score == 0 || rounded(f.score) < reach) continue;
-                const int at = atomicAdd(&sh.listed, 1);
-                if (at < kList) {
-                    sh.list[at] = f.score;
-                    sh.list_at[at] = f.at;
-                    sh.list_z[at] = f.z;
+            while (strip < strips) {
+                constexpr int kBatch = 8;
+                float z[kBatch];
+                int strip_of[kBatch], off_of[kBatch];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    strip_of[k] = strip;
+                    off_of[k] = off;
+                    z[k] = none;
+                    if (strip < strips) {
+                        if (level == 0) {
+                            z[k] = __ldcg(&p.block_max[(int64_t)(row0 + strip) * p.blocks + off]);
+                        } else {
+                            const int r = sh.strip_row[strip], e = sh.strip_at[strip] + off - (r >= 0 ? sh.skew_of[r] : 0);
+                            const int64_t at = (int64_t)(row0 + r) * p.row_stride + e;
+                            if (r >= 0 && e >= 0 && e < p.vocab)
+                                z[k] = kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p.logits)[at] << 16)
+                                             : static_cast<const float*>(p.logits)[at];
+                        }
+                    }
+                    for (off += kThreads; off >= length && strip < strips; off -= length) ++strip;
+                }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    if (strip_of[k] >= strips) break;
+                    const int r = level == 0 ? strip_of[k] : max(sh.strip_row[strip_of[k]], 0);
+                    const float d = z[k] - sh.top_of[r], c = sh.const_of[r];
+                    const float a = d + c, off_by = (fabsf(d) + fabsf(c)) * 2.4e-7f;   // two steps of 2^-23
+                    if (bound) {
+                        mine = fmaxf(mine, a - off_by);
+                    } else if (a + off_by >= reach && a > none) {
+                        const int n = atomicAdd(&sh.listed, 1);
+                        if (n < kList) {
+                            sh.list_at[n] = ((unsigned long long)r << 32) |
+                                (uint32_t)(level == 0 ? off_of[k] : sh.strip_at[strip_of[k]] + off_of[k] - sh.skew_of[r]);
+                            sh.list_z[n] = z[k];
+                        }
+                    }
                 }
             }
-        }
-        __syncthreads();
-        n = sh.listed;
-        if (n <= kList || again == 1) break;
-        __syncthreads();
-        if (tid == 0) sh.listed = 0;
-        reach = reach_by_threads(mine, sh.maxima, &sh.bound, p.n_out);
-    }
-    if (n <= kList) {
+            // ended beams: one item each
+            for (int r = tid; r < p.group; r += kThreads)
+                if (sh.ended_row[r] && sh.total_of[r] > -INFINITY) {
+                    const float t = (float)sh.total_of[r];
+                    if (bound) {
+                        mine = fmaxf(mine, t);
+                    } else if (t >= reach) {
+                        const int n = atomicAdd(&sh.listed, 1);
+                        if (n < kList) {
+                            sh.list_at[n] = (unsigned long long)r << 32;
+                            sh.list_z[n] = 0.f;
+                        }
+                    }
+                }
+        };
+        int n = 0;
 #pragma unroll 1
-        for (int i = tid; i < n; i += kThreads) {
-            const unsigned long long score = sh.list[i], at = sh.list_at[i];
-            int rank = 0;
+        for (int pass = 0; pass < 3; ++pass) {
+            visit(pass == 0);
+            if (pass == 0) {
+                float top;
+                reach = reach_by_warps(mine, from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(mine))), none, p.n_out, sh.tops,
+                                       sh.bounds, sh.nths, top);
+                continue;
+            }
+            __syncthreads();
+            n = sh.listed;
+            if (n <= kList || pass == 2) break;
+            __syncthreads();
+            if (tid == 0) sh.listed = 0;
+            reach = reach_by_threads(mine, sh.maxima, &sh.bound, p.n_out);
+        }
+        Found* const chosen = sh.chosen[level];
+        for (int i = tid; i < p.n_out; i += kThreads) chosen[i].score = 0;
+        if (n <= kList) {
+            for (int i = tid; i < n; i += kThreads) sh.list[i] = key64_of(sh.score(sh.list_at[i], sh.list_z[i]));
+            __syncthreads();
+#pragma unroll 1
+            for (int i = tid; i < n; i += kThreads) {
+                const unsigned long long score = sh.list[i], at = sh.list_at[i];
+                const float z = sh.list_z[i];
+                int rank = 0;
 #pragma unroll 4
-            for (int j = 0; j < n; ++j) {
-                const unsigned long long x = sh.list[j];
-                rank += x > score;
-                if (x == score) rank += sh.list_at[j] < at;
+                for (int j = 0; j < n; ++j) {
+                    const unsigned long long x = sh.list[j];
+                    rank += x > score;
+                    if (x == score) rank += ahead(sh.list_at[j], sh.list_z[j], at, z);
+                }
+                if (rank < p.n_out) chosen[rank] = {score, at, z};
             }
-            if (rank < p.n_out) sh.chosen[rank] = {score, at, sh.list_z[i]};
-        }
-    } else {
-        unsigned long long last_score = ~0ull, last_at = 0;
-#pragma unroll 1
-        for (int r = 0; r < p.n_out; ++r) {
-            Found own;
-            own.score = 0;
-            own.at = ~0ull;
-            own.z = 0.f;
-            for (int i = tid; i < n_cands; i += kThreads) {
-                Found f;
-                candidate(i, f);
-                if (f.score == 0 || !better(last_score, last_at, f.score, f.at)) continue;
-                if (better(f.score, f.at, own.score, own.at)) own = f;
-            }
-            for (int x = 16; x > 0; x >>= 1) {
-                Found o;
-                o.score = __shfl_xor_sync(0xFFFFFFFFu, own.score, x);
-                o.at = __shfl_xor_sync(0xFFFFFFFFu, own.at, x);
-                o.z = __shfl_xor_sync(0xFFFFFFFFu, own.z, x);
-                if (better(o.score, o.at, own.score, own.at)) own = o;
-            }
-            if (lane == 0) sh.warp_found[warp] = own;
             __syncthreads();
-            for (int w = 0; w < kWarps; ++w)
-                if (better(sh.warp_found[w].score, sh.warp_found[w].at, own.score, own.at)) own = sh.warp_found[w];
-            if (tid == 0) sh.chosen[r] = own;
-            last_score = own.score;
-            last_at = own.at;
-            __syncthreads();
-            if (own.score == 0) break;
+        } else {
+            best_of_many<kBf16>(p, sh, g, level);
         }
     }
     if (tid < kBeamMaxGroup) sh.first_of[tid] = kBeamMaxOut;
     if (tid < 2) sh.taken[tid] = 0;
     __syncthreads();
     // ---- out: in order, or a stream's best in the stream's own place and the others in the free ones ---
-    const Found f = sh.chosen[tid < p.n_out ? tid : 0];
+    const Found f = sh.chosen[1][tid < p.n_out ? tid : 0];
     const bool real = tid < p.n_out && f.score != 0;
     const int r = real ? (int)(f.at >> 32) : -1;
     int place = tid;
@@ -501,33 +491,36 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
     }
 }
 
-template <bool kBf16, int kVecs>
+template <bool kBf16>
 __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const BeamParams p) {
     __shared__ BeamShared sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int row = blockIdx.x / p.parts, part = blockIdx.x - row * p.parts;
-    const int g = row / p.group;
-    if (p.totals[row] > -INFINITY && !(p.ended != nullptr && p.ended[row] != 0)) scan_chunk<kBf16, kVecs>(p, sh, row, part);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        int before;
-        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(&p.tickets[g]) : "memory");
-        sh.last_one = before == p.group * p.parts - 1;
-        if (sh.last_one) p.tickets[g] = 0;  // for the next call
+    // segment: all of a row's, then the next row's
+    const int64_t segment = (int64_t)blockIdx.x * kWarps + warp;
+    int ended_group = -1;
+    if (segment < (int64_t)p.n_streams * p.parts) {
+        const int row = (int)(segment / p.parts), g = row / p.group;
+        if (p.totals[row] > -INFINITY && !(p.ended != nullptr && p.ended[row] != 0))
+            scan_segment<kBf16>(p, row, (int)(segment - (int64_t)row * p.parts));
+        __syncwarp();
+        if (lane == 0) {
+            int before;
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(&p.tickets[g]) : "memory");
+            if (before == p.group * p.parts - 1) {
+                p.tickets[g] = 0;  // for the next call
+                ended_group = g;
+            }
+        }
     }
+    if (lane == 0) sh.ended_groups[warp] = ended_group;
     __syncthreads();
-    if (sh.last_one) join_group(p, sh, g);
-}
-
-template <bool kBf16>
-cudaError_t launch_vecs(const cudaLaunchConfig_t& cfg, const BeamParams& p) {
-    switch (p.vecs) {
-        case 1: return cudaLaunchKernelEx(&cfg, beam_kernel<kBf16, 1>, p);
-        case 2: return cudaLaunchKernelEx(&cfg, beam_kernel<kBf16, 2>, p);
-        case 4: return cudaLaunchKernelEx(&cfg, beam_kernel<kBf16, 4>, p);
-        default: return cudaLaunchKernelEx(&cfg, beam_kernel<kBf16, 8>, p);
-    }
+    for (int w = 0; w < kWarps; ++w)
+        if (sh.ended_groups[w] >= 0) {
+            join_group<kBf16>(p, sh, sh.ended_groups[w]);
+            __syncthreads();
+        }
 }
 
 }  // namespace
@@ -535,7 +528,7 @@ cudaError_t launch_vecs(const cudaLaunchConfig_t& cfg, const BeamParams& p) {
 cudaError_t launch_beam(const BeamParams& p, cudaStream_t st) {
     TraceRange trace("sirllm:beam_select");
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.n_streams * p.parts));
+    cfg.gridDim = dim3((unsigned)(((int64_t)p.n_streams * p.parts + kWarps - 1) / kWarps));
     cfg.blockDim = dim3(kThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -543,7 +536,8 @@ cudaError_t launch_beam(const BeamParams& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return p.logits_dtype == SIRLLM_BF16 ? launch_vecs<true>(cfg, p) : launch_vecs<false>(cfg, p);
+    return p.logits_dtype == SIRLLM_BF16 ? cudaLaunchKernelEx(&cfg, beam_kernel<true>, p)
+                                         : cudaLaunchKernelEx(&cfg, beam_kernel<false>, p);
 }
 
 }  // namespace sirllm

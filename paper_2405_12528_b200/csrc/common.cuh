@@ -272,18 +272,19 @@ struct HeadTiling {
 constexpr int kBeamThreads = 256;
 constexpr int kBeamMaxGroup = SIRLLM_MAX_BEAMS;
 constexpr int kBeamMaxOut = SIRLLM_MAX_BEAMS;
-// How the rows are cut: `parts` chunks of vecs * kBeamThreads 16-byte vectors each.
+constexpr int kBeamTripBytes = 2048;  // what a warp takes in at a time
+// How the rows are cut: `parts` segments of `trips` trips each; blocks of 512 bytes.
 struct BeamTiling {
-    int32_t vecs;
+    int32_t trips, blocks;
     int64_t parts;
 };
 // ---- its workspace ------------------------------------------------------------------------
 //   [0, 256)                      header: int32 status word
 //   tickets[n_streams]            arrivals per group
-//   pairs[n_streams][parts]       (max, sum exp) of a chunk
-//   cands[n_streams][parts][64]   a chunk's best logits, order key << 32 | ~token
+//   pairs[n_streams][parts]       (max, sum exp) of a segment
+//   block_max[n_streams][blocks]  the largest logit of a block
 struct BeamLayout {
-    size_t tickets_off, pairs_off, cands_off, zeroed, total;
+    size_t tickets_off, pairs_off, block_max_off, zeroed, total;
     BeamTiling tiling;
 };
 struct BeamParams {
@@ -296,9 +297,9 @@ struct BeamParams {
     int32_t* ended_out;              // nullable
     int32_t* tickets;
     float2* pairs;
-    unsigned long long* cands;
+    float* block_max;
     int64_t vocab, row_stride;
-    int32_t n_streams, group, n_out, end_token, places, parts, vecs, logits_dtype;
+    int32_t n_streams, group, n_out, end_token, places, parts, trips, blocks, logits_dtype;
 };
 
 struct ReorderParams {
