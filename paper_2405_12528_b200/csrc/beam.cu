@@ -6,17 +6,17 @@
 // The logits are read once and that is the bound: rows * V elements, a few bytes out.  A warp streams a
 // segment of one row and keeps the running maximum and sum per lane; of every block of 512 bytes it leaves
 // the largest logit, and looks for no candidates.  The CTA whose warp finishes a group last joins its
-// segments (sums in fp64) and takes the n_out best BLOCKS of the group, by their largest logit's score and
-// then by place: they hold the n_out best candidates, for each of n_out better blocks would bring a
-// better candidate.  Only those few blocks are read again.  Scores are compared in fp64; within a row
-// the order of the logits is the order of the scores.
-// The n_out best of many: every thread knows the best of its own.  The k-th largest of every warp's,
-// k * warps >= n_out, the least of them over the warps, is a bound that n_out values reach (and so is the
-// largest of the warps' n_out-th); what reaches it is listed and ranked by counting.  A list that
-// overflows is made again with the n_out-th largest of all threads' as the bound, and if that overflows
-// too (thousands of equal scores) the best come out in n_out rounds of maximum: slow, and right.
+// segments (sums in fp64) and takes the n_out best SEGMENTS of the group, by their largest logit's score
+// and then by place: they hold the n_out best candidates, for each of n_out better segments would bring
+// a better candidate.  In the same way the n_out best blocks of these, and then the n_out best logits
+// of these blocks, the only ones that are read again; the last of the n_out is the bound for the next level.
+// Scores are compared in fp64; within a row the order of the logits is the order of the scores.
+// What reaches the bound is listed and ranked by counting.  A list that overflows is made again with the
+// n_out-th largest of all threads' best as the bound, and if that overflows too (thousands of equal
+// scores) the best come out in n_out rounds of maximum: slow, and right.
 // On the way here, 512 x 128256 bf16: chunks of 32 KB per CTA, with barriers between loading, bounding,
-// listing and ranking, 61 us; warps that keep lists of their own while they stream, 83 us.
+// listing and ranking, 61 us; warps that keep lists of their own while they stream, 83 us; blocks
+// without segments, bounds taken anew at every level, 53 us.
 #include "common.cuh"
 
 namespace sirllm {
@@ -26,6 +26,9 @@ namespace {
 constexpr int kThreads = kBeamThreads;
 constexpr int kWarps = kThreads / 32;
 constexpr int kList = 1024;
+constexpr int kLevels = 3;
+constexpr int kRankAll = 64;
+constexpr int kBatch = 8;  // items that a lane asks for at a time
 constexpr int kStep = 4;   // vectors of a lane per trip: blocks of a trip
 static_assert(kStep * 512 == kBeamTripBytes, "a trip is kStep blocks");
 
@@ -152,8 +155,8 @@ struct BeamShared {
     uint32_t maxima[kThreads];
     uint32_t bound;
     float tops[kWarps], bounds[kWarps], nths[kWarps];
-    int listed, ended_groups[kWarps];
-    Found warp_found[kWarps], chosen[2][kBeamMaxOut];  // the best blocks, the best candidates
+    int listed;
+    Found warp_found[kWarps], chosen[kLevels][kBeamMaxOut];  // the best segments, blocks, candidates
     // of a group's rows.  Score of a logit: total + ((z - top) - log sum), top the row's maximum: the
     // differences stay exact where a mask of the type's lowest value is all there is.  A row without
     // candidates has total -inf.
@@ -164,7 +167,6 @@ struct BeamShared {
         const int r = (int)(at >> 32);
         return ended_row[r] ? total_of[r] : total_of[r] + (((double)z - (double)top_of[r]) - log_of[r]);
     }
-    int strip_row[kBeamMaxOut], strip_at[kBeamMaxOut];     // the best blocks: row (-1: none), first element
     unsigned char ended_row[kBeamMaxGroup];
     int first_of[kBeamMaxGroup];       // the first candidate of every row
     uint32_t placed[2], taken[2];      // candidates with a place of their own, places taken
@@ -244,12 +246,37 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
     if (lane == 0) p.pairs[(int64_t)row * p.parts + part] = make_float2(all, sum);  // (a sum of 0: nothing but -inf)
 }
 
-// What the list could not hold, in rounds of maximum: blocks (level 0) or candidates (level 1).
+// The three levels: a group's segments, the best segments' blocks, the best blocks' logits.  A strip is what
+// one row (level 0) or one of the best of the level before brings.
+struct Strip {
+    int row, first, length;   // row -1: nothing
+};
+template <bool kBf16>
+__device__ __forceinline__ Strip strip_of(const BeamParams& p, const BeamShared& sh, int level, int i) {
+    constexpr int kBlock = kBf16 ? 256 : 128;
+    if (level == 0) return {i, 0, p.parts};
+    const Found f = sh.chosen[level - 1][i];
+    if (f.score == 0) return {-1, 0, 0};
+    const int row = (int)(f.at >> 32), at = (int)(uint32_t)f.at;
+    if (level == 1) return {row, at * p.trips * kStep, min(p.trips * kStep, p.blocks - at * p.trips * kStep)};
+    return {row, at * kBlock - sh.skew_of[row], kBlock};
+}
+// item b of a row at a level: a segment's or a block's maximum, or a logit; -inf outside the row
+template <bool kBf16>
+__device__ __forceinline__ float item_of(const BeamParams& p, int level, int64_t row, int b) {
+    if (level == 0) return __ldcg(&p.pairs[row * p.parts + b].x);
+    if (level == 1) return __ldcg(&p.block_max[row * p.blocks + b]);
+    if (b < 0 || b >= p.vocab) return __uint_as_float(0xFF800000u);
+    const int64_t at = row * p.row_stride + b;
+    return kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p.logits)[at] << 16)
+                 : static_cast<const float*>(p.logits)[at];
+}
+
+// What the list could not hold, in rounds of maximum.
 template <bool kBf16>
 __device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, int g, int level) {
-    constexpr int kBlock = kBf16 ? 256 : 128;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row0 = g * p.group;
-    const int strips = level == 0 ? p.group : p.n_out, length = level == 0 ? p.blocks : kBlock;
+    const int strips = level == 0 ? p.group : p.n_out;
     Found last = {~0ull, 0, 0.f};
     __syncthreads();
     for (int round = 0; round < p.n_out; ++round) {
@@ -259,21 +286,13 @@ __device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, i
             const Found f = {key64_of(sh.score(at, z)), at, z};
             if (better(last, f) && better(f, own)) own = f;
         };
-        for (int i = tid; i < strips * length; i += kThreads) {
-            const int strip = i / length, off = i - strip * length, r = level == 0 ? strip : sh.strip_row[strip];
-            if (r < 0 || sh.ended_row[r] || !(sh.total_of[r] > -INFINITY)) continue;
-            float z = __uint_as_float(0xFF800000u);
-            int b = off;
-            if (level == 0) {
-                z = __ldcg(&p.block_max[(int64_t)(row0 + r) * p.blocks + b]);
-            } else {
-                b = sh.strip_at[strip] + off - sh.skew_of[r];
-                const int64_t at = (int64_t)(row0 + r) * p.row_stride + b;
-                if (b >= 0 && b < p.vocab)
-                    z = kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p.logits)[at] << 16)
-                              : static_cast<const float*>(p.logits)[at];
+        for (int i = warp; i < strips; i += kWarps) {
+            const Strip t = strip_of<kBf16>(p, sh, level, i);
+            if (t.row < 0 || sh.ended_row[t.row] || !(sh.total_of[t.row] > -INFINITY)) continue;
+            for (int off = lane; off < t.length; off += 32) {
+                const float z = item_of<kBf16>(p, level, row0 + t.row, t.first + off);
+                if (z > -INFINITY) offer(t.row, t.first + off, z);
             }
-            if (z > -INFINITY) offer(r, b, z);
         }
         for (int r = tid; r < p.group; r += kThreads)
             if (sh.ended_row[r] && sh.total_of[r] > -INFINITY) offer(r, 0, 0.f);
@@ -297,7 +316,8 @@ __device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, i
 
 // the group's candidates, and what comes of them
 template <bool kBf16>
-__device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int g) {
+__device__ __noinline__ void join_group(const BeamParams& p, int g) {
+    __shared__ BeamShared sh;  // (handed in by reference it is read by generic loads, several times slower)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row0 = g * p.group;
     for (int r = warp; r < p.group; r += kWarps) {
@@ -334,65 +354,49 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
         }
     }
     __syncthreads();
-    // First the best blocks, then the best of their elements: strips of items, one per row or per block.
-    constexpr int kBlock = kBf16 ? 256 : 128;
     const float none = __uint_as_float(0xFF800000u);   // no item
 #pragma unroll 1
-    for (int level = 0; level < 2; ++level) {
-        const int strips = level == 0 ? p.group : p.n_out, length = level == 0 ? p.blocks : kBlock;
-        if (level == 1) {
-            for (int c = tid; c < p.n_out; c += kThreads) {
-                const Found block = sh.chosen[0][c];
-                sh.strip_row[c] = block.score != 0 ? (int)(block.at >> 32) : -1;
-                sh.strip_at[c] = (int)(uint32_t)block.at * kBlock;
-            }
-        }
+    for (int level = 0; level < kLevels; ++level) {
+        const int strips = level == 0 ? p.group : p.n_out;
+        Found* const chosen = sh.chosen[level];
+        for (int i = tid; i < p.n_out; i += kThreads) chosen[i].score = 0;
         if (tid == 0) sh.listed = 0;
         __syncthreads();
         float mine = none, reach = none;
+        if (level > 0) {
+            const Found f = sh.chosen[level - 1][p.n_out - 1];
+            if (f.score != 0) {
+                reach = (float)from_key64(f.score);
+                reach -= fabsf(reach) * 1.2e-7f;  // (rounded: a step of 2^-23)
+            }
+        }
         // Scores to fp32 accuracy with what they may be off by (the difference to the row's maximum, the row's
-        // constant and their sum are rounded once each): the bound is taken among the least they can be,
+        // constant and their sum are rounded once each): a bound is taken among the least they can be,
         // and listed is what can reach it.
         auto visit = [&](bool bound) {
-            int strip = 0, off = tid;
-            for (; off >= length; off -= length) ++strip;
 #pragma unroll 1
-            while (strip < strips) {
-                constexpr int kBatch = 8;
-                float z[kBatch];
-                int strip_of[kBatch], off_of[kBatch];
+            for (int i = warp; i < strips; i += kWarps) {
+                const Strip t = strip_of<kBf16>(p, sh, level, i);
+                if (t.row < 0 || sh.ended_row[t.row]) continue;
+                const float c = sh.const_of[t.row], top = sh.top_of[t.row];
+                if (!(c > none)) continue;
+#pragma unroll 1
+                for (int off = lane; off < t.length; off += 32 * kBatch) {
+                    float z[kBatch];
 #pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    strip_of[k] = strip;
-                    off_of[k] = off;
-                    z[k] = none;
-                    if (strip < strips) {
-                        if (level == 0) {
-                            z[k] = __ldcg(&p.block_max[(int64_t)(row0 + strip) * p.blocks + off]);
-                        } else {
-                            const int r = sh.strip_row[strip], e = sh.strip_at[strip] + off - (r >= 0 ? sh.skew_of[r] : 0);
-                            const int64_t at = (int64_t)(row0 + r) * p.row_stride + e;
-                            if (r >= 0 && e >= 0 && e < p.vocab)
-                                z[k] = kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p.logits)[at] << 16)
-                                             : static_cast<const float*>(p.logits)[at];
-                        }
-                    }
-                    for (off += kThreads; off >= length && strip < strips; off -= length) ++strip;
-                }
+                    for (int k = 0; k < kBatch; ++k)
+                        z[k] = off + k * 32 < t.length ? item_of<kBf16>(p, level, row0 + t.row, t.first + off + k * 32) : none;
 #pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    if (strip_of[k] >= strips) break;
-                    const int r = level == 0 ? strip_of[k] : max(sh.strip_row[strip_of[k]], 0);
-                    const float d = z[k] - sh.top_of[r], c = sh.const_of[r];
-                    const float a = d + c, off_by = (fabsf(d) + fabsf(c)) * 2.4e-7f;   // two steps of 2^-23
-                    if (bound) {
-                        mine = fmaxf(mine, a - off_by);
-                    } else if (a + off_by >= reach && a > none) {
-                        const int n = atomicAdd(&sh.listed, 1);
-                        if (n < kList) {
-                            sh.list_at[n] = ((unsigned long long)r << 32) |
-                                (uint32_t)(level == 0 ? off_of[k] : sh.strip_at[strip_of[k]] + off_of[k] - sh.skew_of[r]);
-                            sh.list_z[n] = z[k];
+                    for (int k = 0; k < kBatch; ++k) {
+                        const float d = z[k] - top, a = d + c, off_by = (fabsf(d) + fabsf(c)) * 2.4e-7f;  // two steps of 2^-23
+                        if (bound) {
+                            mine = fmaxf(mine, a - off_by);
+                        } else if (a + off_by >= reach && a > none) {
+                            const int n = atomicAdd(&sh.listed, 1);
+                            if (n < kList) {
+                                sh.list_at[n] = ((unsigned long long)t.row << 32) | (uint32_t)(t.first + off + k * 32);
+                                sh.list_z[n] = z[k];
+                            }
                         }
                     }
                 }
@@ -412,25 +416,26 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
                     }
                 }
         };
+        // A few segments are ranked as they are; more want a bound first (ranking 256 takes 4 us).
         int n = 0;
 #pragma unroll 1
-        for (int pass = 0; pass < 3; ++pass) {
-            visit(pass == 0);
+        for (int pass = level > 0 || p.group * p.parts <= kRankAll ? 1 : 0; pass < 4; ++pass) {
+            // 0: a bound, 1: the list; if that overflows 2: another bound, 3: the list again
+            visit((pass & 1) == 0);
             if (pass == 0) {
                 float top;
                 reach = reach_by_warps(mine, from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(mine))), none, p.n_out, sh.tops,
                                        sh.bounds, sh.nths, top);
-                continue;
+            } else if (pass == 2) {
+                if (tid == 0) sh.listed = 0;
+                reach = fmaxf(reach, reach_by_threads(mine, sh.maxima, &sh.bound, p.n_out));
+            } else {
+                __syncthreads();
+                n = sh.listed;
+                __syncthreads();
+                if (n <= kList) break;
             }
-            __syncthreads();
-            n = sh.listed;
-            if (n <= kList || pass == 2) break;
-            __syncthreads();
-            if (tid == 0) sh.listed = 0;
-            reach = reach_by_threads(mine, sh.maxima, &sh.bound, p.n_out);
         }
-        Found* const chosen = sh.chosen[level];
-        for (int i = tid; i < p.n_out; i += kThreads) chosen[i].score = 0;
         if (n <= kList) {
             for (int i = tid; i < n; i += kThreads) sh.list[i] = key64_of(sh.score(sh.list_at[i], sh.list_z[i]));
             __syncthreads();
@@ -439,11 +444,17 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
                 const unsigned long long score = sh.list[i], at = sh.list_at[i];
                 const float z = sh.list_z[i];
                 int rank = 0;
+                bool hidden = false;
 #pragma unroll 4
-                for (int j = 0; j < n; ++j) {
-                    const unsigned long long x = sh.list[j];
-                    rank += x > score;
-                    if (x == score) rank += ahead(sh.list_at[j], sh.list_z[j], at, z);
+                for (int j = 0; j < n; ++j) {  // (without a branch: equal scores are frequent with 16-bit logits)
+                    const unsigned long long x = sh.list[j], at_j = sh.list_at[j];
+                    const bool same = x == score;
+                    rank += (x > score) | (same & (at_j < at));
+                    hidden |= same & (sh.list_z[j] != z) & ((at_j >> 32) == (at >> 32));
+                }
+                if (hidden) {  // a total so large that it hides the order of the logits
+                    rank = 0;
+                    for (int j = 0; j < n; ++j) rank += better({sh.list[j], sh.list_at[j], sh.list_z[j]}, {score, at, z});
                 }
                 if (rank < p.n_out) chosen[rank] = {score, at, z};
             }
@@ -456,7 +467,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
     if (tid < 2) sh.taken[tid] = 0;
     __syncthreads();
     // ---- out: in order, or a stream's best in the stream's own place and the others in the free ones ---
-    const Found f = sh.chosen[1][tid < p.n_out ? tid : 0];
+    const Found f = sh.chosen[kLevels - 1][tid < p.n_out ? tid : 0];
     const bool real = tid < p.n_out && f.score != 0;
     const int r = real ? (int)(f.at >> 32) : -1;
     int place = tid;
@@ -493,7 +504,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, BeamShared& sh, int
 
 template <bool kBf16>
 __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const BeamParams p) {
-    __shared__ BeamShared sh;
+    __shared__ int ended_groups[kWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
     grid_launch_dependents();
@@ -514,11 +525,11 @@ __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const BeamParams p) {
             }
         }
     }
-    if (lane == 0) sh.ended_groups[warp] = ended_group;
+    if (lane == 0) ended_groups[warp] = ended_group;
     __syncthreads();
     for (int w = 0; w < kWarps; ++w)
-        if (sh.ended_groups[w] >= 0) {
-            join_group<kBf16>(p, sh, sh.ended_groups[w]);
+        if (ended_groups[w] >= 0) {
+            join_group<kBf16>(p, ended_groups[w]);
             __syncthreads();
         }
 }
