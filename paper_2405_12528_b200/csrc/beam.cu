@@ -250,26 +250,29 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
 // one row (level 0) or one of the best of the level before brings.
 struct Strip {
     int row, first, length;   // row -1: nothing
+    const char* base;         // the item numbered `first`
+    int step;                 // bytes from one to the next: 8 (pairs), 4, or 2 (bf16)
+    __device__ __forceinline__ float item(int i) const {
+        const char* at = base + (int64_t)i * step;
+        if (step == 2) return __uint_as_float((uint32_t)__ldcg(reinterpret_cast<const unsigned short*>(at)) << 16);
+        return __ldcg(reinterpret_cast<const float*>(at));
+    }
 };
 template <bool kBf16>
-__device__ __forceinline__ Strip strip_of(const BeamParams& p, const BeamShared& sh, int level, int i) {
-    constexpr int kBlock = kBf16 ? 256 : 128;
-    if (level == 0) return {i, 0, p.parts};
+__device__ __forceinline__ Strip strip_of(const BeamParams& p, const BeamShared& sh, int level, int row0, int i) {
+    constexpr int kBlock = kBf16 ? 256 : 128, kSize = kBf16 ? 2 : 4;
+    if (level == 0) return {i, 0, p.parts, reinterpret_cast<const char*>(p.pairs + (int64_t)(row0 + i) * p.parts), 8};
     const Found f = sh.chosen[level - 1][i];
-    if (f.score == 0) return {-1, 0, 0};
     const int row = (int)(f.at >> 32), at = (int)(uint32_t)f.at;
-    if (level == 1) return {row, at * p.trips * kStep, min(p.trips * kStep, p.blocks - at * p.trips * kStep)};
-    return {row, at * kBlock - sh.skew_of[row], kBlock};
-}
-// item b of a row at a level: a segment's or a block's maximum, or a logit; -inf outside the row
-template <bool kBf16>
-__device__ __forceinline__ float item_of(const BeamParams& p, int level, int64_t row, int b) {
-    if (level == 0) return __ldcg(&p.pairs[row * p.parts + b].x);
-    if (level == 1) return __ldcg(&p.block_max[row * p.blocks + b]);
-    if (b < 0 || b >= p.vocab) return __uint_as_float(0xFF800000u);
-    const int64_t at = row * p.row_stride + b;
-    return kBf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p.logits)[at] << 16)
-                 : static_cast<const float*>(p.logits)[at];
+    if (f.score == 0 || sh.ended_row[row]) return {-1, 0, 0, nullptr, 4};
+    if (level == 1) {
+        const int first = at * p.trips * kStep;
+        return {row, first, min(p.trips * kStep, p.blocks - first),
+                reinterpret_cast<const char*>(p.block_max + (int64_t)(row0 + row) * p.blocks + first), 4};
+    }
+    const int64_t e0 = (int64_t)at * kBlock - sh.skew_of[row], first = max(e0, (int64_t)0);
+    return {row, (int)first, (int)(min(e0 + kBlock, p.vocab) - first),
+            static_cast<const char*>(p.logits) + ((int64_t)(row0 + row) * p.row_stride + first) * kSize, kSize};
 }
 
 // What the list could not hold, in rounds of maximum.
@@ -287,10 +290,10 @@ __device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, i
             if (better(last, f) && better(f, own)) own = f;
         };
         for (int i = warp; i < strips; i += kWarps) {
-            const Strip t = strip_of<kBf16>(p, sh, level, i);
-            if (t.row < 0 || sh.ended_row[t.row] || !(sh.total_of[t.row] > -INFINITY)) continue;
+            const Strip t = strip_of<kBf16>(p, sh, level, row0, i);
+            if (t.row < 0 || !(sh.const_of[t.row] > -INFINITY)) continue;
             for (int off = lane; off < t.length; off += 32) {
-                const float z = item_of<kBf16>(p, level, row0 + t.row, t.first + off);
+                const float z = t.item(off);
                 if (z > -INFINITY) offer(t.row, t.first + off, z);
             }
         }
@@ -376,27 +379,28 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
         auto visit = [&](bool bound) {
 #pragma unroll 1
             for (int i = warp; i < strips; i += kWarps) {
-                const Strip t = strip_of<kBf16>(p, sh, level, i);
-                if (t.row < 0 || sh.ended_row[t.row]) continue;
+                const Strip t = strip_of<kBf16>(p, sh, level, row0, i);
+                if (t.row < 0) continue;
                 const float c = sh.const_of[t.row], top = sh.top_of[t.row];
                 if (!(c > none)) continue;
 #pragma unroll 1
                 for (int off = lane; off < t.length; off += 32 * kBatch) {
                     float z[kBatch];
 #pragma unroll
-                    for (int k = 0; k < kBatch; ++k)
-                        z[k] = off + k * 32 < t.length ? item_of<kBf16>(p, level, row0 + t.row, t.first + off + k * 32) : none;
+                    for (int k = 0; k < kBatch; ++k) z[k] = t.item(min(off + k * 32, t.length - 1));
+                    uint32_t hits = 0;
 #pragma unroll
                     for (int k = 0; k < kBatch; ++k) {
                         const float d = z[k] - top, a = d + c, off_by = (fabsf(d) + fabsf(c)) * 2.4e-7f;  // two steps of 2^-23
-                        if (bound) {
-                            mine = fmaxf(mine, a - off_by);
-                        } else if (a + off_by >= reach && a > none) {
-                            const int n = atomicAdd(&sh.listed, 1);
-                            if (n < kList) {
-                                sh.list_at[n] = ((unsigned long long)t.row << 32) | (uint32_t)(t.first + off + k * 32);
-                                sh.list_z[n] = z[k];
-                            }
+                        if (off + k * 32 < t.length) mine = fmaxf(mine, a - off_by);
+                        hits |= (uint32_t)(a + off_by >= reach && a > none && off + k * 32 < t.length) << k;
+                    }
+#pragma unroll 1
+                    for (hits = bound ? 0 : hits; hits != 0; hits &= hits - 1) {  // one copy of this code, the item again
+                        const int at = off + (__ffs(hits) - 1) * 32, n = atomicAdd(&sh.listed, 1);
+                        if (n < kList) {
+                            sh.list_at[n] = ((unsigned long long)t.row << 32) | (uint32_t)(t.first + at);
+                            sh.list_z[n] = t.item(at);
                         }
                     }
                 }
