@@ -143,7 +143,7 @@ struct AttendSharedLayout {
     AttendLayout own;
     PrefixPlan plan;   // no pointers yet
     int how;
-    int32_t blocks, part_rows;   // blocks of query heads of a K/V head, query heads of one
+    int32_t blocks, lead_blocks, part_rows;   // blocks of query heads of a K/V head, of a stream and of a group; heads of one
     size_t parts_off, part_ml_off, part_o_off, own_parts_off, own_ml_off, own_o_off, total;
 };
 static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t group, int32_t n_heads) {
@@ -155,7 +155,7 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
     const int64_t most = (int64_t)c.n_streams * c.n_kv_heads * c.capacity * c.head_dim * 4;
     L.how = kSharedRead;
     if (group > 1 && most > kSharedReadBytes) {
-        if (rows <= attend_unit_heads((int)rows, c.head_dim))
+        if (rows <= kSharedUnitRows)
             L.how = kSharedUnits;
         else if (prefix_plan(c, group, n_heads, &L.plan))
             L.how = kSharedProduct;
@@ -171,11 +171,12 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
         L.part_o_off = align_up(L.part_ml_off + part_rows * sizeof(float2), 256);
         off = align_up(L.part_o_off + part_rows * c.head_dim * sizeof(float), 256);
     }
-    const int heads = n_heads / c.n_kv_heads, unit = attend_unit_heads(heads, c.head_dim);
-    L.blocks = L.how == kSharedUnits ? 1 : (heads + unit - 1) / unit;
-    L.part_rows = L.how == kSharedUnits ? (int32_t)rows : heads < unit ? heads : unit;
-    const size_t members = (L.how == kSharedUnits ? groups : 0) + c.n_streams;
-    const size_t units = members * c.n_kv_heads * L.blocks, own = (units + kAttendMaxCtas * kAttendMaxWarps) * L.part_rows;
+    const int heads = n_heads / c.n_kv_heads, most_rows = L.how == kSharedUnits ? (int)rows : heads;
+    const int unit = attend_unit_heads(most_rows, c.head_dim);
+    L.blocks = (heads + unit - 1) / unit;
+    L.lead_blocks = L.how == kSharedUnits ? (most_rows + unit - 1) / unit : 0;
+    L.part_rows = most_rows < unit ? most_rows : unit;
+    const size_t units = (groups * L.lead_blocks + (size_t)c.n_streams * L.blocks) * c.n_kv_heads, own = (units + kAttendMaxCtas * kAttendMaxWarps) * L.part_rows;
     L.own_parts_off = off;
     L.own_ml_off = align_up(off + units * sizeof(int2), 256);
     L.own_o_off = align_up(L.own_ml_off + own * sizeof(float2), 256);
@@ -840,7 +841,7 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
     if (shared_len != nullptr) {
         const AttendSharedLayout S = attend_shared_layout(*cfg, group, n_heads);
         if (S.how != kSharedRead) {
-            if (cfg->n_kv_heads > 65535) return SIRLLM_ERR_TOO_LARGE;  // (a grid's second dimension)
+            if (n_heads > 65535) return SIRLLM_ERR_TOO_LARGE;  // (a grid's second dimension)
             p.own_ml = (float2*)((char*)ws + S.own_ml_off);
             p.own_o = (float*)((char*)ws + S.own_o_off);
             p.own_parts = (int2*)((char*)ws + S.own_parts_off);
@@ -851,7 +852,9 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
         if (S.how == kSharedUnits) {
             p.lead_units = cfg->n_streams / group;
             p.walk += p.lead_units;
-            const int64_t walk_units = (int64_t)p.walk * p.units;
+            p.lead_blocks = S.lead_blocks;
+            p.lead_member_units = cfg->n_kv_heads * S.lead_blocks;
+            const int64_t walk_units = (int64_t)cfg->n_streams * p.units + (int64_t)p.lead_units * p.lead_member_units;
             if (walk_units > 0x1FFFFFF || walk_units * most_tiles > 0x7FFFFFFF - kAttendMaxCtas) return SIRLLM_ERR_TOO_LARGE;
         }
         if (S.how == kSharedProduct) {

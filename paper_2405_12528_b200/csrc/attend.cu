@@ -57,7 +57,8 @@ constexpr int kSoloLongest = 32;
 constexpr int kMaxCluster = 8;
 // kParts: the least a warp takes, in tiles, and what the end of a unit counts there.
 constexpr int kPartLeast = 2;
-constexpr int kJoinWarps = 4;
+// Parts of a unit, about, at most: joining them takes its time, too.
+constexpr int kPartsMost = 64;
 __device__ __forceinline__ int part_gap(int head_dim) { return head_dim > 64 ? 2 : 4; }
 // Powers of two between the reference of the probabilities and the largest: where it is set, and
 // where it has to move.
@@ -176,6 +177,15 @@ __device__ __forceinline__ int first_slot(const AttendParams& p, int shared, int
     const int n = p.lead_units > 0 ? shared : prefix_slots(shared);
     return live > n ? n : 0;
 }
+// Units of walk member i, and the number of its unit u among all members'.
+template <int kUse>
+__device__ __forceinline__ int units_of(const AttendParams& p, int i) {
+    return kUse == kParts && i < p.lead_units ? p.lead_member_units : p.units;
+}
+__device__ __forceinline__ int64_t unit_number(const AttendParams& p, int i, int u) {
+    return i < p.lead_units ? (int64_t)i * p.lead_member_units + u
+                            : (int64_t)p.lead_units * p.lead_member_units + (int64_t)(i - p.lead_units) * p.units + u;
+}
 // slots of walk member i: a group's shared ones (i < lead_units), else those of stream i - lead_units
 template <int kUse>
 __device__ __forceinline__ int unit_slots(const AttendParams& p, int i) {
@@ -246,7 +256,7 @@ struct Walk {
         if (left <= 0) return;
         unit0 += tiles() + gap;
         t0 = 0;
-        if (++unit == p.units) {
+        if (++unit == units_of<kUse>(p, s)) {
             unit = 0;
             for (len = 0; len == 0;) {  // positions are left, so a stream with slots follows
                 if (++s >= p.walk) {  // (unless the lengths changed under the call)
@@ -296,7 +306,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     for (int s = s_lo; s < s_hi; ++s) {
         const int T = (unit_slots<kUse>(p, s) + kKeys - 1) / kKeys;
         if (T == 0) continue;
-        mine += (T + gap) * p.units;
+        mine += (T + gap) * units_of<kUse>(p, s);
         ++live;
         long_unit = max(long_unit, T);
     }
@@ -330,13 +340,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     int part_per = 0;
     if (kUse == kParts) {
         const int n_warps = (int)gridDim.x * kWarps;
-        const int per = part_per = max((line + n_warps - 1) / n_warps, kPartLeast);
+        const int per = part_per = max((line + n_warps - 1) / n_warps, max((long_unit + kPartsMost - 1) / kPartsMost, kPartLeast));
         if (tid < kWarps) first_of[tid].left = 0;
         __syncthreads();
         int at = before;
         for (int s = s_lo; s < s_hi; ++s) {
             const int len = unit_slots<kUse>(p, s);
-            const int T = len > 0 ? (len + kKeys - 1) / kKeys + gap : 0, end = at + T * p.units;
+            const int T = len > 0 ? (len + kKeys - 1) / kKeys + gap : 0, end = at + T * units_of<kUse>(p, s);
             for (int w = 0; w < kWarps && T > 0; ++w) {
                 const int no = w * (int)gridDim.x + (int)blockIdx.x;
                 const int r0 = line / per >= no ? no * per : line;  // (no overflow)
@@ -482,7 +492,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             ahead_tile = ahead.t0 + lead;
         }
         if (ahead.more()) {
-            const int g = ahead.unit / p.blocks;
+            const int g = ahead.unit / (kUse == kParts && ahead.stream < 0 ? p.lead_blocks : p.blocks);
             const int from = kUse == kPlain ? ahead.s : ahead.stream < 0 ? ahead.lead : ahead.stream;
             const int64_t plane = (int64_t)from * p.planes_per_stream + p.layer_plane + g;
             const int key0 = ahead_tile * kKeys;
@@ -518,14 +528,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
     // ---- the units ------------------------------------------------------------------------
     const int hc = 2 * (lane & 3);  // this lane's two heads within a block of 8
     for (Walk<kUse> w = start; w.more(); w.next(p, gap_all)) {
-        const int g = w.unit / p.blocks, block = w.unit - g * p.blocks;
+        const bool of_group = kUse == kParts && w.stream < 0;      // all streams' heads: group * heads rows
+        const int blocks = of_group ? p.lead_blocks : p.blocks;
+        const int g = w.unit / blocks, block = w.unit - g * blocks;
         const int head0 = g * p.group + block * kHeads;            // first query head of the unit
-        const bool of_group = kUse == kParts && w.stream < 0;      // all streams' heads: group * heads rows, one block
         const int heads = min(kHeads, (of_group ? p.stream_group * p.group : p.group) - block * kHeads);  // it really has
         if (kUse == kParts && w.t0 == 0 && lane == 0)  // where the unit's parts are, for join_kernel
-            p.own_parts[(int64_t)w.s * p.units + w.unit] = make_int2(warp_no, (w.unit0 + w.tiles() - 1) / part_per - warp_no + 1);
+            p.own_parts[unit_number(p, w.s, w.unit)] = make_int2(warp_no, (w.unit0 + w.tiles() - 1) / part_per - warp_no + 1);
         // kParts: the place of the warp's part of the unit
-        const int64_t place = ((int64_t)w.s * p.units + w.unit + warp_no) * p.part_rows;
+        const int64_t place = (unit_number(p, w.s, w.unit) + warp_no) * p.part_rows;
         // queries as the right operand: lane holds elements 2(lane%4), +1 (and +8, +9) of head lane/4
         uint32_t qf[kTiles][kDim / 16][2];
         const char* qrow = p.q + ((int64_t)(kUse == kPlain ? w.s : w.stream) * p.q_stride + (int64_t)head0 * p.head_dim) * 2;
@@ -534,8 +545,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
             const int h = n * 8 + (lane >> 2);
             const char* qhead = qrow + (int64_t)h * p.head_dim * 2;
             if (of_group) {
-                const int local = h / p.group;
-                qhead = p.q + ((w.lead + local) * p.q_stride + (int64_t)(g * p.group + h - local * p.group) * p.head_dim) * 2;
+                const int row = block * kHeads + h, local = row / p.group;
+                qhead = p.q + ((w.lead + local) * p.q_stride + (int64_t)(g * p.group + row - local * p.group) * p.head_dim) * 2;
             }
 #pragma unroll
             for (int ks = 0; ks < kDim / 16; ++ks) {
@@ -910,94 +921,122 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 }
 
 // The parts of every stream's heads into the result: those of the stream's own slots, then those of the
-// group's.  A block per stream, K/V head and 128 elements, a warp per query head, four elements per lane.
+// group's.  A block per stream, query head and 128 elements; the warps share the parts, four elements per lane.
 // (What is executed once costs its way from L2 into the instruction cache, 250 cycles and more per 8
 // instructions: with divisions for the places of the parts, and unrolled, this took 13 us.)
-template <bool kBf16>
+template <bool kBf16, int kJoinWarps>
 __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const AttendParams p) {
-    const int lane = threadIdx.x & 31, s = blockIdx.x, kv_head = blockIdx.y, e = (int)blockIdx.z * 128 + lane * 4;
-    const int g = s / p.stream_group, local = s - g * p.stream_group, kv_heads = gridDim.y;
+    __shared__ float4 sums[kJoinWarps][32];
+    __shared__ float2 stats[kJoinWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int s = blockIdx.x, head = blockIdx.y, e = (int)blockIdx.z * 128 + lane * 4;
+    const int g = s / p.stream_group, local = s - g * p.stream_group, kv_head = head / p.group, hq = head - kv_head * p.group;
     grid_launch_dependents();
     const bool on = e < p.head_dim, product = p.lead_units == 0;
-    int lead_unit = g * kv_heads + kv_head, in_block = 0;
-    if (product && p.prefix.pair) {
-        in_block = local / p.prefix.block_streams;
-        lead_unit = lead_unit * p.prefix.units + (in_block >> 1);
+    // where the parts are noted, and which row of theirs is this head's
+    const int block = hq >= p.part_rows ? hq / p.part_rows : 0;
+    const int64_t own_unit = unit_number(p, p.lead_units + s, kv_head * p.blocks + block);
+    int lead_row = local * p.group + hq, lead_step = p.part_rows;
+    int64_t lead_unit;
+    if (product) {
+        const PrefixPlan& x = p.prefix;
+        const int in_block = x.pair ? local / x.block_streams : 0;
+        lead_unit = ((int64_t)g * (p.n_heads / p.group) + kv_head) * x.units + (in_block >> 1);
+        lead_row += (in_block & 1) * kPrefixRows - in_block * x.block_streams * p.group;
+        lead_step = x.rows;
+    } else {
+        const int lead_block = lead_row >= p.part_rows ? lead_row / p.part_rows : 0;
+        lead_unit = unit_number(p, g, kv_head * p.lead_blocks + lead_block);
+        lead_row -= lead_block * p.part_rows;
     }
+    const float2* const lead_ml = product ? p.prefix.part_ml : p.own_ml;
+    const float* const lead_o = product ? p.prefix.part_o : p.own_o;
     // The first time round is a rehearsal, in the shadow of the kernel before: it writes nothing.
     int n = 1;
-    int2 lead = make_int2(0, 0);
+    int2 own = make_int2(0, 1), lead = make_int2(0, 0);
     bool real = false;
 again:
-    for (int hq = threadIdx.x >> 5; hq < p.group; hq += kJoinWarps) {
-        const int64_t head = kv_head * p.group + hq;
-        const int block = hq >= p.part_rows ? hq / p.part_rows : 0;
-        const int64_t unit = (int64_t)(p.lead_units + s) * p.units + kv_head * p.blocks + block;
-        const int2 own = n == 0 ? make_int2(0, 0) : real ? __ldcg(p.own_parts + unit) : make_int2(0, 1);
-        const int parts = own.y + lead.y, lead_row = (local - in_block * p.prefix.block_streams) * p.group + hq;
-        // from part i - own.y on: rows of the group's
-        const int64_t own_at = real ? (unit + own.x) * p.part_rows + hq - block * p.part_rows : 0;
-        const int64_t lead_at = product ? ((int64_t)lead_unit + lead.x) * p.prefix.rows + lead_row + (in_block & 1) * kPrefixRows
-                                        : ((int64_t)g * p.units + kv_head + lead.x) * p.part_rows + lead_row;
-        const int lead_step = product ? p.prefix.rows : p.part_rows;
-        const float2* const lead_ml = product ? p.prefix.part_ml : p.own_ml;
-        const float* const lead_o = product ? p.prefix.part_o : p.own_o;
-        float m = kNegHuge, l = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int parts = own.y + lead.y;
+    const int64_t own_at = real ? (own_unit + own.x) * p.part_rows + hq - block * p.part_rows : 0;
+    const int64_t lead_at = (lead_unit + lead.x) * lead_step + lead_row;  // from part own.y on
+    float m = kNegHuge, l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-        for (int i0 = 0; i0 < parts; i0 += 32) {
-            const int i = i0 + lane;
-            const bool is_own = i < own.y;
-            const int64_t at = is_own ? own_at + (int64_t)i * p.part_rows : lead_at + (int64_t)(i - own.y) * lead_step;
-            const float2 mine = i >= parts ? make_float2(kNegHuge, 0.f) : __ldcg((is_own ? p.own_ml : lead_ml) + at);
-            const unsigned long long from = (unsigned long long)((is_own ? p.own_o : lead_o) + at * p.head_dim);
-            float up = mine.x;
+    for (int i0 = 0; i0 < parts; i0 += 32 * kJoinWarps) {
+        const int i = i0 + lane * kJoinWarps + warp;
+        const bool is_own = i < own.y;
+        const int64_t at = is_own ? own_at + (int64_t)i * p.part_rows : lead_at + (int64_t)(i - own.y) * lead_step;
+        const float2 mine = i >= parts ? make_float2(kNegHuge, 0.f) : __ldcg((is_own ? p.own_ml : lead_ml) + at);
+        const unsigned long long from = (unsigned long long)((is_own ? p.own_o : lead_o) + at * p.head_dim);
+        float up = mine.x;
 #pragma unroll
-            for (int x = 16; x > 0; x >>= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, x));
-            up = fmaxf(up, m);
-            const float f = ex2_approx(m - up), fi = ex2_approx(mine.x - up);
-            l = fmaf(l, f, mine.y * fi);  // this lane's parts
-            m = up;
-            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-            const int last = min(32, parts - i0);
+        for (int x = 16; x > 0; x >>= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, x));
+        up = fmaxf(up, m);
+        const float f = ex2_approx(m - up), fi = ex2_approx(mine.x - up);
+        l = fmaf(l, f, mine.y * fi);  // this lane's parts
+        m = up;
+        acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+        const int last = min(32, (parts - i0 - warp + kJoinWarps - 1) / kJoinWarps);
 #pragma unroll 1
-            for (int k0 = 0; k0 < last; k0 += 4) {
-                float4 v[4];
-                float w[4];
+        for (int k0 = 0; k0 < last; k0 += 8) {
+            float4 v[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {  // (a lane behind the last part has weight 0)
-                    const unsigned long long a = __shfl_sync(0xFFFFFFFFu, from, k0 + k);
-                    w[k] = __shfl_sync(0xFFFFFFFFu, fi, k0 + k);
-                    v[k] = on && k0 + k < last ? __ldcg(reinterpret_cast<const float4*>(a) + (e >> 2)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
+            for (int k = 0; k < 8; ++k) {
+                const unsigned long long a = __shfl_sync(0xFFFFFFFFu, from, k0 + k);
+                v[k] = on && k0 + k < last ? __ldcg(reinterpret_cast<const float4*>(a) + (e >> 2)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    acc.x = fmaf(v[k].x, w[k], acc.x);
-                    acc.y = fmaf(v[k].y, w[k], acc.y);
-                    acc.z = fmaf(v[k].z, w[k], acc.z);
-                    acc.w = fmaf(v[k].w, w[k], acc.w);
-                }
+            for (int k = 0; k < 8; ++k) {  // (a lane behind the last part has weight 0)
+                const float w = __shfl_sync(0xFFFFFFFFu, fi, k0 + k);
+                acc.x = fmaf(v[k].x, w, acc.x);
+                acc.y = fmaf(v[k].y, w, acc.y);
+                acc.z = fmaf(v[k].z, w, acc.z);
+                acc.w = fmaf(v[k].w, w, acc.w);
             }
         }
+    }
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
-        const float f = n == 0 ? 0.f : 1.0f / l;
+    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
+    sums[warp][lane] = acc;
+    if (lane == 0) stats[warp] = make_float2(m, l);
+    __syncthreads();
+    if (warp == 0) {
+        float up = stats[0].x;
+#pragma unroll
+        for (int w = 1; w < kJoinWarps; ++w) up = fmaxf(up, stats[w].x);
+        float sum = 0.f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) {
+            const float f = ex2_approx(stats[w].x - up);
+            const float4 v = sums[w][lane];
+            sum = fmaf(stats[w].y, f, sum);
+            acc.x = fmaf(v.x, f, acc.x);
+            acc.y = fmaf(v.y, f, acc.y);
+            acc.z = fmaf(v.z, f, acc.z);
+            acc.w = fmaf(v.w, f, acc.w);
+        }
+        const float f = n == 0 ? 0.f : 1.0f / sum;
         if (on && real)
-            *reinterpret_cast<uint2*>(p.out + (int64_t)s * p.out_stride + head * p.head_dim + e) =
+            *reinterpret_cast<uint2*>(p.out + (int64_t)s * p.out_stride + (int64_t)head * p.head_dim + e) =
                 make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
         if (lane == 0 && blockIdx.z == 0 && p.lse != nullptr && real)
-            p.lse[(int64_t)s * p.n_heads + head] = n == 0 ? __uint_as_float(0xFF800000u) : (m + log2f(l)) * (float)kLn2;
+            p.lse[(int64_t)s * p.n_heads + head] = n == 0 ? __uint_as_float(0xFF800000u) : (up + log2f(sum)) * (float)kLn2;
     }
     if (real) return;
     grid_dependency_wait();
     n = p.kv_len[s];
     const int shared = p.shared_len[g];
+    own = __ldcg(p.own_parts + own_unit);  // (of a stream without slots: whatever stands there)
+    lead = __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
     if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
         if (threadIdx.x == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
         return;
     }
-    if (first_slot(p, shared, n) > 0) lead = __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
+    if (n == 0) own = make_int2(0, 0);
+    if (first_slot(p, shared, n) == 0) lead = make_int2(0, 0);
     real = true;
+    __syncthreads();
     goto again;
 }
 
@@ -1017,7 +1056,7 @@ cudaError_t launch(const AttendParams& p, const DeviceProps& dp, cudaStream_t st
     q.cluster = 1;
     int grid = dp.n_sm < kAttendMaxCtas ? dp.n_sm : kAttendMaxCtas;
     static std::atomic<int> held_cache[kMaxDevices][4];
-    for (int i = 3; i > 0; --i) {
+    for (int i = 3; i > 0 && kUse != kParts; --i) {
         const int size = 1 << i;
         if (n_units * size > grid) continue;
         const bool cached = dp.device >= 0 && dp.device < kMaxDevices;
@@ -1088,15 +1127,18 @@ cudaError_t launch_use(const AttendParams& p, const DeviceProps& dp, cudaStream_
     cudaError_t e = launch_dim<kBf16, kParts>(p, dp, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.n_streams, p.n_heads / p.group, (p.head_dim + 127) / 128);
-    cfg.blockDim = dim3(kJoinWarps * 32);
+    cfg.gridDim = dim3(p.n_streams, p.n_heads, (p.head_dim + 127) / 128);
+    // Four warps to a head as long as the GPU holds them all at once (eight beams of 12001 slots 44 -> 31 us
+    // with them); one where there are more heads (16 x 8 beams of 1000 slots 38 us, 48 with four).
+    const bool shared_by_four = (int64_t)p.n_streams * p.n_heads * 4 <= dp.n_sm * 64;
+    cfg.blockDim = dim3(shared_by_four ? 128 : 32);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, join_kernel<kBf16>, p);
+    return shared_by_four ? cudaLaunchKernelEx(&cfg, join_kernel<kBf16, 4>, p) : cudaLaunchKernelEx(&cfg, join_kernel<kBf16, 1>, p);
 }
 
 }  // namespace

@@ -185,6 +185,7 @@ struct AttendDeal {
 // its tiles of 128 slots stand in one line with the other units', cut into equal stretches for the CTAs.
 // The part of unit u (of all groups) that CTA c computes is in place u + c.
 constexpr int64_t kSharedReadBytes = 8 << 20;
+constexpr int kSharedUnitRows = 32;
 constexpr int kPrefixTile = 128;
 constexpr int kPrefixRows = 128;   // rows of a block, at most
 struct PrefixPlan {
@@ -236,7 +237,8 @@ struct AttendParams {
     float2* own_ml;                          // [place][part_rows] (reference in units of log2, sum)
     int2* own_parts;                         // [unit] its first part's warp, how many parts
     int32_t part_rows;                       // query heads of a unit, at most
-    int32_t lead_units;                      // groups whose shared slots are units of this kernel: all or none
+    int32_t lead_units;                      // groups whose shared slots are units of this kernel: all or none;
+    int32_t lead_blocks, lead_member_units;  // blocks of their rows per K/V head, units of one of them
     int32_t walk;                            // what the kernel walks through: lead_units + n_streams
     // set by the launcher
     int32_t cluster, cluster_log2;           // CTAs of a cluster
