@@ -184,7 +184,7 @@ struct AttendDeal {
 // stream r / heads.  A unit is one block of up to 128 rows, or two (pair), of one K/V head of a group;
 // its tiles of 128 slots stand in one line with the other units', cut into equal stretches for the CTAs.
 // The part of unit u (of all groups) that CTA c computes is in place u + c.
-constexpr int64_t kSharedReadBytes = 8 << 20;
+constexpr int64_t kSharedReadBytes = 160 << 20;
 constexpr int kSharedUnitRows = 32;
 constexpr int kPrefixTile = 128;
 constexpr int kPrefixRows = 128;   // rows of a block, at most

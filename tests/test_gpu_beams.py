@@ -365,7 +365,22 @@ def test_reorder_past_32_bits():
 # attend
 # --------------------------------------------------------------------------------------
 
-def shared_case(S, G, H, KH, D, C, shared, lens, kv="bf16", L=1, layer=0, seed=0, scale=None, fill=None, some=None):
+PARTS_FROM = 160 * 2**20    # bytes of K and V of a layer from which on shared slots are computed once for the group
+
+
+def capacities(S, KH, D, C):
+    """The capacity as it is, and one that takes the other way through the call, where there is one."""
+    need = PARTS_FROM // (S * KH * D * 4) + 1
+    return [C] + ([need] if C < need <= B.MAX_CAPACITY else [])
+
+
+def shared_case(S, G, H, KH, D, C, shared, lens, **kw):
+    for c in capacities(S, KH, D, C):
+        result = shared_once(S, G, H, KH, D, c, shared, lens, **kw)
+    return result
+
+
+def shared_once(S, G, H, KH, D, C, shared, lens, kv="bf16", L=1, layer=0, seed=0, scale=None, fill=None, some=None):
     g = gen(seed)
     dt = DT[kv]
     cfg = config(S=S, L=L, KH=KH, D=D, C=C, kv=kv)
@@ -450,7 +465,7 @@ def test_shared_ragged_groups_of_very_different_prefixes():
 def test_shared_one_stream_per_group_is_attend():
     S, H, KH, D, C = 6, 8, 2, 128, 700
     shared = [0, 10, 128, 300, 512, 700]
-    cfg, q, k, v, out, lse, ws = shared_case(S, 1, H, KH, D, C, shared, [700] * 6, seed=5)
+    cfg, q, k, v, out, lse, ws = shared_once(S, 1, H, KH, D, C, shared, [700] * 6, seed=5)
     o2, l2 = torch.empty_like(out), torch.empty_like(lse)
     B.sirllm_attend(cfg, 0, q, k, v, i32(*[700] * 6), None, o2, l2, B.new_attend_workspace(cfg))
     tol = ref_attend(q[0], k[0, 0], v[0, 0], 700, D ** -0.5)[2]
@@ -465,57 +480,60 @@ def test_shared_scales(scale, kv):
 
 @pytest.mark.parametrize("kv", ["bf16", "f16"])
 @pytest.mark.parametrize("order", [1, -1])
-def test_shared_scores_that_keep_rising_and_falling(kv, order):
+@pytest.mark.parametrize("cap", [4000, 24000])
+def test_shared_scores_that_keep_rising_and_falling(kv, order, cap):
     g = gen(12)
-    S, H, KH, D, C, n = 32, 8, 1, 64, 4000, 3900
+    S, H, KH, D, C, n = 32, 8, 1, 64, cap, 3900
     cfg = config(S=S, KH=KH, D=D, C=C, kv=kv)
     q = torch.zeros(S, H, D, dtype=DT[kv], device="cuda")
     q[..., 0] = 1.0
     k = torch.zeros(S, 1, KH, C, D, dtype=DT[kv], device="cuda")
-    k[..., 0] = torch.linspace(-2000, 2000, C, device="cuda") * order
+    k[..., :4000, 0] = torch.linspace(-2000, 2000, 4000, device="cuda") * order
     v = randn(g, S, 1, KH, C, D, dtype=DT[kv])
     out, lse = torch.empty_like(q), torch.empty(S, H, device="cuda")
-    B.sirllm_attend_shared(cfg, 0, S, i32(n), q, k, v, i32(*[C] * S), 1.0, out, lse,
+    B.sirllm_attend_shared(cfg, 0, S, i32(n), q, k, v, i32(*[4000] * S), 1.0, out, lse,
                            B.new_attend_shared_workspace(cfg, S, H))
     for s in (0, 5, 31):
         ks, vs = torch.cat([k[0, 0, :, :n], k[s, 0, :, n:]], 1), torch.cat([v[0, 0, :, :n], v[s, 0, :, n:]], 1)
-        o, l, to, tl = ref_attend(q[s], ks, vs, C, 1.0)
+        o, l, to, tl = ref_attend(q[s], ks, vs, 4000, 1.0)
         assert ((out[s].double() - o).abs() <= to).all() and ((lse[s].double() - l).abs() <= tl).all()
 
 
 @pytest.mark.parametrize("kv", ["bf16", "f16"])
 @pytest.mark.parametrize("G,H,at", [(2, 1, 5), (64, 4, 5), (64, 4, 16000), (64, 4, 16500)])
 @pytest.mark.parametrize("faint", [22.0, 25.5, 30.0])
-def test_shared_one_dominant_slot_and_many_faint_ones(kv, G, H, at, faint):
+@pytest.mark.parametrize("KH", [1, 2, 19])
+def test_shared_one_dominant_slot_and_many_faint_ones(kv, G, H, at, KH, faint):
     # as for sirllm_attend: an fp16 weight is off by u of itself or by 2^-36 of the maximum
     g = gen(17)
     n, C, D, dt = 16384, 16600, 64, DT[kv]
-    cfg = config(S=G, D=D, C=C, kv=kv)
+    H = H * KH
+    cfg = config(S=G, KH=KH, D=D, C=C, kv=kv)
     q = torch.zeros(G, H, D, dtype=dt, device="cuda")
     q[..., 0] = 1.0
-    k = torch.zeros(G, 1, 1, C, D, dtype=dt, device="cuda")
+    k = torch.zeros(G, 1, KH, C, D, dtype=dt, device="cuda")
     k[..., at, 0] = 1.0
-    v = (1 + randn(g, 1, 1, 1, C, D, scale=0.2)).to(dt).expand(G, 1, 1, C, D).contiguous()
+    v = (1 + randn(g, 1, 1, 1, C, D, scale=0.2)).to(dt).expand(G, 1, KH, C, D).contiguous()
     v[..., at, :] = 0.0
     scale = faint * math.log(2)
     out, lse = torch.empty_like(q), torch.empty(G, H, device="cuda")
     B.sirllm_attend_shared(cfg, 0, G, i32(n), q, k, v, i32(*[C] * G), scale, out, lse,
                            B.new_attend_shared_workspace(cfg, G, H))
     want, l, tol, tol_l = ref_attend(q[0], k[0, 0], v[0, 0], C, scale)
-    tol = tol + 2.0 ** -36 * v[0].double().abs().sum(-2).amax()
+    tol = tol + 2.0 ** -36 * v[0, 0, 0].double().abs().sum(-2).amax()
     d = (out.double() - want).abs()
     assert (d <= tol).all(), f"worst {float((d / tol).max()):.2f} x tol"
     assert ((lse.double() - l).abs() <= tol_l).all()
 
 
-@pytest.mark.parametrize("G", [2, 64])
-def test_shared_infinite_scores_follow_the_formula(G):
+@pytest.mark.parametrize("G,cap", [(2, 300), (16, 45000), (64, 300), (64, 12000)])
+def test_shared_infinite_scores_follow_the_formula(G, cap):
     n, C = 256, 300
-    cfg = config(S=G, D=64, C=C)
+    cfg = config(S=G, D=64, C=cap)
     ws = B.new_attend_shared_workspace(cfg, G, 1)
     q = torch.ones(G, 1, 64, dtype=torch.bfloat16, device="cuda")
-    k = torch.zeros(G, 1, 1, C, 64, dtype=torch.bfloat16, device="cuda")
-    v = torch.arange(C, device="cuda").view(1, 1, 1, C, 1).expand(G, 1, 1, C, 64).to(torch.bfloat16).contiguous()
+    k = torch.zeros(G, 1, 1, cap, 64, dtype=torch.bfloat16, device="cuda")
+    v = torch.arange(cap, device="cuda").view(1, 1, 1, cap, 1).expand(G, 1, 1, cap, 64).to(torch.bfloat16).contiguous()
     out, lse = torch.empty_like(q), torch.empty(G, 1, device="cuda")
     shared = i32(n)
     k[0, 0, 0, 5:, 0] = -math.inf          # of the shared slots only the first five weigh
@@ -531,13 +549,13 @@ def test_shared_infinite_scores_follow_the_formula(G):
     assert out.isnan().all() and lse.isnan().all()
 
 
-@pytest.mark.parametrize("G", [2, 32])
-def test_shared_lengths_outside_the_planes_leave_their_rows_alone(G):
-    S, H, KH, D, C = 2 * G, 4, 2, 64, 200
-    cfg, q, k, v, out, lse, ws = shared_case(S, G, H, KH, D, C, [150, 130], [200] * S, seed=4)
+@pytest.mark.parametrize("G,group,C", [(2, 2, 200), (32, 2, 200), (32, 1, 5200), (32, 2, 5200)])
+def test_shared_lengths_outside_the_planes_leave_their_rows_alone(G, group, C):
+    S, H, KH, D = 2 * G, 2 * group, 2, 64
+    cfg, q, k, v, out, lse, ws = shared_once(S, G, H, KH, D, C, [150, 130], [200] * S, seed=4)
     want, want_l = out.clone(), lse.clone()
     lens = [200] * S
-    lens[1], lens[G] = 201, -1
+    lens[1], lens[G] = C + 1, -1
     out.fill_(3.0), lse.fill_(3.0)
     B.sirllm_attend_shared(cfg, 0, G, i32(150, 130), q, k, v, i32(*lens), None, out, lse, ws)
     assert B.sirllm_status(ws, clear=True) == B.STATUS_OVERFLOW
@@ -546,7 +564,7 @@ def test_shared_lengths_outside_the_planes_leave_their_rows_alone(G):
             assert (out[s] == 3).all() and (lse[s] == 3).all()
         else:
             assert same_bits(out[s], want[s]) and torch.equal(lse[s], want_l[s])
-    for bad in (-1, 201, 2**31 - 1, -2**31):
+    for bad in (-1, C + 1, 2**31 - 1, -2**31):
         out.fill_(3.0), lse.fill_(3.0)
         B.sirllm_attend_shared(cfg, 0, G, i32(bad, 130), q, k, v, i32(*[200] * S), None, out, lse, ws)
         assert B.sirllm_status(ws, clear=True) == B.STATUS_OVERFLOW
@@ -554,11 +572,11 @@ def test_shared_lengths_outside_the_planes_leave_their_rows_alone(G):
         assert (out[G:].double() - want[G:].double()).abs().max() <= 2 ** -7
 
 
-@pytest.mark.parametrize("G", [3, 48])
-def test_shared_graph_replays_follow_the_device_and_repeat_bits(G):
-    S, H, KH, D, C = 2 * G, 8, 2, 128, 1500
+@pytest.mark.parametrize("G,KH,C", [(3, 2, 1500), (6, 8, 3600), (48, 2, 1500), (48, 2, 1800)])
+def test_shared_graph_replays_follow_the_device_and_repeat_bits(G, KH, C):
+    S, H, D = 2 * G, 4 * KH, 128
     shared, lens = i32(1000, 600), i32(*[1000 + s % 400 if s < G else 600 + s % 99 for s in range(S)])
-    cfg, q, k, v, out, lse, ws = shared_case(S, G, H, KH, D, C, shared.tolist(), lens.tolist(), seed=6)
+    cfg, q, k, v, out, lse, ws = shared_once(S, G, H, KH, D, C, shared.tolist(), lens.tolist(), seed=6)
     want, want_l = out.clone(), lse.clone()
     call = B.prepared(B.sirllm_attend_shared, cfg, 0, G, shared, q, k, v, lens, None, out, lse, ws)
     graph = torch.cuda.CUDAGraph()
@@ -577,10 +595,11 @@ def test_shared_graph_replays_follow_the_device_and_repeat_bits(G):
     assert same_bits(out, eager) and torch.equal(lse, eager_l)
 
 
-def test_shared_on_two_streams_at_once():
+@pytest.mark.parametrize("C", [2600, 10500])
+def test_shared_on_two_streams_at_once(C):
     S = G = 32
-    a = shared_case(S, G, 8, 2, 128, 2600, [2500], [2501 + s for s in range(S)], seed=21)
-    b = shared_case(S, G, 8, 2, 64, 2600, [2300], [2301 + s for s in range(S)], kv="f16", seed=22)
+    a = shared_once(S, G, 8, 2, 128, C, [2500], [2501 + s for s in range(S)], seed=21)
+    b = shared_once(S, G, 8, 2, 64, C, [2300], [2301 + s for s in range(S)], kv="f16", seed=22)
     calls, wants = [], []
     for (cfg, q, k, v, out, lse, ws), n in ((a, 2500), (b, 2300)):
         wants.append((out.clone(), lse.clone()))
