@@ -855,7 +855,7 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
             p.lead_blocks = S.lead_blocks;
             p.lead_member_units = cfg->n_kv_heads * S.lead_blocks;
             const int64_t walk_units = (int64_t)cfg->n_streams * p.units + (int64_t)p.lead_units * p.lead_member_units;
-            if (walk_units > 0x1FFFFFF || walk_units * most_tiles > 0x7FFFFFFF - kAttendMaxCtas) return SIRLLM_ERR_TOO_LARGE;
+            if (walk_units > 0x1FFFFFF || walk_units * most_tiles > 0x7FFFFFFF - kAttendMaxCtas * kAttendMaxWarps) return SIRLLM_ERR_TOO_LARGE;
         }
         if (S.how == kSharedProduct) {
             p.prefix = S.plan;

@@ -951,13 +951,18 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const AttendParam
     }
     const float2* const lead_ml = product ? p.prefix.part_ml : p.own_ml;
     const float* const lead_o = product ? p.prefix.part_o : p.own_o;
-    // The first time round is a rehearsal, in the shadow of the kernel before: it writes nothing.
-    int n = 1;
-    int2 own = make_int2(0, 1), lead = make_int2(0, 0);
-    bool real = false;
-again:
+    grid_dependency_wait();
+    const int n = p.kv_len[s], shared = p.shared_len[g];
+    int2 own = __ldcg(p.own_parts + own_unit);  // (of a stream without slots: whatever stands there)
+    int2 lead = __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
+    if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
+        if (threadIdx.x == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
+        return;
+    }
+    if (n == 0) own = make_int2(0, 0);
+    if (first_slot(p, shared, n) == 0) lead = make_int2(0, 0);
     const int parts = own.y + lead.y;
-    const int64_t own_at = real ? (own_unit + own.x) * p.part_rows + hq - block * p.part_rows : 0;
+    const int64_t own_at = (own_unit + own.x) * p.part_rows + hq - block * p.part_rows;
     const int64_t lead_at = (lead_unit + lead.x) * lead_step + lead_row;  // from part own.y on
     float m = kNegHuge, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1017,27 +1022,12 @@ again:
             acc.w = fmaf(v.w, f, acc.w);
         }
         const float f = n == 0 ? 0.f : 1.0f / sum;
-        if (on && real)
+        if (on)
             *reinterpret_cast<uint2*>(p.out + (int64_t)s * p.out_stride + (int64_t)head * p.head_dim + e) =
                 make_uint2(pack16<kBf16>(acc.x * f, acc.y * f), pack16<kBf16>(acc.z * f, acc.w * f));
-        if (lane == 0 && blockIdx.z == 0 && p.lse != nullptr && real)
+        if (lane == 0 && blockIdx.z == 0 && p.lse != nullptr)
             p.lse[(int64_t)s * p.n_heads + head] = n == 0 ? __uint_as_float(0xFF800000u) : (up + log2f(sum)) * (float)kLn2;
     }
-    if (real) return;
-    grid_dependency_wait();
-    n = p.kv_len[s];
-    const int shared = p.shared_len[g];
-    own = __ldcg(p.own_parts + own_unit);  // (of a stream without slots: whatever stands there)
-    lead = __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
-    if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
-        if (threadIdx.x == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
-        return;
-    }
-    if (n == 0) own = make_int2(0, 0);
-    if (first_slot(p, shared, n) == 0) lead = make_int2(0, 0);
-    real = true;
-    __syncthreads();
-    goto again;
 }
 
 template <bool kBf16, int kDim, int kTiles, int kWarps, int kStages, int kUse>

@@ -203,6 +203,46 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
     tmem_fence_after();
     const uint32_t tmem = tmem_base;
 
+    grid_dependency_wait();
+    if (warp == 2) {
+        // the line: its length, and this CTA's stretch
+        const int per_group = p.n_kv_heads * p.plan.units;
+        const int T0 = lane < p.n_groups ? group_tiles(p, lane) : 0;
+        int total = __reduce_add_sync(0xFFFFFFFFu, T0 * per_group);
+        for (int g0 = 32; g0 < p.n_groups; g0 += 32)
+            total += __reduce_add_sync(0xFFFFFFFFu, g0 + lane < p.n_groups ? group_tiles(p, g0 + lane) * per_group : 0);
+        const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 2);
+        const int begin = (int)min((int64_t)blockIdx.x * per, (int64_t)total);
+        Stretch w;
+        w.left = min(per, total - begin);
+        int before = 0;
+        for (int g0 = 0; g0 < p.n_groups && before <= begin; g0 += 32) {
+            const int g = g0 + lane;
+            const int T = g0 == 0 ? T0 : g < p.n_groups ? group_tiles(p, g) : 0;
+            int upto = T * per_group;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            const int start = before + upto - T * per_group;
+            if (w.left > 0 && T > 0 && begin >= start && begin < before + upto) {  // one lane, once
+                w.g = g;
+                w.u = (begin - start) / T;
+                w.t0 = begin - start - w.u * T;
+                w.tiles = T;
+                first = w;
+            }
+            before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+        }
+        if (lane == 0) tiles_per_cta = per;
+        if (w.left <= 0 && lane == 0) {
+            w.left = 0;
+            first = w;
+        }
+    }
+    __syncthreads();
+    grid_launch_dependents();
+
     // A wait that runs out raises the flag and every role leaves; the others see it or run out too.
     auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
         for (uint32_t i = 0; i < kSpinLimit; ++i) {
@@ -215,45 +255,6 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
     constexpr int kTilesAtOnce = kPair ? 1 : 2;  // tiles that the two lanes take together
 
     if (warp < 4) {
-        grid_dependency_wait();
-        if (warp == 2) {
-            // the line: its length, and this CTA's stretch
-            const int per_group = p.n_kv_heads * p.plan.units;
-            const int T0 = lane < p.n_groups ? group_tiles(p, lane) : 0;
-            int total = __reduce_add_sync(0xFFFFFFFFu, T0 * per_group);
-            for (int g0 = 32; g0 < p.n_groups; g0 += 32)
-                total += __reduce_add_sync(0xFFFFFFFFu, g0 + lane < p.n_groups ? group_tiles(p, g0 + lane) * per_group : 0);
-            const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 2);
-            const int begin = (int)min((int64_t)blockIdx.x * per, (int64_t)total);
-            Stretch w;
-            w.left = min(per, total - begin);
-            int before = 0;
-            for (int g0 = 0; g0 < p.n_groups && before <= begin; g0 += 32) {
-                const int g = g0 + lane;
-                const int T = g0 == 0 ? T0 : g < p.n_groups ? group_tiles(p, g) : 0;
-                int upto = T * per_group;
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-                    if (lane >= o) upto += v;
-                }
-                const int start = before + upto - T * per_group;
-                if (w.left > 0 && T > 0 && begin >= start && begin < before + upto) {  // one lane, once
-                    w.g = g;
-                    w.u = (begin - start) / T;
-                    w.t0 = begin - start - w.u * T;
-                    w.tiles = T;
-                    first = w;
-                }
-                before += __shfl_sync(0xFFFFFFFFu, upto, 31);
-            }
-            if (lane == 0) tiles_per_cta = per;
-            if (w.left <= 0 && lane == 0) {
-                w.left = 0;
-                first = w;
-            }
-        }
-        __syncthreads();
-        grid_launch_dependents();
         if (warp == 0) {  // ---- loads
             const bool issuer = elect_one();
             // K and V that only one CTA reads shall not push other things out of L2 (this kernel's
@@ -401,28 +402,23 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
         const float scale = p.scale_log2;
         const uint32_t flip = scale < 0.f ? 0x80000000u : 0u;  // the largest score is the smallest product then
         bool ok = true;
-        // The first time round is a rehearsal, on whatever is there, in the shadow of the kernel before: what is
-        // not in the instruction cache comes in at 250 cycles and more per 8 instructions, 4 us in all.
-        bool real = false;
-        Stretch w = {1, 0, 0, 0, kTilesAtOnce};
         // (a warp that gave up goes on to meet the others at their barriers)
-        while (w.left > 0) {
+        for (Stretch w = first; w.left > 0; w.next(p)) {
             const int kv_head = w.u / p.plan.units, block0 = kPair ? (w.u - kv_head * p.plan.units) * 2 : 0;
             const int block = block0 + (kPair ? ln : 0);
             const int used = max(0, min(p.plan.block_streams, p.stream_group - block * p.plan.block_streams)) * p.heads;
             const bool any = quarter * 32 < used;   // rows of this warp that are somebody's
-            const int tiles = real ? w.count() : kTilesAtOnce;
+            const int tiles = w.count();
             float m = kNegHuge, l = 0.f;
             bool fresh = true;
-            // Twice over a row's scores, 64 columns at a time, in loops (unrolled over the row, the first tile
-            // of a call took 2 us more; in steps of 32 columns the others 0.3 us more).
+            // Twice over a row's scores, 64 columns at a time, in loops: what is not in the instruction cache
+            // comes in at 250 cycles and more per 8 instructions (unrolled over the row, the first tile of a call
+            // took 2 us more; in steps of 32 columns the others 0.3 us more).
             for (int t = kPair ? 0 : ln; t < tiles && ok; t += kTilesAtOnce, fresh = false) {
-                if (real) {
-                    ok = __all_sync(0xFFFFFFFFu, wait(&s_full[ln], s_phase));
-                    if (!ok) break;
-                    s_phase ^= 1u;
-                    tmem_fence_after();
-                }
+                ok = __all_sync(0xFFFFFFFFu, wait(&s_full[ln], s_phase));
+                if (!ok) break;
+                s_phase ^= 1u;
+                tmem_fence_after();
                 if (any) {
                     float top[4] = {kLowest, kLowest, kLowest, kLowest};
 #pragma unroll 1
@@ -437,7 +433,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                                                       __uint_as_float(s[j >> 5][(j & 31) + 1] ^ flip));
                     }
                     const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(scale);
-                    if (__any_sync(0xFFFFFFFFu, !real || high > m + kMoveAt<kBf16>)) {
+                    if (__any_sync(0xFFFFFFFFu, high > m + kMoveAt<kBf16>)) {
                         const float up = fmaxf(m, high - kSetBelow<kBf16>);
                         const float f = ex2_approx(m - up);
                         m = up;
@@ -471,11 +467,11 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                             sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], pack2(e0, e1));
                             w16[j >> 1] = pack16<kBf16>(e0, e1);
                         }
-                        if (real) tmem_give32(s_at + i * 32, w16);  // half of the weights, over scores that have been read
+                        tmem_give32(s_at + i * 32, w16);  // half of the weights, over scores that have been read
                         tmem_wait_stores();
                         tmem_fence_before();
                         __syncwarp();
-                        if (lane == 0 && real) mbar_arrive(&p_full[ln][i]);
+                        if (lane == 0) mbar_arrive(&p_full[ln][i]);
                     }
                     float s0, s1;
                     unpack2(add2(sum[0], sum[1]), s0, s1);
@@ -483,7 +479,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                 } else {
                     tmem_fence_before();
                     __syncwarp();
-                    if (lane < 2 && real) mbar_arrive(&p_full[ln][lane]);
+                    if (lane < 2) mbar_arrive(&p_full[ln][lane]);
                 }
             }
             // ---- the unit's part -----------------------------------------------------------------
@@ -491,11 +487,11 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
             const int64_t place =
                 ((int64_t)w.g * p.n_kv_heads * p.plan.units + w.u + blockIdx.x) * p.plan.rows + row + (kPair ? ln * kPrefixRows : 0);
             for (int x = 0; x < 2; ++x)
-                if (x < lanes_used && (!kPair || x == ln) && ok && real) {
+                if (x < lanes_used && (!kPair || x == ln) && ok) {
                     ok = __all_sync(0xFFFFFFFFu, wait(&o_full[x], o_phase[x]));
                     o_phase[x] ^= 1u;
                 }
-            if (w.t0 == 0 && tid == kThreads - 1 && real) {  // where the unit's parts are
+            if (w.t0 == 0 && tid == kThreads - 1) {  // where the unit's parts are
                 const int behind = w.tiles - w.count();
                 p.plan.parts[w.g * p.n_kv_heads * p.plan.units + w.u] =
                     make_int2(blockIdx.x, 1 + (behind + tiles_per_cta - 1) / tiles_per_cta);
@@ -509,13 +505,13 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                         uint32_t o[32];
                         tmem_ask32(o, o_at + i * 32);
                         tmem_wait_loads();
-                        if (row < used && real) {
+                        if (row < used) {
 #pragma unroll
                             for (int j = 0; j < 32; j += 8)
                                 if (i * 32 + j < p.head_dim) store8(dst + i * 32 + j, o + j);
                         }
                     }
-                    if (row < used && real) p.plan.part_ml[place] = make_float2(m, l);
+                    if (row < used) p.plan.part_ml[place] = make_float2(m, l);
                 }
             } else {
                 // the even and the odd tiles into one; each of a row's two threads takes half of the columns
@@ -527,7 +523,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                     const float up = fmaxf(m, odd.x);
                     f = make_float2(ex2_approx(m - up), ex2_approx(odd.x - up));
                     stats[row] = f;
-                    if (row < used && ok && real) p.plan.part_ml[place] = make_float2(up, l * f.x + odd.y * f.y);
+                    if (row < used && ok) p.plan.part_ml[place] = make_float2(up, l * f.x + odd.y * f.y);
                 }
                 asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
                 if (ln == 1) f = stats[row];
@@ -540,7 +536,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                         tmem_ask32(o, lanes + kOutCol + col);
                         tmem_ask32(q, lanes + kOutCol + kLaneCols + col);
                         tmem_wait_loads();
-                        if (row < used && real) {
+                        if (row < used) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) {
                                 float v = __uint_as_float(o[j]) * f.x;
@@ -556,16 +552,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
             }
             tmem_fence_before();
             __syncwarp();
-            if (real) {
-                if (lane == 0) mbar_arrive(&o_empty);
-                w.next(p);
-            } else {
-                grid_dependency_wait();
-                __syncthreads();
-                grid_launch_dependents();
-                w = first;
-                real = true;
-            }
+            if (lane == 0) mbar_arrive(&o_empty);
         }
     }
     tmem_fence_before();

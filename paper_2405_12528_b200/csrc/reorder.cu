@@ -229,8 +229,13 @@ cudaError_t launch_reorder(const ReorderParams& p, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     ReorderParams q = p;
     const int groups = p.n_streams / p.group;
-    // two waves of CTAs: a group without moves leaves its room to others, and SMs differ in speed
-    q.ctas = (2 * kCtasPerSm * dp.n_sm + groups - 1) / groups;
+    // Two waves of CTAs: a group without moves leaves its room to others, and SMs differ in speed.  But no more
+    // than have eight pieces each if all streams move whole planes: 1184 CTAs of which a hundred had work
+    // took 2 us for their arrivals alone.
+    const int64_t pieces = ((int64_t)p.capacity * p.row_bytes + kPiece - 1) / kPiece * p.planes *
+                           ((p.k != nullptr) + (p.v != nullptr)) * p.group;
+    const int64_t waves = (2 * kCtasPerSm * dp.n_sm + groups - 1) / groups;
+    q.ctas = (int)(pieces / 8 + 1 < waves ? pieces / 8 + 1 : waves);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(groups * q.ctas));
     cfg.blockDim = dim3(32);
