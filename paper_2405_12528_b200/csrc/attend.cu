@@ -1118,9 +1118,13 @@ cudaError_t launch_use(const AttendParams& p, const DeviceProps& dp, cudaStream_
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.n_streams, p.n_heads, (p.head_dim + 127) / 128);
-    // Four warps to a head as long as the GPU holds them all at once (eight beams of 12001 slots 44 -> 31 us
-    // with them); one where there are more heads (16 x 8 beams of 1000 slots 38 us, 48 with four).
-    const bool shared_by_four = (int64_t)p.n_streams * p.n_heads * 4 <= dp.n_sm * 64;
+    // A head's parts are those that the shared slots' line was cut into, per unit, at most (the lengths may leave
+    // fewer).  Four warps to a head where they are many (eight beams of 12001 slots, 60 parts, 44 -> 31 us with
+    // four), as long as the GPU holds them all at once (16 x 8 beams of 1000 slots 38 us, 48 with four).
+    const int64_t lead = p.lead_units > 0 ? (int64_t)p.lead_units * p.lead_member_units
+                                          : (int64_t)(p.n_streams / p.stream_group) * (p.n_heads / p.group) * p.prefix.units;
+    const int64_t parts = (p.lead_units > 0 ? 8 : 1) * (int64_t)dp.n_sm / lead;
+    const bool shared_by_four = parts > 24 && (int64_t)p.n_streams * p.n_heads * 4 <= dp.n_sm * 64;
     cfg.blockDim = dim3(shared_by_four ? 128 : 32);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
