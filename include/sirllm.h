@@ -359,7 +359,9 @@ int sirllm_attend(const sirllm_config *cfg, int32_t layer, const void *q, int32_
  *   group       divides n_streams;  shared_len int32 [n_streams / group]
  *   ws          a workspace of its own kind, for this group and n_heads: sirllm_attend_shared_workspace_bytes()
  *               bytes (0 for an invalid combination); the rules of sirllm_attend's hold for it
- * All other arguments, limits and results as in sirllm_attend.
+ * All other arguments, limits and results as in sirllm_attend; n_heads at most 65535 and q's rows at most
+ * 2^38 elements apart where the shared slots are computed once for the group, else SIRLLM_ERR_TOO_LARGE.
+ * SIRLLM_STATUS_TIMEOUT: a device-side wait gave up, results are unreliable.
  */
 size_t sirllm_attend_shared_workspace_bytes(const sirllm_config *cfg, int32_t group, int32_t n_heads);
 int sirllm_attend_shared_workspace_init(const sirllm_config *cfg, int32_t group, int32_t n_heads, void *ws,

@@ -841,7 +841,8 @@ static int attend_impl(const sirllm_config* cfg, int32_t layer, int32_t group, c
     if (shared_len != nullptr) {
         const AttendSharedLayout S = attend_shared_layout(*cfg, group, n_heads);
         if (S.how != kSharedRead) {
-            if (n_heads > 65535) return SIRLLM_ERR_TOO_LARGE;  // (a grid's second dimension)
+            // a grid's second dimension, a tensor map's strides
+            if (n_heads > 65535 || q_row_stride > ((int64_t)1 << 38)) return SIRLLM_ERR_TOO_LARGE;
             p.own_ml = (float2*)((char*)ws + S.own_ml_off);
             p.own_o = (float*)((char*)ws + S.own_o_off);
             p.own_parts = (int2*)((char*)ws + S.own_parts_off);
