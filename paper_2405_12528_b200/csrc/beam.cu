@@ -328,14 +328,15 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row0 = g * p.group;
     for (int r = warp; r < p.group; r += kWarps) {
+        const float2* pairs = p.pairs + (int64_t)(row0 + r) * p.parts;
+        const float2 early = __ldcg(&pairs[min(lane, p.parts - 1)]);  // (of a row without a beam: whatever stands there)
         const float t = p.totals[row0 + r];
         const bool e = p.ended != nullptr && p.ended[row0 + r] != 0;
         float top = __uint_as_float(0xFF800000u);
         double sum = 0.0;
         if (t > -INFINITY && !e) {
-            const float2* pairs = p.pairs + (int64_t)(row0 + r) * p.parts;
             for (int i = lane; i < p.parts; i += 32) {
-                const float2 v = __ldcg(&pairs[i]);
+                const float2 v = i < 32 ? early : __ldcg(&pairs[i]);
                 if (v.y > 0.f) {  // (running: a row of more than 32 segments)
                     const float up = fmaxf(top, v.x);
                     sum = sum * exp_of(top - up) + (double)v.y * exp_of(v.x - up);
@@ -401,11 +402,14 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
                         hits |= (uint32_t)(a + off_by >= reach && a > none && off + k * 32 < t.length) << k;
                     }
 #pragma unroll 1
-                    for (hits = bound ? 0 : hits; hits != 0; hits &= hits - 1) {  // one copy of this code, the item again
-                        const int at = off + (__ffs(hits) - 1) * 32, n = atomicAdd(&sh.listed, 1);
+                    for (hits = bound ? 0 : hits; hits != 0; hits &= hits - 1) {  // one copy of this code
+                        const int k = __ffs(hits) - 1, n = atomicAdd(&sh.listed, 1);
+                        float hit = z[0];
+#pragma unroll
+                        for (int x = 1; x < kBatch; ++x) hit = k == x ? z[x] : hit;
                         if (n < kList) {
-                            sh.list_at[n] = ((unsigned long long)t.row << 32) | (uint32_t)(t.first + at);
-                            sh.list_z[n] = t.item(at);
+                            sh.list_at[n] = ((unsigned long long)t.row << 32) | (uint32_t)(t.first + off + k * 32);
+                            sh.list_z[n] = hit;
                         }
                     }
                 }
