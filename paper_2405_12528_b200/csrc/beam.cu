@@ -14,6 +14,9 @@
 // What reaches the bound is listed and ranked by counting.  A list that overflows is made again with the
 // n_out-th largest of all threads' best as the bound, and if that overflows too (thousands of equal
 // scores) the best come out in n_out rounds of maximum: slow, and right.
+// Measured, bf16: 512 rows x 128256 (8 to a group, four fifths of them live) 42.5 us, of which the stream takes 15.5
+// (6.8 TB/s) and the search 15; 128 x 128256, 16 candidates 27.0; 4 x 32000 11.2.  The search waits for loads
+// that depend on one another and for instructions that are executed once.
 // On the way here, 512 x 128256 bf16: chunks of 32 KB per CTA, with barriers between loading, bounding,
 // listing and ranking, 61 us; warps that keep lists of their own while they stream, 83 us; blocks
 // without segments, bounds taken anew at every level, 53 us.

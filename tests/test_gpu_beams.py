@@ -200,6 +200,27 @@ def test_select_extreme_totals_and_logits():
     check_select(z - 1e6, 1, 1, totals)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_select_negative_zero_is_zero(dtype):
+    z = torch.full((2, 600), -3.0, dtype=dtype, device="cuda")
+    z[:, 50:400:7] = 0.0
+    z[:, 57] = -0.0                              # equal to its neighbours, ahead of all but one of them
+    z[1, 43] = -0.0
+    check_select(z, 1, 20, torch.tensor([-1.0, -1.0], device="cuda"))
+    check_select(z, 2, 40, torch.tensor([-1.0, -1.0], device="cuda"))
+
+
+@pytest.mark.parametrize("G,N", [(8, 8), (4, 16), (64, 64)])
+def test_select_wide_rows_masked_but_for_a_few_tokens(G, N):
+    g = gen(16)
+    z, totals = beams(16, G, 128256, torch.bfloat16)
+    keep = torch.rand(G, 128256, generator=g, device="cuda") < 0.0005
+    z[~keep] = -math.inf
+    check_select(z, G, N, totals)
+    z[:, 64000:64300] = 1.0                      # and a run of equal ones
+    check_select(z, G, N, totals)
+
+
 def test_select_reads_one_row_per_stream_whatever_max_new_is():
     z, totals = beams(13, 6, 800, torch.float32)
     check_select(z, 3, 3, totals, cfg=config(S=6, V=800, M=64))
@@ -446,6 +467,22 @@ def test_shared_streams_shorter_than_the_shared_slots(G, group):
     lens = [(0, 1, 100, 383, 384, 385, 699, 700, 701, 900)[s % 10] for s in range(2 * G)]
     shared_case(2 * G, G, 2 * group, 2, 128, 1000, shared, lens, seed=G)
     shared_case(2 * G, G, 2 * group, 2, 64, 1000, shared, [n if s % 3 else 0 for s, n in enumerate(lens)], kv="f16", seed=G)
+
+
+@pytest.mark.parametrize("D", [128, 256])
+@pytest.mark.parametrize("G,group,KH", [(2, 16, 2), (2, 16, 16), (3, 10, 16), (8, 8, 16)])
+def test_shared_groups_of_many_heads(D, G, group, KH):
+    # units of one and of several blocks, with heads of a stream that two blocks share
+    lens = [900 + 31 * s for s in range(2 * G)]
+    shared_case(2 * G, G, group * KH, KH, D, 1400, [900, 333], lens, seed=D + group, fill=math.nan)
+
+
+@pytest.mark.parametrize("G,C", [(8, 600), (4, 45000), (40, 6000)])
+def test_shared_without_log_sums(G, C):
+    cfg, q, k, v, out, lse, ws = shared_once(G, G, 4, 2, 64, C, [400], [401 + s for s in range(G)], seed=9)
+    again = torch.zeros_like(out)
+    B.sirllm_attend_shared(cfg, 0, G, i32(400), q, k, v, i32(*[401 + s for s in range(G)]), None, again, None, ws)
+    assert same_bits(again, out)
 
 
 @pytest.mark.parametrize("n,D", [(16384, 128), (48990, 64), (30011, 128)])
