@@ -150,11 +150,9 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
     AttendSharedLayout L;
     L.own = attend_layout(c);
     const int64_t rows = (int64_t)group * (n_heads / c.n_kv_heads);   // query heads of a group that share a K/V head
-    // Few rows and little to read (a stream's shared slots as often as there are streams, at most): every
-    // stream reads them itself, in one launch.
     const int64_t most = (int64_t)c.n_streams * c.n_kv_heads * c.capacity * c.head_dim * 4;
     L.how = kSharedRead;
-    if (group > 1 && most > kSharedReadBytes) {
+    if (group > 1 && (most > kSharedReadBytes || most / group > kSharedReadOnce)) {
         if (rows <= kSharedUnitRows)
             L.how = kSharedUnits;
         else if (prefix_plan(c, group, n_heads, &L.plan))

@@ -386,7 +386,7 @@ def test_reorder_past_32_bits():
 # attend
 # --------------------------------------------------------------------------------------
 
-PARTS_FROM = 160 * 2**20    # bytes of K and V of a layer from which on shared slots are computed once for the group
+PARTS_FROM = 160 * 2**20    # bytes of K and V of a layer from which on shared slots are computed once at any group
 
 
 def capacities(S, KH, D, C):
