@@ -520,34 +520,24 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
 
 template <bool kBf16>
 __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const BeamParams p) {
-    __shared__ int ended_groups[kWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ int last_one;
+    const int warp = threadIdx.x >> 5;
     grid_dependency_wait();
     grid_launch_dependents();
-    // segment: all of a row's, then the next row's
-    const int64_t segment = (int64_t)blockIdx.x * kWarps + warp;
-    int ended_group = -1;
-    if (segment < (int64_t)p.n_streams * p.parts) {
-        const int row = (int)(segment / p.parts), g = row / p.group;
-        if (p.totals[row] > -INFINITY && !(p.ended != nullptr && p.ended[row] != 0))
-            scan_segment<kBf16>(p, row, (int)(segment - (int64_t)row * p.parts));
-        __syncwarp();
-        if (lane == 0) {
-            int before;
-            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(&p.tickets[g]) : "memory");
-            if (before == p.group * p.parts - 1) {
-                p.tickets[g] = 0;  // for the next call
-                ended_group = g;
-            }
-        }
-    }
-    if (lane == 0) ended_groups[warp] = ended_group;
+    // A CTA works for one group: eight of its segments, all of a row's, then the next row's.
+    const int g = blockIdx.x / p.group_ctas, cta = blockIdx.x - g * p.group_ctas, segment = cta * kWarps + warp;
+    const int in_group = segment / p.parts, row = g * p.group + in_group;
+    if (in_group < p.group && p.totals[row] > -INFINITY && !(p.ended != nullptr && p.ended[row] != 0))
+        scan_segment<kBf16>(p, row, segment - in_group * p.parts);
     __syncthreads();
-    for (int w = 0; w < kWarps; ++w)
-        if (ended_groups[w] >= 0) {
-            join_group<kBf16>(p, ended_groups[w]);
-            __syncthreads();
-        }
+    if (threadIdx.x == 0) {
+        int before;
+        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(&p.tickets[g]) : "memory");
+        last_one = before == p.group_ctas - 1;
+        if (last_one) p.tickets[g] = 0;  // for the next call
+    }
+    __syncthreads();
+    if (last_one) join_group<kBf16>(p, g);
 }
 
 }  // namespace
@@ -555,7 +545,9 @@ __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const BeamParams p) {
 cudaError_t launch_beam(const BeamParams& p, cudaStream_t st) {
     TraceRange trace("sirllm:beam_select");
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(((int64_t)p.n_streams * p.parts + kWarps - 1) / kWarps));
+    BeamParams q = p;
+    q.group_ctas = (p.group * p.parts + kWarps - 1) / kWarps;
+    cfg.gridDim = dim3((unsigned)(p.n_streams / p.group * q.group_ctas));
     cfg.blockDim = dim3(kThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -563,8 +555,8 @@ cudaError_t launch_beam(const BeamParams& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return p.logits_dtype == SIRLLM_BF16 ? cudaLaunchKernelEx(&cfg, beam_kernel<true>, p)
-                                         : cudaLaunchKernelEx(&cfg, beam_kernel<false>, p);
+    return p.logits_dtype == SIRLLM_BF16 ? cudaLaunchKernelEx(&cfg, beam_kernel<true>, q)
+                                         : cudaLaunchKernelEx(&cfg, beam_kernel<false>, q);
 }
 
 }  // namespace sirllm

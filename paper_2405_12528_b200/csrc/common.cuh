@@ -311,6 +311,7 @@ struct BeamParams {
     float* block_max;
     int64_t vocab, row_stride;
     int32_t n_streams, group, n_out, end_token, places, parts, trips, blocks, logits_dtype;
+    int32_t group_ctas;              // of a group, set by the launcher
 };
 
 struct ReorderParams {
