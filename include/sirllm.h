@@ -84,6 +84,7 @@ extern "C" {
 /* Largest groups of streams: beams of sirllm_beam_select (and its candidates), streams of
  * sirllm_reorder_streams. */
 #define SIRLLM_MAX_BEAMS 64
+#define SIRLLM_MAX_BEAM_VOCAB (1 << 26) /* largest vocabulary of sirllm_beam_select */
 #define SIRLLM_MAX_GROUP 256
 
 typedef struct sirllm_config {
@@ -393,7 +394,8 @@ int sirllm_attend_shared(const sirllm_config *cfg, int32_t layer, int32_t group,
  *   totals      fp32 [n_streams];  ended int32 [n_streams] or NULL (none has);  end_token in [0, vocab) or -1 (none)
  *   outputs     [n_streams / group * n_out]; entropy and ended_out may be NULL.  Where n_out == group,
  *               totals_out may be totals itself and ended_out may be ended itself; else nothing overlaps
- *   limits      group and n_out at most SIRLLM_MAX_BEAMS, else SIRLLM_ERR_TOO_LARGE
+ *   limits      group and n_out at most SIRLLM_MAX_BEAMS, vocab at most SIRLLM_MAX_BEAM_VOCAB, else
+ *               SIRLLM_ERR_TOO_LARGE
  *   ws          its own kind of workspace: sirllm_beam_workspace_bytes() bytes, 256-byte aligned, set up once
  *               with sirllm_beam_workspace_init(); calls that can overlap on the GPU need one each
  */

@@ -22,7 +22,7 @@ OK, ERR_NULL, ERR_BAD_CONFIG, ERR_ALIGN, ERR_CUDA, ERR_TOO_LARGE = 0, -1, -2, -3
 STATUS_TOKEN_RANGE, STATUS_OVERFLOW, STATUS_TIMEOUT, STATUS_BAD_KEEP, STATUS_BAD_SOURCE = 1, 2, 4, 8, 16
 MAX_CAPACITY = 49152
 MAX_ATTEND_HEAD_DIM = 256
-MAX_BEAMS, MAX_GROUP = 64, 256
+MAX_BEAMS, MAX_GROUP, MAX_BEAM_VOCAB = 64, 256, 1 << 26
 POLICY_STREAM, POLICY_RANDOM, POLICY_INTERVAL = 1, 2, 3
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 

@@ -942,7 +942,8 @@ int sirllm_beam_select(const sirllm_config* cfg, const void* logits, int32_t gro
     if (group < 1 || cfg->n_streams % group != 0 || n_out < 1 || (places && n_out != group) || end_token < -1 ||
         end_token >= cfg->vocab)
         return SIRLLM_ERR_BAD_CONFIG;
-    if (group > SIRLLM_MAX_BEAMS || n_out > SIRLLM_MAX_BEAMS) return SIRLLM_ERR_TOO_LARGE;
+    if (group > SIRLLM_MAX_BEAMS || n_out > SIRLLM_MAX_BEAMS || cfg->vocab > SIRLLM_MAX_BEAM_VOCAB)
+        return SIRLLM_ERR_TOO_LARGE;
     if (n_out != group && (totals_out == totals || (ended && ended_out == ended))) return SIRLLM_ERR_BAD_CONFIG;
     const BeamLayout L = beam_layout(*cfg);
     if (L.tiling.parts * cfg->n_streams > 0x7FFFFFFF || (int64_t)L.tiling.blocks * group > 0x7FFFFFFF - kBeamThreads)

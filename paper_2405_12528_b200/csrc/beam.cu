@@ -14,12 +14,13 @@
 // What reaches the bound is listed and ranked by counting.  A list that overflows is made again with the
 // n_out-th largest of all threads' best as the bound, and if that overflows too (thousands of equal
 // scores) the best come out in n_out rounds of maximum: slow, and right.
-// Measured, bf16: 512 rows x 128256 (8 to a group, four fifths of them live) 42.5 us, of which the stream takes 15.5
-// (6.8 TB/s) and the search 15; 128 x 128256, 16 candidates 27.0; 4 x 32000 11.2.  The search waits for loads
+// Measured, bf16: 512 rows x 128256 (8 to a group, four fifths of them live) 42.9 us, of which the stream takes 15.5
+// (6.8 TB/s) and the search 15; 128 x 128256, 16 candidates 25.5; 4 x 32000 10.4; 64 beams and candidates 40 - 65.  The search waits for loads
 // that depend on one another and for instructions that are executed once.
 // On the way here, 512 x 128256 bf16: chunks of 32 KB per CTA, with barriers between loading, bounding,
 // listing and ranking, 61 us; warps that keep lists of their own while they stream, 83 us; blocks
-// without segments, bounds taken anew at every level, 53 us.
+// without segments, bounds taken anew at every level, 53 us.  Ranking
+// by one 128-bit entry per candidate, eight at a time, in place of three arrays: two groups of 64 beams 73 -> 57 us.
 #include "common.cuh"
 
 namespace sirllm {
@@ -29,6 +30,7 @@ namespace {
 constexpr int kThreads = kBeamThreads;
 constexpr int kWarps = kThreads / 32;
 constexpr int kList = 1024;
+constexpr int kRankStep = 8;  // entries compared with at a time
 constexpr int kLevels = 3;
 constexpr int kFewBlocks = 2048;
 constexpr int kRankAll = 64;
@@ -111,17 +113,22 @@ __device__ __noinline__ float reach_by_threads(float mine, uint32_t* all, uint32
     return from_key(*found);
 }
 
-struct Found {                // one candidate of a group
-    unsigned long long score;  // order key of its fp64 score
-    unsigned long long at;     // (row within the group) << 32 | token
-    float z;                   // its logit
+// One candidate of a group (or segment, or block).  Of equal scores the better one has the lower place: the lower
+// stream, then the larger logit (a huge total hides it), then the lower token.
+constexpr int kIndexBits = 26;
+struct __align__(16) Found {
+    unsigned long long score;  // order key of its fp64 score; 0: none
+    unsigned long long place;  // row within the group (6 bits), order key of its logit inverted, index
+    __device__ __forceinline__ int row() const { return (int)(place >> (32 + kIndexBits)); }
+    __device__ __forceinline__ int index() const { return (int)(place & ((1u << kIndexBits) - 1u)); }
+    __device__ __forceinline__ float logit() const { return from_key(~(uint32_t)(place >> kIndexBits)); }
 };
-// Of equal scores: the lower stream, then the larger logit (a huge total hides it), then the lower token.
-__device__ __forceinline__ bool ahead(unsigned long long at_a, float za, unsigned long long at_b, float zb) {
-    return (at_a >> 32) == (at_b >> 32) && za != zb ? za > zb : at_a < at_b;
+static_assert(SIRLLM_MAX_BEAMS <= 64 && SIRLLM_MAX_BEAM_VOCAB <= 1 << kIndexBits, "a place fits 64 bits");
+__device__ __forceinline__ unsigned long long place_of(int row, float z, int index) {
+    return ((unsigned long long)row << (32 + kIndexBits)) | ((unsigned long long)~key_of(z) << kIndexBits) | (uint32_t)index;
 }
 __device__ __forceinline__ bool better(const Found& a, const Found& b) {
-    return a.score > b.score || (a.score == b.score && ahead(a.at, a.z, b.at, b.z));
+    return a.score > b.score || (a.score == b.score && a.place < b.place);
 }
 
 // 16 bytes of a row of which some elements lie outside [0, vocab): those count as -inf
@@ -153,9 +160,7 @@ __device__ __forceinline__ float largest(const uint4& v) {
 }
 
 struct BeamShared {
-    unsigned long long list[kList];    // what reaches the bound: scores,
-    unsigned long long list_at[kList]; // places
-    float list_z[kList];               // and logits
+    Found list[kList + kRankStep];  // what reaches the bound
     uint32_t maxima[kThreads];
     uint32_t bound;
     float tops[kWarps], bounds[kWarps], nths[kWarps];
@@ -167,9 +172,11 @@ struct BeamShared {
     double total_of[kBeamMaxGroup], log_of[kBeamMaxGroup];
     float top_of[kBeamMaxGroup], const_of[kBeamMaxGroup];  // const: total - log sum, -inf for a row without logits that count
     int skew_of[kBeamMaxGroup];                            // elements between a row and its first block's start
-    __device__ __forceinline__ double score(unsigned long long at, float z) const {
-        const int r = (int)(at >> 32);
-        return ended_row[r] ? total_of[r] : total_of[r] + (((double)z - (double)top_of[r]) - log_of[r]);
+    __device__ __forceinline__ unsigned long long score(unsigned long long place) const {  // its order key
+        const Found f = {0, place};
+        const int r = f.row();
+        return key64_of(ended_row[r] ? total_of[r]
+                                     : total_of[r] + (((double)f.logit() - (double)top_of[r]) - log_of[r]));
     }
     unsigned char ended_row[kBeamMaxGroup];
     int first_of[kBeamMaxGroup];       // the first candidate of every row
@@ -270,7 +277,7 @@ __device__ __forceinline__ Strip strip_of(const BeamParams& p, const BeamShared&
     if (level == 0 && !few_blocks(p)) return {i, 0, p.parts, reinterpret_cast<const char*>(p.pairs + (int64_t)(row0 + i) * p.parts), 8};
     if (level == 0) return {i, 0, p.blocks, reinterpret_cast<const char*>(p.block_max + (int64_t)(row0 + i) * p.blocks), 4};
     const Found f = sh.chosen[level - (few_blocks(p) ? 2 : 1)][i];
-    const int row = (int)(f.at >> 32), at = (int)(uint32_t)f.at;
+    const int row = f.row(), at = f.index();
     if (f.score == 0 || sh.ended_row[row]) return {-1, 0, 0, nullptr, 4};
     if (level == 1) {
         const int first = at * p.trips * kStep;
@@ -287,13 +294,13 @@ template <bool kBf16>
 __device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, int g, int level) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row0 = g * p.group;
     const int strips = level == 0 ? p.group : p.n_out;
-    Found last = {~0ull, 0, 0.f};
+    Found last = {~0ull, 0};
     __syncthreads();
     for (int round = 0; round < p.n_out; ++round) {
-        Found own = {0, ~0ull, 0.f};
+        Found own = {0, ~0ull};
         auto offer = [&](int r, int b, float z) {
-            const unsigned long long at = ((unsigned long long)r << 32) | (uint32_t)b;
-            const Found f = {key64_of(sh.score(at, z)), at, z};
+            const unsigned long long place = place_of(r, z, b);
+            const Found f = {sh.score(place), place};
             if (better(last, f) && better(f, own)) own = f;
         };
         for (int i = warp; i < strips; i += kWarps) {
@@ -309,8 +316,7 @@ __device__ __noinline__ void best_of_many(const BeamParams& p, BeamShared& sh, i
         for (int x = 16; x > 0; x >>= 1) {
             Found o;
             o.score = __shfl_xor_sync(0xFFFFFFFFu, own.score, x);
-            o.at = __shfl_xor_sync(0xFFFFFFFFu, own.at, x);
-            o.z = __shfl_xor_sync(0xFFFFFFFFu, own.z, x);
+            o.place = __shfl_xor_sync(0xFFFFFFFFu, own.place, x);
             if (better(o, own)) own = o;
         }
         if (lane == 0) sh.warp_found[warp] = own;
@@ -410,10 +416,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
                         float hit = z[0];
 #pragma unroll
                         for (int x = 1; x < kBatch; ++x) hit = k == x ? z[x] : hit;
-                        if (n < kList) {
-                            sh.list_at[n] = ((unsigned long long)t.row << 32) | (uint32_t)(t.first + off + k * 32);
-                            sh.list_z[n] = hit;
-                        }
+                        if (n < kList) sh.list[n].place = place_of(t.row, hit, t.first + off + k * 32);
                     }
                 }
             }
@@ -425,10 +428,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
                         mine = fmaxf(mine, t);
                     } else if (t >= reach) {
                         const int n = atomicAdd(&sh.listed, 1);
-                        if (n < kList) {
-                            sh.list_at[n] = (unsigned long long)r << 32;
-                            sh.list_z[n] = 0.f;
-                        }
+                        if (n < kList) sh.list[n].place = place_of(r, 0.f, 0);
                     }
                 }
         };
@@ -453,26 +453,25 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
             }
         }
         if (n <= kList) {
-            for (int i = tid; i < n; i += kThreads) sh.list[i] = key64_of(sh.score(sh.list_at[i], sh.list_z[i]));
+            for (int i = tid; i < n + kRankStep; i += kThreads) {
+                if (i < n) sh.list[i].score = sh.score(sh.list[i].place);
+                else sh.list[i] = {0, ~0ull};  // behind the last one: not better than any
+            }
             __syncthreads();
 #pragma unroll 1
             for (int i = tid; i < n; i += kThreads) {
-                const unsigned long long score = sh.list[i], at = sh.list_at[i];
-                const float z = sh.list_z[i];
+                const Found mine_now = sh.list[i];
                 int rank = 0;
-                bool hidden = false;
-#pragma unroll 4
-                for (int j = 0; j < n; ++j) {  // (without a branch: equal scores are frequent with 16-bit logits)
-                    const unsigned long long x = sh.list[j], at_j = sh.list_at[j];
-                    const bool same = x == score;
-                    rank += (x > score) | (same & (at_j < at));
-                    hidden |= same & (sh.list_z[j] != z) & ((at_j >> 32) == (at >> 32));
+#pragma unroll 1
+                for (int j = 0; j < n; j += kRankStep) {
+                    Found x[kRankStep];
+#pragma unroll
+                    for (int k = 0; k < kRankStep; ++k) x[k] = sh.list[j + k];
+#pragma unroll
+                    for (int k = 0; k < kRankStep; ++k)
+                        rank += (x[k].score > mine_now.score) | ((x[k].score == mine_now.score) & (x[k].place < mine_now.place));
                 }
-                if (hidden) {  // a total so large that it hides the order of the logits
-                    rank = 0;
-                    for (int j = 0; j < n; ++j) rank += better({sh.list[j], sh.list_at[j], sh.list_z[j]}, {score, at, z});
-                }
-                if (rank < p.n_out) chosen[rank] = {score, at, z};
+                if (rank < p.n_out) chosen[rank] = mine_now;
             }
             __syncthreads();
         } else {
@@ -485,7 +484,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
     // ---- out: in order, or a stream's best in the stream's own place and the others in the free ones ---
     const Found f = sh.chosen[kLevels - 1][tid < p.n_out ? tid : 0];
     const bool real = tid < p.n_out && f.score != 0;
-    const int r = real ? (int)(f.at >> 32) : -1;
+    const int r = real ? f.row() : -1;
     int place = tid;
     if (p.places) {  // n_out == group
         if (real) atomicMin(&sh.first_of[r], tid);
@@ -507,13 +506,13 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
     }
     if (tid < p.n_out) {
         const bool was_ended = real && sh.ended_row[r];
-        const int token = !real ? -1 : was_ended ? p.end_token : (int)(uint32_t)f.at;
+        const int token = !real ? -1 : was_ended ? p.end_token : f.index();
         const int64_t at = (int64_t)g * p.n_out + place;
         p.totals_out[at] = real ? (float)from_key64(f.score) : -INFINITY;
         p.source[at] = real ? row0 + r : -1;
         p.token_ids[at] = token;
         if (p.entropy != nullptr)
-            p.entropy[at] = real && !was_ended ? (float)(sh.log_of[r] - ((double)f.z - (double)sh.top_of[r])) : 0.f;
+            p.entropy[at] = real && !was_ended ? (float)(sh.log_of[r] - ((double)f.logit() - (double)sh.top_of[r])) : 0.f;
         if (p.ended_out != nullptr) p.ended_out[at] = real && (was_ended || (p.end_token >= 0 && token == p.end_token));
     }
 }

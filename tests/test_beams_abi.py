@@ -51,6 +51,7 @@ def test_select_refusals(lib, want, kw):
 def test_select_refuses_large_groups_and_bad_configurations(lib):
     assert select(lib, cfg(n_streams=130), group=65, n_out=4, totals_out=2 * P) == B.ERR_TOO_LARGE
     assert select(lib, cfg(budget=5)) == B.ERR_BAD_CONFIG
+    assert select(lib, cfg(vocab=2**26 + 1)) == B.ERR_TOO_LARGE
     assert select(lib, cfg(n_streams=2**24, n_layers=1, vocab=2**31 - 1), group=1, n_out=1) == B.ERR_TOO_LARGE
 
 
