@@ -157,6 +157,10 @@ static AttendSharedLayout attend_shared_layout(const sirllm_config& c, int32_t g
             L.how = kSharedUnits;
         else if (prefix_plan(c, group, n_heads, &L.plan))
             L.how = kSharedProduct;
+        else if (n_heads / c.n_kv_heads < attend_unit_heads((int)rows, c.head_dim))
+            // heads too wide for prefix_kernel's tensor memory: units of eight rows, not of one stream's few
+            // (64 streams x 4000 slots, heads of 192 229 -> 55 us, four heads of 256 each 233 -> 157)
+            L.how = kSharedUnits;
     }
     L.parts_off = L.own.total;
     L.part_ml_off = L.part_o_off = L.own_parts_off = L.own_ml_off = L.own_o_off = L.total = L.parts_off;
