@@ -175,7 +175,7 @@ __device__ __forceinline__ bool group_ok(const AttendParams& p, int g) {
 // whole group, unless the stream ends among them.
 __device__ __forceinline__ int first_slot(const AttendParams& p, int shared, int live) {
     const int n = p.lead_units > 0 ? shared : prefix_slots(shared);
-    return live > n ? n : 0;
+    return live >= n ? n : 0;
 }
 // Units of walk member i, and the number of its unit u among all members'.
 template <int kUse>
@@ -953,14 +953,15 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const AttendParam
     const float* const lead_o = product ? p.prefix.part_o : p.own_o;
     grid_dependency_wait();
     const int n = p.kv_len[s], shared = p.shared_len[g];
-    int2 own = __ldcg(p.own_parts + own_unit);  // (of a stream without slots: whatever stands there)
+    int2 own = __ldcg(p.own_parts + own_unit);  // (of a stream without slots of its own: whatever stands there)
     int2 lead = __ldcg((product ? p.prefix.parts : p.own_parts) + lead_unit);
     if (n < 0 || n > p.capacity || shared < 0 || shared > p.capacity) {
         if (threadIdx.x == 0) atomicOr(p.status, SIRLLM_STATUS_OVERFLOW);
         return;
     }
-    if (n == 0) own = make_int2(0, 0);
-    if (first_slot(p, shared, n) == 0) lead = make_int2(0, 0);
+    const int base = first_slot(p, shared, n);
+    if (n == base) own = make_int2(0, 0);
+    if (base == 0) lead = make_int2(0, 0);
     const int parts = own.y + lead.y;
     const int64_t own_at = (own_unit + own.x) * p.part_rows + hq - block * p.part_rows;
     const int64_t lead_at = (lead_unit + lead.x) * lead_step + lead_row;  // from part own.y on

@@ -469,6 +469,16 @@ def test_shared_streams_shorter_than_the_shared_slots(G, group):
     shared_case(2 * G, G, 2 * group, 2, 64, 1000, shared, [n if s % 3 else 0 for s, n in enumerate(lens)], kv="f16", seed=G)
 
 
+@pytest.mark.parametrize("D", [64, 192])
+@pytest.mark.parametrize("G,group", [(2, 4), (16, 4)])
+def test_shared_streams_without_slots_of_their_own(D, G, group):
+    # the shared slots are all that most streams see, whole tiles of them or not, or all that all do
+    shared = [512, 777, 40]
+    lens = [shared[s // G] + (s % 5 == 4) for s in range(3 * G)]
+    shared_case(3 * G, G, 4 * group, 4, D, 800, shared, lens, seed=D + G, fill=math.nan)
+    shared_case(3 * G, G, 4 * group, 4, D, 800, shared, [shared[s // G] for s in range(3 * G)], seed=D, fill=math.nan)
+
+
 @pytest.mark.parametrize("D", [128, 256])
 @pytest.mark.parametrize("G,group,KH", [(2, 16, 2), (2, 16, 16), (3, 10, 16), (8, 8, 16)])
 def test_shared_groups_of_many_heads(D, G, group, KH):
