@@ -254,7 +254,8 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
     sum *= exp_of(top - all);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-    if (lane == 0) p.pairs[(int64_t)row * p.parts + part] = make_float2(all, sum);  // (a sum of 0: nothing but -inf)
+    // a sum of 0: nothing but -inf, no candidate (the lowest value would be one)
+    if (lane == 0) p.pairs[(int64_t)row * p.parts + part] = make_float2(sum == 0.f ? __uint_as_float(0xFF800000u) : all, sum);
 }
 
 // The three levels: a group's segments, the best segments' blocks, the best blocks' logits; few blocks are

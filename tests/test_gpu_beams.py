@@ -168,6 +168,22 @@ def test_select_fewer_candidates_than_asked_for_and_masked_logits():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_select_rows_masked_with_infinities_beside_rows_masked_with_lowest_values(dtype):
+    lowest = torch.finfo(dtype).min
+    z = torch.full((4, 128256), -math.inf, dtype=dtype, device="cuda")
+    z[0, [5, 100000]] = torch.tensor([1.0, 2.0], dtype=dtype, device="cuda")
+    z[1, 77] = 0.5
+    z[2] = lowest
+    z[2, [3000, 90001]] = torch.tensor([0.25, 3.0], dtype=dtype, device="cuda")
+    totals = torch.tensor([-1.0, -2.0, -3.0, -math.inf], device="cuda")
+    check_select(z, 4, 16, totals)
+    z = torch.full((1, 600001), -math.inf, dtype=dtype, device="cuda")
+    z[0, 300007:] = lowest
+    z[0, [9, 500000]] = torch.tensor([1.0, 0.5], dtype=dtype, device="cuda")
+    check_select(z, 1, 8, totals[:1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("V", [5, 3000, 70000])
 def test_select_ties_go_to_the_lower_stream_and_token(dtype, V):
     z = torch.zeros(8, V, dtype=dtype, device="cuda")
