@@ -379,8 +379,8 @@ int sirllm_attend_shared(const sirllm_config *cfg, int32_t layer, int32_t group,
  *     (s, v) with score totals[s] - e_s(v)   for every token v with a logit above -inf
  * and, if ended[s] is not 0, the one candidate (s, end_token) with score totals[s] and entropy 0.  The
  * n_out best candidates of the group go out, higher score first (compared in fp64; within a stream by
- * logit); equal -> the lower stream, then the lower token.  Candidate j of group g stands at
- * [g*n_out + j]:
+ * logit); equal -> the lower stream, then the lower token (streams with equal rows and totals tie, wherever
+ * their rows begin).  Candidate j of group g stands at [g*n_out + j]:
  *     source = s    token_ids = v    totals_out = its score    entropy = e_s(v)
  *     ended_out = 1 if ended[s] is not 0 or v is end_token, else 0
  * If there are fewer, the rest is  source -1, token -1, total -inf, entropy 0, ended 0:  such a stream

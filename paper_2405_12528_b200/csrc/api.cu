@@ -126,14 +126,14 @@ AttendLayout attend_layout(const sirllm_config& c) {
 // the GPU holds (148 SMs, 32 warps each; on another one only the balance differs), 64 at most.
 static BeamTiling beam_tiling(const sirllm_config& c) {
     const int64_t trip = kBeamTripBytes / logits_elem_bytes(c.logits_dtype), per = 16 / logits_elem_bytes(c.logits_dtype);
-    const int64_t row_trips = (c.vocab + per - 1 + trip - 1) / trip;  // a row may begin anywhere within a vector
+    const int64_t row_trips = (c.vocab + trip - 1) / trip;
     BeamTiling t;
     int64_t trips = (row_trips * c.n_streams + 148 * 32 - 1) / (148 * 32);
     if (trips > 64) trips = 64;
     if (trips > row_trips) trips = row_trips;
     t.trips = (int32_t)trips;
     t.parts = (row_trips + trips - 1) / trips;
-    t.blocks = (int32_t)((c.vocab + per - 1 + 32 * per - 1) / (32 * per));
+    t.blocks = (int32_t)((c.vocab + 32 * per - 1) / (32 * per));
     return t;
 }
 

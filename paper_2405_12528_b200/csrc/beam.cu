@@ -14,9 +14,9 @@
 // What reaches the bound is listed and ranked by counting.  A list that overflows is made again with the
 // n_out-th largest of all threads' best as the bound, and if that overflows too (thousands of equal
 // scores) the best come out in n_out rounds of maximum: slow, and right.
-// Measured, bf16: 512 rows x 128256 (8 to a group, four fifths of them live) 42.9 us, of which the stream takes 15.5
-// (6.8 TB/s) and the search 15; 128 x 128256, 16 candidates 25.5; 4 x 32000 10.4; 64 beams and candidates 40 - 65.  The search waits for loads
-// that depend on one another and for instructions that are executed once.
+// Measured, bf16: 512 rows x 128256 (8 to a group, four fifths of them live) 41.0 us, of which the search takes 15; all of
+// them live and off the 16-byte boundaries (128257 wide) 48.1; 128 x 128256, 16 candidates 24.5; 4 x 32000 10.4; 64 beams and
+// candidates 40 - 65.  The search waits for loads that depend on one another and for instructions that are executed once.
 // On the way here, 512 x 128256 bf16: chunks of 32 KB per CTA, with barriers between loading, bounding,
 // listing and ranking, 61 us; warps that keep lists of their own while they stream, 83 us; blocks
 // without segments, bounds taken anew at every level, 53 us.  Ranking
@@ -133,15 +133,15 @@ __device__ __forceinline__ bool better(const Found& a, const Found& b) {
 
 // 16 bytes of a row of which some elements lie outside [0, vocab): those count as -inf
 template <bool kBf16>
-__device__ __noinline__ uint4 edge_vector(const char* at, int64_t e0, int64_t vocab) {
+__device__ __noinline__ uint4 edge_vector(const char* at, int e0, int vocab) {
     uint32_t w[4];
     for (int j = 0; j < 4; ++j) {
         if (kBf16) {
-            const int64_t a = e0 + 2 * j, b = a + 1;
+            const int a = e0 + 2 * j, b = a + 1;
             const uint16_t* q = reinterpret_cast<const uint16_t*>(at);
             w[j] = (a >= 0 && a < vocab ? q[2 * j] : 0xFF80u) | (uint32_t)(b >= 0 && b < vocab ? q[2 * j + 1] : 0xFF80u) << 16;
         } else {
-            const int64_t a = e0 + j;
+            const int a = e0 + j;
             w[j] = a >= 0 && a < vocab ? reinterpret_cast<const uint32_t*>(at)[j] : 0xFF800000u;
         }
     }
@@ -171,7 +171,6 @@ struct BeamShared {
     // candidates has total -inf.
     double total_of[kBeamMaxGroup], log_of[kBeamMaxGroup];
     float top_of[kBeamMaxGroup], const_of[kBeamMaxGroup];  // const: total - log sum, -inf for a row without logits that count
-    int skew_of[kBeamMaxGroup];                            // elements between a row and its first block's start
     __device__ __forceinline__ unsigned long long score(unsigned long long place) const {  // its order key
         const Found f = {0, place};
         const int r = f.row();
@@ -183,31 +182,73 @@ struct BeamShared {
     uint32_t placed[2], taken[2];      // candidates with a place of their own, places taken
 };
 
-// One warp's segment of a row: p.trips trips of kStep vectors per lane.
-template <bool kBf16>
+// One warp's segment of a row: p.trips trips of kStep vectors per lane.  Segments, blocks and lanes go by the
+// elements' indices, so that equal rows have equal sums wherever they begin (a tie between streams is one then).
+// kWords >= 0: the row begins off a 16-byte boundary, so many words and perhaps half a word behind it.  A lane puts
+// its vector together from the aligned one that it loads and words of the next lane's; those behind a trip's last
+// vector come by a load of lane 31's own.
+constexpr int kAligned = -1;
+template <bool kBf16, int kWords>
 __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int part) {
     constexpr int kPer = kBf16 ? 8 : 4;  // elements of a vector
     constexpr int kSize = kBf16 ? 2 : 4;
     const int lane = threadIdx.x & 31;
     // as aligned vectors; what lies outside the row counts as -inf
     const char* row_at = static_cast<const char*>(p.logits) + (int64_t)row * p.row_stride * kSize;
-    const int skew = (int)(((uintptr_t)row_at & 15) / kSize);  // elements in front of the row
+    const int skew = kWords == kAligned ? 0 : (int)((uintptr_t)row_at & 15);  // bytes in front of the row
     const int first_block = part * p.trips * kStep;
     const int trips = min(p.trips, (p.blocks - first_block + kStep - 1) / kStep);
-    int64_t e_next = ((int64_t)first_block * 32 + lane) * kPer - skew;  // first element of the lane's next vector
-    auto load = [&](uint4 (&v)[kStep]) {
+    const int vocab = (int)p.vocab;
+    int e_next = (first_block * 32 + lane) * kPer - skew / kSize;  // first element of the lane's next vector
+    auto load_in = [&](uint4& v, int e0) {
+        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "l"(row_at + (int64_t)e0 * kSize));
+    };
+    auto load_one = [&](uint4& v, int e0) {
+        if (e0 >= 0 && e0 + kPer <= vocab)
+            load_in(v, e0);
+        else
+            v = edge_vector<kBf16>(row_at + (int64_t)e0 * kSize, e0, vocab);
+    };
+    // Inside the row there is nothing to check per vector (512 x 128256 bf16 42.7 -> 40.7 us; off the boundaries 50.1 -> 47.9).
+    auto load = [&](uint4 (&v)[kStep], uint4& behind) {
+        const int e_first = e_next - lane * kPer;
+        if (e_first >= 0 && e_first + (kStep * 32 + 1) * kPer <= vocab) {
+#pragma unroll
+            for (int i = 0; i < kStep; ++i) load_in(v[i], e_next + i * 32 * kPer);
+            if (kWords != kAligned && lane == 31) load_in(behind, e_next + ((kStep - 1) * 32 + 1) * kPer);
+            e_next += kStep * 32 * kPer;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) load_one(v[i], e_next + i * 32 * kPer);
+        if (kWords != kAligned && lane == 31) load_one(behind, e_next + ((kStep - 1) * 32 + 1) * kPer);
+        e_next += kStep * 32 * kPer;
+    };
+    // vector i of a trip: kWords words (and, bf16, perhaps half a word) behind where v[i] begins
+    constexpr int kFrom = kWords == kAligned ? 0 : kWords + (kBf16 ? 1 : 0);  // words of the next lane
+    const int half = kBf16 ? (skew & 2) * 8 : 0;
+    auto word = [](const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; };
+    auto assemble = [&](uint4 (&v)[kStep], const uint4& behind) {
 #pragma unroll
         for (int i = 0; i < kStep; ++i) {
-            const int64_t e0 = e_next + i * 32 * kPer;
-            const char* at = row_at + e0 * kSize;
-            if (e0 >= 0 && e0 + kPer <= p.vocab)
-                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                             : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
-                             : "l"(at));
+            uint32_t x[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = word(v[i], j);
+#pragma unroll
+            for (int j = 0; j < kFrom; ++j) {
+                const uint32_t give = i + 1 < kStep && lane == 0 ? word(v[(i + 1) % kStep], j) : x[j];
+                x[4 + j] = __shfl_sync(0xFFFFFFFFu, give, lane + 1);  // (lane 31 from lane 0)
+                if (i + 1 == kStep && lane == 31) x[4 + j] = word(behind, j);
+            }
+            constexpr int k = kWords == kAligned ? 0 : kWords;
+            if (kBf16)
+                v[i] = make_uint4(__funnelshift_r(x[k], x[k + 1], half), __funnelshift_r(x[k + 1], x[k + 2], half),
+                                  __funnelshift_r(x[k + 2], x[k + 3], half), __funnelshift_r(x[k + 3], x[k + 4], half));
             else
-                v[i] = edge_vector<kBf16>(at, e0, p.vocab);
+                v[i] = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
         }
-        e_next += kStep * 32 * kPer;
     };
     auto value = [&](const uint4& v, int j) {  // element j
         const uint32_t w = (kBf16 ? j >> 1 : j) == 0 ? v.x : (kBf16 ? j >> 1 : j) == 1 ? v.y : (kBf16 ? j >> 1 : j) == 2 ? v.z : v.w;
@@ -216,13 +257,15 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
     };
     float top = -3.4028235e38f, sum = 0.f;
     float* block_max = p.block_max + (int64_t)row * p.blocks + first_block;
-    uint4 cur[kStep], next[kStep];
-    if (trips > 0) load(next);
+    uint4 cur[kStep], next[kStep], behind = make_uint4(0, 0, 0, 0);
+    if (trips > 0) load(next, behind);
 #pragma unroll 1
     for (int t = 0; t < trips; ++t) {
 #pragma unroll
         for (int i = 0; i < kStep; ++i) cur[i] = next[i];
-        if (t + 1 < trips) load(next);
+        const uint4 last = behind;
+        if (t + 1 < trips) load(next, behind);
+        if (kWords != kAligned) assemble(cur, last);
         float m = top;
         uint32_t mine = 0;
 #pragma unroll
@@ -233,7 +276,7 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
             if (lane == i) mine = key;
         }
         if (lane < kStep && first_block + t * kStep + lane < p.blocks) block_max[t * kStep + lane] = from_key(mine);
-        sum *= exp_of(top - m);
+        sum = __fmul_rn(sum, exp_of(top - m));  // (fused into the addition below in all forms of this code, or in none)
         top = m;
         const uint64_t minus_top = pack2(-top, -top), hi = pack2(kLog2eHi, kLog2eHi), lo = pack2(kLog2eLo, kLog2eLo);
         uint64_t sum2[2] = {0, 0};
@@ -248,7 +291,7 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
             }
         float s0, s1;
         unpack2(add2(sum2[0], sum2[1]), s0, s1);
-        sum += s0 + s1;
+        sum = __fadd_rn(sum, __fadd_rn(s0, s1));
     }
     const float all = from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(top)));
     sum *= exp_of(top - all);
@@ -256,6 +299,18 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
     for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
     // a sum of 0: nothing but -inf, no candidate (the lowest value would be one)
     if (lane == 0) p.pairs[(int64_t)row * p.parts + part] = make_float2(sum == 0.f ? __uint_as_float(0xFF800000u) : all, sum);
+}
+// a row that begins off a 16-byte boundary
+template <bool kBf16>
+__device__ __noinline__ void scan_shifted(const BeamParams& p, int row, int part, int words) {
+    if (kBf16 && words == 0)
+        scan_segment<kBf16, 0>(p, row, part);
+    else if (words == 1)
+        scan_segment<kBf16, 1>(p, row, part);
+    else if (words == 2)
+        scan_segment<kBf16, 2>(p, row, part);
+    else
+        scan_segment<kBf16, 3>(p, row, part);
 }
 
 // The three levels: a group's segments, the best segments' blocks, the best blocks' logits; few blocks are
@@ -285,8 +340,8 @@ __device__ __forceinline__ Strip strip_of(const BeamParams& p, const BeamShared&
         return {row, first, min(p.trips * kStep, p.blocks - first),
                 reinterpret_cast<const char*>(p.block_max + (int64_t)(row0 + row) * p.blocks + first), 4};
     }
-    const int64_t e0 = (int64_t)at * kBlock - sh.skew_of[row], first = max(e0, (int64_t)0);
-    return {row, (int)first, (int)(min(e0 + kBlock, p.vocab) - first),
+    const int64_t first = (int64_t)at * kBlock;
+    return {row, (int)first, (int)(min(first + kBlock, p.vocab) - first),
             static_cast<const char*>(p.logits) + ((int64_t)(row0 + row) * p.row_stride + first) * kSize, kSize};
 }
 
@@ -367,8 +422,6 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
             sh.log_of[r] = log_sum;
             sh.total_of[r] = e || counts ? (double)t : -INFINITY;
             sh.const_of[r] = counts ? (float)((double)t - log_sum) : __uint_as_float(0xFF800000u);
-            const char* row_at = static_cast<const char*>(p.logits) + (int64_t)(row0 + r) * p.row_stride * (kBf16 ? 2 : 4);
-            sh.skew_of[r] = (int)(((uintptr_t)row_at & 15) / (kBf16 ? 2 : 4));
         }
     }
     __syncthreads();
@@ -518,7 +571,8 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
     }
 }
 
-template <bool kBf16>
+// kAll: all rows begin at 16-byte boundaries (a kernel without the code for others: 4 x 32000 10.8 -> 10.3 us)
+template <bool kBf16, bool kAll>
 __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const BeamParams p) {
     __shared__ int last_one;
     const int warp = threadIdx.x >> 5;
@@ -527,8 +581,14 @@ __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const BeamParams p) {
     // A CTA works for one group: eight of its segments, all of a row's, then the next row's.
     const int g = blockIdx.x / p.group_ctas, cta = blockIdx.x - g * p.group_ctas, segment = cta * kWarps + warp;
     const int in_group = segment / p.parts, row = g * p.group + in_group;
-    if (in_group < p.group && p.totals[row] > -INFINITY && !(p.ended != nullptr && p.ended[row] != 0))
-        scan_segment<kBf16>(p, row, segment - in_group * p.parts);
+    if (in_group < p.group && p.totals[row] > -INFINITY && !(p.ended != nullptr && p.ended[row] != 0)) {
+        const uintptr_t row_at = (uintptr_t)p.logits + (int64_t)row * p.row_stride * (kBf16 ? 2 : 4);
+        const int part = segment - in_group * p.parts, words = (int)(row_at & 15) >> 2;
+        if (kAll || (row_at & 15) == 0)
+            scan_segment<kBf16, kAligned>(p, row, part);
+        else
+            scan_shifted<kBf16>(p, row, part, words);
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
         int before;
@@ -555,8 +615,10 @@ cudaError_t launch_beam(const BeamParams& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return p.logits_dtype == SIRLLM_BF16 ? cudaLaunchKernelEx(&cfg, beam_kernel<true>, q)
-                                         : cudaLaunchKernelEx(&cfg, beam_kernel<false>, q);
+    const bool bf16 = p.logits_dtype == SIRLLM_BF16;
+    const bool all = (uintptr_t)p.logits % 16 == 0 && (p.n_streams == 1 || p.row_stride * (bf16 ? 2 : 4) % 16 == 0);
+    if (bf16) return all ? cudaLaunchKernelEx(&cfg, beam_kernel<true, true>, q) : cudaLaunchKernelEx(&cfg, beam_kernel<true, false>, q);
+    return all ? cudaLaunchKernelEx(&cfg, beam_kernel<false, true>, q) : cudaLaunchKernelEx(&cfg, beam_kernel<false, false>, q);
 }
 
 }  // namespace sirllm

@@ -1,0 +1,60 @@
+"""Streams with a past in common, on the GPU, where a call's answer hangs on the last bits or on the ends of
+the number range: equal streams at every alignment, totals and logits of the lowest value, segments of
+many trips, a retention round between two tokens."""
+import math
+
+import pytest
+import torch
+
+from paper_2405_12528_b200 import binding as B
+from test_gpu_beams import beams, check_select, select
+from test_gpu_decode import gen
+
+pytestmark = pytest.mark.gpu
+
+
+def at_skew(z, skew, stride):
+    """The same rows, the first one ``skew`` elements behind a 16-byte boundary, ``stride`` elements apart."""
+    S, V = z.shape
+    buf = torch.full((skew + S * stride + 16,), 50.0, dtype=z.dtype, device="cuda")
+    view = buf[skew:skew + S * stride].view(S, stride)[:, :V]
+    view.copy_(z)
+    return view
+
+
+# --------------------------------------------------------------------------------------
+# equal streams: the lower one wins, wherever the rows begin
+# --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [1, 9, 300, 1029, 5003, 50257])
+def test_select_equal_streams_tie_at_every_alignment(dtype, V):
+    z, _ = beams(V, 1, V, dtype)
+    N = min(40, 8 * V)
+    order = torch.sort(z[0].double(), descending=True, stable=True).indices.tolist()
+    # the eight streams of a group are the same: token by token (equal logits: token behind token in a stream)
+    want, i = [], 0
+    while len(want) < N:
+        run = [v for v in order[i:] if z[0, v] == z[0, order[i]]]
+        want += [(s, v) for s in range(8) for v in run]
+        i += len(run)
+    want = want[:N]
+    rows = z.expand(8, V)
+    for skew in range(0, 16 // z.element_size()):
+        for stride in (V, V + 1, V + 3):
+            tot, src, tok, ent, _ = select(at_skew(rows, skew, stride), 8, N, torch.full((8,), -3.0, device="cuda"), end=-1)
+            assert list(zip(src.tolist(), tok.tolist())) == want, (skew, stride)
+            for v in set(tok.tolist()):
+                assert tot[tok == v].unique().numel() == 1 and ent[tok == v].unique().numel() == 1, (skew, stride, v)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [3, 513, 4099, 50257])
+def test_select_same_bits_at_every_alignment(dtype, V):
+    z, totals = beams(V + 1, 6, V, dtype)
+    per = 16 // z.element_size()
+    want = select(at_skew(z, 0, (V + per - 1) // per * per), 3, 7, totals, end=-1)
+    for skew in range(per):
+        for stride in range(V, V + per, 1 if V < 5000 else 3):
+            got = select(at_skew(z, skew, stride), 3, 7, totals, end=-1)
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), (skew, stride)
