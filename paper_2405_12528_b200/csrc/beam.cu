@@ -42,6 +42,7 @@ static_assert(kStep * 512 == kBeamTripBytes, "a trip is kStep blocks");
 constexpr float kLog2eHi = 1.4426950216293335f, kLog2eLo = 1.9259629e-8f;
 
 __device__ __forceinline__ float exp_of(float t) { return ex2_approx(fmaf(t, kLog2eLo, t * kLog2eHi)); }
+constexpr float kLowest = -3.4028235e38f;  // of all numbers
 // order keys of numbers: -0 counts as 0
 __device__ __forceinline__ uint32_t key_of(float x) { return order_key(__float_as_uint(x + 0.0f)); }
 __device__ __forceinline__ float from_key(uint32_t k) {
@@ -83,6 +84,7 @@ __device__ __forceinline__ float reach_by_warps(float mine, float warp_top, floa
             if (lane == __ffs(who) - 1) key = 0;
         }
     }
+    if (with == 0) return lowest;
     // (more than 32 rounds, or lanes without a value, end at or below the lowest)
     if (lane == 0) {
         bounds[warp] = warp_top > lowest ? (bound == 0 ? lowest : from_key(bound)) : __uint_as_float(0x7F800000u);
@@ -255,7 +257,7 @@ __device__ __forceinline__ void scan_segment(const BeamParams& p, int row, int p
         if (!kBf16) return __uint_as_float(w);
         return __uint_as_float((j & 1) ? (w & 0xFFFF0000u) : (w << 16));
     };
-    float top = -3.4028235e38f, sum = 0.f;
+    float top = kLowest, sum = 0.f;
     float* block_max = p.block_max + (int64_t)row * p.blocks + first_block;
     uint4 cur[kStep], next[kStep], behind = make_uint4(0, 0, 0, 0);
     if (trips > 0) load(next, behind);
@@ -461,7 +463,8 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
 #pragma unroll
                     for (int k = 0; k < kBatch; ++k) {
                         const float d = z[k] - top, a = d + c, off_by = (fabsf(d) + fabsf(c)) * 2.4e-7f;  // two steps of 2^-23
-                        if (off + k * 32 < t.length) mine = fmaxf(mine, a - off_by);
+                        // (next to the lowest number the difference overflows: still a candidate)
+                        if (off + k * 32 < t.length && a > none) mine = fmaxf(mine, fmaxf(a - off_by, kLowest));
                         hits |= (uint32_t)(a + off_by >= reach && a > none && off + k * 32 < t.length) << k;
                     }
 #pragma unroll 1

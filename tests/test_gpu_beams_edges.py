@@ -58,3 +58,46 @@ def test_select_same_bits_at_every_alignment(dtype, V):
         for stride in range(V, V + per, 1 if V < 5000 else 3):
             got = select(at_skew(z, skew, stride), 3, 7, totals, end=-1)
             assert all(torch.equal(a, b) for a, b in zip(got, want)), (skew, stride)
+
+
+# --------------------------------------------------------------------------------------
+# totals and logits at the ends of the number range: only -inf says that there is no candidate
+# --------------------------------------------------------------------------------------
+
+LOWEST = torch.finfo(torch.float32).min
+
+
+def check_first_stream(z, G, N, totals, alive=None):
+    """All totals so low that no logit shows beside them: the lowest live stream's best logits, in order."""
+    tot, src, tok, ent, fin = select(z, G, N, totals, end=-1)
+    for g in range(z.shape[0] // G):
+        s = g * G + (0 if alive is None else alive)
+        order = torch.sort(z[s].double(), descending=True, stable=True).indices[:N]
+        out = slice(g * N, g * N + N)
+        assert src[out].tolist() == [s] * N
+        assert torch.equal(tok[out].long(), order)
+        assert (tot[out] == LOWEST).all() and (fin[out] == 0).all()
+        want = -torch.log_softmax(z[s].double(), -1)[order]
+        assert ((ent[out].double() - want).abs() <= 2.0 ** -18 + 2.0 ** -24 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [40, 300, 3000, 5003, 128256])
+@pytest.mark.parametrize("G,N", [(1, 1), (4, 4), (4, 33), (16, 16)])
+def test_select_all_totals_of_the_lowest_value(dtype, V, G, N):
+    z, _ = beams(V, 2 * G, V, dtype)
+    totals = torch.full((2 * G,), LOWEST, device="cuda")
+    check_first_stream(z, G, N, totals)
+    if G > 1:
+        totals.view(2, G)[:, 0] = -math.inf          # and a stream without a beam in front
+        check_first_stream(z, G, N, totals, alive=1)
+
+
+def test_select_lowest_totals_beside_ended_beams():
+    z, _ = beams(3, 8, 9001, torch.float32)
+    totals = torch.full((8,), LOWEST, device="cuda")
+    ended = torch.tensor([0, 1, 0, 0, 1, 1, 1, 1], dtype=torch.int32, device="cuda")
+    tot, src, tok, _, fin = select(z, 4, 4, totals, ended)
+    order = torch.sort(z[0], descending=True, stable=True).indices[:4].tolist()
+    assert src.tolist() == [0, 0, 0, 0, 4, 5, 6, 7] and tok.tolist() == order + [2] * 4
+    assert (tot == LOWEST).all() and fin.tolist() == [int(t == 2) for t in order] + [1] * 4
