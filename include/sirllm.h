@@ -385,8 +385,9 @@ int sirllm_attend_shared(const sirllm_config *cfg, int32_t layer, int32_t group,
  *     ended_out = 1 if ended[s] is not 0 or v is end_token, else 0
  * If there are fewer, the rest is  source -1, token -1, total -inf, entropy 0, ended 0:  such a stream
  * holds no beam; a stream with total -inf gives no candidates and its logits are not read.  (Start: total 0
- * for a group's first stream, -inf for the others.)  source feeds sirllm_reorder_streams, token_ids the
- * next step, entropy the entropy cache.
+ * for a group's first stream, -inf for the others.)  A candidate whose score or entropy is beyond fp32 (logits
+ * more than 3.4e38 apart) is ranked as any other, and goes out with total -inf, entropy inf.  source feeds
+ * sirllm_reorder_streams, token_ids the next step, entropy the entropy cache.
  *   places      not 0 (n_out == group): the best candidate of every stream stands in that stream's own
  *               place, the others, in order, in the free places: no stream is then both overwritten and
  *               still needed, and sirllm_reorder_streams moves as little as possible

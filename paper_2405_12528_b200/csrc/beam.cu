@@ -463,9 +463,11 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
 #pragma unroll
                     for (int k = 0; k < kBatch; ++k) {
                         const float d = z[k] - top, a = d + c, off_by = (fabsf(d) + fabsf(c)) * 2.4e-7f;  // two steps of 2^-23
-                        // (next to the lowest number the difference overflows: still a candidate)
-                        if (off + k * 32 < t.length && a > none) mine = fmaxf(mine, fmaxf(a - off_by, kLowest));
-                        hits |= (uint32_t)(a + off_by >= reach && a > none && off + k * 32 < t.length) << k;
+                        // (d, a and a - off_by may pass the lowest number: only a logit of -inf is no candidate, and what
+                        // is then not a number reaches any bound)
+                        const bool real = z[k] > none && off + k * 32 < t.length;
+                        if (real) mine = fmaxf(mine, fmaxf(a - off_by, kLowest));
+                        hits |= (uint32_t)(real && !(a + off_by < reach)) << k;
                     }
 #pragma unroll 1
                     for (hits = bound ? 0 : hits; hits != 0; hits &= hits - 1) {  // one copy of this code
@@ -483,7 +485,7 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
                     const float t = (float)sh.total_of[r];
                     if (bound) {
                         mine = fmaxf(mine, t);
-                    } else if (t >= reach) {
+                    } else if (!(t < reach)) {
                         const int n = atomicAdd(&sh.listed, 1);
                         if (n < kList) sh.list[n].place = place_of(r, 0.f, 0);
                     }

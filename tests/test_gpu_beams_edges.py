@@ -101,3 +101,35 @@ def test_select_lowest_totals_beside_ended_beams():
     order = torch.sort(z[0], descending=True, stable=True).indices[:4].tolist()
     assert src.tolist() == [0, 0, 0, 0, 4, 5, 6, 7] and tok.tolist() == order + [2] * 4
     assert (tot == LOWEST).all() and fin.tolist() == [int(t == 2) for t in order] + [1] * 4
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [5, 300, 5003, 128256])
+def test_select_logits_further_apart_than_fp32_reaches(dtype, V):
+    # 3e38 and -3e38: a difference that only fp64 holds; such tokens are candidates, their totals round to -inf
+    z = torch.full((4, V), -3e38, dtype=dtype, device="cuda")
+    z[:, V // 2] = 3e38
+    z[3, :V // 2 - 1] = -math.inf
+    totals = torch.tensor([0.0, -1.0, -math.inf, -3.0], device="cuda")
+    tot, src, tok, ent, _ = select(z, 2, 5, totals, end=-1)
+    low = [v for v in range(V) if v != V // 2]
+    behind = [v for v in range(V // 2 - 1, V) if v != V // 2]
+    n = min(4, len(behind))
+    assert src.tolist() == [0, 1, 0, 0, 0, 3] + [3] * n + [-1] * (4 - n)
+    assert tok.tolist() == [V // 2, V // 2] + low[:3] + [V // 2] + behind[:n] + [-1] * (4 - n)
+    assert tot.tolist() == [0.0, -1.0] + [-math.inf] * 3 + [-3.0] + [-math.inf] * 4
+    assert ent.tolist() == [0.0, 0.0] + [math.inf] * 3 + [0.0] + [math.inf] * n + [0.0] * (4 - n)
+
+
+@pytest.mark.parametrize("V", [300, 128256])
+def test_select_lowest_totals_and_rows_masked_by_the_lowest_value(V):
+    z, _ = beams(V, 4, V, torch.float32)
+    z[:, 20:] = LOWEST
+    tot, src, tok, _, _ = select(z, 4, 30, torch.full((4,), LOWEST, device="cuda"), end=-1)
+    best = torch.sort(z[:, :20], descending=True, stable=True).indices
+    # total + logit rounds to the lowest value in all streams where the logit counts: 20 and 10 of them
+    assert src.tolist() == [0] * 20 + [1] * 10 and (tot == LOWEST).all()
+    assert tok.tolist() == best[0].tolist() + best[1, :10].tolist()
+    tot, src, tok, _, _ = select(z[:1], 1, 30, torch.full((1,), LOWEST, device="cuda"), end=-1)
+    assert src.tolist() == [0] * 30 and tok.tolist() == best[0].tolist() + list(range(20, 30))
+    assert tot.tolist() == [LOWEST] * 20 + [-math.inf] * 10
