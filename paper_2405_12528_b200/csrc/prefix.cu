@@ -247,14 +247,17 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
     __syncthreads();
     grid_launch_dependents();
 
-    // A wait that runs out raises the flag and every role leaves; the others see it or run out too.
+    // A wait that runs out raises the flag and every role leaves; the others see it or run out too.  Of whole
+    // warps, which leave as one: lanes poll at different times, and what follows (a lane elected among 32, loads and
+    // stores of tensor memory) wants them all.
     auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-        for (uint32_t i = 0; i < kSpinLimit; ++i) {
-            if (mbar_try_wait(bar, parity)) return true;
-            if (gave_up) return false;
+        bool there = false;
+        for (uint32_t i = 0; i < kSpinLimit && !there; ++i) {
+            there = mbar_try_wait(bar, parity);
+            if (!there && gave_up) break;
         }
-        gave_up = 1;
-        return false;
+        if (!there) gave_up = 1;
+        return __all_sync(0xFFFFFFFFu, there);
     };
     constexpr int kTilesAtOnce = kPair ? 1 : 2;  // tiles that the two lanes take together
 
@@ -419,7 +422,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
             // comes in at 250 cycles and more per 8 instructions (unrolled over the row, the first tile of a call
             // took 2 us more; in steps of 32 columns the others 0.3 us more).
             for (int t = kPair ? 0 : ln; t < tiles && ok; t += kTilesAtOnce, fresh = false) {
-                ok = __all_sync(0xFFFFFFFFu, wait(&s_full[ln], s_phase));
+                ok = wait(&s_full[ln], s_phase);
                 if (!ok) break;
                 s_phase ^= 1u;
                 tmem_fence_after();
@@ -492,7 +495,7 @@ prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map_q, c
                 ((int64_t)w.g * p.n_kv_heads * p.plan.units + w.u + blockIdx.x) * p.plan.rows + row + (kPair ? ln * kPrefixRows : 0);
             for (int x = 0; x < 2; ++x)
                 if (x < lanes_used && (!kPair || x == ln) && ok) {
-                    ok = __all_sync(0xFFFFFFFFu, wait(&o_full[x], o_phase[x]));
+                    ok = wait(&o_full[x], o_phase[x]);
                     o_phase[x] ^= 1u;
                 }
             if (w.t0 == 0 && tid == kThreads - 1) {  // where the unit's parts are
