@@ -274,9 +274,17 @@ def prepared(func, *args, **kwargs) -> Prepared:
     return _preparing.out
 
 
+def _fits(n: int) -> bool:
+    """Whether ctypes hands ``n`` on as it is (it cuts larger numbers down to 32 bits without a word)."""
+    return -2**31 <= n < 2**31
+
+
 def _call(fn, cfg, *args) -> None:
-    """Checks every tensor argument (shapes of all first, then residence), then calls ``fn``
-    (or, under :func:`prepared`, hands back the marshalled call instead of making it)."""
+    """Checks every argument (numbers, then the shapes of all tensors, then their residence), then calls
+    ``fn`` (or, under :func:`prepared`, hands back the marshalled call instead of making it)."""
+    for a, t in zip(args, fn.argtypes[1:]):
+        if t is ctypes.c_int32 and not _fits(a):
+            raise SirllmError(ERR_BAD_CONFIG, f"{a} does not fit 32 bits")
     for a in args:
         if isinstance(a, _Arg):
             a.check_shape()
@@ -631,6 +639,8 @@ def _groups(cfg: Config, group: int) -> int:
 
 
 def sirllm_attend_shared_workspace_bytes(cfg: Config, group: int, n_heads: int) -> int:
+    if not (_fits(group) and _fits(n_heads)):
+        return 0
     return lib().sirllm_attend_shared_workspace_bytes(ctypes.byref(cfg), int(group), int(n_heads))
 
 
