@@ -11,6 +11,8 @@
 // a better candidate.  In the same way the n_out best blocks of these, and then the n_out best logits
 // of these blocks, the only ones that are read again; the last of the n_out is the bound for the next level.
 // Scores are compared in fp64; within a row the order of the logits is the order of the scores.
+// A lane's sum is fp32 over up to 64 trips, each at most 6 roundings of 2^-24 (an addition, and an exp and a product where
+// the maximum moves); segments are joined in fp64.
 // What reaches the bound is listed and ranked by counting.  A list that overflows is made again with the
 // n_out-th largest of all threads' best as the bound, and if that overflows too (thousands of equal
 // scores) the best come out in n_out rounds of maximum: slow, and right.

@@ -8,7 +8,7 @@ import torch
 
 from paper_2405_12528_b200 import binding as B
 from test_gpu_beams import beams, check_select, select
-from test_gpu_decode import gen
+from test_gpu_decode import gen, ref_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,48 @@ def test_select_lowest_totals_and_rows_masked_by_the_lowest_value(V):
     tot, src, tok, _, _ = select(z[:1], 1, 30, torch.full((1,), LOWEST, device="cuda"), end=-1)
     assert src.tolist() == [0] * 30 and tok.tolist() == best[0].tolist() + list(range(20, 30))
     assert tot.tolist() == [LOWEST] * 20 + [-math.inf] * 10
+
+
+# --------------------------------------------------------------------------------------
+# long segments: what a lane adds up in fp32
+# --------------------------------------------------------------------------------------
+
+def log_sum_bound(trips, V):
+    """What lse may be off by, u = 2^-24.  A term: exp to 4u, its argument (a difference, a product, a sum: 3u of
+    it, and the arguments' mean, weighted by the terms, is at most ln V).  A trip of a lane: 8 additions in each of
+    four sums, 2 to join them, 1 onto the lane's sum, which a new maximum multiplies by an exp first (6u a trip; the
+    arguments of all these together weigh little: T e^-T).  Lanes and segments: another exp and 5 additions, another
+    exp, the rest in fp64."""
+    return (6 * trips + 10 + 4 + 3 * math.log(V) + 10 + 6) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("ascending", [False, True])
+@pytest.mark.parametrize("rows,V,dtype,trips", [
+    (2600, 131071, torch.bfloat16, 64),     # more than 64 trips would bring a segment per warp: two segments a row
+    (1200, 70001, torch.float32, 35),
+    (640, 40001, torch.bfloat16, 6),
+])
+def test_select_segments_of_many_trips(rows, V, dtype, trips, ascending):
+    size = 2 if dtype == torch.bfloat16 else 4
+    whole = -(-V * size // 2048)
+    assert min(64, whole, -(-whole * rows // (148 * 32))) == trips
+    if ascending:   # every trip brings a new maximum
+        z = torch.linspace(-4, 14, V, device="cuda").to(dtype).expand(rows, V).contiguous()
+        z += torch.linspace(0, 3, rows, device="cuda").to(dtype)[:, None]
+        totals = torch.linspace(-9, -1, rows, device="cuda")
+    else:
+        z, totals = beams(V, rows, V, dtype)
+    N = 4
+    tot, src, tok, ent, _ = select(z, 1, N, totals, end=-1)
+    assert torch.equal(src, torch.arange(rows, dtype=torch.int32, device="cuda").repeat_interleave(N))
+    tol = log_sum_bound(trips, V)
+    for r in range(0, rows, 100):
+        x = z[r:r + 100].double()
+        order = torch.sort(x, dim=-1, descending=True, stable=True).indices[:, :N]
+        out = slice(r * N, min(rows, r + 100) * N)
+        assert torch.equal(tok[out].view(-1, N).long(), order)
+        e = torch.logsumexp(x, -1, keepdim=True) - x.gather(1, order)
+        t = totals[r:r + 100].double()[:, None] - e
+        for got, want in ((ent, e), (tot, t)):
+            d = (got[out].view(-1, N).double() - want).abs()
+            assert (d <= tol + 2.0 ** -24 * want.abs()).all(), float(d.max())
