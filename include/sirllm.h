@@ -357,6 +357,13 @@ int sirllm_attend(const sirllm_config *cfg, int32_t layer, const void *q, int32_
  * streams' planes hold below shared_len is not read.  kv_len[s] counts the shared slots; it may be
  * smaller than shared_len.  shared_len outside [0, capacity] raises SIRLLM_STATUS_OVERFLOW and leaves
  * the group's out and lse as they were.
+ * Retention between tokens: a round (sirllm_step, sirllm_compact_kv, whatever the keep list's policy) moves and drops
+ * slots within each stream's own planes and knows of no sharing.  The shared slots have to be sinks then,
+ * n_sink >= shared_len[g] for every group: sinks stay where they are, and what is shared stays shared.  With fewer
+ * sinks a follower would keep rows that its planes do not hold, and the first stream would drop rows that the
+ * others still see; the library cannot tell and does not refuse it.  (sirllm_reorder_streams gives every stream its own
+ * copy first: source = the group's first stream, shared_len NULL, live_len an array of its own that holds
+ * shared_len[g] for all streams of group g.)
  *   group       divides n_streams;  shared_len int32 [n_streams / group]
  *   ws          a workspace of its own kind, for this group and n_heads: sirllm_attend_shared_workspace_bytes()
  *               bytes (0 for an invalid combination); the rules of sirllm_attend's hold for it

@@ -178,3 +178,96 @@ def test_select_segments_of_many_trips(rows, V, dtype, trips, ascending):
         for got, want in ((ent, e), (tot, t)):
             d = (got[out].view(-1, N).double() - want).abs()
             assert (d <= tol + 2.0 ** -24 * want.abs()).all(), float(d.max())
+
+
+# --------------------------------------------------------------------------------------
+# retention rounds between tokens: sinks that cover the shared slots leave them in place
+# --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("G,C,layout", [(3, 160, None), (3, 160, B.ROPE_HALF), (40, 6000, None)])
+@pytest.mark.parametrize("shared", [[64, 40], [1, 64], [384, 301]])
+def test_rounds_between_tokens_of_streams_that_share_their_sinks(G, C, layout, shared):
+    """A cache whose followers hold nothing below shared_len (NaN) against one with the shared slots copied to every
+    stream, round for round: the same slots stay, and attention over them is the same."""
+    S, H, KH, D, V, new, sink = 2 * G, 4, 2, 64, 500, 5, max(shared)
+    C = max(C, sink + 60)
+    cfg = B.make_config(n_streams=S, n_layers=1, n_kv_heads=KH, head_dim=D, capacity=C, budget=sink + 36, n_sink=sink,
+                        n_recent=8, threshold=sink + 46, max_new=new, vocab=V, logits_dtype="f32", kv_dtype="bf16")
+    g = gen(G + C)
+    ws, wa, wp = B.new_workspace(cfg), B.new_attend_shared_workspace(cfg, G, H), B.new_attend_workspace(cfg)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    live = [sink + 6 + 7 * (s % 5) for s in range(S)]
+    plain = [torch.randn(S, 1, KH, C, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    for s in range(S):
+        for x in plain:
+            x[s, :, :, :shared[s // G]] = x[s // G * G, :, :, :shared[s // G]]
+    held = [x.clone() for x in plain]
+    for s in range(S):
+        for x in held:
+            if s % G:
+                x[s, :, :, :shared[s // G]] = math.nan
+    E = torch.rand(S, C, generator=g, device="cuda") * 9
+    E_held = E.clone()
+    for s in range(S):
+        if s % G:
+            E_held[s, :shared[s // G]] = 1e30       # whatever stands there
+    lens, lens_held = i32(*live), i32(*live)
+    keeps = [torch.zeros(S, cfg.threshold, dtype=torch.int32, device="cuda") for _ in range(2)]
+    n_keep = [torch.zeros(S, dtype=torch.int32, device="cuda") for _ in range(2)]
+    decay = torch.full((S,), 0.9, device="cuda")
+    evicted = False
+    for rnd in range(12):
+        n_new = i32(*[1 + (s + rnd) % new for s in range(S)])
+        logits = torch.randn(S * new, V, generator=g, device="cuda") * 2
+        ids = torch.randint(0, V, (S * new,), generator=g, device="cuda", dtype=torch.int32)
+        rows = [torch.randn(S, KH, new, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+        for s, n in enumerate(lens.tolist()):
+            for x, y, r in zip(plain, held, rows):
+                x[s, 0, :, n:n + new] = y[s, 0, :, n:n + new] = r[s]
+        for i, (kv, e, n) in enumerate(((plain, E, lens), (held, E_held, lens_held))):
+            B.sirllm_step(cfg, logits, ids, n_new, e, None, n, decay, *kv, keeps[i], n_keep[i], None, ws)
+            if layout is not None:
+                B.sirllm_rerotate_keys(cfg, kv[0], keeps[i], n_keep[i], 1e4, layout)
+        assert torch.equal(lens, lens_held) and torch.equal(n_keep[0], n_keep[1])
+        evicted |= bool((n_keep[0] == cfg.budget).any())
+        q = torch.randn(S, H, D, generator=g, device="cuda").to(torch.bfloat16)
+        out, want = torch.empty_like(q), torch.empty_like(q)
+        B.sirllm_attend_shared(cfg, 0, G, i32(*shared), q, *held, lens_held, None, out, None, wa)
+        B.sirllm_attend(cfg, 0, q, *plain, lens, None, want, None, wp)
+        for s, n in enumerate(lens.tolist()):
+            assert torch.equal(keeps[0][s, :n], keeps[1][s, :n])
+            lo = shared[s // G]
+            for x, y in zip(plain, held):
+                assert torch.equal(x[s, 0, :, lo:n], y[s, 0, :, lo:n])
+                assert torch.equal(x[s, 0, :, :lo], y[s // G * G, 0, :, :lo])
+            # both are within the tolerance of the same formula
+            tol = ref_attend(q[s], plain[0][s, 0], plain[1][s, 0], n, D ** -0.5)[2]
+            assert ((out[s].double() - want[s].double()).abs() <= 2 * tol).all()
+    assert evicted and B.sirllm_status(ws) == 0 and B.sirllm_status(wa) == 0
+
+
+def test_shared_slots_handed_out_make_plain_streams():
+    G, S, H, KH, D, C = 4, 8, 4, 2, 64, 300
+    shared, lens = [200, 37], [205, 290, 200, 231, 40, 37, 300, 99]
+    cfg = B.make_config(n_streams=S, n_layers=1, n_kv_heads=KH, head_dim=D, capacity=C, budget=C, n_sink=0, n_recent=0,
+                        max_new=1, vocab=1, logits_dtype="f32", kv_dtype="bf16")
+    g = gen(77)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(S, 1, KH, C, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    E = torch.rand(S, C, generator=g, device="cuda")
+    was = [x.clone() for x in (k, v, E)]
+    q = torch.randn(S, H, D, generator=g, device="cuda").to(torch.bfloat16)
+    out, want = torch.empty_like(q), torch.empty_like(q)
+    B.sirllm_attend_shared(cfg, 0, G, i32(*shared), q, k, v, i32(*lens), None, want, None, B.new_attend_shared_workspace(cfg, G, H))
+    ws, held = B.new_workspace(cfg), i32(*[shared[s // G] for s in range(S)])
+    B.sirllm_reorder_streams(cfg, G, i32(*[s // G * G for s in range(S)]), None, E, None, held, k, v, ws)
+    assert B.sirllm_status(ws) == 0 and held.tolist() == [shared[s // G] for s in range(S)]
+    for s in range(S):
+        lo = shared[s // G]
+        for x, y in zip((k[:, 0], v[:, 0]), (was[0][:, 0], was[1][:, 0])):
+            assert torch.equal(x[s, :, :lo], y[s // G * G, :, :lo]) and torch.equal(x[s, :, lo:], y[s, :, lo:])
+        assert torch.equal(E[s, :lo], was[2][s // G * G, :lo]) and torch.equal(E[s, lo:], was[2][s, lo:])
+    B.sirllm_attend(cfg, 0, q, k, v, i32(*lens), None, out, None, B.new_attend_workspace(cfg))
+    for s in range(S):
+        tol = ref_attend(q[s], k[s, 0], v[s, 0], lens[s], D ** -0.5)[2]
+        assert ((out[s].double() - want[s].double()).abs() <= 2 * tol).all()
