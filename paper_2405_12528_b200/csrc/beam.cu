@@ -61,17 +61,13 @@ __device__ __forceinline__ double from_key64(unsigned long long k) {
 // A bound that n of the threads' values reach, or the lowest value where too few threads have one
 // (`lowest` says that a thread has none); syncs.
 __device__ __forceinline__ float reach_by_warps(float mine, float warp_top, float lowest, int n, float (&tops)[kWarps],
-                                                float (&bounds)[kWarps], float (&nths)[kWarps], float& top) {
+                                                float (&bounds)[kWarps], float (&nths)[kWarps]) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) tops[warp] = warp_top;
     __syncthreads();
     int with = 0;
-    top = lowest;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        with += tops[w] > lowest;
-        top = fmaxf(top, tops[w]);
-    }
+    for (int w = 0; w < kWarps; ++w) with += tops[w] > lowest;
     // The k-th largest of the warp, k * warps >= n: the least of those is reached by n values.  And the n-th
     // largest of the warp, for small n: the largest of those is, too.
     uint32_t key = key_of(mine), bound = 0, nth = 0;
@@ -500,9 +496,8 @@ __device__ __noinline__ void join_group(const BeamParams& p, int g) {
             // 0: a bound, 1: the list; if that overflows 2: another bound, 3: the list again
             visit((pass & 1) == 0);
             if (pass == 0) {
-                float top;
                 reach = reach_by_warps(mine, from_key(__reduce_max_sync(0xFFFFFFFFu, key_of(mine))), none, p.n_out, sh.tops,
-                                       sh.bounds, sh.nths, top);
+                                       sh.bounds, sh.nths);
             } else if (pass == 2) {
                 if (tid == 0) sh.listed = 0;
                 reach = fmaxf(reach, reach_by_threads(mine, sh.maxima, &sh.bound, p.n_out));

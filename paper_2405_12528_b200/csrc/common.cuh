@@ -359,8 +359,8 @@ cudaError_t launch_append(const AppendParams& p, bool bf16, cudaStream_t st);
 // query heads of a unit: 16 where more than 8 share a K/V head, so that K and V are read once for
 // them - unless the head is so wide that two blocks' queries and sums do not fit the registers
 inline int attend_unit_heads(int group, int head_dim) { return group > 8 && head_dim <= 128 ? 16 : 8; }
-// Whether the shared slots of groups of `stream_group` streams with `heads` query heads per K/V head go
-// to the kernel that computes them once for all (else every stream reads them for itself), and how.
+// Whether prefix_kernel can take the shared slots of groups of `stream_group` streams (heads of at most 128 elements,
+// at most kPrefixRows query heads per K/V head), and how.  What becomes of the others is attend_shared_layout's.
 bool prefix_plan(const sirllm_config& c, int32_t stream_group, int32_t n_heads, PrefixPlan* plan);
 cudaError_t launch_prefix(const PrefixParams& p, const void* q, int64_t q_stride, int32_t n_streams, const void* k,
                           const void* v, cudaStream_t st);

@@ -3,7 +3,7 @@
 // K/V head are the rows of one product,
 //     S = Q K^T [rows x slots],   P = 2^(scale log2e S - reference),   O = P V,
 // and every row's (reference, sum of P, O) over a stretch of the slots goes to the workspace, where
-// attend_kernel takes it up as the start of the stream's own slots.
+// join_kernel adds it to what attend_kernel makes of the stream's own slots.
 //
 // Read once for up to 256 rows, K and V cost 4 * rows operations per element: HBM's bound up to about 250
 // rows, the tensor core's beyond.  tcgen05 for both products: 128 rows on the lanes, S and O in tensor
@@ -609,7 +609,7 @@ cudaError_t launch(const PrefixParams& p, const DeviceProps& dp, const CUtensorM
 
 bool prefix_plan(const sirllm_config& c, int32_t stream_group, int32_t n_heads, PrefixPlan* plan) {
     const int heads = n_heads / c.n_kv_heads;
-    if (heads > kPrefixRows || c.head_dim > 128 || (int64_t)stream_group * heads <= 16) return false;
+    if (heads > kPrefixRows || c.head_dim > 128) return false;
     *plan = PrefixPlan{};
     plan->block_streams = stream_group < kPrefixRows / heads ? stream_group : kPrefixRows / heads;
     plan->blocks = (stream_group + plan->block_streams - 1) / plan->block_streams;

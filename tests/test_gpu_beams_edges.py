@@ -271,3 +271,12 @@ def test_shared_slots_handed_out_make_plain_streams():
     for s in range(S):
         tol = ref_attend(q[s], k[s, 0], v[s, 0], lens[s], D ** -0.5)[2]
         assert ((out[s].double() - want[s].double()).abs() <= 2 * tol).all()
+
+
+def test_select_totals_that_are_no_numbers():
+    z, _ = beams(21, 8, 20001, torch.float32)
+    totals = torch.tensor([0.0, math.inf, math.nan, -1.0, math.nan, math.nan, -math.inf, math.nan], device="cuda")
+    tot, src, tok, _, _ = select(z, 4, 40, totals, end=-1)      # +inf: ahead of all; NaN: no beam
+    assert src[:40].tolist() == [1] * 40 and (tot[:40] == math.inf).all()
+    assert tok[:40].tolist() == torch.sort(z[1], descending=True, stable=True).indices[:40].tolist()
+    assert (src[40:] == -1).all() and (tok[40:] == -1).all() and (tot[40:] == -math.inf).all()
