@@ -212,9 +212,9 @@ struct Walk {
     // slots below `shared` are those of the stream `lead`
     int stream, base, shared, lead;
 
-    // the walk's member s: its slots, and where they are
-    __device__ __forceinline__ void look_up(const AttendParams& p) {
-        len = unit_slots<kUse>(p, s);
+    // the walk's member s of `slots` slots: where they are
+    __device__ __forceinline__ void look_up(const AttendParams& p, int slots) {
+        len = slots;
         if (kUse == kPlain) return;
         stream = s - p.lead_units;
         const int g = stream < 0 ? s : stream / p.stream_group;
@@ -236,7 +236,7 @@ struct Walk {
         for (; unit0 < n_units; unit0 += step) {
             s = unit0 / p.units;
             unit = unit0 - s * p.units;
-            look_up(p);
+            look_up(p, unit_slots<kUse>(p, s));
             if (len > 0) {
                 left = 1;
                 break;
@@ -263,7 +263,7 @@ struct Walk {
                     left = 0;
                     return;
                 }
-                look_up(p);
+                look_up(p, unit_slots<kUse>(p, s));
             }
         }
         set_end();
@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
                 f.step = 0;
                 f.left = min(per, line - r0);
                 f.s = s;
-                f.look_up(p);
+                f.look_up(p, len);
                 f.unit = (r0 - at) / T;
                 f.unit0 = at + f.unit * T;
                 f.t0 = r0 - f.unit0;
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
         first.left = s < s_hi ? r1 - r0 : 0;
         if (s < s_hi) {
             first.s = s;
-            first.look_up(p);
+            first.look_up(p, len);
             first.unit = (r0 - at) / T;
             first.unit0 = at + first.unit * T;
             first.t0 = r0 - first.unit0;
@@ -543,15 +543,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const AttendPara
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
             const int h = n * 8 + (lane >> 2);
-            const char* qhead = qrow + (int64_t)h * p.head_dim * 2;
+            const char* qhead = qrow;
+            int64_t first_e = (int64_t)h * p.head_dim;
             if (of_group) {
                 const int row = block * kHeads + h, local = row / p.group;
+                first_e = 0;
                 qhead = p.q + ((w.lead + local) * p.q_stride + (int64_t)(g * p.group + row - local * p.group) * p.head_dim) * 2;
             }
 #pragma unroll
             for (int ks = 0; ks < kDim / 16; ++ks) {
                 const int e = ks * 16 + hc;
-                const char* src = qhead + e * 2;
+                const char* src = qhead + (first_e + e) * 2;
                 qf[n][ks][0] = h < heads && e < p.head_dim ? *reinterpret_cast<const uint32_t*>(src) : 0u;
                 qf[n][ks][1] = h < heads && e + 8 < p.head_dim ? *reinterpret_cast<const uint32_t*>(src + 16) : 0u;
             }
