@@ -181,9 +181,10 @@ struct AttendDeal {
 
 // ---- slots shared by a group of streams: how a call goes about them ---------------------------
 // Up to so many bytes of K and V of all streams (by capacity), and of one stream of every group, each stream reads
-// the shared slots for itself, in one launch; L2 serves the repeats.  4 beams x 1000 slots x 8 heads of 128 (17 MB)
+// the shared slots for itself, in one launch; L2 serves the repeats.  Full caches: 4 beams x 1000 slots x 8 heads of 128 (17 MB)
 // 10.1 us, 16.1 the other way; 8 x 2000 (69 MB) 14.7 and 18.8; 16 x 1500 (100 MB) 15.8 and 23.8; 64 x 1000 (275 MB) 40.4
-// and 37.8; 8 x 12001 (400 MB) 46 and 31; 2 x 12001 (99 MB, 50 per stream) 26.1 and 22.8.
+// and 37.8; 8 x 12001 (400 MB) 46 and 31; 2 x 12001 (99 MB, 50 per stream) 26.1 and 22.8.  (The lengths are on the device:
+// few slots in planes of a large capacity take the second figure.)
 constexpr int64_t kSharedReadBytes = 160 << 20, kSharedReadOnce = 40 << 20;
 // Beyond that, up to so many query heads of a group per K/V head, the shared slots are units of attend_kernel, above
 // prefix_kernel's.  8 beams x 12001 slots: 32 heads 30.9 us as units, 30.4 as products, 64 heads 39.6 and 32.0; 2000 slots:

@@ -17,10 +17,10 @@
 // The reference moves only when a score passes it by more than 2^8 (bf16; fp16: the weights stand 2^11 to
 // 2^15 above the reference, see attend_kernel), so O is rarely rescaled.  Sums, references and O are
 // fp32; P is rounded to 16 bits on its way into the second product.
-// Measured, 64 streams x 32 heads on 8 x 15873 slots: 27 us of the call's 54 (floor 10.4, the products).  A tile takes both
+// Measured, 64 streams x 32 heads on 8 x 15873 slots: 24 us of the call's 50 (floor 10.4, the products).  A tile takes both
 // lanes 3900 cycles: weights 2400, then products and the next scores 1470, in turns; the tensor core alone would
-// take 2050.  The rest is the start (5000 - 9000 cycles to the first scores, mostly instructions on their way into the
-// cache) and the end (7700).
+// take 2050, the exponentials alone (32768 at 16 a cycle) 2048.  The rest is the start (thousands of cycles to the
+// first scores, mostly instructions on their way into the cache) and the end.
 // Whole tiles only: what is left of the shared slots (fewer than 128) attend_kernel reads itself, so
 // nothing here is masked and no slot behind the shared ones is read.
 #include <cuda_bf16.h>

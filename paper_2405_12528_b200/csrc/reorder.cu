@@ -12,7 +12,8 @@
 // A warp is a CTA with a ring of its own (6 pieces of 8 KB, four such CTAs to an SM).
 // Measured: two of four streams forked in each of four groups, 600 slots x 512 planes of 256 bytes, 1.25 GB in 182 us
 // (1.05 of the copy rate, sources in L2); one stream to seven others, 1.07 GB in 189 us (0.86: seven of eight bytes are
-// written); 30 slots x 64 planes of 128 bytes 5.9 us.
+// written); 30 slots x 64 planes of 128 bytes 5.9 us.  Exchanges, 600 slots x 512 planes: 4 x 8 streams 5.7 TB/s (0.87); one group of
+// 64 streams 1.9 TB/s (0.29: its pieces are 128 bytes).
 #include "common.cuh"
 
 namespace sirllm {
