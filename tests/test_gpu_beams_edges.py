@@ -280,3 +280,111 @@ def test_select_totals_that_are_no_numbers():
     assert src[:40].tolist() == [1] * 40 and (tot[:40] == math.inf).all()
     assert tok[:40].tolist() == torch.sort(z[1], descending=True, stable=True).indices[:40].tolist()
     assert (src[40:] == -1).all() and (tok[40:] == -1).all() and (tot[40:] == -math.inf).all()
+
+
+# --------------------------------------------------------------------------------------
+# the largest vocabulary; calls captured first, and behind other streams
+# --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("skew", [0, 3])
+def test_select_largest_vocabulary(skew):
+    V = B.MAX_BEAM_VOCAB
+    z = at_skew(torch.zeros(2, V, dtype=torch.bfloat16, device="cuda"), skew, V + 8)
+    for s, (at, value) in enumerate(((V - 1, 3.0), (V // 2 + 7, 2.0))):
+        z[s, at] = value
+    z[0, 0] = 1.0
+    totals = torch.tensor([-1.0, -1.5], device="cuda")
+    tot, src, tok, ent, _ = select(z, 2, 8, totals, end=V - 1)
+    assert src.tolist() == [0, 1, 0] + [0] * 5 and tok.tolist() == [V - 1, V // 2 + 7, 0, 1, 2, 3, 4, 5]
+    lse = [math.log(math.fsum([V - 2, math.exp(3.0), math.e])), math.log(math.fsum([V - 1, math.exp(2.0)]))]
+    want = [lse[0] - 3.0, lse[1] - 2.0, lse[0] - 1.0] + [lse[0]] * 5
+    for e, t, s, w in zip(ent.tolist(), tot.tolist(), src.tolist(), want):
+        tol = log_sum_bound(64, V) + 2.0 ** -24 * 20
+        assert abs(e - w) <= tol and abs(t - (totals[s].item() - w)) <= tol
+
+
+FIRST_CALLS = """
+import torch
+from paper_2405_12528_b200 import binding as B
+G, H, KH, D, C, V = {G}, {H}, 2, {D}, {C}, 40001
+cfg = B.make_config(G, 1, KH, D, C, C, 0, 0, 1, V, "f32", "bf16")
+i32 = dict(dtype=torch.int32, device="cuda")
+ws, wb, wa = B.new_workspace(cfg), B.new_beam_workspace(cfg), B.new_attend_shared_workspace(cfg, G, H)
+k, v = (torch.randn(G, KH, C, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+q = torch.randn(G, H, D, device="cuda").to(torch.bfloat16)
+out, logits = torch.zeros_like(q), torch.randn(G, V, device="cuda")
+shared, live = torch.full((1,), 500, **i32), torch.full((G,), 520, **i32)
+totals, source, tokens = torch.zeros(G, device="cuda"), torch.zeros(G, **i32), torch.zeros(G, **i32)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    B.sirllm_attend_shared(cfg, 0, G, shared, q, k, v, live, None, out, None, wa)
+    B.sirllm_beam_select(cfg, logits, G, G, totals, None, -1, True, totals, source, tokens, None, None, wb)
+    B.sirllm_reorder_streams(cfg, G, source, shared, None, None, live, k, v, ws)
+g.replay()
+torch.cuda.synchronize()
+assert float(out[0].abs().sum()) > 0 and float(totals.max()) < 0 and int(source.min()) >= 0
+assert all(B.sirllm_status(w) == 0 for w in (ws, wb, wa))
+print("captured")
+"""
+
+
+@pytest.mark.parametrize("G,H,D,C", [(4, 4, 64, 600), (4, 8, 128, 45000), (40, 4, 64, 9000), (16, 8, 256, 3000)])
+def test_the_process_first_calls_may_be_captured_ones(G, H, D, C):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(G=G, H=H, D=D, C=C)], capture_output=True, text=True,
+                         cwd=root, timeout=300)
+    assert run.returncode == 0 and "captured" in run.stdout, run.stderr[-2000:]
+
+
+@pytest.mark.parametrize("G,C", [(4, 600), (4, 45000), (40, 9000)])
+def test_shared_calls_behind_a_join_of_two_captured_streams(G, C):
+    # lengths, queries, rows and sources that another stream writes just before each call
+    H, KH, D, V = 4, 2, 64, 3001
+    cfg = B.make_config(G, 1, KH, D, C, C, 0, 0, 1, V, "f32", "bf16")
+    g = gen(C)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    ws, wb, wa = B.new_workspace(cfg), B.new_beam_workspace(cfg), B.new_attend_shared_workspace(cfg, G, H)
+    k, v = (torch.randn(G, 1, KH, C, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    was = k.clone(), v.clone()
+    q_from = torch.randn(G, H, D, generator=g, device="cuda").to(torch.bfloat16)
+    z_from, totals = torch.randn(G, V, generator=g, device="cuda") * 3, -torch.rand(G, generator=g, device="cuda")
+    q, z, out = torch.zeros_like(q_from), torch.zeros_like(z_from), torch.zeros_like(q_from)
+    shared, live = i32(0), i32(*[0] * G)
+    tot, src, tok = torch.zeros(G, device="cuda"), i32(*[0] * G), i32(*[0] * G)
+    lens = [512 + 2 * s for s in range(G)]
+    lens_from = i32(*lens)
+    main, other = torch.cuda.Stream(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=main):
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            shared.fill_(512)
+            live.copy_(lens_from)
+            q.copy_(q_from)
+            k.copy_(was[0])
+        v.copy_(was[1])
+        main.wait_stream(other)
+        B.sirllm_attend_shared(cfg, 0, G, shared, q, k, v, live, None, out, None, wa)
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            z.copy_(z_from)
+        main.wait_stream(other)
+        B.sirllm_beam_select(cfg, z, G, G, totals, None, -1, True, tot, src, tok, None, None, wb)
+        B.sirllm_reorder_streams(cfg, G, src, shared, None, None, live, k, v, ws)
+    want = select(z_from, G, G, totals, end=-1, places=True, cfg=cfg)
+    for _ in range(4):
+        for x in (shared, live, q, z, k, v, out, tot, src, tok):
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tot, want[0]) and torch.equal(src, want[1]) and torch.equal(tok, want[2])
+        for s, f in enumerate(src.tolist()):
+            ks, vs = (torch.cat([x[0, 0, :, :512], x[s, 0, :, 512:]], 1) for x in was)
+            o, _, to, _ = ref_attend(q_from[s], ks, vs, lens[s], D ** -0.5)
+            assert ((out[s].double() - o).abs() <= to).all()
+            assert int(live[s]) == lens[f] and torch.equal(k[s, 0, :, 512:lens[f]], was[0][f, 0, :, 512:lens[f]])
