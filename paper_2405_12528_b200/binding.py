@@ -274,6 +274,9 @@ def prepared(func, *args, **kwargs) -> Prepared:
     return _preparing.out
 
 
+_int32_places = {}   # of every call's arguments, those that are 32-bit numbers
+
+
 def _fits(n: int) -> bool:
     """Whether ctypes hands ``n`` on as it is (it cuts larger numbers down to 32 bits without a word)."""
     return -2**31 <= n < 2**31
@@ -282,9 +285,12 @@ def _fits(n: int) -> bool:
 def _call(fn, cfg, *args) -> None:
     """Checks every argument (numbers, then the shapes of all tensors, then their residence), then calls
     ``fn`` (or, under :func:`prepared`, hands back the marshalled call instead of making it)."""
-    for a, t in zip(args, fn.argtypes[1:]):
-        if t is ctypes.c_int32 and not _fits(a):
-            raise SirllmError(ERR_BAD_CONFIG, f"{a} does not fit 32 bits")
+    places = _int32_places.get(fn.__name__)
+    if places is None:
+        places = _int32_places[fn.__name__] = [i for i, t in enumerate(fn.argtypes[1:]) if t is ctypes.c_int32]
+    for i in places:
+        if not _fits(args[i]):
+            raise SirllmError(ERR_BAD_CONFIG, f"{args[i]} does not fit 32 bits")
     for a in args:
         if isinstance(a, _Arg):
             a.check_shape()
